@@ -108,13 +108,17 @@ def _batch(case):
             lens = np.asarray([int(v) for v in case["prompts"].split(",") if v], np.int64)
         before = rng.choice([0, case["before"]], len(lens)) if case["op"] == "mixed" else np.full(len(lens), case["before"])
         ctx, new = np.concatenate([ctx, before]).astype(np.int64), np.concatenate([np.ones(case["tokens"], np.int64), lens])
-    # page by page, a page for every request that needs one more: the pages of a request lie apart, as in a cache that has been in use
-    need = -(-(ctx + new) // case["page"])
+    # what is cached came page by page, a page for every request that needed one more: the pages of a request lie apart.  The new
+    # tokens' pages are taken as the batch is made, request by request
+    had, need = -(-ctx // case["page"]), -(-(ctx + new) // case["page"])
     table, at = np.zeros((len(need), int(need.max())), np.int64), 0
-    for k in range(table.shape[1]):
-        for i in np.flatnonzero(need > k):
-            table[i, k] = at
-            at += 1
+    for k in range(int(had.max())):
+        who = np.flatnonzero(had > k)
+        table[who, k] = at + np.arange(len(who))
+        at += len(who)
+    for i in np.flatnonzero(need > had):
+        table[i, had[i] : need[i]] = at + np.arange(need[i] - had[i])
+        at += int(need[i] - had[i])
     return ctx, new, need, table, at
 
 
@@ -174,17 +178,19 @@ def prepare(case, seed):
         cache = KvCache(layers, heads, kv, dim, n_pages, page_tokens=page, max_seqs=len(new) + more, max_batch_tokens=max(1, T, more),
                         max_batch_seqs=len(new) + more, dtype=B.LORA_BF16 if case["dtype"] == "bf16" else B.LORA_F32, pages=pages)
         cache.add(np.arange(len(new)))
-        for k in range(table.shape[1]):
-            who = np.flatnonzero(need > k)
-            cache.extend(who, np.minimum(page, (ctx + new)[who] - k * page))
-        assert all(np.array_equal(cache.pages_of(i), table[i, : need[i]]) for i in range(len(new)))
+        for at in range(0, int(ctx.max()), page):
+            who = np.flatnonzero(ctx > at)
+            cache.extend(who, np.minimum(page, ctx[who] - at))
         state["cache"], state["ids"] = cache, np.arange(len(new), dtype=np.int64)
         state["offsets"] = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
         state["ctx"] = ctx
-        if case["op"] != "pages":  # the batch's own tokens come with the batch
-            cache.truncate(state["ids"], ctx)
+        plan = cache.batch(state["ids"], state["offsets"])
+        assert all(np.array_equal(cache.pages_of(i), table[i, : need[i]]) for i in range(len(new)))
         if case["op"] in ("attend", "append"):
-            state["plan"] = cache.batch(state["ids"], state["offsets"])
+            state["plan"] = plan
+        else:  # a batch of its own in every pass
+            cache.batch_destroy(plan)
+            cache.truncate(state["ids"], ctx)
     return state
 
 
