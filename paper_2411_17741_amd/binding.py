@@ -23,6 +23,8 @@ LORA_F32, LORA_BF16 = 0, 1
 LORA_SLOT_EMPTY, LORA_SLOT_FILLING, LORA_SLOT_READY = 0, 1, 2
 LORA_CACHE_HOST_ONLY, LORA_CACHE_FUSED_GEMV, LORA_CACHE_SPLIT_GEMV, LORA_CACHE_DIRECT_FILL, LORA_CACHE_NO_OVERLAP = 1, 2, 4, 8, 16
 LORA_CACHE_SMALL_SCRATCH = 32
+LORA_KV_HOST_ONLY, LORA_KV_MAX_TOKENS = 1, 1 << 28
+LORA_ROPE_HALVES, LORA_ROPE_NEIGHBOURS = 0, 1
 LORA_MAX_RANK, LORA_TILE_TOKENS, LORA_MFMA_MIN_TOKENS, LORA_MFMA_MIN_TOKENS_MIXED = 128, 64, 16, 8
 
 
@@ -97,6 +99,29 @@ class lora_plan_unit_t(ctypes.Structure):
     _fields_ = [(n, c_int32) for n in ("kind", "tok_off", "n_tok", "slot", "rank", "lo", "hi", "where")] + [("alpha", c_float)]
 
 
+class lora_kv_config_t(ctypes.Structure):
+    _fields_ = [(n, c_int32) for n in ("n_layers", "n_heads", "n_kv_heads", "head_dim", "page_tokens", "n_pages", "max_seqs", "max_batch_seqs",
+                                       "max_batch_tokens", "max_batch_pages", "n_batches", "dtype", "flags")]
+
+
+class lora_kv_seq_info_t(ctypes.Structure):
+    _fields_ = [(n, c_int32) for n in ("n_tokens", "n_pages", "n_shared")]
+
+
+class lora_kv_stats_t(ctypes.Structure):
+    _fields_ = [(n, c_int32) for n in ("limit", "pages_used", "pages_free", "pages_shared", "pages_end", "seqs")] + [("pages_copied", c_int64)]
+
+
+class lora_kv_batch_info_t(ctypes.Structure):
+    _fields_ = [(n, c_int32) for n in ("n_tokens", "n_segments", "n_pages", "n_groups", "n_row_items", "n_tile_items", "n_joins")]
+
+
+class lora_kv_append_t(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_stride", c_int64), ("v_stride", c_int64), ("q", c_void_p), ("q_out", c_void_p),
+                ("q_stride", c_int64), ("q_out_stride", c_int64), ("rope", c_void_p), ("rope_positions", c_int32), ("rope_dim", c_int32),
+                ("rope_pairs", c_int32)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(
         f"{LIB_PATH} is missing: build it with `python -m paper_2411_17741_amd.build` "
@@ -106,6 +131,7 @@ _lib = ctypes.CDLL(LIB_PATH)
 
 _i32p = POINTER(c_int32)
 _i32a = c_void_p  # an int32 array by its address (see _ptr)
+_i64a = c_void_p  # an int64 array likewise
 _SIGS = {
     "lora_adapter_bytes": (c_size_t, [c_int32, c_int32, c_int32, c_int32]),
     "lora_cache_bytes_required": (c_size_t, [POINTER(lora_cache_config_t)]),
@@ -156,6 +182,26 @@ _SIGS = {
     "lora_sched_fit_queues": (c_int, [POINTER(ctypes.c_double), c_int32, c_int32, _i32p, POINTER(ctypes.c_double)]),
     "lora_sched_min_quota": (c_int64, [ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double]),
     "lora_sched_assign_quotas": (c_int, [c_int64, POINTER(c_int64), POINTER(ctypes.c_double), c_int32, POINTER(c_int64)]),
+    "lora_kv_page_bytes": (c_size_t, [POINTER(lora_kv_config_t)]),
+    "lora_kv_pages_bytes": (c_size_t, [POINTER(lora_kv_config_t)]),
+    "lora_kv_work_bytes": (c_size_t, [POINTER(lora_kv_config_t)]),
+    "lora_kv_create": (c_int, [POINTER(lora_kv_config_t), c_void_p, c_size_t, c_void_p, c_size_t, POINTER(c_void_p)]),
+    "lora_kv_destroy": (c_int, [c_void_p]),
+    "lora_kv_seq_add": (c_int, [c_void_p, c_int32, _i64a]),
+    "lora_kv_seq_fork": (c_int, [c_void_p, c_int64, c_int32, _i64a, c_int32]),
+    "lora_kv_seq_extend": (c_int, [c_void_p, c_int32, _i64a, _i32a, c_void_p]),
+    "lora_kv_seq_truncate": (c_int, [c_void_p, c_int32, _i64a, _i32a]),
+    "lora_kv_seq_free": (c_int, [c_void_p, c_int32, _i64a]),
+    "lora_kv_seq_info": (c_int, [c_void_p, c_int64, POINTER(lora_kv_seq_info_t)]),
+    "lora_kv_seq_pages": (c_int, [c_void_p, c_int64, _i32a, c_int32, _i32p]),
+    "lora_kv_compact": (c_int, [c_void_p, c_void_p, _i32p]),
+    "lora_kv_set_limit": (c_int, [c_void_p, c_int32]),
+    "lora_kv_stats": (c_int, [c_void_p, POINTER(lora_kv_stats_t)]),
+    "lora_kv_batch_create": (c_int, [c_void_p, c_int32, _i64a, _i32a, c_void_p, POINTER(c_void_p)]),
+    "lora_kv_batch_destroy": (c_int, [c_void_p, c_void_p]),
+    "lora_kv_batch_info": (c_int, [c_void_p, POINTER(lora_kv_batch_info_t)]),
+    "lora_kv_append": (c_int, [c_void_p, c_void_p, c_int32, POINTER(lora_kv_append_t), c_void_p]),
+    "lora_kv_attend": (c_int, [c_void_p, c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_float, c_void_p]),
     "lora_strerror": (c_char_p, [c_int]),
     "lora_last_hip_error": (c_int, []),
 }
@@ -535,6 +581,141 @@ def lora_apply(cache, layer: int, proj: int, x: int, base_out: int, T: int, seg_
     so, ss, sr = _i32(seg_offsets), _i32(seg_slot), _i32(seg_rank)
     return _lib.lora_apply(cache, layer, proj, c_void_p(x or None), c_void_p(base_out or None), T, _ptr(so), _ptr(ss),
                            _ptr(sr), len(ss), scale, c_void_p(stream or None))
+
+
+# ---- paged key-value cache (include/lora_kv.h) ---------------------------------------------------
+
+def _i64(a) -> np.ndarray:
+    return np.ascontiguousarray(a, dtype=np.int64).reshape(-1)
+
+
+def make_kv_config(n_layers, n_heads, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs, max_batch_seqs, max_batch_tokens, max_batch_pages,
+                   n_batches, dtype, flags=0) -> lora_kv_config_t:
+    return lora_kv_config_t(int(n_layers), int(n_heads), int(n_kv_heads), int(head_dim), int(page_tokens), int(n_pages), int(max_seqs),
+                            int(max_batch_seqs), int(max_batch_tokens), int(max_batch_pages), int(n_batches), int(dtype), int(flags))
+
+
+def lora_kv_page_bytes(cfg) -> int:
+    return int(_lib.lora_kv_page_bytes(ctypes.byref(cfg)))
+
+
+def lora_kv_pages_bytes(cfg) -> int:
+    return int(_lib.lora_kv_pages_bytes(ctypes.byref(cfg)))
+
+
+def lora_kv_work_bytes(cfg) -> int:
+    return int(_lib.lora_kv_work_bytes(ctypes.byref(cfg)))
+
+
+def lora_kv_create(cfg, dev_pages: int, pages_bytes: int, dev_work: int, work_bytes: int):
+    """-> (status, handle)"""
+    h = c_void_p()
+    rc = _lib.lora_kv_create(ctypes.byref(cfg), c_void_p(dev_pages or None), pages_bytes, c_void_p(dev_work or None), work_bytes, ctypes.byref(h))
+    return rc, h
+
+
+def lora_kv_destroy(kv) -> int:
+    return _lib.lora_kv_destroy(kv)
+
+
+def lora_kv_seq_add(kv, ids) -> int:
+    a = _i64(ids)
+    return _lib.lora_kv_seq_add(kv, a.size, _ptr(a))
+
+
+def lora_kv_seq_fork(kv, parent: int, ids, n_tokens: int = -1) -> int:
+    a = _i64(ids)
+    return _lib.lora_kv_seq_fork(kv, parent, a.size, _ptr(a), n_tokens)
+
+
+def _ids_and_counts(ids, n_tokens):
+    a, n = _i64(ids), _i32(n_tokens).reshape(-1)
+    if a.size != n.size:
+        raise ValueError(f"{a.size} sequences, {n.size} counts of tokens")
+    return a, n
+
+
+def lora_kv_seq_extend(kv, ids, n_tokens, stream: int = 0) -> int:
+    a, n = _ids_and_counts(ids, n_tokens)
+    return _lib.lora_kv_seq_extend(kv, a.size, _ptr(a), _ptr(n), c_void_p(stream or None))
+
+
+def lora_kv_seq_truncate(kv, ids, n_tokens) -> int:
+    a, n = _ids_and_counts(ids, n_tokens)
+    return _lib.lora_kv_seq_truncate(kv, a.size, _ptr(a), _ptr(n))
+
+
+def lora_kv_seq_free(kv, ids) -> int:
+    a = _i64(ids)
+    return _lib.lora_kv_seq_free(kv, a.size, _ptr(a))
+
+
+def lora_kv_seq_info(kv, seq: int):
+    """-> (status, lora_kv_seq_info_t)"""
+    info = lora_kv_seq_info_t()
+    rc = _lib.lora_kv_seq_info(kv, seq, ctypes.byref(info))
+    return rc, info
+
+
+def lora_kv_seq_pages(kv, seq: int):
+    """-> (status, page numbers as an int32 array)"""
+    n = c_int32(0)
+    rc = _lib.lora_kv_seq_pages(kv, seq, None, 0, ctypes.byref(n))
+    if rc != LORA_OK:
+        return rc, None
+    pages = np.zeros(n.value, np.int32)
+    rc = _lib.lora_kv_seq_pages(kv, seq, _ptr(pages) if n.value else None, n.value, ctypes.byref(n))
+    return rc, pages
+
+
+def lora_kv_compact(kv, stream: int = 0):
+    """-> (status, pages moved)"""
+    n = c_int32(0)
+    rc = _lib.lora_kv_compact(kv, c_void_p(stream or None), ctypes.byref(n))
+    return rc, n.value
+
+
+def lora_kv_set_limit(kv, limit: int) -> int:
+    return _lib.lora_kv_set_limit(kv, limit)
+
+
+def lora_kv_stats(kv):
+    """-> (status, lora_kv_stats_t)"""
+    st = lora_kv_stats_t()
+    rc = _lib.lora_kv_stats(kv, ctypes.byref(st))
+    return rc, st
+
+
+def lora_kv_batch_create(kv, seg_seq, seg_offsets, stream: int = 0):
+    """-> (status, batch handle)"""
+    ids, off = _i64(seg_seq), _i32(seg_offsets).reshape(-1)
+    if off.size != ids.size + 1:
+        raise ValueError(f"{ids.size} segments, {off.size} offsets")
+    b = c_void_p()
+    rc = _lib.lora_kv_batch_create(kv, ids.size, _ptr(ids), _ptr(off), c_void_p(stream or None), ctypes.byref(b))
+    return rc, b
+
+
+def lora_kv_batch_destroy(kv, batch) -> int:
+    return _lib.lora_kv_batch_destroy(kv, batch)
+
+
+def lora_kv_batch_info(batch):
+    """-> (status, lora_kv_batch_info_t)"""
+    info = lora_kv_batch_info_t()
+    rc = _lib.lora_kv_batch_info(batch, ctypes.byref(info))
+    return rc, info
+
+
+def lora_kv_append(kv, batch, layer: int, k: int, v: int, k_stride: int, v_stride: int, q: int = 0, q_out: int = 0, q_stride: int = 0,
+                   q_out_stride: int = 0, rope: int = 0, rope_positions: int = 0, rope_dim: int = 0, rope_pairs: int = 0, stream: int = 0) -> int:
+    a = lora_kv_append_t(k or None, v or None, k_stride, v_stride, q or None, q_out or None, q_stride, q_out_stride, rope or None, rope_positions,
+                         rope_dim, rope_pairs)
+    return _lib.lora_kv_append(kv, batch, layer, ctypes.byref(a), stream or None)
+
+
+def lora_kv_attend(kv, batch, layer: int, q: int, q_stride: int, out: int, out_stride: int, scale: float, stream: int = 0) -> int:
+    return _lib.lora_kv_attend(kv, batch, layer, q or None, q_stride, out or None, out_stride, scale, stream or None)
 
 
 KERNEL_KINDS = ("mfma_reduce", "mfma_shrink", "gemv_shrink", "mfma_expand", "gemv_expand", "gemv_fused", "linear")

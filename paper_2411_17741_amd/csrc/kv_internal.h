@@ -1,0 +1,88 @@
+// Shared by the host side of the paged key-value cache (kv_cache.cpp) and its kernels: the records of a batch's lists
+// and the launchers.  include/lora_kv.h has the contract and the layout of the pages.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "lora_kv.h"
+
+namespace lora {
+
+constexpr int KV_ROW_ITEM = 16;   // rows of a row item: the query side of one 16 x 16 x k product
+constexpr int KV_TILE = 128;      // rows of a tile item
+constexpr int KV_MAX_MOVES = 128; // page copies of one launch (they travel as its arguments)
+
+// One new token: where it stands and the page it lies in.
+struct KvToken {
+    int32_t pos, page;
+};
+
+// Up to u new tokens (u: tokens of a chunk of values) of one sequence that share their chunks: tokens tok .. tok + n - 1 of the packed
+// batch at positions pos .. pos + n - 1 of page `page`.
+struct KvGroup {
+    int32_t tok, pos, n, page;
+};
+
+// One piece of the attention, for every key-value head: rows row0 .. row0 + n_rows - 1 of a segment over tokens kv0 .. kv1 - 1 of its
+// sequence.  Row r is query head kv_head * g + r % g of the segment's token r / g.
+struct AttnItem {
+    int32_t tok0;   // the segment's first token in the packed batch
+    int32_t ctx;    // its position
+    int32_t page0;  // the sequence's first entry of the page list
+    int32_t row0, n_rows;
+    int32_t kv0, kv1;
+    int32_t part;   // -1: writes its rows of the output; else where its partial results go, in rows: head h, row r at part + h * n_rows + r
+};
+
+// Rows whose pieces are joined: n_parts pieces, `stride` rows of partial results apart.
+struct JoinItem {
+    int32_t tok0, row0, n_rows, part, n_parts, stride;
+};
+
+struct KvMoves {
+    int32_t from[KV_MAX_MOVES], to[KV_MAX_MOVES];
+};
+
+struct AppendArgs {
+    const void *q, *k, *v;
+    void *q_out;
+    int64_t q_stride, q_out_stride, k_stride, v_stride;
+    const float *rope;
+    char *pages;  // of this layer
+    int64_t page_stride;
+    const KvToken *tokens;
+    const KvGroup *groups;
+    int32_t n_tokens, n_groups, n_heads, n_kv, dim, page_shift, rope_dim, neighbours;
+};
+
+struct AttnArgs {
+    const void *q;
+    void *out;
+    int64_t q_stride, out_stride;
+    const char *pages;  // of this layer
+    int64_t page_stride;
+    const int32_t *page_list;
+    const AttnItem *items;  // of this launch
+    float *part_o, *part_ml;
+    float scale_log2;  // scale * log2(e)
+    int32_t n_items, n_kv, group, page_shift;
+};
+
+struct JoinArgs {
+    void *out;
+    int64_t out_stride;
+    const JoinItem *items;
+    const float *part_o, *part_ml;
+    int32_t n_items, n_kv, group;
+};
+
+hipError_t launch_append(const AppendArgs &a, int dtype, hipStream_t st);
+hipError_t launch_moves(const KvMoves &m, int n, char *pages, int64_t page_stride, hipStream_t st);
+hipError_t launch_attn_rows(const AttnArgs &a, int dtype, int dim, hipStream_t st);
+hipError_t launch_attn_tiles(const AttnArgs &a, int dtype, int dim, hipStream_t st);
+hipError_t launch_attn_join(const JoinArgs &a, int dtype, int dim, hipStream_t st);
+
+}  // namespace lora

@@ -1280,6 +1280,8 @@ void timer_pair(void *ctx, int kind, hipEvent_t *start, hipEvent_t *stop)
 
 }  // namespace
 
+void lora::set_last_hip(int e) { g_last_hip = e; }
+
 // ------------------------------------------------------------------------------------------
 extern "C" {
 

@@ -578,6 +578,7 @@ hipError_t launch_linear_tiles(const ApplyArgs &a, const void *Wt, const LinearL
                                hipStream_t st, const KernelTimer *tm, hipEvent_t done);
 // a plan's work lists (bytes rounded up to 16) from pinned host memory as the device sees it to their place in the pool
 hipError_t launch_upload(void *dst, const void *src, size_t bytes, hipStream_t st, hipEvent_t done);
+void set_last_hip(int e);  // what lora_last_hip_error() returns on this thread
 // A [h_in][r] / B [r][h_out] (16-byte aligned; device memory, or pinned host memory as the device sees it: from_host)
 // -> slab layout, for up to REPACK_MAX_PARTS parts of one adapter in one launch (unit_end, r, rs are set by the launcher)
 constexpr int REPACK_MAX_PARTS = 32;
