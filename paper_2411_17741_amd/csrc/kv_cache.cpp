@@ -406,6 +406,7 @@ int lora_kv_create(const lora_kv_config_t *cfg, void *dev_pages, size_t pages_by
         kv->batches.resize(cfg->n_batches + SPARE_BATCHES);
         for (auto &b : kv->batches) b.member.assign(cfg->max_seqs, 0);
         if (!host_only) {
+            KV_TRY(lora::prepare_attn_kernels());
             char *at = kv->work;
             for (auto &b : kv->batches) {
                 b.dev = at;

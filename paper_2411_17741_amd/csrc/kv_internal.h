@@ -79,6 +79,7 @@ struct JoinArgs {
     int32_t n_items, n_kv, group;
 };
 
+hipError_t prepare_attn_kernels();  // once for the current device
 hipError_t launch_append(const AppendArgs &a, int dtype, hipStream_t st);
 hipError_t launch_moves(const KvMoves &m, int n, char *pages, int64_t page_stride, hipStream_t st);
 hipError_t launch_attn_rows(const AttnArgs &a, int dtype, int dim, hipStream_t st);

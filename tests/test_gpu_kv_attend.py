@@ -68,11 +68,11 @@ class Setup:
     def bound(self, out, mass, reach):
         """What rounding can do.  fp32: a score of dim products is off by up to dim * 2^-24 of sum |q||k| (twice: scores and their maximum), the
         exponential by an ulp and its argument's rounding, each of the sums over the tokens by an ulp a step.  bf16 besides: every weight is
-        rounded (2^-9) and so is the output."""
+        rounded to 8 significant bits (a relative error of up to 2^-8) and so is the output."""
         eps = 2.0**-24
         longest = max(c + n for c, n in self.segs)
         f32 = mass * ((2 * self.dim + 8) * eps * reach[..., None] + (longest + 16) * 2 * eps)
-        return f32 if self.dt == torch.float32 else f32 + 2.0**-9 * mass + 2.0**-9 * (np.abs(out) + 2.0**-8 * mass) + 1e-38
+        return f32 if self.dt == torch.float32 else f32 + 2.0**-8 * mass + 2.0**-8 * (np.abs(out) + 2.0**-7 * mass) + 1e-38
 
     def run(self, scale, q=None, layer=0):
         q = (self.q if q is None else q).cuda()
