@@ -178,6 +178,16 @@ __device__ __forceinline__ uint4 from_lds(const unsigned char *p)
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+template <typename E> __device__ __forceinline__ void put_four(E *to, const floatx4 &v)
+{
+    struct alignas(4 * sizeof(E)) Four {
+        E v[4];
+    } four;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) four.v[e] = (E)v[e];
+    *reinterpret_cast<Four *>(to) = four;
+}
+
 // Entries of a sequence's page list, 64 at a time in the lanes of a register: the page of a step is named without a trip to memory.
 struct PageList {
     const int32_t *list;
@@ -230,14 +240,15 @@ __device__ __forceinline__ void put_row(const AttnArgs &a, const AttnItem &it, i
 // (O^T = V^T P^T) wants them, with no exchange at all: lane group g = lane / 16 holds tokens u g .. u g + u - 1 of the step, a chunk
 // of values (u = 8 with bf16, where two products of 16 tokens make a step: row 4 g + i of product t is token 8 g + 4 t + i).
 template <typename E, int D> constexpr bool ROWS_AHEAD = D <= 128;  // else two steps' registers are too many
+constexpr int ROW_WAVES = 4, ROW_JOIN = 128;  // ROW_JOIN: columns that go through LDS at a time
 
 template <typename E, int D>
-__global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a)
+__global__ __launch_bounds__(64 * ROW_WAVES, 2) void attn_rows_kernel(AttnArgs a)
 {
-    constexpr int U = CHUNK<E>, NT = U / 4, STEP = 16 * NT, KC = D / U / 4, VJ = D / 16;
-    constexpr int DP = D < 128 ? D : 128, LD = DP + 4;  // columns joined in one go through LDS; padded against bank conflicts
-    __shared__ __align__(16) float lds_o[4][KV_ROW_ITEM][LD];
-    __shared__ float lds_m[4][KV_ROW_ITEM], lds_l[4][KV_ROW_ITEM];
+    constexpr int U = CHUNK<E>, NT = U / 4, STEP = 16 * NT, KC = D / U / 4, VJ = D / 16, NW = ROW_WAVES;
+    constexpr int DP = D < ROW_JOIN ? D : ROW_JOIN, LD = DP + 4;  // columns joined in one go through LDS; padded against bank conflicts
+    __shared__ __align__(16) float lds_o[NW][KV_ROW_ITEM][LD];
+    __shared__ float lds_m[NW][KV_ROW_ITEM], lds_l[NW][KV_ROW_ITEM];
     __shared__ int lds_redo;
     const AttnItem it = a.items[blockIdx.x / a.n_kv];
     const int kv_head = blockIdx.x % a.n_kv;
@@ -254,7 +265,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a)
         for (int c = 0; c < KC; ++c) q[c] = *reinterpret_cast<const uint4 *>(p + (4 * c + g) * U);
     }
 
-    const int steps = (it.kv1 - it.kv0 + STEP - 1) / STEP, per_wave = (steps + 3) / 4;
+    const int steps = (it.kv1 - it.kv0 + STEP - 1) / STEP, per_wave = (steps + NW - 1) / NW;
     const int first = it.kv0 + wave * per_wave * STEP, last = min(it.kv1, first + per_wave * STEP);
     PageList pages(a.page_list + it.page0, (it.kv1 - 1) >> a.page_shift, min(first, it.kv1 - 1) >> a.page_shift);
     const auto page_at = [&](int pos) { return pages[pos >> a.page_shift]; };
@@ -346,7 +357,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a)
         if (none != 0.f) lds_redo = 1;
         __syncthreads();
         if (lds_redo) {
-            for (int i = wave; i < it.n_rows; i += 4) {
+            for (int i = wave; i < it.n_rows; i += NW) {
                 RowState<E, D> st;
                 one_row<E, D>(a, it, kv_head, it.row0 + i, it.kv0, it.kv1, st);
                 put_row<E, D>(a, it, kv_head, i, st);
@@ -361,13 +372,15 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a)
 #pragma unroll
         for (int j = 0; j < DP / 16; ++j) *reinterpret_cast<floatx4 *>(&lds_o[wave][r][16 * j + 4 * g]) = o[pass * (DP / 16) + j];
         __syncthreads();
-        for (int i = threadIdx.x; i < it.n_rows * (DP / 4); i += 256) {
+        for (int i = threadIdx.x; i < it.n_rows * (DP / 4); i += 64 * NW) {
             const int rr = i / (DP / 4), d = i % (DP / 4) * 4;
-            const float top = fmaxf(fmaxf(lds_m[0][rr], lds_m[1][rr]), fmaxf(lds_m[2][rr], lds_m[3][rr]));
+            float top = lds_m[0][rr];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) top = fmaxf(top, lds_m[w][rr]);
             float sum = 0.f;
             floatx4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
+            for (int w = 0; w < NW; ++w) {
                 const float f = __builtin_amdgcn_exp2f(lds_m[w][rr] - top);
                 sum += lds_l[w][rr] * f;
                 v += *reinterpret_cast<const floatx4 *>(&lds_o[w][rr][d]) * f;
@@ -380,12 +393,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a)
                 const int rw = it.row0 + rr;
                 const float f = sum == 0.f ? 0.f : 1.f / sum;
                 E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + rw / a.group) * a.out_stride + (kv_head * a.group + rw % a.group) * D + pass * DP + d;
-                struct alignas(4 * sizeof(E)) Four {
-                    E v[4];
-                } four;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) four.v[e] = (E)(v[e] * f);
-                *reinterpret_cast<Four *>(out) = four;
+                put_four(out, v * f);
             }
         }
     }
@@ -590,26 +598,38 @@ __global__ __launch_bounds__(256, (TileShape<E, D>::LDS <= 80 * 1024 && sizeof(E
     }
 }
 
-// A block joins the parts of one row: thread d one value of the head
+// A block joins the parts of one row: each wavefront finds the joined maximum and weight from all parts', then groups of D / 4 threads add
+// up every 1024 / D-th part, four values of the head a thread, and the groups' sums are added in their order.
 template <typename E, int D>
-__global__ __launch_bounds__(D) void attn_join_kernel(JoinArgs a)
+__global__ __launch_bounds__(256) void attn_join_kernel(JoinArgs a)
 {
+    constexpr int GROUPS = 1024 / D;
+    __shared__ __align__(16) float sums[GROUPS][D];
     const JoinItem it = a.items[blockIdx.x / a.n_kv];
-    const int kv_head = blockIdx.x % a.n_kv, d = threadIdx.x;
-    for (int r = blockIdx.y; r < it.n_rows; r += gridDim.y) {
-        const int64_t first = it.part + (int64_t)kv_head * it.n_rows + r;
-        float m = -FLT_MAX;
-        for (int i = 0; i < it.n_parts; ++i) m = fmaxf(m, a.part_ml[2 * (first + (int64_t)i * it.stride)]);
-        float l = 0.f, o = 0.f;
-        for (int i = 0; i < it.n_parts; ++i) {
-            const int64_t at = first + (int64_t)i * it.stride;
-            const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * at] - m);
-            l += a.part_ml[2 * at + 1] * f;
-            o += a.part_o[at * D + d] * f;
-        }
+    const int r = blockIdx.y;
+    if (r >= it.n_rows) return;
+    const int kv_head = blockIdx.x % a.n_kv, lane = threadIdx.x & 63, g = threadIdx.x / (D / 4), d = threadIdx.x % (D / 4) * 4;
+    const int64_t first = it.part + (int64_t)kv_head * it.n_rows + r;
+    float m = -FLT_MAX, l = 0.f;
+    for (int i = lane; i < it.n_parts; i += 64) m = fmaxf(m, a.part_ml[2 * (first + (int64_t)i * it.stride)]);
+    m = wave_max(m);
+    for (int i = lane; i < it.n_parts; i += 64) {
+        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (first + (int64_t)i * it.stride));
+        l += ml.y * __builtin_amdgcn_exp2f(ml.x - m);
+    }
+    l = wave_sum(l);
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int i = g; i < it.n_parts; i += GROUPS) {
+        const int64_t at = first + (int64_t)i * it.stride;
+        o += *reinterpret_cast<const floatx4 *>(a.part_o + at * D + d) * __builtin_amdgcn_exp2f(a.part_ml[2 * at] - m);
+    }
+    *reinterpret_cast<floatx4 *>(&sums[g][d]) = o;
+    __syncthreads();
+    if (g == 0) {
+        for (int i = 1; i < GROUPS; ++i) o += *reinterpret_cast<const floatx4 *>(&sums[i][d]);
         const int row = it.row0 + r;
-        E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D;
-        out[d] = (E)(l == 0.f ? 0.f : o / l);
+        const float f = l == 0.f ? 0.f : 1.f / l;
+        put_four(static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D + d, o * f);
     }
 }
 
@@ -649,7 +669,7 @@ hipError_t launch_attn_rows(const AttnArgs &a, int dtype, int dim, hipStream_t s
 {
     if ((int64_t)a.n_items * a.n_kv > INT32_MAX) return hipErrorInvalidValue;
     return by_type(dtype, dim, [&](auto e, auto d) {
-        hipLaunchKernelGGL((attn_rows_kernel<decltype(e), decltype(d)::value>), dim3(a.n_items * a.n_kv), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((attn_rows_kernel<decltype(e), decltype(d)::value>), dim3(a.n_items * a.n_kv), dim3(64 * ROW_WAVES), 0, st, a);
     });
 }
 
@@ -666,8 +686,7 @@ hipError_t launch_attn_join(const JoinArgs &a, int dtype, int dim, hipStream_t s
 {
     if ((int64_t)a.n_items * a.n_kv > INT32_MAX) return hipErrorInvalidValue;
     return by_type(dtype, dim, [&](auto e, auto d) {
-        constexpr int D = decltype(d)::value;
-        hipLaunchKernelGGL((attn_join_kernel<decltype(e), D>), dim3(a.n_items * a.n_kv, KV_ROW_ITEM), dim3(D), 0, st, a);
+        hipLaunchKernelGGL((attn_join_kernel<decltype(e), decltype(d)::value>), dim3(a.n_items * a.n_kv, a.max_rows), dim3(256), 0, st, a);
     });
 }
 

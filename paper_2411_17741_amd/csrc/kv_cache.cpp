@@ -30,7 +30,7 @@ constexpr size_t PART_BYTES = (size_t)64 << 20;
 // Lists of a batch that was destroyed may still be on their way up: that many more of them than batches alive.
 constexpr int SPARE_BATCHES = 2;
 // The attention over long caches with few rows is cut along the cache until about so many blocks have work, in pieces of no fewer tokens.
-constexpr int ROW_BLOCKS = 1024, ROW_MIN_TOKENS = 256;
+constexpr int ROW_BLOCKS = 512, ROW_MIN_TOKENS = 512;
 constexpr int TILE_BLOCKS = 512, TILE_MIN_TOKENS = 512;
 constexpr int MAX_EXTRA = ROW_BLOCKS + TILE_BLOCKS + 2;  // pieces beyond one for each block of rows
 
@@ -51,6 +51,7 @@ struct lora_kv_batch {
     hipEvent_t uploaded = nullptr;
     lora_kv_batch_info_t info{};
     int32_t max_pos = -1;  // of the batch's tokens
+    int32_t join_rows = 0;  // the most rows of a join
     size_t off_tokens = 0, off_groups = 0, off_pages = 0, off_rows = 0, off_tiles = 0, off_joins = 0;
     std::vector<uint8_t> member;  // by sequence slot
 };
@@ -739,6 +740,8 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
         std::copy(cut.rows.begin(), cut.rows.end(), reinterpret_cast<AttnItem *>(b->pinned + b->off_rows));
         std::copy(cut.tiles.begin(), cut.tiles.end(), reinterpret_cast<AttnItem *>(b->pinned + b->off_tiles));
         std::copy(cut.joins.begin(), cut.joins.end(), reinterpret_cast<JoinItem *>(b->pinned + b->off_joins));
+        b->join_rows = 0;
+        for (const JoinItem &j : cut.joins) b->join_rows = std::max(b->join_rows, j.n_rows);
         b->info = {T, n_seg, (int32_t)n_pages, (int32_t)groups.size(), (int32_t)cut.rows.size(), (int32_t)cut.tiles.size(), (int32_t)cut.joins.size()};
         if (const int rc = copy_pages(*kv, g.from, g.to, st)) return rc;
         KV_TRY(lora::launch_upload(b->dev, b->pinned_dev, at, st, nullptr));
@@ -844,7 +847,7 @@ int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const v
         j.out = out, j.out_stride = out_stride;
         j.items = reinterpret_cast<const JoinItem *>(batch->dev + batch->off_joins);
         j.part_o = kv->part_o, j.part_ml = kv->part_ml;
-        j.n_items = batch->info.n_joins, j.n_kv = c.n_kv_heads, j.group = kv->group();
+        j.n_items = batch->info.n_joins, j.n_kv = c.n_kv_heads, j.group = kv->group(), j.max_rows = batch->join_rows;
         KV_TRY(lora::launch_attn_join(j, c.dtype, c.head_dim, st));
     }
     return LORA_OK;

@@ -76,7 +76,7 @@ struct JoinArgs {
     int64_t out_stride;
     const JoinItem *items;
     const float *part_o, *part_ml;
-    int32_t n_items, n_kv, group;
+    int32_t n_items, n_kv, group, max_rows;
 };
 
 hipError_t prepare_attn_kernels();  // once for the current device

@@ -15,12 +15,15 @@ template <typename E> struct alignas(16) Vals {
 
 }  // namespace
 
-// Keys and queries: a thread takes two chunks of one head of one token whose values turn together (HALVES: chunk p and the one rope_dim / 2
-// values on; NEIGHBOURS and unturned values: two chunks in a row).  8 tokens go with a run of 8 threads: a token's key chunks
-// lie page_tokens chunks apart in the page, the same chunk of the next token right beside, so that a prompt is read and
-// written in runs of 128 bytes.
-// Values: a thread takes u values of a head of the tokens that share their chunks, turns the u x u square round in its registers
-// and writes u chunks that lie in a row; chunks that are not filled by this group are written value by value.
+// Keys and queries: a thread takes two chunks of one token whose values turn together (HALVES: chunk p and the one rope_dim / 2 values on;
+// NEIGHBOURS and unturned values: two chunks in a row), of 4 heads: the position's cosines and sines are fetched once for
+// them.  8 tokens go with a run of 8 threads: a token's key chunks lie page_tokens chunks apart in the page, the same chunk of
+// the next token right beside, so that a prompt is read and written in runs of 128 bytes.
+// Values: a thread takes u values of a head of the tokens that share their chunks, turns the u x u square round in its registers,
+// and the wavefront hands the chunks round through LDS to store them 1 KB at a time; chunks that this group does not fill
+// are written value by value.
+constexpr int APPEND_HEADS = 4;
+
 template <typename E>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t key_blocks)
 {
@@ -34,64 +37,81 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t key_
         i >>= 3;
         const int p = i % n_pairs;
         i /= n_pairs;
-        const int heads = (a.q ? a.n_heads : 0) + a.n_kv;
-        int h = i % heads;
-        const int t = (int)(i / heads) * 8 + t8;
+        const int heads = (a.q ? a.n_heads : 0) + a.n_kv, head_groups = (heads + APPEND_HEADS - 1) / APPEND_HEADS;
+        const int h0 = i % head_groups * APPEND_HEADS;
+        const int t = (int)(i / head_groups) * 8 + t8;
         if (t >= a.n_tokens) return;
-        const bool is_key = h < a.n_kv;
-        if (!is_key) h -= a.n_kv;
         const KvToken tok = a.tokens[t];
-        const E *src = is_key ? static_cast<const E *>(a.k) + t * a.k_stride : static_cast<const E *>(a.q) + t * a.q_stride;
-        src += h * a.dim;
         const int turned = a.rope_dim / (2 * U);  // pairs of chunks that turn
         const bool turn = p < turned, halves = turn && !a.neighbours;
         const int c0 = halves ? p : 2 * p, c1 = halves ? p + turned : 2 * p + 1;
-        Vals<E> x = *reinterpret_cast<const Vals<E> *>(src + c0 * U), y = *reinterpret_cast<const Vals<E> *>(src + c1 * U);
+        // keys come first, then queries
+        const auto source = [&](int h) {
+            return h < a.n_kv ? static_cast<const E *>(a.k) + t * a.k_stride + h * a.dim : static_cast<const E *>(a.q) + t * a.q_stride + (h - a.n_kv) * a.dim;
+        };
+        Vals<E> x[APPEND_HEADS], y[APPEND_HEADS];
+#pragma unroll
+        for (int k = 0; k < APPEND_HEADS; ++k) {
+            const E *src = source(min(h0 + k, heads - 1));
+            x[k] = *reinterpret_cast<const Vals<E> *>(src + c0 * U);
+            y[k] = *reinterpret_cast<const Vals<E> *>(src + c1 * U);
+        }
         if (turn) {
-            const float *cs = a.rope + (size_t)tok.pos * a.rope_dim, *sn = cs + a.rope_dim / 2;
+            // HALVES: entries c0 U .. c0 U + U - 1 turn x with y; NEIGHBOURS: entries p U .. turn the pairs of x, then those of y
+            float c[U], s[U];
+            const float *cs = a.rope + (size_t)tok.pos * a.rope_dim + p * U, *sn = cs + a.rope_dim / 2;
+#pragma unroll
+            for (int e = 0; e < U; ++e) c[e] = cs[e], s[e] = sn[e];
             if (halves) {
 #pragma unroll
-                for (int e = 0; e < U; ++e) {
-                    const float c = cs[c0 * U + e], s = sn[c0 * U + e], u = (float)x.v[e], w = (float)y.v[e];
-                    x.v[e] = (E)(u * c - w * s);
-                    y.v[e] = (E)(w * c + u * s);
-                }
-            } else {
+                for (int k = 0; k < APPEND_HEADS; ++k)
 #pragma unroll
-                for (int e = 0; e < U; e += 2) {
-                    const auto pair = [&](Vals<E> &z, int chunk) {
-                        const int j = (chunk * U + e) / 2;
-                        const float c = cs[j], s = sn[j], u = (float)z.v[e], w = (float)z.v[e + 1];
-                        z.v[e] = (E)(u * c - w * s);
-                        z.v[e + 1] = (E)(w * c + u * s);
-                    };
-                    pair(x, c0);
-                    pair(y, c1);
-                }
+                    for (int e = 0; e < U; ++e) {
+                        const float u = (float)x[k].v[e], w = (float)y[k].v[e];
+                        x[k].v[e] = (E)(u * c[e] - w * s[e]);
+                        y[k].v[e] = (E)(w * c[e] + u * s[e]);
+                    }
+            } else {
+                const auto pairs = [&](Vals<E> &z, int first) {
+#pragma unroll
+                    for (int e = 0; e < U; e += 2) {
+                        const float u = (float)z.v[e], w = (float)z.v[e + 1];
+                        z.v[e] = (E)(u * c[first + e / 2] - w * s[first + e / 2]);
+                        z.v[e + 1] = (E)(w * c[first + e / 2] + u * s[first + e / 2]);
+                    }
+                };
+#pragma unroll
+                for (int k = 0; k < APPEND_HEADS; ++k) pairs(x[k], 0), pairs(y[k], U / 2);
             }
         }
-        if (is_key) {
-            E *page = reinterpret_cast<E *>(a.pages + tok.page * a.page_stride) + h * head_values + (size_t)(tok.pos & (page_tokens - 1)) * U;
-            *reinterpret_cast<Vals<E> *>(page + ((size_t)c0 << a.page_shift) * U) = x;
-            *reinterpret_cast<Vals<E> *>(page + ((size_t)c1 << a.page_shift) * U) = y;
-        } else {
-            E *to = static_cast<E *>(a.q_out) + t * a.q_out_stride + h * a.dim;
-            *reinterpret_cast<Vals<E> *>(to + c0 * U) = x;
-            *reinterpret_cast<Vals<E> *>(to + c1 * U) = y;
+#pragma unroll
+        for (int k = 0; k < APPEND_HEADS; ++k) {
+            const int h = h0 + k;
+            if (h < a.n_kv) {
+                E *page = reinterpret_cast<E *>(a.pages + tok.page * a.page_stride) + h * head_values + (size_t)(tok.pos & (page_tokens - 1)) * U;
+                *reinterpret_cast<Vals<E> *>(page + ((size_t)c0 << a.page_shift) * U) = x[k];
+                *reinterpret_cast<Vals<E> *>(page + ((size_t)c1 << a.page_shift) * U) = y[k];
+            } else if (h < heads) {
+                E *to = static_cast<E *>(a.q_out) + t * a.q_out_stride + (h - a.n_kv) * a.dim;
+                *reinterpret_cast<Vals<E> *>(to + c0 * U) = x[k];
+                *reinterpret_cast<Vals<E> *>(to + c1 * U) = y[k];
+            }
         }
         return;
     }
-    const int n_chunks = a.dim / U;
+    __shared__ Vals<E> turned[4][64 * U];
+    const int n_chunks = a.dim / U, lane = threadIdx.x & 63;
     uint32_t i = (blockIdx.x - key_blocks) * 256u + threadIdx.x;
     const int c = i % n_chunks;
     i /= n_chunks;
     const int h = i % a.n_kv;
     const int g = i / a.n_kv;
-    if (g >= a.n_groups) return;
-    const KvGroup grp = a.groups[g];
+    KvGroup grp{0, 0, 0, 0};
+    if (g < a.n_groups) grp = a.groups[g];
     const E *src = static_cast<const E *>(a.v) + (int64_t)grp.tok * a.v_stride + h * a.dim + c * U;
     const int at = grp.pos & (page_tokens - 1);
-    E *to = reinterpret_cast<E *>(a.pages + grp.page * a.page_stride) + (a.n_kv + h) * head_values + ((size_t)(at / U) * a.dim + c * U) * U;
+    E *to = reinterpret_cast<E *>(a.pages + grp.page * a.page_stride) + (a.n_kv + h) * head_values + (size_t)(at / U) * a.dim * U;  // the chunks of value 0, 1, ... of the head
+    Vals<E> *const mine = turned[threadIdx.x >> 6];
     if (grp.n == U) {
         Vals<E> in[U];
 #pragma unroll
@@ -101,14 +121,25 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t key_
             Vals<E> o;
 #pragma unroll
             for (int t = 0; t < U; ++t) o.v[t] = in[t].v[d];
-            *reinterpret_cast<Vals<E> *>(to + d * U) = o;
+            mine[lane * U + (d ^ (lane & (U - 1)))] = o;  // (a lane's chunks in an order of its own: the lanes' banks differ)
         }
     } else {
         for (int t = 0; t < grp.n; ++t) {
             const Vals<E> in = *reinterpret_cast<const Vals<E> *>(src + t * a.v_stride);
 #pragma unroll
-            for (int d = 0; d < U; ++d) to[d * U + at % U + t] = in.v[d];
+            for (int d = 0; d < U; ++d) to[(c * U + d) * U + at % U + t] = in.v[d];
         }
+    }
+    __builtin_amdgcn_wave_barrier();
+    // chunk n of the wavefront's 64 u is lane n / u's; the 64 / u lanes of a store belong to one group and head (dim is a multiple of 64)
+    const uint64_t base = reinterpret_cast<uint64_t>(to);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        const int from = k * (64 / U), owner = from + lane / U;
+        const bool whole = __builtin_amdgcn_readlane(grp.n, from) == U;
+        const uint64_t there = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(base >> 32), from) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)base, from);
+        const int first = __builtin_amdgcn_readlane(c, from) * U;
+        if (whole) reinterpret_cast<Vals<E> *>(there)[first + lane] = mine[owner * U + ((lane & (U - 1)) ^ (owner & (U - 1)))];
     }
 }
 
@@ -116,7 +147,7 @@ hipError_t launch_append(const AppendArgs &a, int dtype, hipStream_t st)
 {
     const int u = dtype == LORA_BF16 ? 8 : 4;
     const int64_t heads = (a.q ? a.n_heads : 0) + a.n_kv;
-    const int64_t keys = ((int64_t)(a.n_tokens + 7) / 8 * heads * (a.dim / (2 * u)) * 8 + 255) / 256;
+    const int64_t keys = ((int64_t)(a.n_tokens + 7) / 8 * ((heads + APPEND_HEADS - 1) / APPEND_HEADS) * (a.dim / (2 * u)) * 8 + 255) / 256;
     const int64_t vals = ((int64_t)a.n_groups * a.n_kv * (a.dim / u) + 255) / 256;
     if (keys * 256 > UINT32_MAX || vals * 256 > UINT32_MAX || keys + vals > INT32_MAX) return hipErrorInvalidValue;
     const dim3 grid((unsigned)(keys + vals));
