@@ -56,14 +56,14 @@ typedef struct {
     int32_t n_pages;
     int32_t max_seqs;            /* sequences alive at once */
     int32_t max_batch_seqs;      /* segments of a batch */
-    int32_t max_batch_tokens;    /* tokens of a batch */
+    int32_t max_batch_tokens;    /* tokens of a batch; times n_heads / n_kv_heads at most LORA_KV_MAX_TOKENS */
     int32_t max_batch_pages;     /* pages of all sequences of a batch together (a shared page counts for each) */
     int32_t n_batches;           /* batches alive at once */
     int32_t dtype;               /* LORA_F32 | LORA_BF16: q, k, v, out and the pages */
     int32_t flags;
 } lora_kv_config_t;
 
-/* ---- sizes (pure host arithmetic; 0 on a bad config) -------------------------------- */
+/* ---- sizes (pure host arithmetic; 0 on a bad config: a page, all layers, is less than 4 GB) ---- */
 size_t lora_kv_page_bytes(const lora_kv_config_t *cfg);  /* one page, all layers */
 size_t lora_kv_pages_bytes(const lora_kv_config_t *cfg); /* the pages' buffer */
 /* The other buffer: lists of n_batches batches, and 64 MB in which attention over parts of a cache keeps what is joined afterwards. */

@@ -110,6 +110,24 @@ template <> __device__ __forceinline__ void mma32<float>(floatx16 &acc, const ui
     for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], y[e], acc, 0, 0, 0);
 }
 
+// fmaxf of three values, of which none is a signalling NaN
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// acc = a . b
+template <typename E> __device__ __forceinline__ void mma32_first(floatx16 &acc, const uint4 &a, const uint4 &b)
+{
+    floatx16 zero;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) zero[i] = 0.f;
+    acc = zero;
+    mma32<E>(acc, a, b);
+}
+
 // the largest / the sum of the values of lanes 32 apart, and of lanes 16 and 32 apart
 __device__ __forceinline__ float swap32(float v, float &other)
 {
@@ -190,6 +208,7 @@ template <typename E> __device__ __forceinline__ void put_four(E *to, const floa
 
 // Entries of a sequence's page list, 64 at a time in the lanes of a register: the page of a step is named without a trip to memory.
 struct PageList {
+    static constexpr int BACK = 4;  // entries may be asked for that lie so many before the highest asked for yet
     const int32_t *list;
     int last, at, held;  // the last entry there is; lane i holds entry at + i
     __device__ __forceinline__ PageList(const int32_t *l, int last_entry, int first) : list(l), last(last_entry) { fetch(first); }
@@ -197,11 +216,12 @@ struct PageList {
     {
         at = first;
         held = list[min(at + (int)(threadIdx.x & 63), last)];
+        asm volatile("" : "+v"(held));  // waited for here: not wherever an entry is used
     }
-    __device__ __forceinline__ int operator[](int entry)  // the same in all lanes, no smaller than in earlier calls
+    __device__ __forceinline__ int operator[](int entry)  // the same in all lanes
     {
         entry = min(entry, last);
-        if (entry - at >= 64) fetch(entry);
+        if (entry - at >= 64) fetch(entry - BACK);
         return __builtin_amdgcn_readlane(held, entry - at);
     }
 };
@@ -210,14 +230,22 @@ struct PageList {
 // up to 2^8 lose nothing in fp32 sums or in rounding, and the outputs are hardly ever scaled.
 constexpr float SLACK = 8.f;
 
-template <typename E, int D>
+// Where value d of row r of 32 lies among a tile's partial results: as the wavefront that has them stores them, 4 values a lane
+__device__ __forceinline__ int tile_part(int r, int d) { return ((d / 8) * 64 + (d / 4 % 2) * 32 + r) * 4 + d % 4; }
+
+// A row that one_row() has done: to its place in the output, or with the partial results (`at`: the row's; tiles keep theirs in another order)
+template <typename E, int D, bool TILE>
 __device__ __forceinline__ void put_row(const AttnArgs &a, const AttnItem &it, int kv_head, int r, const RowState<E, D> &st)
 {
     const int lane = threadIdx.x & 63;
     if (it.part >= 0) {
-        const int64_t at = it.part + (int64_t)kv_head * it.n_rows + r;
+        const int64_t at = it.part + (int64_t)kv_head * (TILE ? (it.n_rows + 31) & ~31 : it.n_rows) + r;
 #pragma unroll
-        for (int j = 0; j < D / 64; ++j) a.part_o[at * D + lane + 64 * j] = st.o[j];
+        for (int j = 0; j < D / 64; ++j) {
+            const int d = lane + 64 * j;
+            if (TILE) a.part_o[(at & ~(int64_t)31) * D + tile_part(r & 31, d)] = st.o[j];
+            else a.part_o[at * D + d] = st.o[j];
+        }
         if (lane == 0) a.part_ml[2 * at] = st.m, a.part_ml[2 * at + 1] = st.l;
     } else {
         const int row = it.row0 + r;
@@ -242,19 +270,20 @@ __device__ __forceinline__ void put_row(const AttnArgs &a, const AttnItem &it, i
 template <typename E, int D> constexpr bool ROWS_AHEAD = D <= 128;  // else two steps' registers are too many
 constexpr int ROW_WAVES = 4, ROW_JOIN = 128;  // ROW_JOIN: columns that go through LDS at a time
 
+template <int D> struct RowsLds {
+    static constexpr int DP = D < ROW_JOIN ? D : ROW_JOIN;  // columns joined in one go; padded against bank conflicts
+    alignas(16) float o[ROW_WAVES][KV_ROW_ITEM][DP + 4];
+    float m[ROW_WAVES][KV_ROW_ITEM], l[ROW_WAVES][KV_ROW_ITEM];
+    int redo;
+};
+
 template <typename E, int D>
-__global__ __launch_bounds__(64 * ROW_WAVES, 2) void attn_rows_kernel(AttnArgs a)
+__device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it, int kv_head, RowsLds<D> &lds)
 {
-    constexpr int U = CHUNK<E>, NT = U / 4, STEP = 16 * NT, KC = D / U / 4, VJ = D / 16, NW = ROW_WAVES;
-    constexpr int DP = D < ROW_JOIN ? D : ROW_JOIN, LD = DP + 4;  // columns joined in one go through LDS; padded against bank conflicts
-    __shared__ __align__(16) float lds_o[NW][KV_ROW_ITEM][LD];
-    __shared__ float lds_m[NW][KV_ROW_ITEM], lds_l[NW][KV_ROW_ITEM];
-    __shared__ int lds_redo;
-    const AttnItem it = a.items[blockIdx.x / a.n_kv];
-    const int kv_head = blockIdx.x % a.n_kv;
+    constexpr int U = CHUNK<E>, NT = U / 4, STEP = 16 * NT, KC = D / U / 4, VJ = D / 16, NW = ROW_WAVES, DP = RowsLds<D>::DP;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int in_page = (1 << a.page_shift) - 1;
-    if (threadIdx.x == 0) lds_redo = 0;
+    if (threadIdx.x == 0) lds.redo = 0;
 
     const int row = it.row0 + min(r, it.n_rows - 1);
     const int end = it.ctx + row / a.group + 1;  // tokens that this lane's row sees
@@ -354,36 +383,36 @@ __global__ __launch_bounds__(64 * ROW_WAVES, 2) void attn_rows_kernel(AttnArgs a
 #pragma unroll
             for (int i = 0; i < 4; ++i) none += o[j][i] * 0.f;
         __syncthreads();
-        if (none != 0.f) lds_redo = 1;
+        if (none != 0.f) lds.redo = 1;
         __syncthreads();
-        if (lds_redo) {
+        if (lds.redo) {
             for (int i = wave; i < it.n_rows; i += NW) {
                 RowState<E, D> st;
                 one_row<E, D>(a, it, kv_head, it.row0 + i, it.kv0, it.kv1, st);
-                put_row<E, D>(a, it, kv_head, i, st);
+                put_row<E, D, false>(a, it, kv_head, i, st);
             }
             return;
         }
     }
-    if (g == 0) lds_m[wave][r] = m, lds_l[wave][r] = l;
+    if (g == 0) lds.m[wave][r] = m, lds.l[wave][r] = l;
 #pragma unroll
     for (int pass = 0; pass < D / DP; ++pass) {
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < DP / 16; ++j) *reinterpret_cast<floatx4 *>(&lds_o[wave][r][16 * j + 4 * g]) = o[pass * (DP / 16) + j];
+        for (int j = 0; j < DP / 16; ++j) *reinterpret_cast<floatx4 *>(&lds.o[wave][r][16 * j + 4 * g]) = o[pass * (DP / 16) + j];
         __syncthreads();
         for (int i = threadIdx.x; i < it.n_rows * (DP / 4); i += 64 * NW) {
             const int rr = i / (DP / 4), d = i % (DP / 4) * 4;
-            float top = lds_m[0][rr];
+            float top = lds.m[0][rr];
 #pragma unroll
-            for (int w = 1; w < NW; ++w) top = fmaxf(top, lds_m[w][rr]);
+            for (int w = 1; w < NW; ++w) top = fmaxf(top, lds.m[w][rr]);
             float sum = 0.f;
             floatx4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
-                const float f = __builtin_amdgcn_exp2f(lds_m[w][rr] - top);
-                sum += lds_l[w][rr] * f;
-                v += *reinterpret_cast<const floatx4 *>(&lds_o[w][rr][d]) * f;
+                const float f = __builtin_amdgcn_exp2f(lds.m[w][rr] - top);
+                sum += lds.l[w][rr] * f;
+                v += *reinterpret_cast<const floatx4 *>(&lds.o[w][rr][d]) * f;
             }
             if (it.part >= 0) {
                 const int64_t at = it.part + (int64_t)kv_head * it.n_rows + rr;
@@ -399,100 +428,96 @@ __global__ __launch_bounds__(64 * ROW_WAVES, 2) void attn_rows_kernel(AttnArgs a
     }
 }
 
-// Tiles of 128 rows of one key-value head (its query heads token by token): 4 wavefronts of 32 rows each share the keys and values, which
-// go through LDS stage by stage (TK tokens), a stage ahead of the products.  As in the kernel above scores are formed
-// transposed, here in products of 32 tokens by 32 rows: lane half h holds, of 32 tokens, rows 8 j + 4 h + i of the product for its row, and the
-// second product wants chunks of u tokens in a lane.  With bf16 (u = 8) the keys of a product are therefore taken in the order that makes
-// them so: product row 16 s + 8 b + 4 h + i is token 16 s + 8 h + 4 b + i (bits 2 and 3 of the number change places), which
-// costs nothing as every lane names the chunk that it brings to LDS.
+template <typename E, int D>
+__global__ __launch_bounds__(64 * ROW_WAVES, 2) void attn_rows_kernel(AttnArgs a)
+{
+    __shared__ RowsLds<D> lds;
+    const AttnItem it = a.rows[blockIdx.x / a.n_kv];
+    attn_rows<E, D>(a, it, blockIdx.x % a.n_kv, lds);
+}
+
+// Tiles of rows of one key-value head (its query heads token by token): wavefronts of 32 rows share the keys and values, which go through
+// LDS stage by stage.  As in the kernel above scores are formed transposed, here in products of 32 tokens by 32 rows: lane half h holds,
+// of 32 tokens, rows 8 j + 4 h + i of the product for its row, and the second product wants chunks of u tokens in a lane.  With bf16
+// (u = 8) the keys of a product are therefore taken in the order that makes them so: product row 16 s + 8 b + 4 h + i is
+// token 16 s + 8 h + 4 b + i (bits 2 and 3 of the number change places), which costs nothing as every lane names the chunk that
+// it brings to LDS.
 template <typename E> __device__ __forceinline__ int key_of_row(int row) { return sizeof(E) == 2 ? (row & ~12) | (row & 4) << 1 | (row & 8) >> 1 : row; }
 
-template <typename E, int D> struct TileShape {
-    static constexpr int TK = sizeof(E) == 2 && D <= 128 ? 64 : 32;  // tokens of a stage
-    static constexpr int HALF = TK * D * (int)sizeof(E);             // bytes of its keys, and of its values
-    static constexpr int LDS = 4 * HALF;                             // two stages
+// Requests of 4 wavefronts for stages of TK tokens to LDS, keys as [D / u][TK] chunks, values as [TK / u][D].  A wavefront's request brings 64
+// chunks: keys of 64 tokens (32 in a page, 32 perhaps in another) or two chunks of 32, values of u tokens (in one page).  The values are
+// asked for after the keys: their pages are the ones that the keys were in.  Past the last stage requests may go on: they
+// bring the last page's.
+template <typename E, int D, int TK> struct Stages {
+    static constexpr int U = CHUNK<E>, HALF = TK * D * (int)sizeof(E), PER = HALF / 4096;  // bytes of a stage's keys or values; a wavefront's requests for them
+    PageList pages;
+    const char *head, *k_lane;  // the head's keys in page 0, and the lane's first chunk of them
+    uint32_t page_stride;
+    int page_shift, loader, lane, values_at, page[2], at, t0;
+    __device__ __forceinline__ Stages(const AttnArgs &a, const AttnItem &it, int kv_head, int which_loader, int first)
+        : pages(a.page_list + it.page0, (it.kv1 - 1) >> a.page_shift, it.kv0 >> a.page_shift), page_stride((uint32_t)a.page_stride), page_shift(a.page_shift),
+          loader(which_loader), lane(threadIdx.x & 63), values_at(((a.n_kv * D) << a.page_shift) * (int)sizeof(E)), at(0), t0(first)
+    {
+        head = a.pages + ((size_t)kv_head * D << a.page_shift) * sizeof(E);
+        const int slot = lane % TK, tok = (slot & 32) | key_of_row<E>(slot & 31), chunk = TK == 64 ? loader : 2 * loader + lane / 32;
+        k_lane = head + ((chunk << a.page_shift) + (a.page_shift == 5 ? tok & 31 : tok)) * 16;
+        page[0] = page[1] = 0;
+    }
+    __device__ __forceinline__ void keys(unsigned char *to)  // of the next stage
+    {
+        page[0] = pages[t0 >> page_shift];
+        if (TK == 64) page[1] = pages[(t0 + 32) >> page_shift];
+        at = t0 & ((1 << page_shift) - 1);
+        const char *const from = k_lane + (uint64_t)page_stride * (uint32_t)(TK == 32 || lane < 32 ? page[0] : page[1]) + at * 16;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) request16(reinterpret_cast<const __bf16 *>(from + (((TK == 64 ? 4 : 8) * i) << page_shift) * 16), to + loader * 1024 + i * 4096);
+        t0 += TK;
+    }
+    __device__ __forceinline__ void values(unsigned char *to)  // of the stage whose keys were asked for last
+    {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int g = (4 * i + loader) * 64, tok = g / D * U;
+            const int pg = tok < 32 ? page[0] : page[1], off = (tok < 32 || page_shift > 5 ? tok : tok - 32) + at;
+            const char *const from = head + values_at + (uint64_t)page_stride * (uint32_t)pg + off * (D * (int)sizeof(E)) + (g % D + lane) * 16;
+            request16(reinterpret_cast<const __bf16 *>(from), to + loader * 1024 + i * 4096);
+        }
+    }
 };
 
-template <typename E, int D>
-__global__ __launch_bounds__(256, (TileShape<E, D>::LDS <= 80 * 1024 && sizeof(E) * D <= 256) ? 2 : 1) void attn_tiles_kernel(AttnArgs a)
-{
-    using Shape = TileShape<E, D>;
-    constexpr int U = CHUNK<E>, TK = Shape::TK, HALF = Shape::HALF, SUB = TK / 32, QC = D / (2 * U), DJ = D / 32, PK = 32 / (2 * U);
-    extern __shared__ __align__(16) unsigned char lds[];
-    const AttnItem it = a.items[blockIdx.x / a.n_kv];
-    const int kv_head = blockIdx.x % a.n_kv;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
-    const int in_page = (1 << a.page_shift) - 1;
-    PageList pages(a.page_list + it.page0, (it.kv1 - 1) >> a.page_shift, it.kv0 >> a.page_shift);
-
-    // which chunk a lane brings: of the i-th request of the stage's keys, chunk (i * 64 + lane) of [D / U][TK]; of its values, of [TK / U][D]
-    const auto request = [&](int t0, int buf) {
-        unsigned char *const to = lds + buf * 2 * HALF;
-        int page[SUB];
-#pragma unroll
-        for (int i = 0; i < SUB; ++i) page[i] = pages[(t0 + 32 * i) >> a.page_shift];
-#pragma unroll
-        for (int i = 0; i < HALF / 4096; ++i) {
-            const int n = (4 * i + wave) * 64 + lane, slot = n % TK, tok = (slot & ~31) + key_of_row<E>(slot & 31);
-            const int pg = SUB == 1 ? page[0] : slot < 32 ? page[0] : page[SUB - 1];
-            const E *from = half_page<E, D>(a, pg, kv_head, 0) + (((n / TK) << a.page_shift) + ((t0 + tok) & in_page)) * U;
-            request16(reinterpret_cast<const __bf16 *>(from), to + (4 * i + wave) * 1024);
-        }
-#pragma unroll
-        for (int i = 0; i < HALF / 4096; ++i) {
-            const int n = (4 * i + wave) * 64 + lane, tok = n / D * U;
-            const int pg = SUB == 1 ? page[0] : tok < 32 ? page[0] : page[SUB - 1];
-            const E *from = half_page<E, D>(a, pg, kv_head, 1) + (size_t)((t0 + tok) & in_page) * D + n % D * U;
-            request16(reinterpret_cast<const __bf16 *>(from), to + HALF + (4 * i + wave) * 1024);
-        }
-    };
-    request(it.kv0, 0);
-
-    const int my = wave * 32 + r, row = it.row0 + min(my, it.n_rows - 1);
-    const int end = it.ctx + row / a.group + 1;  // tokens that this lane's row sees
-    const int least = it.ctx + (it.row0 + min(wave * 32, it.n_rows - 1)) / a.group + 1, most = it.ctx + (it.row0 + min(wave * 32 + 31, it.n_rows - 1)) / a.group + 1;
-    uint4 q[QC];
+// 32 rows of a wavefront: lane r + 32 h has row r's queries (chunks 2 c + h), its maximum, half of its weights and outputs.  s: scores of
+// the stage; w: its weights; o[j][4 k + i]: value 32 j + 8 k + 4 h + i
+template <typename E, int D, int TK> struct TileRows {
+    static constexpr int U = CHUNK<E>, SUB = TK / 32, QC = D / (2 * U), DJ = D / 32, PK = 32 / (2 * U);
+    uint4 q[QC], w[SUB * PK];
+    floatx16 o[DJ], s[SUB];
+    float m, l;
+    int end, least;  // tokens that the lane's row sees, and the wavefront's first
+    __device__ __forceinline__ TileRows(const AttnArgs &a, const AttnItem &it, int kv_head, int part)
     {
-        const E *p = static_cast<const E *>(a.q) + (int64_t)(it.tok0 + row / a.group) * a.q_stride + (kv_head * a.group + row % a.group) * D;
+        const int lane = threadIdx.x & 63, h = lane >> 5, row = it.row0 + min(part * 32 + (lane & 31), it.n_rows - 1);
+        const int t = row / a.group;
+        end = it.ctx + t + 1;
+        least = it.ctx + (it.row0 + min(part * 32, it.n_rows - 1)) / a.group + 1;
+        const E *p = static_cast<const E *>(a.q) + (int64_t)(it.tok0 + t) * a.q_stride + (kv_head * a.group + row - t * a.group) * D;
 #pragma unroll
         for (int c = 0; c < QC; ++c) q[c] = *reinterpret_cast<const uint4 *>(p + (2 * c + h) * U);
+        m = -FLT_MAX;
+        l = 0.f;
+#pragma unroll
+        for (int j = 0; j < DJ; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[j][i] = 0.f;
     }
-
+    __device__ __forceinline__ void wait_for_queries()  // here, and nowhere below
+    {
 #pragma unroll
-    for (int c = 0; c < QC; ++c) asm volatile("" : "+v"(q[c].x), "+v"(q[c].y), "+v"(q[c].z), "+v"(q[c].w));  // they have come: no wait for them below
-    float m = -FLT_MAX, l = 0.f;
-    floatx16 o[DJ];
-#pragma unroll
-    for (int j = 0; j < DJ; ++j)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[j][i] = 0.f;
-
-    for (int t0 = it.kv0, buf = 0; t0 < it.kv1; t0 += TK, buf ^= 1) {
-        wait_requests<0>();
-        __syncthreads();  // this stage has come, and nobody reads the other buffer any more
-        if (t0 + TK < it.kv1) request(t0 + TK, buf ^ 1);
-        if (t0 >= most || wave * 32 >= it.n_rows) continue;  // none of the wavefront's rows sees any of it
-        const unsigned char *const keys = lds + buf * 2 * HALF, *const vals = keys + HALF;
-        floatx16 s[SUB];
-#pragma unroll
-        for (int b = 0; b < SUB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
-        // the operands of the first products are all requested before the first is used
-        constexpr int AHEAD = QC < 8 ? QC : 8;
-#pragma unroll
-        for (int c0 = 0; c0 < QC; c0 += AHEAD) {
-            uint4 k[SUB][AHEAD];
-#pragma unroll
-            for (int c = 0; c < AHEAD; ++c)
-#pragma unroll
-                for (int b = 0; b < SUB; ++b) k[b][c] = from_lds(keys + ((2 * (c0 + c) + h) * TK + 32 * b + r) * 16);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int c = 0; c < AHEAD; ++c)
-#pragma unroll
-                for (int b = 0; b < SUB; ++b) mma32<E>(s[b], k[b][c], q[c0 + c]);
-        }
+        for (int c = 0; c < QC; ++c) asm volatile("" : "+v"(q[c].x), "+v"(q[c].y), "+v"(q[c].z), "+v"(q[c].w));
+    }
+    // the stage at t0: its scores become weights
+    __device__ __forceinline__ void weigh(int t0, float scale_log2)
+    {
+        const int h = (threadIdx.x & 63) >> 5;
         if (t0 + TK > least) {
 #pragma unroll
             for (int b = 0; b < SUB; ++b)
@@ -500,12 +525,15 @@ __global__ __launch_bounds__(256, (TileShape<E, D>::LDS <= 80 * 1024 && sizeof(E
                 for (int i = 0; i < 16; ++i)
                     if (t0 + 32 * b + i / U * 2 * U + h * U + i % U >= end) s[b][i] = -INFINITY;
         }
-        float top = s[0][0];
+        // (the compiler does not know of the instructions that max3 is: products' results may be read so many cycles after them)
+#pragma unroll
+        for (int b = 0; b < SUB; ++b) asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s[b]));
+        float top = -INFINITY;
 #pragma unroll
         for (int b = 0; b < SUB; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-        top = max32(top) * a.scale_log2;
+            for (int i = 0; i < 16; i += 2) top = max3(top, s[b][i], s[b][i + 1]);
+        top = max32(top) * scale_log2;
         if (__any(top > m + SLACK)) {
             const float now = fmaxf(m, top), fade = __builtin_amdgcn_exp2f(m - now);
             m = now;
@@ -513,65 +541,49 @@ __global__ __launch_bounds__(256, (TileShape<E, D>::LDS <= 80 * 1024 && sizeof(E
 #pragma unroll
             for (int j = 0; j < DJ; ++j) o[j] *= fade;
         }
-        uint4 w[SUB][PK];
 #pragma unroll
-        for (int b = 0; b < SUB; ++b)
+        for (int k = 0; k < SUB * PK; ++k) {
+            float p[U];
 #pragma unroll
-            for (int k = 0; k < PK; ++k) {
-                float p[U];
-#pragma unroll
-                for (int e = 0; e < U; ++e) {
-                    p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][k * U + e], a.scale_log2, -m));
-                    l += p[e];
-                }
-                w[b][k] = weights(p);
+            for (int e = 0; e < U; ++e) {
+                p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k / PK][k % PK * U + e], scale_log2, -m));
+                l += p[e];
             }
-        const bool tail = t0 + TK > it.kv1;
-#pragma unroll
-        for (int b = 0; b < SUB; ++b) {
-            uint4 v[PK][DJ];
-#pragma unroll
-            for (int k = 0; k < PK; ++k)
-#pragma unroll
-                for (int j = 0; j < DJ; ++j) v[k][j] = from_lds(vals + ((32 / U * b + 2 * k + h) * D + 32 * j + r) * 16);
-            if (tail) {  // behind the last token: whatever is there, it is no value
-#pragma unroll
-                for (int k = 0; k < PK; ++k)
-#pragma unroll
-                    for (int j = 0; j < DJ; ++j) v[k][j] = first_values<E>(v[k][j], it.kv1 - t0 - (32 / U * b + 2 * k + h) * U);
-            }
-#pragma unroll
-            for (int k = 0; k < PK; ++k)
-#pragma unroll
-                for (int j = 0; j < DJ; ++j) mma32<E>(o[j], v[k][j], w[b][k]);
+            w[k] = weights(p);
+            asm volatile("" : "+v"(w[k].x), "+v"(w[k].y), "+v"(w[k].z), "+v"(w[k].w), "+v"(l));  // now, not where they are used
         }
     }
-    if (wave * 32 >= it.n_rows) return;
-    l = sum32(l);
+};
+
+// The end of a wavefront's 32 rows
+template <typename E, int D, int TK>
+__device__ __forceinline__ void finish_tile(const AttnArgs &a, const AttnItem &it, int kv_head, int part, const TileRows<E, D, TK> &t)
+{
+    constexpr int DJ = D / 32;
+    const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5, my = part * 32 + r, row = it.row0 + min(my, it.n_rows - 1);
+    const float l = sum32(t.l);
     // a value behind a row's own position had weight 0, but 0 times infinity is no number: such rows are done again without touching it
     float none = 0.f;
 #pragma unroll
     for (int j = 0; j < DJ; ++j)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) none += o[j][i] * 0.f;
+        for (int i = 0; i < 16; ++i) none += t.o[j][i] * 0.f;
     if (__any(none != 0.f)) {
-        for (int i = wave * 32; i < min(it.n_rows, wave * 32 + 32); ++i) {
+        for (int i = part * 32; i < min(it.n_rows, part * 32 + 32); ++i) {
             RowState<E, D> st;
             one_row<E, D>(a, it, kv_head, it.row0 + i, it.kv0, it.kv1, st);
-            put_row<E, D>(a, it, kv_head, i, st);
+            put_row<E, D, true>(a, it, kv_head, i, st);
         }
         return;
     }
-    // o[j][4 k + i] is value 32 j + 8 k + 4 h + i of this lane's row
     if (it.part >= 0) {
-        if (my >= it.n_rows) return;
-        const int64_t at = it.part + (int64_t)kv_head * it.n_rows + my;
+        const int64_t at = it.part + (int64_t)kv_head * ((it.n_rows + 31) & ~31) + part * 32;
 #pragma unroll
         for (int j = 0; j < DJ; ++j)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                *reinterpret_cast<floatx4 *>(a.part_o + at * D + 32 * j + 8 * k + 4 * h) = floatx4{o[j][4 * k], o[j][4 * k + 1], o[j][4 * k + 2], o[j][4 * k + 3]};
-        if (h == 0) a.part_ml[2 * at] = m, a.part_ml[2 * at + 1] = l;
+                *reinterpret_cast<floatx4 *>(a.part_o + at * D + ((4 * j + k) * 64 + lane) * 4) = floatx4{t.o[j][4 * k], t.o[j][4 * k + 1], t.o[j][4 * k + 2], t.o[j][4 * k + 3]};
+        if (h == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * (at + r)) = make_float2(t.m, l);
         return;
     }
     const float f = l == 0.f ? 0.f : 1.f / l;
@@ -584,7 +596,7 @@ __global__ __launch_bounds__(256, (TileShape<E, D>::LDS <= 80 * 1024 && sizeof(E
                 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
                 bf16x4 x, y;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = (__bf16)(o[j][4 * k + i] * f), y[i] = (__bf16)(o[j][4 * k + 4 + i] * f);
+                for (int i = 0; i < 4; ++i) x[i] = (__bf16)(t.o[j][4 * k + i] * f), y[i] = (__bf16)(t.o[j][4 * k + 4 + i] * f);
                 const uint2 xu = __builtin_bit_cast(uint2, x), yu = __builtin_bit_cast(uint2, y);
                 const auto a0 = __builtin_amdgcn_permlane32_swap(xu.x, yu.x, false, false), a1 = __builtin_amdgcn_permlane32_swap(xu.y, yu.y, false, false);
                 if (my < it.n_rows) *reinterpret_cast<uint4 *>(out + 32 * j + 8 * k + 8 * h) = make_uint4(a0[0], a1[0], a0[1], a1[1]);
@@ -593,9 +605,207 @@ __global__ __launch_bounds__(256, (TileShape<E, D>::LDS <= 80 * 1024 && sizeof(E
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (my < it.n_rows)
-                    *reinterpret_cast<floatx4 *>(out + 32 * j + 8 * k + 4 * h) = floatx4{o[j][4 * k], o[j][4 * k + 1], o[j][4 * k + 2], o[j][4 * k + 3]} * f;
+                    *reinterpret_cast<floatx4 *>(out + 32 * j + 8 * k + 4 * h) = floatx4{t.o[j][4 * k], t.o[j][4 * k + 1], t.o[j][4 * k + 2], t.o[j][4 * k + 3]} * f;
         }
     }
+}
+
+// Tiles of 128 rows, four wavefronts, two stages in LDS: one is requested while the other is worked on.
+template <typename E, int D> struct TileShape {
+    static constexpr int TK = sizeof(E) == 2 && D <= 128 ? 64 : 32;  // tokens of a stage
+    static constexpr int LDS = 4 * TK * D * (int)sizeof(E);
+};
+
+template <typename E, int D>
+__device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it, int kv_head, unsigned char *lds)
+{
+    constexpr int TK = TileShape<E, D>::TK, U = CHUNK<E>, HALF = TK * D * (int)sizeof(E);
+    typedef TileRows<E, D, TK> Rows;
+    constexpr int SUB = Rows::SUB, QC = Rows::QC, DJ = Rows::DJ, PK = Rows::PK, NK = SUB * QC, NV = SUB * PK * DJ, AHEAD = 8;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
+    Stages<E, D, TK> stages(a, it, kv_head, wave, it.kv0);
+    stages.keys(lds);
+    stages.values(lds + HALF);
+    Rows t(a, it, kv_head, wave);
+    // stages that there are, and of which the wavefront's rows see something
+    const int n = (it.kv1 - it.kv0 + TK - 1) / TK, most = it.ctx + (it.row0 + min(wave * 32 + 31, it.n_rows - 1)) / a.group + 1;
+    const int mine = wave * 32 < it.n_rows ? min(n, (most - it.kv0 + TK - 1) / TK) : 0;
+    t.wait_for_queries();
+    int buf = 0, t0 = it.kv0;
+    const auto next = [&](int i) {  // waits for stage i and requests the one behind it
+        wait_requests<0>();
+        __syncthreads();  // (nobody reads the other buffer any more)
+        if (i + 1 < n) {
+            stages.keys(lds + (buf ^ 1) * 2 * HALF);
+            stages.values(lds + (buf ^ 1) * 2 * HALF + HALF);
+        }
+    };
+    uint4 f[AHEAD];
+    const unsigned char *const my_keys = lds + (h * TK + r) * 16, *const my_values = lds + HALF + (h * D + r) * 16;
+    const auto key = [&](int i) { return from_lds(my_keys + buf * 2 * HALF + (2 * (i / SUB) * TK + 32 * (i % SUB)) * 16); };
+    const auto value = [&](int i) { return from_lds(my_values + buf * 2 * HALF + (2 * (i / DJ) * D + 32 * (i % DJ)) * 16); };
+    // operands come out of LDS AHEAD products before they are used, in this order, whatever the compiler thinks of it
+    const auto scores = [&] {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) f[i] = key(i);
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (i < SUB) mma32_first<E>(t.s[i % SUB], f[i % AHEAD], t.q[i / SUB]);
+            else mma32<E>(t.s[i % SUB], f[i % AHEAD], t.q[i / SUB]);
+            if (i + AHEAD < NK) f[i % AHEAD] = key(i + AHEAD);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const int whole = min(mine, n - 1);
+    for (int i = 0; i < whole; ++i) {
+        next(i);
+        scores();
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) f[e] = value(e);
+        __builtin_amdgcn_sched_barrier(0);
+        t.weigh(t0, a.scale_log2);
+#pragma unroll
+        for (int e = 0; e < NV; ++e) {
+            __builtin_amdgcn_sched_barrier(0);
+            mma32<E>(t.o[e % DJ], f[e % AHEAD], t.w[e / DJ]);
+            if (e + AHEAD < NV) f[e % AHEAD] = value(e + AHEAD);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        t0 += TK;
+        buf ^= 1;
+    }
+    for (int i = whole; i < n - 1; ++i) {
+        next(i);
+        buf ^= 1;
+    }
+    next(n - 1);
+    if (mine == n) {
+        scores();
+        t.weigh(t0, a.scale_log2);
+        // behind the last token: whatever is there, it is no value
+#pragma unroll
+        for (int i = 0; i < NV; ++i) mma32<E>(t.o[i % DJ], first_values<E>(value(i), it.kv1 - t0 - (2 * (i / DJ) + h) * U), t.w[i / DJ]);
+    }
+    if (wave * 32 < it.n_rows) finish_tile<E, D, TK>(a, it, kv_head, wave, t);
+}
+
+template <typename E, int D>
+__global__ __launch_bounds__(256, (TileShape<E, D>::LDS <= 80 * 1024 && sizeof(E) * D <= 256) ? 2 : 1) void attn_tiles_kernel(AttnArgs a)
+{
+    extern __shared__ __align__(16) unsigned char lds[];
+    const AttnItem it = a.tiles[blockIdx.x / a.n_kv];
+    attn_tile<E, D>(a, it, blockIdx.x % a.n_kv, lds);
+}
+
+// The same for bf16 heads of 64 or 128 values and long prompts, where the scores' exponentials take the vector units as long as the products
+// take the matrix units: tiles of 256 rows, 8 wavefronts in two groups, one of each on a SIMD, that take turns.  In a time slot one group has
+// its products -- O += P V of the last stage, S = K Q of the next -- while the other has its weights -- P = exp2(S - m) --, and a barrier
+// ends the slot; group 1 is a slot behind group 0 all along.
+//   group 0: slot 2 i products of stage i (S of it, O of i - 1), slot 2 i + 1 weights of stage i;   group 1: the same a slot later
+// Keys and values have three places each in LDS.  Group 0 requests the keys of stage j and the values of stage j - 1 beside its products in
+// slot 2 j - 4 (their places were last read by group 1 in slot 2 j - 5); they have come when slot 2 j - 2 ends, a slot
+// before the first that needs them, so that a wavefront takes its first operands out of LDS before the barrier that starts its
+// products.
+constexpr int TURN_TOKENS = 64;
+constexpr int turn_lds(int dim) { return 6 * TURN_TOKENS * dim * 2; }
+
+template <int D>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_turns_kernel(AttnArgs a)
+{
+    typedef __bf16 E;
+    constexpr int U = 8, TK = TURN_TOKENS, HALF = TK * D * 2, PER = Stages<E, D, TK>::PER, DJ = D / 32;
+    constexpr int AHEAD = 8, NV = 4 * DJ, NK = D / 8;  // products of values, of keys
+    extern __shared__ __align__(16) unsigned char lds[];  // keys of three stages, values of three
+    const AttnItem it = a.tiles[blockIdx.x / a.n_kv];
+    const int kv_head = blockIdx.x % a.n_kv;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
+    const bool second = wave >= 4;
+    const int n = (it.kv1 - it.kv0 + TK - 1) / TK;
+    const auto after = [](int place) { return place == 2 * HALF ? 0 : place + HALF; };
+    Stages<E, D, TK> stages(a, it, kv_head, wave & 3, it.kv0);
+    int put = 0, put_v = 0;
+    const auto request_keys = [&] {
+        stages.keys(lds + put);
+        put_v = put;
+        put = after(put);
+    };
+    const auto request_values = [&] { stages.values(lds + 3 * HALF + put_v); };
+    const auto turn_over = [] {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if (!second) {
+        request_keys();
+        request_values();
+        request_keys();
+    }
+    TileRows<E, D, TK> t(a, it, kv_head, wave);
+    t.wait_for_queries();
+
+    // The products of a slot, NV of the values in place `v` of LDS and then NK of the keys in place `k`: operands come out of LDS AHEAD
+    // products before they are used, in this order, whatever the compiler thinks of it
+    uint4 f[AHEAD];
+    const unsigned char *const my_keys = lds + (h * TK + r) * 16, *const my_values = lds + 3 * HALF + (h * D + r) * 16;
+    const auto operand = [&](int i, int v, int k) {
+        return i < NV ? from_lds(my_values + v + (2 * (i / DJ) * D + 32 * (i % DJ)) * 16) : from_lds(my_keys + k + (2 * ((i - NV) / 2) * TK + 32 * ((i - NV) % 2)) * 16);
+    };
+    const auto fetch_first = [&](int v, int k, auto from) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) f[i] = operand(decltype(from)::value + i, v, k);
+    };
+    const auto products = [&](int v, int k, auto from) {
+        constexpr int FROM = decltype(from)::value, TO = NV + NK;
+#pragma unroll
+        for (int i = FROM; i < TO; ++i) {
+            const int n_f = (i - FROM) % AHEAD;
+            __builtin_amdgcn_sched_barrier(0);
+            if (i < NV) mma32<E>(t.o[i % DJ], f[n_f], t.w[i / DJ]);
+            else if (i - NV < 2) mma32_first<E>(t.s[(i - NV) % 2], f[n_f], t.q[(i - NV) / 2]);
+            else mma32<E>(t.s[(i - NV) % 2], f[n_f], t.q[(i - NV) / 2]);
+            if (i + AHEAD < TO) f[n_f] = operand(i + AHEAD, v, k);
+            if (i == FROM + 2) {  // (beside the products)
+                __builtin_amdgcn_sched_barrier(0);
+                if (!second) {
+                    request_values();
+                    request_keys();
+                }
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    typedef std::integral_constant<int, 0> All;
+    typedef std::integral_constant<int, NV> Keys;
+
+    int v = 0, k = 0, t0 = it.kv0;  // places of the stage's values and the next one's keys
+    wait_requests<2 * PER>();       // (of group 0: the others have none)
+    turn_over();                    // the keys of the first stage have come
+    if (second) turn_over();
+    fetch_first(0, 0, Keys{});
+    products(0, 0, Keys{});
+    if (!second) wait_requests<2 * PER>();
+    turn_over();
+    for (int i = 0; i + 1 < n; ++i) {
+        t.weigh(t0, a.scale_log2);
+        t0 += TK;
+        k = after(k);
+        fetch_first(v, k, All{});
+        turn_over();
+        __builtin_amdgcn_s_setprio(1);
+        products(v, k, All{});
+        __builtin_amdgcn_s_setprio(0);
+        v = after(v);
+        if (!second) wait_requests<2 * PER>();
+        turn_over();
+    }
+    t.weigh(t0, a.scale_log2);
+    if (!second) turn_over();
+    // behind the last token: whatever is there, it is no value
+#pragma unroll
+    for (int i = 0; i < NV; ++i) mma32<E>(t.o[i % DJ], first_values<E>(operand(i, v, 0), it.kv1 - t0 - (2 * (i / DJ) + h) * U), t.w[i / DJ]);
+    wait_requests<0>();  // none is on its way to LDS when the block ends
+    if (wave * 32 < it.n_rows) finish_tile<E, D, TK>(a, it, kv_head, wave, t);
 }
 
 // A block joins the parts of one row: each wavefront finds the joined maximum and weight from all parts', then groups of D / 4 threads add
@@ -633,6 +843,38 @@ __global__ __launch_bounds__(256) void attn_join_kernel(JoinArgs a)
     }
 }
 
+// A block joins the parts of 32 rows of a tile: a thread has D / 32 times 4 values of one row
+template <typename E, int D>
+__global__ __launch_bounds__(256) void attn_join_tiles_kernel(JoinArgs a)
+{
+    constexpr int N = D / 32;
+    const JoinItem it = a.items[blockIdx.x / a.n_kv];
+    const int group = blockIdx.y, lane = threadIdx.x & 63, r = lane & 31;
+    if (group * 32 >= it.n_rows) return;
+    const int kv_head = blockIdx.x % a.n_kv;
+    const int64_t first = it.part + (int64_t)kv_head * ((it.n_rows + 31) & ~31) + group * 32;
+    const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + first + r;
+    float m = -FLT_MAX, l = 0.f;
+    for (int i = 0; i < it.n_parts; ++i) m = fmaxf(m, ml[(int64_t)i * it.stride].x);
+    floatx4 o[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) o[k] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < it.n_parts; ++i) {
+        const float2 x = ml[(int64_t)i * it.stride];
+        const float f = __builtin_amdgcn_exp2f(x.x - m);
+        l += x.y * f;
+        const float *from = a.part_o + (first + (int64_t)i * it.stride) * D + threadIdx.x * 4;
+#pragma unroll
+        for (int k = 0; k < N; ++k) o[k] += *reinterpret_cast<const floatx4 *>(from + k * 1024) * f;
+    }
+    if (group * 32 + r >= it.n_rows) return;
+    const int row = it.row0 + group * 32 + r;
+    const float f = l == 0.f ? 0.f : 1.f / l;
+    E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D;
+#pragma unroll
+    for (int k = 0; k < N; ++k) put_four(out + (k * 4 + threadIdx.x / 64) * 8 + lane / 32 * 4, o[k] * f);
+}
+
 namespace {
 
 template <typename F>
@@ -660,33 +902,40 @@ hipError_t prepare_attn_kernels()
         if (e == hipSuccess)
             e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_tiles_kernel<decltype(t), decltype(d)::value>), hipFuncAttributeMaxDynamicSharedMemorySize, Shape::LDS);
     };
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_turns_kernel<128>), hipFuncAttributeMaxDynamicSharedMemorySize, turn_lds(128));
     for (int dim : {64, 128, 256})
         for (int dtype : {LORA_BF16, LORA_F32}) (void)by_type(dtype, dim, lds);
     return e;
 }
 
-hipError_t launch_attn_rows(const AttnArgs &a, int dtype, int dim, hipStream_t st)
+hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, bool turns, hipStream_t st)
 {
-    if ((int64_t)a.n_items * a.n_kv > INT32_MAX) return hipErrorInvalidValue;
+    const int64_t n_tiles = (int64_t)a.n_tiles * a.n_kv, n_rows = (int64_t)a.n_rows * a.n_kv;
+    if (n_tiles + n_rows + 16 > INT32_MAX) return hipErrorInvalidValue;
+    const dim3 tiles((unsigned)n_tiles), rows((unsigned)n_rows);
     return by_type(dtype, dim, [&](auto e, auto d) {
-        hipLaunchKernelGGL((attn_rows_kernel<decltype(e), decltype(d)::value>), dim3(a.n_items * a.n_kv), dim3(64 * ROW_WAVES), 0, st, a);
+        typedef decltype(e) E;
+        constexpr int D = decltype(d)::value;
+        constexpr unsigned lds = TileShape<E, D>::LDS;
+        if constexpr (kv_turns(sizeof(E) == 2 ? LORA_BF16 : LORA_F32, D))
+            if (turns) {
+                if (n_tiles) hipLaunchKernelGGL((attn_turns_kernel<D>), tiles, dim3(512), turn_lds(D), st, a);
+                if (n_rows) hipLaunchKernelGGL((attn_rows_kernel<E, D>), rows, dim3(64 * ROW_WAVES), 0, st, a);
+                return;
+            }
+        if (n_tiles) hipLaunchKernelGGL((attn_tiles_kernel<E, D>), tiles, dim3(256), lds, st, a);
+        if (n_rows) hipLaunchKernelGGL((attn_rows_kernel<E, D>), rows, dim3(64 * ROW_WAVES), 0, st, a);
     });
 }
 
-hipError_t launch_attn_tiles(const AttnArgs &a, int dtype, int dim, hipStream_t st)
+hipError_t launch_attn_join(const JoinArgs &a, int dtype, int dim, bool tiles, hipStream_t st)
 {
     if ((int64_t)a.n_items * a.n_kv > INT32_MAX) return hipErrorInvalidValue;
     return by_type(dtype, dim, [&](auto e, auto d) {
-        using Shape = TileShape<decltype(e), decltype(d)::value>;
-        hipLaunchKernelGGL((attn_tiles_kernel<decltype(e), decltype(d)::value>), dim3(a.n_items * a.n_kv), dim3(256), Shape::LDS, st, a);
-    });
-}
-
-hipError_t launch_attn_join(const JoinArgs &a, int dtype, int dim, hipStream_t st)
-{
-    if ((int64_t)a.n_items * a.n_kv > INT32_MAX) return hipErrorInvalidValue;
-    return by_type(dtype, dim, [&](auto e, auto d) {
-        hipLaunchKernelGGL((attn_join_kernel<decltype(e), decltype(d)::value>), dim3(a.n_items * a.n_kv, a.max_rows), dim3(256), 0, st, a);
+        typedef decltype(e) E;
+        constexpr int D = decltype(d)::value;
+        if (tiles) hipLaunchKernelGGL((attn_join_tiles_kernel<E, D>), dim3(a.n_items * a.n_kv, (a.max_rows + 31) / 32), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((attn_join_kernel<E, D>), dim3(a.n_items * a.n_kv, a.max_rows), dim3(256), 0, st, a);
     });
 }
 

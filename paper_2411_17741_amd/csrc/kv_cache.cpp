@@ -31,8 +31,9 @@ constexpr size_t PART_BYTES = (size_t)64 << 20;
 constexpr int SPARE_BATCHES = 2;
 // The attention over long caches with few rows is cut along the cache until about so many blocks have work, in pieces of no fewer tokens.
 constexpr int ROW_BLOCKS = 512, ROW_MIN_TOKENS = 512;
-constexpr int TILE_BLOCKS = 512, TILE_MIN_TOKENS = 512;
-constexpr int MAX_EXTRA = ROW_BLOCKS + TILE_BLOCKS + 2;  // pieces beyond one for each block of rows
+constexpr int TILE_MIN_TOKENS = 512;
+constexpr int PIECE_STEP = 64;  // pieces begin at multiples of it: a whole number of every kernel's steps, in one page or at the start of one
+constexpr int MAX_EXTRA = 2048;  // pieces beyond one for each block of rows
 
 struct Seq {
     int64_t id = 0;
@@ -51,8 +52,9 @@ struct lora_kv_batch {
     hipEvent_t uploaded = nullptr;
     lora_kv_batch_info_t info{};
     int32_t max_pos = -1;  // of the batch's tokens
-    int32_t join_rows = 0;  // the most rows of a join
-    size_t off_tokens = 0, off_groups = 0, off_pages = 0, off_rows = 0, off_tiles = 0, off_joins = 0;
+    int32_t n_joins = 0, n_tile_joins = 0, join_rows = 0;  // join_rows: the most rows of a join of row items
+    bool turns = false;
+    size_t off_tokens = 0, off_groups = 0, off_pages = 0, off_rows = 0, off_tiles = 0, off_joins = 0, off_tile_joins = 0;
     std::vector<uint8_t> member;  // by sequence slot
 };
 
@@ -63,7 +65,7 @@ struct lora_kv {
     size_t layer_bytes = 0, page_bytes = 0, list_cap = 0;
     float *part_o = nullptr, *part_ml = nullptr;
     int64_t part_rows = 0;
-    int page_shift = 0;
+    int page_shift = 0, n_cu = 256;
 
     std::vector<Seq> seqs;
     std::vector<int32_t> free_seqs;
@@ -141,6 +143,10 @@ using lora::KvToken;
 
 size_t elem_bytes(int32_t dtype) { return dtype == LORA_BF16 ? 2 : 4; }
 
+constexpr size_t MAX_PAGE_BYTES = ((size_t)1 << 32) - 1;  // the kernels multiply a page's number by 32 bits
+
+size_t layer_bytes(const lora_kv_config_t &c) { return (size_t)2 * c.n_kv_heads * c.page_tokens * c.head_dim * elem_bytes(c.dtype); }
+
 bool good(const lora_kv_config_t *c)
 {
     if (!c || c->n_layers < 1 || c->n_kv_heads < 1 || c->n_heads < c->n_kv_heads || c->n_heads % c->n_kv_heads) return false;
@@ -148,11 +154,11 @@ bool good(const lora_kv_config_t *c)
     if (c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128 && c->page_tokens != 256) return false;
     if (c->n_pages < 1 || c->max_seqs < 1 || c->max_batch_seqs < 1 || c->max_batch_tokens < 1 || c->max_batch_pages < 1 || c->n_batches < 1)
         return false;
+    if ((int64_t)c->max_batch_tokens * (c->n_heads / c->n_kv_heads) > LORA_KV_MAX_TOKENS) return false;
     if (c->n_heads > 4096 || c->n_layers > 65536 || c->n_batches > 1024 || c->max_batch_tokens > LORA_KV_MAX_TOKENS) return false;
-    return (c->dtype == LORA_BF16 || c->dtype == LORA_F32) && (c->flags & ~LORA_KV_HOST_ONLY) == 0;
+    if ((c->dtype != LORA_BF16 && c->dtype != LORA_F32) || (c->flags & ~LORA_KV_HOST_ONLY)) return false;
+    return layer_bytes(*c) <= MAX_PAGE_BYTES / (size_t)c->n_layers;
 }
-
-size_t layer_bytes(const lora_kv_config_t &c) { return (size_t)2 * c.n_kv_heads * c.page_tokens * c.head_dim * elem_bytes(c.dtype); }
 
 int64_t max_items(const lora_kv_config_t &c)
 {
@@ -164,7 +170,7 @@ size_t list_bytes(const lora_kv_config_t &c)
 {
     const size_t T = c.max_batch_tokens;
     return align_up(T * sizeof(KvToken)) + align_up(T * sizeof(KvGroup)) + align_up((size_t)c.max_batch_pages * 4) +
-           align_up((size_t)max_items(c) * sizeof(AttnItem)) + align_up((size_t)MAX_EXTRA * sizeof(JoinItem)) + ALIGN;
+           align_up((size_t)max_items(c) * sizeof(AttnItem)) + align_up((size_t)MAX_EXTRA * sizeof(JoinItem)) + 3 * ALIGN;
 }
 
 // Work of a call on a stream waits for the work of the one before it on another.
@@ -272,15 +278,16 @@ void reserve(const lora_kv &kv, Growth &g)
 
 // How the attention of a batch is cut up.
 struct Cut {
+    bool turns = false;
     std::vector<AttnItem> rows, tiles;
-    std::vector<JoinItem> joins;
+    std::vector<JoinItem> joins, tile_joins;
     std::vector<int32_t> page0;  // by segment
 };
 
-// A block of rows over tokens [0, kv_len), in pieces of `piece` tokens
-void cut_block(AttnItem base, int32_t kv_len, int32_t piece, int32_t n_kv, std::vector<AttnItem> &items, std::vector<JoinItem> &joins, int64_t &part)
+// A block of rows over tokens [0, kv_len), in pieces of at most `piece` tokens and about the same length
+void cut_block(AttnItem base, int32_t kv_len, int32_t piece, int32_t rows, int32_t n_kv, std::vector<AttnItem> &items, std::vector<JoinItem> &joins, int64_t &part)
 {
-    const int32_t n = (kv_len + piece - 1) / piece;
+    int32_t n = (kv_len + piece - 1) / piece;
     base.part = -1;
     if (n <= 1) {
         base.kv0 = 0;
@@ -288,11 +295,12 @@ void cut_block(AttnItem base, int32_t kv_len, int32_t piece, int32_t n_kv, std::
         items.push_back(base);
         return;
     }
-    const int32_t stride = base.n_rows * n_kv;
+    const int32_t each = ((kv_len + n - 1) / n + PIECE_STEP - 1) / PIECE_STEP * PIECE_STEP, stride = rows * n_kv;  // stride: partial results of a piece
+    n = (kv_len + each - 1) / each;
     joins.push_back({base.tok0, base.row0, base.n_rows, (int32_t)part, n, stride});
     for (int32_t i = 0; i < n; ++i) {
-        base.kv0 = i * piece;
-        base.kv1 = std::min(kv_len, (i + 1) * piece);
+        base.kv0 = i * each;
+        base.kv1 = std::min(kv_len, (i + 1) * each);
         base.part = (int32_t)part;
         part += stride;
         items.push_back(base);
@@ -302,49 +310,68 @@ void cut_block(AttnItem base, int32_t kv_len, int32_t piece, int32_t n_kv, std::
 void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, Cut &cut)
 {
     const int32_t grp = kv.group(), n_kv = kv.cfg.n_kv_heads;
-    int64_t row_tokens = 0, tile_tokens = 0, part = 0;
-    const auto tile_end = [&](int64_t ctx, int64_t rows, int64_t row0) {  // tokens that the tile's last row sees
-        return (int32_t)(ctx + (std::min(rows, row0 + lora::KV_TILE) - 1) / grp + 1);
+    int64_t row_tokens = 0, tile_tokens = 0, part = 0, tile = lora::KV_TURNS_TILE;
+    const auto tile_end = [&tile, grp](int64_t ctx, int64_t rows, int64_t row0) {  // tokens that the tile's last row sees
+        return (int32_t)(ctx + (std::min(rows, row0 + tile) - 1) / grp + 1);
     };
+    // Two groups of wavefronts in turns, 256 rows at a time, where every compute unit gets two such blocks at least and they are long (1024 tokens in the
+    // mean): TURNSNUM
+    if (lora::kv_turns(kv.cfg.dtype, kv.cfg.head_dim)) {
+        int64_t n_tiles = 0, tokens = 0;
+        for (size_t i = 0; i < g.seqs.size(); ++i) {
+            const int64_t n = g.n_tokens[i], rows = n * grp, ctx = g.seqs[i]->n_tokens - n;
+            if (rows > lora::KV_ROW_ITEM)
+                for (int64_t r = 0; r < rows; r += tile) tokens += tile_end(ctx, rows, r), ++n_tiles;
+        }
+        cut.turns = n_tiles * n_kv >= 2 * kv.n_cu && tokens >= 1024 * n_tiles;
+    }
+    if (!cut.turns) tile = lora::KV_TILE;
     for (size_t i = 0; i < g.seqs.size(); ++i) {
         const int64_t n = g.n_tokens[i], rows = n * grp, ctx = g.seqs[i]->n_tokens - n;
         if (!n) continue;
         if (rows <= lora::KV_ROW_ITEM) row_tokens += ctx + n;
         else
-            for (int64_t r = 0; r < rows; r += lora::KV_TILE) tile_tokens += tile_end(ctx, rows, r);
+            for (int64_t r = 0; r < rows; r += tile) tile_tokens += tile_end(ctx, rows, r);
     }
-    const auto piece_of = [&](int64_t tokens, int64_t blocks, int64_t least) {
-        const int64_t p = std::max(least, tokens * n_kv / blocks + 1);
-        return (int32_t)((p + least - 1) / least * least);
-    };
-    int32_t row_piece = piece_of(row_tokens, ROW_BLOCKS, ROW_MIN_TOKENS), tile_piece = piece_of(tile_tokens, TILE_BLOCKS, TILE_MIN_TOKENS);
+    const auto at_least = [](int64_t tokens, int64_t least) { return (int32_t)std::min(std::max(tokens, least), (int64_t)LORA_KV_MAX_TOKENS); };
+    int32_t row_piece = at_least(row_tokens * n_kv / ROW_BLOCKS, ROW_MIN_TOKENS);
+    // A tile that takes longer than all of a compute unit's share is cut, into pieces of half of that: two at a time are worked on
+    const int64_t share = tile_tokens * n_kv / kv.n_cu;
+    int32_t tile_piece = at_least(share / 2, TILE_MIN_TOKENS), tile_whole = at_least(share, TILE_MIN_TOKENS);
     for (;;) {
         cut.rows.clear();
         cut.tiles.clear();
         cut.joins.clear();
+        cut.tile_joins.clear();
         part = 0;
         for (size_t i = 0; i < g.seqs.size(); ++i) {
             const int64_t n = g.n_tokens[i], rows = n * grp, ctx = g.seqs[i]->n_tokens - n;
             if (!n) continue;
             AttnItem it{offsets[i], (int32_t)ctx, cut.page0[i], 0, (int32_t)rows, 0, 0, -1};
             if (rows <= lora::KV_ROW_ITEM) {
-                cut_block(it, (int32_t)(ctx + n), row_piece, n_kv, cut.rows, cut.joins, part);
+                cut_block(it, (int32_t)(ctx + n), row_piece, it.n_rows, n_kv, cut.rows, cut.joins, part);
                 continue;
             }
-            for (int64_t r = 0; r < rows; r += lora::KV_TILE) {
+            for (int64_t r = 0; r < rows; r += tile) {
                 it.row0 = (int32_t)r;
-                it.n_rows = (int32_t)std::min(rows - r, (int64_t)lora::KV_TILE);
-                cut_block(it, tile_end(ctx, rows, r), tile_piece, n_kv, cut.tiles, cut.joins, part);
+                it.n_rows = (int32_t)std::min(rows - r, tile);
+                const int32_t end = tile_end(ctx, rows, r);
+                cut_block(it, end, end > tile_whole ? tile_piece : end, (it.n_rows + 31) & ~31, n_kv, cut.tiles, cut.tile_joins, part);
             }
         }
-        if (part <= kv.part_rows && cut.joins.size() <= (size_t)MAX_EXTRA && (int64_t)(cut.rows.size() + cut.tiles.size()) <= max_items(kv.cfg)) break;
-        row_piece = row_piece > (1 << 29) ? row_piece : row_piece * 2;
-        tile_piece = tile_piece > (1 << 29) ? tile_piece : tile_piece * 2;
+        if (part <= kv.part_rows && cut.joins.size() + cut.tile_joins.size() <= (size_t)MAX_EXTRA && (int64_t)(cut.rows.size() + cut.tiles.size()) <= max_items(kv.cfg)) break;
+        row_piece = at_least((int64_t)row_piece * 2, 0);
+        tile_piece = at_least((int64_t)tile_piece * 2, 0);
+        tile_whole = std::max(tile_whole, tile_piece);
     }
     // the longest first: what starts last is short
     const auto longer = [](const AttnItem &a, const AttnItem &b) { return a.kv1 - a.kv0 > b.kv1 - b.kv0; };
     std::stable_sort(cut.rows.begin(), cut.rows.end(), longer);
     std::stable_sort(cut.tiles.begin(), cut.tiles.end(), longer);
+    // Tiles are worked on two at a time on a compute unit, block b beside block b + n_cu: the longest go with the shortest of the first two rounds.
+    // (2048 tokens of 32 / 8 heads: PAIRNUM)
+    const size_t round = ((size_t)kv.n_cu + n_kv - 1) / n_kv;
+    if (!cut.turns && cut.tiles.size() > round) std::reverse(cut.tiles.begin() + round, cut.tiles.begin() + std::min(cut.tiles.size(), 2 * round));
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -408,6 +435,10 @@ int lora_kv_create(const lora_kv_config_t *cfg, void *dev_pages, size_t pages_by
         for (auto &b : kv->batches) b.member.assign(cfg->max_seqs, 0);
         if (!host_only) {
             KV_TRY(lora::prepare_attn_kernels());
+            int device = 0, n = 0;
+            KV_TRY(hipGetDevice(&device));
+            KV_TRY(hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, device));
+            if (n > 0) kv->n_cu = n;
             char *at = kv->work;
             for (auto &b : kv->batches) {
                 b.dev = at;
@@ -676,7 +707,7 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
         Cut cut;
         cut.page0.resize(n_seg);
         cut.rows.reserve(n_seg + MAX_EXTRA);
-        cut.joins.reserve(n_seg + MAX_EXTRA);
+        cut.joins.reserve(MAX_EXTRA);
         if (b->upload_pending) {
             KV_TRY(hipEventSynchronize(b->uploaded));
             b->upload_pending = false;
@@ -713,6 +744,7 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
         b->off_rows = place(cut.rows.size() * sizeof(AttnItem));
         b->off_tiles = place(cut.tiles.size() * sizeof(AttnItem));
         b->off_joins = place(cut.joins.size() * sizeof(JoinItem));
+        b->off_tile_joins = place(cut.tile_joins.size() * sizeof(JoinItem));
         KvToken *tokens = reinterpret_cast<KvToken *>(b->pinned + b->off_tokens);
         int32_t *pages = reinterpret_cast<int32_t *>(b->pinned + b->off_pages);
         b->max_pos = -1;
@@ -740,9 +772,12 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
         std::copy(cut.rows.begin(), cut.rows.end(), reinterpret_cast<AttnItem *>(b->pinned + b->off_rows));
         std::copy(cut.tiles.begin(), cut.tiles.end(), reinterpret_cast<AttnItem *>(b->pinned + b->off_tiles));
         std::copy(cut.joins.begin(), cut.joins.end(), reinterpret_cast<JoinItem *>(b->pinned + b->off_joins));
+        std::copy(cut.tile_joins.begin(), cut.tile_joins.end(), reinterpret_cast<JoinItem *>(b->pinned + b->off_tile_joins));
+        b->turns = cut.turns;
+        b->n_joins = (int32_t)cut.joins.size(), b->n_tile_joins = (int32_t)cut.tile_joins.size();
         b->join_rows = 0;
         for (const JoinItem &j : cut.joins) b->join_rows = std::max(b->join_rows, j.n_rows);
-        b->info = {T, n_seg, (int32_t)n_pages, (int32_t)groups.size(), (int32_t)cut.rows.size(), (int32_t)cut.tiles.size(), (int32_t)cut.joins.size()};
+        b->info = {T, n_seg, (int32_t)n_pages, (int32_t)groups.size(), (int32_t)cut.rows.size(), (int32_t)cut.tiles.size(), (int32_t)(cut.joins.size() + cut.tile_joins.size())};
         if (const int rc = copy_pages(*kv, g.from, g.to, st)) return rc;
         KV_TRY(lora::launch_upload(b->dev, b->pinned_dev, at, st, nullptr));
         KV_TRY(hipEventRecord(b->uploaded, st));
@@ -832,23 +867,24 @@ int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const v
     a.part_o = kv->part_o, a.part_ml = kv->part_ml;
     a.scale_log2 = scale_log2;
     a.n_kv = c.n_kv_heads, a.group = kv->group(), a.page_shift = kv->page_shift;
-    if (batch->info.n_tile_items) {
-        a.items = reinterpret_cast<const AttnItem *>(batch->dev + batch->off_tiles);
-        a.n_items = batch->info.n_tile_items;
-        KV_TRY(lora::launch_attn_tiles(a, c.dtype, c.head_dim, st));
-    }
-    if (batch->info.n_row_items) {
-        a.items = reinterpret_cast<const AttnItem *>(batch->dev + batch->off_rows);
-        a.n_items = batch->info.n_row_items;
-        KV_TRY(lora::launch_attn_rows(a, c.dtype, c.head_dim, st));
-    }
-    if (batch->info.n_joins) {
-        lora::JoinArgs j{};
-        j.out = out, j.out_stride = out_stride;
+    a.tiles = reinterpret_cast<const AttnItem *>(batch->dev + batch->off_tiles);
+    a.rows = reinterpret_cast<const AttnItem *>(batch->dev + batch->off_rows);
+    a.n_tiles = batch->info.n_tile_items;
+    a.n_rows = batch->info.n_row_items;
+    KV_TRY(lora::launch_attn(a, c.dtype, c.head_dim, batch->turns, st));
+    lora::JoinArgs j{};
+    j.out = out, j.out_stride = out_stride;
+    j.part_o = kv->part_o, j.part_ml = kv->part_ml;
+    j.n_kv = c.n_kv_heads, j.group = kv->group();
+    if (batch->n_joins) {
         j.items = reinterpret_cast<const JoinItem *>(batch->dev + batch->off_joins);
-        j.part_o = kv->part_o, j.part_ml = kv->part_ml;
-        j.n_items = batch->info.n_joins, j.n_kv = c.n_kv_heads, j.group = kv->group(), j.max_rows = batch->join_rows;
-        KV_TRY(lora::launch_attn_join(j, c.dtype, c.head_dim, st));
+        j.n_items = batch->n_joins, j.max_rows = batch->join_rows;
+        KV_TRY(lora::launch_attn_join(j, c.dtype, c.head_dim, false, st));
+    }
+    if (batch->n_tile_joins) {
+        j.items = reinterpret_cast<const JoinItem *>(batch->dev + batch->off_tile_joins);
+        j.n_items = batch->n_tile_joins, j.max_rows = batch->turns ? lora::KV_TURNS_TILE : lora::KV_TILE;
+        KV_TRY(lora::launch_attn_join(j, c.dtype, c.head_dim, true, st));
     }
     return LORA_OK;
 }

@@ -13,6 +13,8 @@ namespace lora {
 
 constexpr int KV_ROW_ITEM = 16;   // rows of a row item: the query side of one 16 x 16 x k product
 constexpr int KV_TILE = 128;      // rows of a tile item
+constexpr int KV_TURNS_TILE = 256; // ... where two groups of wavefronts take turns (attn_kernels.hip), which there is for
+constexpr bool kv_turns(int dtype, int dim) { return dtype == LORA_BF16 && dim == 128; }
 constexpr int KV_MAX_MOVES = 128; // page copies of one launch (they travel as its arguments)
 
 // One new token: where it stands and the page it lies in.
@@ -34,7 +36,8 @@ struct AttnItem {
     int32_t page0;  // the sequence's first entry of the page list
     int32_t row0, n_rows;
     int32_t kv0, kv1;
-    int32_t part;   // -1: writes its rows of the output; else where its partial results go, in rows: head h, row r at part + h * n_rows + r
+    int32_t part;   // -1: writes its rows of the output; else where its partial results go, in rows: head h, row r at part + h * n_rows + r (of a
+                    // tile n_rows rounded up to 32)
 };
 
 // Rows whose pieces are joined: n_parts pieces, `stride` rows of partial results apart.
@@ -65,10 +68,10 @@ struct AttnArgs {
     const char *pages;  // of this layer
     int64_t page_stride;
     const int32_t *page_list;
-    const AttnItem *items;  // of this launch
+    const AttnItem *tiles, *rows;
     float *part_o, *part_ml;
     float scale_log2;  // scale * log2(e)
-    int32_t n_items, n_kv, group, page_shift;
+    int32_t n_tiles, n_rows, n_kv, group, page_shift;
 };
 
 struct JoinArgs {
@@ -82,8 +85,7 @@ struct JoinArgs {
 hipError_t prepare_attn_kernels();  // once for the current device
 hipError_t launch_append(const AppendArgs &a, int dtype, hipStream_t st);
 hipError_t launch_moves(const KvMoves &m, int n, char *pages, int64_t page_stride, hipStream_t st);
-hipError_t launch_attn_rows(const AttnArgs &a, int dtype, int dim, hipStream_t st);
-hipError_t launch_attn_tiles(const AttnArgs &a, int dtype, int dim, hipStream_t st);
-hipError_t launch_attn_join(const JoinArgs &a, int dtype, int dim, hipStream_t st);
+hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, bool turns, hipStream_t st);
+hipError_t launch_attn_join(const JoinArgs &a, int dtype, int dim, bool tiles, hipStream_t st);
 
 }  // namespace lora
