@@ -110,6 +110,14 @@ template <> __device__ __forceinline__ void mma32<float>(floatx16 &acc, const ui
     for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], y[e], acc, 0, 0, 0);
 }
 
+// 16 bytes that nobody reads again soon: they leave what the caches hold alone
+__device__ __forceinline__ uint4 load_once(const void *p)
+{
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    const words w = __builtin_nontemporal_load(reinterpret_cast<const words *>(p));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // fmaxf of three values, of which none is a signalling NaN
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
@@ -308,9 +316,9 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it,
 #pragma unroll
         for (int c = 0; c < KC; ++c)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) s.k[t][c] = *reinterpret_cast<const uint4 *>(kp + (((4 * c + g) << a.page_shift) + k_lane + 4 * t) * U);
+            for (int t = 0; t < NT; ++t) s.k[t][c] = load_once(kp + (((4 * c + g) << a.page_shift) + k_lane + 4 * t) * U);
 #pragma unroll
-        for (int j = 0; j < VJ; ++j) s.v[j] = *reinterpret_cast<const uint4 *>(vp + (g * D + 16 * j + r) * U);
+        for (int j = 0; j < VJ; ++j) s.v[j] = load_once(vp + (g * D + 16 * j + r) * U);
     };
 
     float m = -FLT_MAX, l = 0.f;

@@ -13,6 +13,17 @@ template <typename E> struct alignas(16) Vals {
     E v[CHUNK<E>];
 };
 
+// 16 bytes past the caches: what is read once, and what is written here to be read when much else has been
+typedef uint32_t Words __attribute__((ext_vector_type(4)));
+template <typename E> __device__ __forceinline__ Vals<E> load_once(const E *p)
+{
+    return __builtin_bit_cast(Vals<E>, __builtin_nontemporal_load(reinterpret_cast<const Words *>(p)));
+}
+template <typename E> __device__ __forceinline__ void store_past(E *p, const Vals<E> &v)
+{
+    __builtin_nontemporal_store(__builtin_bit_cast(Words, v), reinterpret_cast<Words *>(p));
+}
+
 }  // namespace
 
 // Keys and queries: a thread takes two chunks of one token whose values turn together (HALVES: chunk p and the one rope_dim / 2 values on;
@@ -53,8 +64,8 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t key_
 #pragma unroll
         for (int k = 0; k < APPEND_HEADS; ++k) {
             const E *src = source(min(h0 + k, heads - 1));
-            x[k] = *reinterpret_cast<const Vals<E> *>(src + c0 * U);
-            y[k] = *reinterpret_cast<const Vals<E> *>(src + c1 * U);
+            x[k] = load_once(src + c0 * U);
+            y[k] = load_once(src + c1 * U);
         }
         if (turn) {
             // HALVES: entries c0 U .. c0 U + U - 1 turn x with y; NEIGHBOURS: entries p U .. turn the pairs of x, then those of y
@@ -93,8 +104,8 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t key_
                 *reinterpret_cast<Vals<E> *>(page + ((size_t)c1 << a.page_shift) * U) = y[k];
             } else if (h < heads) {
                 E *to = static_cast<E *>(a.q_out) + t * a.q_out_stride + (h - a.n_kv) * a.dim;
-                *reinterpret_cast<Vals<E> *>(to + c0 * U) = x[k];
-                *reinterpret_cast<Vals<E> *>(to + c1 * U) = y[k];
+                store_past(to + c0 * U, x[k]);
+                store_past(to + c1 * U, y[k]);
             }
         }
         return;
@@ -115,7 +126,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t key_
     if (grp.n == U) {
         Vals<E> in[U];
 #pragma unroll
-        for (int t = 0; t < U; ++t) in[t] = *reinterpret_cast<const Vals<E> *>(src + t * a.v_stride);
+        for (int t = 0; t < U; ++t) in[t] = load_once(src + t * a.v_stride);
 #pragma unroll
         for (int d = 0; d < U; ++d) {
             Vals<E> o;
@@ -125,7 +136,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t key_
         }
     } else {
         for (int t = 0; t < grp.n; ++t) {
-            const Vals<E> in = *reinterpret_cast<const Vals<E> *>(src + t * a.v_stride);
+            const Vals<E> in = load_once(src + t * a.v_stride);
 #pragma unroll
             for (int d = 0; d < U; ++d) to[(c * U + d) * U + at % U + t] = in.v[d];
         }
@@ -139,7 +150,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t key_
         const bool whole = __builtin_amdgcn_readlane(grp.n, from) == U;
         const uint64_t there = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(base >> 32), from) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)base, from);
         const int first = __builtin_amdgcn_readlane(c, from) * U;
-        if (whole) reinterpret_cast<Vals<E> *>(there)[first + lane] = mine[owner * U + ((lane & (U - 1)) ^ (owner & (U - 1)))];
+        if (whole) store_past(reinterpret_cast<E *>(there) + (first + lane) * U, mine[owner * U + ((lane & (U - 1)) ^ (owner & (U - 1)))]);
     }
 }
 
@@ -164,13 +175,13 @@ __global__ __launch_bounds__(256) void moves_kernel(KvMoves m, char *pages, int6
     const int64_t at = (int64_t)blockIdx.x * MOVE_BYTES + threadIdx.x * 16;
     const char *from = pages + m.from[blockIdx.y] * page_stride;
     char *to = pages + m.to[blockIdx.y] * page_stride;
-    uint4 v[4];
+    Words v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (at + i * 4096 < page_stride) v[i] = *reinterpret_cast<const uint4 *>(from + at + i * 4096);
+        if (at + i * 4096 < page_stride) v[i] = *reinterpret_cast<const Words *>(from + at + i * 4096);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (at + i * 4096 < page_stride) *reinterpret_cast<uint4 *>(to + at + i * 4096) = v[i];
+        if (at + i * 4096 < page_stride) __builtin_nontemporal_store(v[i], reinterpret_cast<Words *>(to + at + i * 4096));
 }
 
 hipError_t launch_moves(const KvMoves &m, int n, char *pages, int64_t page_stride, hipStream_t st)
