@@ -6,6 +6,7 @@
 // output is o / l.  Parts of a sequence join with M = max m_i as l = sum l_i exp2(m_i - M), o = sum o_i exp2(m_i - M).  A
 // token beyond the row's own position has weight 0 and its value is not multiplied at all.
 #include <cfloat>
+#include <type_traits>
 
 #include "kv_internal.h"
 #include "lora_device.h"
@@ -618,16 +619,21 @@ __device__ __forceinline__ void finish_tile(const AttnArgs &a, const AttnItem &i
     }
 }
 
-// Tiles of 128 rows, four wavefronts, two stages in LDS: one is requested while the other is worked on.
-template <typename E, int D> struct TileShape {
-    static constexpr int TK = sizeof(E) == 2 && D <= 128 ? 64 : 32;  // tokens of a stage
+// Tiles of 128 rows, four wavefronts, two stages in LDS: one is requested while the other is worked on.  Stages of 64 tokens where two
+// blocks on a compute unit have the registers and the LDS for them (bf16 heads of up to 128 values), else of 32.  With more tiles
+// than two for each compute unit (`many`) heads of 128 values are better off with stages of 32 and three blocks, whose waits for first
+// rows and last stores fall beside others' products.
+template <typename E, int D, bool MANY> struct TileShape {
+    static constexpr int TK = sizeof(E) == 2 && D <= 128 && !MANY ? 64 : 32;  // tokens of a stage
     static constexpr int LDS = 4 * TK * D * (int)sizeof(E);
+    static constexpr int BLOCKS = MANY ? 3 : LDS <= 80 * 1024 && sizeof(E) * D <= 256 ? 2 : 1;  // on a compute unit
 };
+template <typename E, int D> constexpr bool TILES_MANY = sizeof(E) == 2 && D == 128;
 
-template <typename E, int D>
+template <typename E, int D, int TK>
 __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it, int kv_head, unsigned char *lds)
 {
-    constexpr int TK = TileShape<E, D>::TK, U = CHUNK<E>, HALF = TK * D * (int)sizeof(E);
+    constexpr int U = CHUNK<E>, HALF = TK * D * (int)sizeof(E);
     typedef TileRows<E, D, TK> Rows;
     constexpr int SUB = Rows::SUB, QC = Rows::QC, DJ = Rows::DJ, PK = Rows::PK, NK = SUB * QC, NV = SUB * PK * DJ, AHEAD = 8;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
@@ -698,15 +704,15 @@ __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it,
     if (wave * 32 < it.n_rows) finish_tile<E, D, TK>(a, it, kv_head, wave, t);
 }
 
-template <typename E, int D>
-__global__ __launch_bounds__(256, (TileShape<E, D>::LDS <= 80 * 1024 && sizeof(E) * D <= 256) ? 2 : 1) void attn_tiles_kernel(AttnArgs a)
+template <typename E, int D, bool MANY>
+__global__ __launch_bounds__(256, (TileShape<E, D, MANY>::BLOCKS)) void attn_tiles_kernel(AttnArgs a)
 {
     extern __shared__ __align__(16) unsigned char lds[];
     const AttnItem it = a.tiles[blockIdx.x / a.n_kv];
-    attn_tile<E, D>(a, it, blockIdx.x % a.n_kv, lds);
+    attn_tile<E, D, TileShape<E, D, MANY>::TK>(a, it, blockIdx.x % a.n_kv, lds);
 }
 
-// The same for bf16 heads of 64 or 128 values and long prompts, where the scores' exponentials take the vector units as long as the products
+// The same for bf16 heads of 128 values and long prompts, where the scores' exponentials take the vector units as long as the products
 // take the matrix units: tiles of 256 rows, 8 wavefronts in two groups, one of each on a SIMD, that take turns.  In a time slot one group has
 // its products -- O += P V of the last stage, S = K Q of the next -- while the other has its weights -- P = exp2(S - m) --, and a barrier
 // ends the slot; group 1 is a slot behind group 0 all along.
@@ -905,33 +911,41 @@ hipError_t by_type(int dtype, int dim, F f)
 hipError_t prepare_attn_kernels()
 {
     hipError_t e = hipSuccess;
-    const auto lds = [&](auto t, auto d) {
-        using Shape = TileShape<decltype(t), decltype(d)::value>;
-        if (e == hipSuccess)
-            e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_tiles_kernel<decltype(t), decltype(d)::value>), hipFuncAttributeMaxDynamicSharedMemorySize, Shape::LDS);
+    const auto allow = [&](const void *kernel, int lds) {
+        if (e == hipSuccess) e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     };
-    e = hipFuncSetAttribute(reinterpret_cast<const void *>(&attn_turns_kernel<128>), hipFuncAttributeMaxDynamicSharedMemorySize, turn_lds(128));
     for (int dim : {64, 128, 256})
-        for (int dtype : {LORA_BF16, LORA_F32}) (void)by_type(dtype, dim, lds);
+        for (int dtype : {LORA_BF16, LORA_F32})
+            (void)by_type(dtype, dim, [&](auto t, auto d) {
+                typedef decltype(t) E;
+                constexpr int D = decltype(d)::value;
+                allow(reinterpret_cast<const void *>(&attn_tiles_kernel<E, D, false>), TileShape<E, D, false>::LDS);
+                if constexpr (TILES_MANY<E, D>) allow(reinterpret_cast<const void *>(&attn_tiles_kernel<E, D, true>), TileShape<E, D, true>::LDS);
+            });
+    allow(reinterpret_cast<const void *>(&attn_turns_kernel<128>), turn_lds(128));
     return e;
 }
 
-hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, bool turns, hipStream_t st)
+hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, bool turns, int n_cu, hipStream_t st)
 {
     const int64_t n_tiles = (int64_t)a.n_tiles * a.n_kv, n_rows = (int64_t)a.n_rows * a.n_kv;
-    if (n_tiles + n_rows + 16 > INT32_MAX) return hipErrorInvalidValue;
+    if (n_tiles > INT32_MAX || n_rows > INT32_MAX) return hipErrorInvalidValue;
     const dim3 tiles((unsigned)n_tiles), rows((unsigned)n_rows);
     return by_type(dtype, dim, [&](auto e, auto d) {
         typedef decltype(e) E;
         constexpr int D = decltype(d)::value;
-        constexpr unsigned lds = TileShape<E, D>::LDS;
+        bool done = n_tiles == 0;
         if constexpr (kv_turns(sizeof(E) == 2 ? LORA_BF16 : LORA_F32, D))
-            if (turns) {
-                if (n_tiles) hipLaunchKernelGGL((attn_turns_kernel<D>), tiles, dim3(512), turn_lds(D), st, a);
-                if (n_rows) hipLaunchKernelGGL((attn_rows_kernel<E, D>), rows, dim3(64 * ROW_WAVES), 0, st, a);
-                return;
+            if (!done && turns) {
+                hipLaunchKernelGGL((attn_turns_kernel<D>), tiles, dim3(512), turn_lds(D), st, a);
+                done = true;
             }
-        if (n_tiles) hipLaunchKernelGGL((attn_tiles_kernel<E, D>), tiles, dim3(256), lds, st, a);
+        if constexpr (TILES_MANY<E, D>)
+            if (!done && n_tiles > 2 * n_cu) {
+                hipLaunchKernelGGL((attn_tiles_kernel<E, D, true>), tiles, dim3(256), (TileShape<E, D, true>::LDS), st, a);
+                done = true;
+            }
+        if (!done) hipLaunchKernelGGL((attn_tiles_kernel<E, D, false>), tiles, dim3(256), (TileShape<E, D, false>::LDS), st, a);
         if (n_rows) hipLaunchKernelGGL((attn_rows_kernel<E, D>), rows, dim3(64 * ROW_WAVES), 0, st, a);
     });
 }

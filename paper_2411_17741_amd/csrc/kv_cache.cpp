@@ -871,7 +871,7 @@ int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const v
     a.rows = reinterpret_cast<const AttnItem *>(batch->dev + batch->off_rows);
     a.n_tiles = batch->info.n_tile_items;
     a.n_rows = batch->info.n_row_items;
-    KV_TRY(lora::launch_attn(a, c.dtype, c.head_dim, batch->turns, st));
+    KV_TRY(lora::launch_attn(a, c.dtype, c.head_dim, batch->turns, kv->n_cu, st));
     lora::JoinArgs j{};
     j.out = out, j.out_stride = out_stride;
     j.part_o = kv->part_o, j.part_ml = kv->part_ml;

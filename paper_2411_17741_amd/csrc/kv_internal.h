@@ -85,7 +85,7 @@ struct JoinArgs {
 hipError_t prepare_attn_kernels();  // once for the current device
 hipError_t launch_append(const AppendArgs &a, int dtype, hipStream_t st);
 hipError_t launch_moves(const KvMoves &m, int n, char *pages, int64_t page_stride, hipStream_t st);
-hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, bool turns, hipStream_t st);
+hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, bool turns, int n_cu, hipStream_t st);
 hipError_t launch_attn_join(const JoinArgs &a, int dtype, int dim, bool tiles, hipStream_t st);
 
 }  // namespace lora
