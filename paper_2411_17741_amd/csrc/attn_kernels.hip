@@ -286,13 +286,13 @@ template <int D> struct RowsLds {
     int redo;
 };
 
-template <typename E, int D>
+template <typename E, int D, bool ALONE>
 __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it, int kv_head, RowsLds<D> &lds)
 {
     constexpr int U = CHUNK<E>, NT = U / 4, STEP = 16 * NT, KC = D / U / 4, VJ = D / 16, NW = ROW_WAVES, DP = RowsLds<D>::DP;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int in_page = (1 << a.page_shift) - 1;
-    if (threadIdx.x == 0) lds.redo = 0;
+    if (!ALONE && threadIdx.x == 0) lds.redo = 0;
 
     const int row = it.row0 + min(r, it.n_rows - 1);
     const int end = it.ctx + row / a.group + 1;  // tokens that this lane's row sees
@@ -304,7 +304,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it,
     }
 
     const int steps = (it.kv1 - it.kv0 + STEP - 1) / STEP, per_wave = (steps + NW - 1) / NW;
-    const int first = it.kv0 + wave * per_wave * STEP, last = min(it.kv1, first + per_wave * STEP);
+    const int first = ALONE ? it.kv0 : it.kv0 + wave * per_wave * STEP, last = ALONE ? it.kv1 : min(it.kv1, first + per_wave * STEP);
     PageList pages(a.page_list + it.page0, (it.kv1 - 1) >> a.page_shift, min(first, it.kv1 - 1) >> a.page_shift);
     const auto page_at = [&](int pos) { return pages[pos >> a.page_shift]; };
 
@@ -354,12 +354,22 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it,
             l += p[e];
         }
         const uint4 w = weights(p);
+        uint4 w_rest = w;  // what the weights lost when they were rounded: there is time for a second product, and the outputs are as exact as with fp32 weights
+        if constexpr (sizeof(E) == 2) {
+            const Vals<E> rounded = __builtin_bit_cast(Vals<E>, w);
+#pragma unroll
+            for (int e = 0; e < U; ++e) p[e] -= (float)rounded.v[e];
+            w_rest = weights(p);
+        }
         if (pos + STEP > it.kv1) {  // behind the sequence's last token: whatever is there, it is no value
 #pragma unroll
             for (int j = 0; j < VJ; ++j) s.v[j] = first_values<E>(s.v[j], it.kv1 - pos - U * g);
         }
 #pragma unroll
-        for (int j = 0; j < VJ; ++j) mma16<E>(o[j], s.v[j], w);
+        for (int j = 0; j < VJ; ++j) {
+            mma16<E>(o[j], s.v[j], w);
+            if constexpr (sizeof(E) == 2) mma16<E>(o[j], s.v[j], w_rest);
+        }
     };
 
     if (first < last) {
@@ -391,17 +401,29 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it,
         for (int j = 0; j < VJ; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) none += o[j][i] * 0.f;
-        __syncthreads();
-        if (none != 0.f) lds.redo = 1;
-        __syncthreads();
-        if (lds.redo) {
-            for (int i = wave; i < it.n_rows; i += NW) {
+        bool redo = __any(none != 0.f);
+        if constexpr (!ALONE) {
+            __syncthreads();
+            if (redo) lds.redo = 1;
+            __syncthreads();
+            redo = lds.redo;
+        }
+        if (redo) {
+            for (int i = ALONE ? 0 : wave; i < it.n_rows; i += ALONE ? 1 : NW) {
                 RowState<E, D> st;
                 one_row<E, D>(a, it, kv_head, it.row0 + i, it.kv0, it.kv1, st);
                 put_row<E, D, false>(a, it, kv_head, i, st);
             }
             return;
         }
+    }
+    if constexpr (ALONE) {  // (items that one wavefront has to itself are whole)
+        if (r >= it.n_rows) return;
+        const float f = l == 0.f ? 0.f : 1.f / l;
+        E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D;
+#pragma unroll
+        for (int j = 0; j < VJ; ++j) put_four(out + 16 * j + 4 * g, o[j] * f);
+        return;
     }
     if (g == 0) lds.m[wave][r] = m, lds.l[wave][r] = l;
 #pragma unroll
@@ -437,12 +459,21 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it,
     }
 }
 
+// The first n_rows items of the list have a block for each key-value head; the others, n_short of them, are short and a wavefront does one
 template <typename E, int D>
 __global__ __launch_bounds__(64 * ROW_WAVES, 2) void attn_rows_kernel(AttnArgs a)
 {
     __shared__ RowsLds<D> lds;
-    const AttnItem it = a.rows[blockIdx.x / a.n_kv];
-    attn_rows<E, D>(a, it, blockIdx.x % a.n_kv, lds);
+    const uint32_t blocks = (uint32_t)a.n_rows * a.n_kv;
+    if (blockIdx.x < blocks) {
+        const AttnItem it = a.rows[blockIdx.x / a.n_kv];
+        attn_rows<E, D, false>(a, it, blockIdx.x % a.n_kv, lds);
+    } else {
+        const uint32_t n = (blockIdx.x - blocks) * ROW_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (n >= (uint32_t)a.n_short * a.n_kv) return;
+        const AttnItem it = a.rows[a.n_rows + n / a.n_kv];
+        attn_rows<E, D, true>(a, it, n % a.n_kv, lds);
+    }
 }
 
 // Tiles of rows of one key-value head (its query heads token by token): wavefronts of 32 rows share the keys and values, which go through
@@ -928,7 +959,7 @@ hipError_t prepare_attn_kernels()
 
 hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, bool turns, int n_cu, hipStream_t st)
 {
-    const int64_t n_tiles = (int64_t)a.n_tiles * a.n_kv, n_rows = (int64_t)a.n_rows * a.n_kv;
+    const int64_t n_tiles = (int64_t)a.n_tiles * a.n_kv, n_rows = (int64_t)a.n_rows * a.n_kv + ((int64_t)a.n_short * a.n_kv + ROW_WAVES - 1) / ROW_WAVES;
     if (n_tiles > INT32_MAX || n_rows > INT32_MAX) return hipErrorInvalidValue;
     const dim3 tiles((unsigned)n_tiles), rows((unsigned)n_rows);
     return by_type(dtype, dim, [&](auto e, auto d) {

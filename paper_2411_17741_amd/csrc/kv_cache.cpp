@@ -31,6 +31,8 @@ constexpr size_t PART_BYTES = (size_t)64 << 20;
 constexpr int SPARE_BATCHES = 2;
 // The attention over long caches with few rows is cut along the cache until about so many blocks have work, in pieces of no fewer tokens.
 constexpr int ROW_BLOCKS = 512, ROW_MIN_TOKENS = 512;
+// Tokens times head_dim up to which a wavefront may have an item to itself.
+constexpr int ROW_SHORT_VALUES = 16384;
 constexpr int TILE_MIN_TOKENS = 512;
 constexpr int PIECE_STEP = 64;  // pieces begin at multiples of it: a whole number of every kernel's steps, in one page or at the start of one
 constexpr int MAX_EXTRA = 2048;  // pieces beyond one for each block of rows
@@ -52,7 +54,7 @@ struct lora_kv_batch {
     hipEvent_t uploaded = nullptr;
     lora_kv_batch_info_t info{};
     int32_t max_pos = -1;  // of the batch's tokens
-    int32_t n_joins = 0, n_tile_joins = 0, join_rows = 0;  // join_rows: the most rows of a join of row items
+    int32_t n_joins = 0, n_tile_joins = 0, join_rows = 0, n_short = 0;  // join_rows: the most rows of a join of row items
     bool turns = false;
     size_t off_tokens = 0, off_groups = 0, off_pages = 0, off_rows = 0, off_tiles = 0, off_joins = 0, off_tile_joins = 0;
     std::vector<uint8_t> member;  // by sequence slot
@@ -279,6 +281,7 @@ void reserve(const lora_kv &kv, Growth &g)
 // How the attention of a batch is cut up.
 struct Cut {
     bool turns = false;
+    int32_t n_short = 0;  // of the rows' items, at the list's end
     std::vector<AttnItem> rows, tiles;
     std::vector<JoinItem> joins, tile_joins;
     std::vector<int32_t> page0;  // by segment
@@ -315,7 +318,8 @@ void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
         return (int32_t)(ctx + (std::min(rows, row0 + tile) - 1) / grp + 1);
     };
     // Two groups of wavefronts in turns, 256 rows at a time, where every compute unit gets two such blocks at least and they are long (1024 tokens in the
-    // mean): TURNSNUM
+    // mean).  Measured, independent wavefronts -> turns: 8192 tokens with 32 / 8 heads 532 -> 472 us, 4096 161 -> 149, 2048 + 2048 86 -> 80; 2048 alone 56 -> 70,
+    // 4 x 1024 with 32 / 32 heads 57 -> 60.
     if (lora::kv_turns(kv.cfg.dtype, kv.cfg.head_dim)) {
         int64_t n_tiles = 0, tokens = 0;
         for (size_t i = 0; i < g.seqs.size(); ++i) {
@@ -368,8 +372,14 @@ void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     const auto longer = [](const AttnItem &a, const AttnItem &b) { return a.kv1 - a.kv0 > b.kv1 - b.kv0; };
     std::stable_sort(cut.rows.begin(), cut.rows.end(), longer);
     std::stable_sort(cut.tiles.begin(), cut.tiles.end(), longer);
-    // Tiles are worked on two at a time on a compute unit, block b beside block b + n_cu: the longest go with the shortest of the first two rounds.
-    // (2048 tokens of 32 / 8 heads: PAIRNUM)
+    // Where there are more items than blocks fit on the machine, a wavefront has a short one to itself: a block on it is mostly waiting for its first
+    // loads and its last stores.  Measured: 512 requests of 20 tokens with 32 heads of 128 96 -> 51 us, 256 of 120 94 -> 78 us; with 200 to 450 tokens, and
+    // with half as many for heads of 256, nothing is gained.
+    size_t n_short = 0;
+    while (n_short < cut.rows.size() && cut.rows[cut.rows.size() - 1 - n_short].part < 0 && cut.rows[cut.rows.size() - 1 - n_short].kv1 <= ROW_SHORT_VALUES / kv.cfg.head_dim) ++n_short;
+    cut.n_short = (int64_t)n_short * n_kv > 2 * kv.n_cu ? (int32_t)n_short : 0;
+    // Tiles are worked on two at a time on a compute unit, block b beside block b + n_cu: the longest go with the shortest of the first two rounds
+    // (2048 tokens with 32 / 8 heads: 70 -> 55 us).
     const size_t round = ((size_t)kv.n_cu + n_kv - 1) / n_kv;
     if (!cut.turns && cut.tiles.size() > round) std::reverse(cut.tiles.begin() + round, cut.tiles.begin() + std::min(cut.tiles.size(), 2 * round));
 }
@@ -774,6 +784,7 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
         std::copy(cut.joins.begin(), cut.joins.end(), reinterpret_cast<JoinItem *>(b->pinned + b->off_joins));
         std::copy(cut.tile_joins.begin(), cut.tile_joins.end(), reinterpret_cast<JoinItem *>(b->pinned + b->off_tile_joins));
         b->turns = cut.turns;
+        b->n_short = cut.n_short;
         b->n_joins = (int32_t)cut.joins.size(), b->n_tile_joins = (int32_t)cut.tile_joins.size();
         b->join_rows = 0;
         for (const JoinItem &j : cut.joins) b->join_rows = std::max(b->join_rows, j.n_rows);
@@ -870,7 +881,8 @@ int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const v
     a.tiles = reinterpret_cast<const AttnItem *>(batch->dev + batch->off_tiles);
     a.rows = reinterpret_cast<const AttnItem *>(batch->dev + batch->off_rows);
     a.n_tiles = batch->info.n_tile_items;
-    a.n_rows = batch->info.n_row_items;
+    a.n_rows = batch->info.n_row_items - batch->n_short;
+    a.n_short = batch->n_short;
     KV_TRY(lora::launch_attn(a, c.dtype, c.head_dim, batch->turns, kv->n_cu, st));
     lora::JoinArgs j{};
     j.out = out, j.out_stride = out_stride;

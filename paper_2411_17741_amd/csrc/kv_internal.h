@@ -71,7 +71,7 @@ struct AttnArgs {
     const AttnItem *tiles, *rows;
     float *part_o, *part_ml;
     float scale_log2;  // scale * log2(e)
-    int32_t n_tiles, n_rows, n_kv, group, page_shift;
+    int32_t n_tiles, n_rows, n_short, n_kv, group, page_shift;  // n_short: items behind the n_rows that a wavefront takes alone
 };
 
 struct JoinArgs {

@@ -110,13 +110,13 @@ class KvCache:
 
     def _rows(self, t: torch.Tensor, name: str, batch, heads: int):
         """(address, values between tokens) of [T][heads][head_dim] or [T][heads * head_dim], the heads of a token one after the other"""
-        d, shape, stride = self.head_dim, t.shape, t.stride()
+        d, n, shape, stride = self.head_dim, batch.n_tokens, t.shape, t.stride()
         flat = len(shape) == 2 and shape[1] == heads * d and stride[1] == 1
-        if not (flat or (len(shape) == 3 and shape[1] == heads and shape[2] == d and stride[2] == 1 and (heads == 1 or stride[1] == d))):
-            raise ValueError(f"{name}: [{batch.n_tokens}][{heads}][{d}] with the heads of a token in a row is wanted, got {tuple(shape)}, strides {stride}")
-        if shape[0] != batch.n_tokens or t.dtype != self.dtype or not t.is_cuda:
-            raise ValueError(f"{name}: {batch.n_tokens} tokens of {self.dtype} on the GPU are wanted, got {tuple(shape)} of {t.dtype} on {t.device}")
-        return t.data_ptr(), stride[0] if shape[0] > 1 else heads * d
+        if not (flat or (len(shape) == 3 and shape[1] == heads and shape[2] == d and stride[2] == 1 and (stride[1] == d or heads == 1))):
+            raise ValueError(f"{name}: [{n}][{heads}][{d}] with the heads of a token in a row is wanted, got {tuple(shape)}, strides {stride}")
+        if shape[0] != n or t.dtype is not self.dtype or not t.is_cuda:
+            raise ValueError(f"{name}: {n} tokens of {self.dtype} on the GPU are wanted, got {tuple(shape)} of {t.dtype} on {t.device}")
+        return t.data_ptr(), stride[0] if n > 1 else heads * d
 
     def append(self, batch, layer: int, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
                rope: Optional[torch.Tensor] = None, neighbours: bool = False, stream: Optional[torch.cuda.Stream] = None) -> None:
