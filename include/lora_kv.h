@@ -89,8 +89,8 @@ int lora_kv_seq_fork(lora_kv_t *kv, int64_t parent, int32_t n, const int64_t *id
 
 /* Add n_tokens[i] tokens to sequence ids[i] whose keys and values the caller puts into the pages himself (restored from
  * elsewhere, say): takes pages -- the free ones with the lowest numbers --, copies a shared page that the tokens begin in.
- * LORA_E_NOMEM if there are too few pages, LORA_E_NOTFOUND, LORA_E_INVAL (a sequence named twice, a negative count), LORA_E_STATE on a
- * stream that is captured. */
+ * Batches with a sequence whose page was copied can't be used any more.  LORA_E_NOMEM if there are too few pages, LORA_E_NOTFOUND,
+ * LORA_E_INVAL (a sequence named twice, a negative count), LORA_E_STATE on a stream that is captured. */
 int lora_kv_seq_extend(lora_kv_t *kv, int32_t n, const int64_t *ids, const int32_t *n_tokens, void *stream);
 
 /* Keep the first n_tokens[i] tokens (rejected drafts, a repeated iteration); pages that hold none of them are given
@@ -130,6 +130,7 @@ int lora_kv_stats(const lora_kv_t *kv, lora_kv_stats_t *out);
 /* The next iteration: segment i is tokens [seg_offsets[i], seg_offsets[i + 1]) of the packed batch and the next tokens of sequence
  * seg_seq[i]; seg_offsets[0] = 0; a segment may be empty.  The sequences get these tokens (pages as lora_kv_seq_extend takes them),
  * and the batch's lists -- pages, what is appended where, how the attention is cut up -- are uploaded.  One batch serves every layer.
+ * (The host waits here only if the lists' memory is still on its way up for a batch that was destroyed: two more than n_batches are kept.)
  * LORA_E_INVAL (malformed offsets, a sequence named twice), LORA_E_NOTFOUND, LORA_E_NOMEM (pages, the config's maxima, batches
  * alive), LORA_E_STATE on a stream that is captured. */
 int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, const int32_t *seg_offsets, void *stream,

@@ -217,7 +217,6 @@ template <typename E> __device__ __forceinline__ void put_four(E *to, const floa
 
 // Entries of a sequence's page list, 64 at a time in the lanes of a register: the page of a step is named without a trip to memory.
 struct PageList {
-    static constexpr int BACK = 4;  // entries may be asked for that lie so many before the highest asked for yet
     const int32_t *list;
     int last, at, held;  // the last entry there is; lane i holds entry at + i
     __device__ __forceinline__ PageList(const int32_t *l, int last_entry, int first) : list(l), last(last_entry) { fetch(first); }
@@ -227,10 +226,10 @@ struct PageList {
         held = list[min(at + (int)(threadIdx.x & 63), last)];
         asm volatile("" : "+v"(held));  // waited for here: not wherever an entry is used
     }
-    __device__ __forceinline__ int operator[](int entry)  // the same in all lanes
+    __device__ __forceinline__ int operator[](int entry)  // the same in all lanes, no smaller than in earlier calls
     {
         entry = min(entry, last);
-        if (entry - at >= 64) fetch(entry - BACK);
+        if (entry - at >= 64) fetch(entry);
         return __builtin_amdgcn_readlane(held, entry - at);
     }
 };

@@ -178,10 +178,11 @@ size_t list_bytes(const lora_kv_config_t &c)
 // Work of a call on a stream waits for the work of the one before it on another.
 int in_order(lora_kv &kv, hipStream_t st)
 {
+    if (kv.any_stream && kv.last == st) return LORA_OK;
     hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
     KV_TRY(hipStreamIsCapturing(st, &cs));
     if (cs != hipStreamCaptureStatusNone) return LORA_OK;  // the caller's to order
-    if (kv.any_stream && kv.last != st) {
+    if (kv.any_stream) {
         KV_TRY(hipEventRecord(kv.order_ev, kv.last));
         KV_TRY(hipStreamWaitEvent(st, kv.order_ev, 0));
     }
@@ -253,6 +254,7 @@ void grow(lora_kv &kv, Growth &g)
         Seq &s = *g.seqs[i];
         if (!g.n_tokens[i]) continue;
         if ((s.n_tokens & (kv.cfg.page_tokens - 1)) && kv.refs[s.pages.back()] > 1) {
+            kv.drop_batches_with(s);  // they name the page that is left to the others
             const int32_t old = s.pages.back();
             s.pages.back() = kv.take();
             kv.give_back(old);

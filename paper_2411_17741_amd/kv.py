@@ -121,12 +121,13 @@ class KvCache:
     def append(self, batch, layer: int, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
                rope: Optional[torch.Tensor] = None, neighbours: bool = False, stream: Optional[torch.cuda.Stream] = None) -> None:
         """rope: [positions][rope_dim] fp32, the cosines of a position and then its sines.  q_out: q itself if not given."""
-        kp, ks = self._rows(k, "k", batch, self.n_kv_heads)
-        vp, vs = self._rows(v, "v", batch, self.n_kv_heads)
+        rows = self._rows
+        kp, ks = rows(k, "k", batch, self.n_kv_heads)
+        vp, vs = rows(v, "v", batch, self.n_kv_heads)
         qp = qs = op = os_ = 0
         if q is not None:
-            qp, qs = self._rows(q, "q", batch, self.n_heads)
-            op, os_ = (qp, qs) if q_out is None else self._rows(q_out, "q_out", batch, self.n_heads)
+            qp, qs = rows(q, "q", batch, self.n_heads)
+            op, os_ = (qp, qs) if q_out is None else rows(q_out, "q_out", batch, self.n_heads)
         elif q_out is not None:
             raise ValueError("q_out without q")
         rp = rn = rd = 0

@@ -81,6 +81,13 @@ def test_append_out_of_a_wider_buffer_and_without_queries(dtype):
     _run([(999, 1)], 1, 1, 64, 64, dtype, 64, False)
 
 
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_append_of_large_batches(neighbours):
+    """Tokens times heads beyond the size from which a thread takes more heads, in numbers of heads that its share does not divide."""
+    _run([(0, 2900), (5, 77), (64, 1)], 42, 7, 64, 64, "bf16", 64, neighbours, layers=1, layer=0)
+    _run([(3, 2990)], 40, 4, 64, 32, "f32", 32, neighbours, strided=True, layers=1, layer=0)
+
+
 def test_what_is_no_number_stays_where_it_was_put():
     """A NaN or infinity in one token changes that token's bits alone, and a value is stored as it is."""
     from paper_2411_17741_amd.kv import KvCache

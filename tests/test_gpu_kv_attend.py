@@ -133,6 +133,72 @@ def test_long_caches_are_cut_and_joined(segs, heads, kv, dim, dtype):
         s.close()
 
 
+def test_a_cache_of_many_pages_and_a_long_sequence():
+    _check([(131073, 1), (70000, 3)], 2, 1, 64, seed=15)
+    _check([(66000, 40)], 2, 2, 64, page=32, seed=16)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pages_beyond_4_gb(dtype):
+    """Pages whose place in the buffer passes 32 bits, in bytes and in values: read, written, copied and moved."""
+    B, KvCache = _mods()
+    dt, u = (torch.bfloat16, 8) if dtype == "bf16" else (torch.float32, 4)
+    kv, dim, page, layers, e = 8, 128, 256, 2, 2 if dtype == "bf16" else 4
+    page_bytes = layers * 2 * kv * page * dim * e
+    low = (9 << 30) // page_bytes  # 9 GB of pages that another sequence holds
+    cache = KvCache(layers, 8, kv, dim, low + 12, page_tokens=page, max_seqs=4, max_batch_seqs=3, max_batch_tokens=1400, dtype=B.LORA_BF16 if dtype == "bf16" else B.LORA_F32)
+    try:
+        cache.add([0, 1, 2])
+        cache.extend([0], [low * page])
+        gen = torch.Generator().manual_seed(1)
+        off = np.asarray([0, 900, 1200], np.int32)
+        batch = cache.batch([1, 2], off)
+        assert min(cache.pages_of(1)) >= low and low * page_bytes > 2**33
+        qkv = torch.randn(1200, 24, dim, generator=gen).to(dt)
+        dev = qkv.cuda()
+        cache.append(batch, 1, dev[:, 8:16], dev[:, 16:])
+        out = torch.empty(1200, 8, dim, dtype=dt, device="cuda")
+
+        def look(rows, at, tokens, seqs):
+            """Output rows `rows` of `tokens` positions from `at` of the sequences against the definition."""
+            got = out.float().cpu().numpy()
+            f = qkv.float().numpy()
+            for i, r in zip(seqs, rows):
+                base = {1: 0, 2: 900, 3: 0}[i]
+                for h in (0, 7):
+                    want, mass, reach = kv_plain.attend(f[base + at : base + at + tokens, h], f[base : base + at + tokens, 8 + h], f[base : base + at + tokens, 16 + h], at, 0.09)
+                    bound = Setup.bound(fake, want, mass, reach)
+                    assert (np.abs(got[r : r + tokens, h] - want) <= bound).all(), (i, h)
+
+        fake = type("Shape", (), dict(dt=dt, dim=dim, segs=[(900, 0)]))
+        cache.attend(batch, 1, dev[:, :8], out, 0.09)
+        torch.cuda.synchronize()
+        look([0], 0, 900, [1])
+        look([900], 0, 300, [2])
+        # one token each, of a fork as well: its last page is copied up there; then everything moves down
+        cache.batch_destroy(batch)
+        cache.fork(1, [3], 899)
+        cache.truncate([1, 2], [899, 299])
+        for moved in (False, True):
+            if moved:
+                cache.truncate([1, 2, 3], [899, 299, 899])
+                cache.free([0])
+                assert cache.compact() > 0 and max(cache.pages_of(3).max(), cache.pages_of(2).max()) < 12
+            one = cache.batch([1, 2, 3], [0, 1, 2, 3])
+            k = torch.stack([dev[899], dev[1199], dev[899]])
+            cache.append(one, 1, k[:, 8:16], k[:, 16:])
+            out.fill_(float("nan"))
+            cache.attend(one, 1, k[:, :8], out[:3], 0.09)
+            torch.cuda.synchronize()
+            look([0], 899, 1, [1])
+            look([1], 299, 1, [2])
+            look([2], 899, 1, [3])
+            cache.batch_destroy(one)
+        assert cache.stats().pages_copied > 0
+    finally:
+        cache.close()
+
+
 def test_long_prompts():
     _check([(0, 1500), (0, 700)], 4, 2, 128, seed=5)
     _check([(513, 1023)], 3, 3, 64, page=32, seed=6)
@@ -310,11 +376,18 @@ def test_refusals():
         for t in (q[:5], q.float(), q.cpu(), q[..., :32], q.transpose(0, 1)):
             with pytest.raises(ValueError):
                 s.cache.attend(s.batch, 0, t, out, 0.1)
-        # a batch whose sequences were cut back, moved or ended is of no use any more
-        s.cache.truncate([1], [3])
+        # a batch whose sequences were cut back, moved, ended or got a page of their own is of no use any more
+        s.cache.fork(1, [2])
+        assert call() == B.LORA_OK
+        s.cache.extend([1], [1])
         assert call() == B.LORA_E_STATE
         s.cache.batch_destroy(s.batch)
-        assert call() == B.LORA_E_INVAL and B.lora_kv_batch_destroy(h, s.batch) == B.LORA_E_INVAL
+        s.batch = s.cache.batch([0, 1], [0, 1, 1])
+        s.cache.free([2])
+        s.cache.truncate([1], [3])
+        assert call(batch=s.batch) == B.LORA_E_STATE
+        s.cache.batch_destroy(s.batch)
+        assert call(batch=s.batch) == B.LORA_E_INVAL and B.lora_kv_batch_destroy(h, s.batch) == B.LORA_E_INVAL
         s.batch = s.cache.batch([0, 1], [0, 1, 2])
         s.cache.free([0])
         assert B.lora_kv_attend(h, s.batch, 0, q.data_ptr(), row, out.data_ptr(), row, 0.1, st) == B.LORA_E_STATE
