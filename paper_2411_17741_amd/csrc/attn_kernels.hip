@@ -530,6 +530,38 @@ template <typename E, int D, int TK> struct Stages {
     }
 };
 
+// The same for stages of 32 tokens, STRIDE tokens apart.  They lie in one page, their values in one run: what differs between lanes is the same for all stages.
+template <typename E, int D, int STRIDE> struct Steps {
+    static constexpr int PER = 32 * D * (int)sizeof(E) / 4096;
+    PageList pages;
+    const char *head, *v_from;  // the head's keys in page 0; the values of the stage whose keys were asked for last
+    uint32_t page_stride, k_lane, v_lane;
+    int page_shift, loader, values_at, t0;
+    __device__ __forceinline__ Steps(const AttnArgs &a, const AttnItem &it, int kv_head, int which_loader, int first)
+        : pages(a.page_list + it.page0, (it.kv1 - 1) >> a.page_shift, it.kv0 >> a.page_shift), v_from(nullptr), page_stride((uint32_t)a.page_stride), page_shift(a.page_shift),
+          loader(which_loader), values_at(((a.n_kv * D) << a.page_shift) * (int)sizeof(E)), t0(first)
+    {
+        const int lane = threadIdx.x & 63;
+        head = a.pages + ((size_t)kv_head * D << a.page_shift) * sizeof(E);
+        k_lane = (((2 * loader + lane / 32) << a.page_shift) + key_of_row<E>(lane & 31)) * 16;
+        v_lane = (loader * 64 + lane) * 16;
+    }
+    __device__ __forceinline__ void keys(unsigned char *to)  // of the next stage
+    {
+        const int page = pages[t0 >> page_shift], at = t0 & ((1 << page_shift) - 1);
+        const char *const base = head + (uint64_t)page_stride * (uint32_t)page;
+        v_from = base + values_at + at * (D * (int)sizeof(E));
+#pragma unroll
+        for (int i = 0; i < PER; ++i) request16(reinterpret_cast<const __bf16 *>(base + (at + (8 * i << page_shift)) * 16 + k_lane), to + loader * 1024 + i * 4096);
+        t0 += STRIDE;
+    }
+    __device__ __forceinline__ void values(unsigned char *to)  // of the stage whose keys were asked for last
+    {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) request16(reinterpret_cast<const __bf16 *>(v_from + i * 4096 + v_lane), to + loader * 1024 + i * 4096);
+    }
+};
+
 // 32 rows of a wavefront: lane r + 32 h has row r's queries (chunks 2 c + h), its maximum, half of its weights and outputs.  s: scores of
 // the stage; w: its weights; o[j][4 k + i]: value 32 j + 8 k + 4 h + i
 template <typename E, int D, int TK> struct TileRows {
@@ -655,25 +687,233 @@ __device__ __forceinline__ void finish_tile(const AttnArgs &a, const AttnItem &i
     }
 }
 
-// Tiles of 128 rows, four wavefronts, two stages in LDS: one is requested while the other is worked on.  Stages of 64 tokens where two
-// blocks on a compute unit have the registers and the LDS for them (bf16 heads of up to 128 values), else of 32.  With more tiles
-// than two for each compute unit (`many`) heads of 128 values are better off with stages of 32 and three blocks, whose waits for first
-// rows and last stores fall beside others' products.
-template <typename E, int D, bool MANY> struct TileShape {
-    static constexpr int TK = sizeof(E) == 2 && D <= 128 && !MANY ? 64 : 32;  // tokens of a stage
-    static constexpr int LDS = 4 * TK * D * (int)sizeof(E);
-    static constexpr int BLOCKS = MANY ? 3 : LDS <= 80 * 1024 && sizeof(E) * D <= 256 ? 2 : 1;  // on a compute unit
+// Tiles of 128 rows, four wavefronts, stages of 32 tokens.  A wavefront has three stages in hand at a time, so that products and exponentials, which take about as long as each
+// other, run side by side: in the step of stage t
+//   O += P V of stage t - 1, beside the second half of its P and the maximum of the scores of stage t;   S = K Q of stage t + 1, beside the first half of P = exp2(S - m) of stage t.
+// Keys and values are requested DEEP steps ahead, values of stage t together with keys of stage t + 1, which the step of stage t waits for.  The keys of a stage are read in one step,
+// its values in that and the next: there are DEEP + 1 places for keys in LDS, DEEP + 2 for values.
+// A step of a wavefront alone on its SIMD takes 0.50 us with heads of 128, 0.9 with 256, 0.45 with 64, where its products are 0.27, 0.53 and 0.13: the rest are its other instructions,
+// one after the other, and the barrier.  5000 tokens with 32 / 8 heads of 256: 431 us, 0.95 PFLOP/s (585 with products and exponentials in turns); 8000 with heads of 64: 297 us.
+template <typename E, int D> struct TileShape {
+    static constexpr int TK = 32, PLACE = TK * D * (int)sizeof(E);
+    static constexpr int BLOCKS = PLACE <= 8192 ? 2 : 1;  // on a compute unit
+    static constexpr int DEEP = PLACE <= 16384 ? 3 : 1;
+    static constexpr int LDS = (2 * DEEP + 3) * PLACE;
 };
-template <typename E, int D> constexpr bool TILES_MANY = sizeof(E) == 2 && D == 128;
 
+template <typename E, int D, int GROUPS>
+__device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it, int kv_head, unsigned char *all_lds)
+{
+    typedef TileShape<E, D> Shape;
+    constexpr int TK = Shape::TK, PLACE = Shape::PLACE, DEEP = Shape::DEEP, K_END = (DEEP + 1) * PLACE, V_END = (DEEP + 2) * PLACE;
+    constexpr int U = CHUNK<E>;
+    typedef TileRows<E, D, TK> Rows;
+    constexpr int QC = Rows::QC, DJ = Rows::DJ, PK = Rows::PK, NV = PK * DJ, AHEAD = NV < 8 ? NV : 8, STRIDE = GROUPS * TK;
+    typedef Steps<E, D, STRIDE> Requests;
+    constexpr int PER = Requests::PER;
+    static_assert(NV % AHEAD == 0 && QC % AHEAD == 0, "the operands' ring");
+    const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = id & 3, group = id >> 2, r = lane & 31, h = lane >> 5;
+    unsigned char *const lds = all_lds + group * Shape::LDS;
+    const int begin = it.kv0 + group * TK;
+    Requests stages(a, it, kv_head, wave, begin);
+    Rows t(a, it, kv_head, wave);
+    stages.keys(lds);
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i) {  // past the last stage too
+        stages.values(lds + K_END + i * PLACE);
+        stages.keys(lds + (i + 1) * PLACE);
+    }
+    // stages that there are (of the first group), and of which the wavefront's rows see something
+    const int n = (it.kv1 - it.kv0 + STRIDE - 1) / STRIDE, most = min(it.kv1, it.ctx + (it.row0 + min(wave * 32 + 31, it.n_rows - 1)) / a.group + 1);
+    const int mine = wave * 32 < it.n_rows && most > begin ? (most - begin + STRIDE - 1) / STRIDE : 0;
+    int put_k = 0, put_v = DEEP * PLACE, k = 0, v = V_END - PLACE, v_last = 0, t0 = begin;  // places of the next requests, of the step's keys and values, of the values of the stage before
+    const auto after = [](int place, int end) { return place + PLACE == end ? 0 : place + PLACE; };
+    const auto meet = [] {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto next = [&] {  // a step begins: its operands have come, and nobody reads any more what its requests will overwrite
+        wait_requests<(DEEP - 1) * 2 * PER>();
+        meet();
+        v_last = v;
+        v = after(v, V_END);
+        k = after(k, K_END);
+    };
+    const auto request = [&] {
+        __builtin_amdgcn_sched_barrier(0);
+        stages.values(lds + K_END + put_v);
+        stages.keys(lds + put_k);
+        put_v = after(put_v, V_END);
+        put_k = after(put_k, K_END);
+    };
+    uint4 fk[AHEAD], fv[AHEAD];
+    const unsigned char *const my_keys = lds + (h * TK + r) * 16, *const my_values = lds + K_END + (h * D + r) * 16;
+    const auto key = [&](int i) { return from_lds(my_keys + k + 2 * i * TK * 16); };
+    const auto value = [&](int i, int place) { return from_lds(my_values + place + (2 * (i / DJ) * D + 32 * (i % DJ)) * 16); };
+    const float scale_log2 = a.scale_log2;
+    const auto hide = [&](floatx16 &s) {  // the scores of tokens that rows don't see
+        if (t0 + TK > t.least) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (t0 + i / U * 2 * U + h * U + i % U >= t.end) s[i] = -INFINITY;
+        }
+    };
+    const auto follow = [&](float top) {  // the maximum of a stage's scores
+        top = max32(top) * scale_log2;
+        if (__any(top > t.m + SLACK)) {
+            const float now = fmaxf(t.m, top), fade = __builtin_amdgcn_exp2f(t.m - now);
+            t.m = now;
+            t.l *= fade;
+#pragma unroll
+            for (int j = 0; j < DJ; ++j) t.o[j] *= fade;
+        }
+    };
+    float p[U];
+    const auto weigh = [&](const floatx16 &s, int from, int to) {  // scores from .. to - 1 of a lane's 16 become weights
+#pragma unroll
+        for (int i = from; i < to; ++i) {
+            p[i % U] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale_log2, -t.m));
+            t.l += p[i % U];
+            if (i % U == U - 1) {
+                t.w[i / U] = weights(p);
+                asm volatile("" : "+v"(t.w[i / U].x), "+v"(t.w[i / U].y), "+v"(t.w[i / U].z), "+v"(t.w[i / U].w), "+v"(t.l));  // now, not where they are used
+            }
+        }
+    };
+    // the step of stage t0: its scores are in s, those of the stage before in `other`, where the next stage's come; operands come out of LDS well before they are used, in
+    // this order, whatever the compiler thinks of it
+    const auto step = [&](floatx16 &s, floatx16 &other, auto first) {
+        constexpr bool FIRST = decltype(first)::value;
+        next();
+        hide(s);
+        float top = -INFINITY;
+        if constexpr (FIRST) {
+            request();
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) fk[i] = key(i);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < NV; ++e) {
+                __builtin_amdgcn_sched_barrier(0);
+                mma32<E>(t.o[e % DJ], fv[e % AHEAD], t.w[e / DJ]);
+                if (e + AHEAD < NV) fv[e % AHEAD] = value(e + AHEAD, v_last);
+                if (e < NV / 2) {
+#pragma unroll
+                    for (int i = e * 2 * AHEAD / NV; i < (e + 1) * 2 * AHEAD / NV; ++i) fk[i] = key(i);
+                    weigh(other, 8 + e * 16 / NV, 8 + (e + 1) * 16 / NV);
+                } else {  // (the compiler does not know of the instructions that max3 is: products lie between it and the scores')
+#pragma unroll
+                    for (int i = (e - NV / 2) * 16 / NV; i < (e + 1 - NV / 2) * 16 / NV; ++i) top = max3(top, s[2 * i], s[2 * i + 1]);
+                }
+                if (e == 1) request();  // (beside the products)
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        follow(top);
+#pragma unroll
+        for (int i = 0; i < QC; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (i == 0) mma32_first<E>(other, fk[i % AHEAD], t.q[i]);
+            else mma32<E>(other, fk[i % AHEAD], t.q[i]);
+            if (i + AHEAD < QC) fk[i % AHEAD] = key(i + AHEAD);
+            if (i < QC / 2) {
+#pragma unroll
+                for (int j = i * 2 * AHEAD / QC; j < (i + 1) * 2 * AHEAD / QC; ++j) fv[j] = value(j, v);
+            }
+            weigh(s, i * 8 / QC, (i + 1) * 8 / QC);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        t0 += STRIDE;
+    };
+    t.wait_for_queries();
+    wait_requests<DEEP * 2 * PER>();
+    meet();
+    if (mine) {
+        floatx16 s0, s1;
+#pragma unroll
+        for (int i = 0; i < QC; ++i) {
+            if (i == 0) mma32_first<E>(s0, key(i), t.q[i]);
+            else mma32<E>(s0, key(i), t.q[i]);
+        }
+        const int last = mine - 1;
+        if (last) {
+            step(s0, s1, std::true_type{});
+            int i = 1;
+            for (; i + 1 < last; i += 2) {
+                step(s1, s0, std::false_type{});
+                step(s0, s1, std::false_type{});
+            }
+            if (i < last) {
+                step(s1, s0, std::false_type{});
+                weigh(s1, 8, 16);
+            } else {
+                weigh(s0, 8, 16);
+                s0 = s1;
+            }
+        }
+        // the last stage, whose tokens may end before it does: whatever is behind the last, it is no value
+        next();
+        request();
+        if (last) {
+#pragma unroll
+            for (int e = 0; e < NV; ++e) mma32<E>(t.o[e % DJ], e < AHEAD ? fv[e] : value(e, v_last), t.w[e / DJ]);
+        }
+        hide(s0);
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s0[i]);
+        follow(top);
+        weigh(s0, 0, 16);
+#pragma unroll
+        for (int e = 0; e < NV; ++e) mma32<E>(t.o[e % DJ], first_values<E>(value(e, v), it.kv1 - t0 - (2 * (e / DJ) + h) * U), t.w[e / DJ]);
+    }
+    for (int i = mine; i < n; ++i) {
+        next();
+        request();
+    }
+    wait_requests<0>();  // none is on its way to LDS when the block ends
+    if constexpr (GROUPS == 2) {  // the second group's maxima, sums and outputs go to the first through LDS
+        meet();
+        floatx4 *const other = reinterpret_cast<floatx4 *>(all_lds) + wave * DJ * 4 * 64 + lane;
+        float2 *const other_ml = reinterpret_cast<float2 *>(all_lds + 4 * 32 * D * 4) + wave * 64 + lane;
+        if (group == 1) {
+#pragma unroll
+            for (int j = 0; j < DJ; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) other[(4 * j + i) * 64] = floatx4{t.o[j][4 * i], t.o[j][4 * i + 1], t.o[j][4 * i + 2], t.o[j][4 * i + 3]};
+            *other_ml = make_float2(t.m, t.l);
+        }
+        __syncthreads();
+        if (group == 1) return;
+        const float2 ml = *other_ml;
+        const float m = fmaxf(t.m, ml.x), f0 = __builtin_amdgcn_exp2f(t.m - m), f1 = __builtin_amdgcn_exp2f(ml.x - m);
+        t.m = m;
+        t.l = t.l * f0 + ml.y * f1;
+#pragma unroll
+        for (int j = 0; j < DJ; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const floatx4 x = other[(4 * j + i) * 64];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t.o[j][4 * i + e] = t.o[j][4 * i + e] * f0 + x[e] * f1;
+            }
+    }
+    if (wave * 32 < it.n_rows) finish_tile<E, D, TK>(a, it, kv_head, wave, t);
+}
+
+// Without the steps' overlap, whose registers would leave room for two blocks on a compute unit, for three: their wavefronts' products and exponentials fall beside each other's, and
+// so do waits for first rows and last stores.  Two stages in LDS: one is requested while the other is worked on.
 template <typename E, int D, int TK>
-__device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it, int kv_head, unsigned char *lds)
+__device__ __forceinline__ void attn_tile_plain(const AttnArgs &a, const AttnItem &it, int kv_head, unsigned char *lds)
 {
     constexpr int U = CHUNK<E>, HALF = TK * D * (int)sizeof(E);
     typedef TileRows<E, D, TK> Rows;
     constexpr int SUB = Rows::SUB, QC = Rows::QC, DJ = Rows::DJ, PK = Rows::PK, NK = SUB * QC, NV = SUB * PK * DJ, AHEAD = 8;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
-    Stages<E, D, TK> stages(a, it, kv_head, wave, it.kv0);
+    Steps<E, D, TK> stages(a, it, kv_head, wave, it.kv0);
     stages.keys(lds);
     stages.values(lds + HALF);
     Rows t(a, it, kv_head, wave);
@@ -740,27 +980,50 @@ __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it,
     if (wave * 32 < it.n_rows) finish_tile<E, D, TK>(a, it, kv_head, wave, t);
 }
 
-template <typename E, int D, bool MANY>
-__global__ __launch_bounds__(256, (TileShape<E, D, MANY>::BLOCKS)) void attn_tiles_kernel(AttnArgs a)
+template <typename E, int D>
+__global__ __launch_bounds__(256, (TileShape<E, D>::BLOCKS)) void attn_tiles_kernel(AttnArgs a)
 {
     extern __shared__ __align__(16) unsigned char lds[];
     const AttnItem it = a.tiles[blockIdx.x / a.n_kv];
-    attn_tile<E, D, TileShape<E, D, MANY>::TK>(a, it, blockIdx.x % a.n_kv, lds);
+    attn_tile<E, D, 1>(a, it, blockIdx.x % a.n_kv, lds);
+}
+
+template <typename E, int D> constexpr int MANY_LDS = 4 * 32 * D * (int)sizeof(E);
+template <typename E, int D>
+__global__ __launch_bounds__(256, 3) void attn_many_kernel(AttnArgs a)
+{
+    extern __shared__ __align__(16) unsigned char lds[];
+    const AttnItem it = a.tiles[blockIdx.x / a.n_kv];
+    attn_tile_plain<E, D, 32>(a, it, blockIdx.x % a.n_kv, lds);
 }
 
 // Tiles, and the blocks of the row items behind them: one launch where all of them are on the machine at once anyway (64 / 8 heads of 128, prompts of 2 to 234
 // tokens 16.1 -> 11.7 us; 196 single tokens beside 3 prompts with 40 / 8 heads, two layers 107 -> 88).  Of larger batches a launch for each does better: here the rows
 // have the tiles' occupancy.
 template <typename E, int D>
-__global__ __launch_bounds__(256, (TileShape<E, D, false>::BLOCKS)) void attn_both_kernel(AttnArgs a)
+__global__ __launch_bounds__(256, (TileShape<E, D>::BLOCKS)) void attn_both_kernel(AttnArgs a)
 {
     extern __shared__ __align__(16) unsigned char lds[];
-    static_assert(TileShape<E, D, false>::LDS >= (int)sizeof(RowsLds<D>), "the rows' LDS is the tiles'");
+    static_assert(TileShape<E, D>::LDS >= (int)sizeof(RowsLds<D>), "the rows' LDS is the tiles'");
     const uint32_t tiles = (uint32_t)a.n_tiles * a.n_kv;
     if (blockIdx.x < tiles) {
         const AttnItem it = a.tiles[blockIdx.x / a.n_kv];
-        attn_tile<E, D, TileShape<E, D, false>::TK>(a, it, blockIdx.x % a.n_kv, lds);
+        attn_tile<E, D, 1>(a, it, blockIdx.x % a.n_kv, lds);
     } else {
+        attn_rows_block<E, D>(a, blockIdx.x - tiles, *reinterpret_cast<RowsLds<D> *>(lds));
+    }
+}
+
+// No more blocks than compute units: eight wavefronts to a tile, two on a SIMD, in two groups that take its stages in turn and join their results at the end
+template <typename E, int D>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_pairs_kernel(AttnArgs a)
+{
+    extern __shared__ __align__(16) unsigned char lds[];
+    const uint32_t tiles = (uint32_t)a.n_tiles * a.n_kv;
+    if (blockIdx.x < tiles) {
+        const AttnItem it = a.tiles[blockIdx.x / a.n_kv];
+        attn_tile<E, D, 2>(a, it, blockIdx.x % a.n_kv, lds);
+    } else if (threadIdx.x < 64 * ROW_WAVES) {
         attn_rows_block<E, D>(a, blockIdx.x - tiles, *reinterpret_cast<RowsLds<D> *>(lds));
     }
 }
@@ -972,15 +1235,19 @@ hipError_t prepare_attn_kernels()
             (void)by_type(dtype, dim, [&](auto t, auto d) {
                 typedef decltype(t) E;
                 constexpr int D = decltype(d)::value;
-                allow(reinterpret_cast<const void *>(&attn_tiles_kernel<E, D, false>), TileShape<E, D, false>::LDS);
-                allow(reinterpret_cast<const void *>(&attn_both_kernel<E, D>), TileShape<E, D, false>::LDS);
-                if constexpr (TILES_MANY<E, D>) allow(reinterpret_cast<const void *>(&attn_tiles_kernel<E, D, true>), TileShape<E, D, true>::LDS);
+                allow(reinterpret_cast<const void *>(&attn_tiles_kernel<E, D>), TileShape<E, D>::LDS);
+                allow(reinterpret_cast<const void *>(&attn_both_kernel<E, D>), TileShape<E, D>::LDS);
+                if constexpr (kv_many(sizeof(E) == 2 ? LORA_BF16 : LORA_F32, D)) allow(reinterpret_cast<const void *>(&attn_many_kernel<E, D>), MANY_LDS<E, D>);
+                if constexpr (kv_pairs(sizeof(E) == 2 ? LORA_BF16 : LORA_F32, D)) {
+                    static_assert(2 * TileShape<E, D>::LDS >= 4 * (32 * D * 4 + 512), "one group's results in LDS");
+                    allow(reinterpret_cast<const void *>(&attn_pairs_kernel<E, D>), 2 * TileShape<E, D>::LDS);
+                }
             });
     allow(reinterpret_cast<const void *>(&attn_turns_kernel<128>), turn_lds(128));
     return e;
 }
 
-hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, bool turns, int n_cu, hipStream_t st)
+hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, KvTiles way, int n_cu, hipStream_t st)
 {
     const int64_t n_tiles = (int64_t)a.n_tiles * a.n_kv, n_rows = (int64_t)a.n_rows * a.n_kv + ((int64_t)a.n_short * a.n_kv + ROW_WAVES - 1) / ROW_WAVES;
     if (n_tiles > INT32_MAX || n_rows > INT32_MAX) return hipErrorInvalidValue;
@@ -988,22 +1255,27 @@ hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, bool turns, int n_
     return by_type(dtype, dim, [&](auto e, auto d) {
         typedef decltype(e) E;
         constexpr int D = decltype(d)::value;
-        if (n_tiles && n_rows && !turns && n_tiles + n_rows <= TileShape<E, D, false>::BLOCKS * n_cu) {
-            hipLaunchKernelGGL((attn_both_kernel<E, D>), dim3((unsigned)(n_tiles + n_rows)), dim3(256), (TileShape<E, D, false>::LDS), st, a);
+        if (n_tiles && n_rows && way == KV_TILES_PLAIN && n_tiles + n_rows <= TileShape<E, D>::BLOCKS * n_cu) {
+            hipLaunchKernelGGL((attn_both_kernel<E, D>), dim3((unsigned)(n_tiles + n_rows)), dim3(256), (TileShape<E, D>::LDS), st, a);
             return;
         }
+        if constexpr (kv_pairs(sizeof(E) == 2 ? LORA_BF16 : LORA_F32, D))
+            if (way == KV_TILES_PAIRS) {
+                hipLaunchKernelGGL((attn_pairs_kernel<E, D>), dim3((unsigned)(n_tiles + n_rows)), dim3(512), (2 * TileShape<E, D>::LDS), st, a);
+                return;
+            }
         bool done = n_tiles == 0;
         if constexpr (kv_turns(sizeof(E) == 2 ? LORA_BF16 : LORA_F32, D))
-            if (!done && turns) {
+            if (!done && way == KV_TILES_TURNS) {
                 hipLaunchKernelGGL((attn_turns_kernel<D>), tiles, dim3(512), turn_lds(D), st, a);
                 done = true;
             }
-        if constexpr (TILES_MANY<E, D>)
-            if (!done && n_tiles > 2 * n_cu) {
-                hipLaunchKernelGGL((attn_tiles_kernel<E, D, true>), tiles, dim3(256), (TileShape<E, D, true>::LDS), st, a);
+        if constexpr (kv_many(sizeof(E) == 2 ? LORA_BF16 : LORA_F32, D))
+            if (!done && way == KV_TILES_MANY) {
+                hipLaunchKernelGGL((attn_many_kernel<E, D>), tiles, dim3(256), (MANY_LDS<E, D>), st, a);
                 done = true;
             }
-        if (!done) hipLaunchKernelGGL((attn_tiles_kernel<E, D, false>), tiles, dim3(256), (TileShape<E, D, false>::LDS), st, a);
+        if (!done) hipLaunchKernelGGL((attn_tiles_kernel<E, D>), tiles, dim3(256), (TileShape<E, D>::LDS), st, a);
         if (n_rows) hipLaunchKernelGGL((attn_rows_kernel<E, D>), rows, dim3(64 * ROW_WAVES), 0, st, a);
     });
 }

@@ -55,7 +55,7 @@ struct lora_kv_batch {
     lora_kv_batch_info_t info{};
     int32_t max_pos = -1;  // of the batch's tokens
     int32_t n_joins = 0, n_tile_joins = 0, join_rows = 0, n_short = 0;  // join_rows: the most rows of a join of row items
-    bool turns = false;
+    lora::KvTiles way = lora::KV_TILES_PLAIN;
     size_t off_tokens = 0, off_groups = 0, off_pages = 0, off_rows = 0, off_tiles = 0, off_joins = 0, off_tile_joins = 0;
     std::vector<uint8_t> member;  // by sequence slot
 };
@@ -282,7 +282,7 @@ void reserve(const lora_kv &kv, Growth &g)
 
 // How the attention of a batch is cut up.
 struct Cut {
-    bool turns = false;
+    lora::KvTiles way = lora::KV_TILES_PLAIN;
     int32_t n_short = 0;  // of the rows' items, at the list's end
     std::vector<AttnItem> rows, tiles;
     std::vector<JoinItem> joins, tile_joins;
@@ -315,35 +315,47 @@ void cut_block(AttnItem base, int32_t kv_len, int32_t piece, int32_t rows, int32
 void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, Cut &cut)
 {
     const int32_t grp = kv.group(), n_kv = kv.cfg.n_kv_heads;
-    int64_t row_tokens = 0, tile_tokens = 0, part = 0, tile = lora::KV_TURNS_TILE;
+    int64_t row_tokens = 0, tile_tokens = 0, n_tiles = 0, longest = 0, part = 0, tile = lora::KV_TURNS_TILE;
     const auto tile_end = [&tile, grp](int64_t ctx, int64_t rows, int64_t row0) {  // tokens that the tile's last row sees
         return (int32_t)(ctx + (std::min(rows, row0 + tile) - 1) / grp + 1);
     };
     // Two groups of wavefronts in turns, 256 rows at a time, where every compute unit gets two such blocks at least and they are long (1024 tokens in the
-    // mean).  Measured, independent wavefronts -> turns: 8192 tokens with 32 / 8 heads 532 -> 472 us, 4096 161 -> 149, 2048 + 2048 86 -> 80; 2048 alone 56 -> 70,
-    // 4 x 1024 with 32 / 32 heads 57 -> 60.
+    // mean).  Measured, tiles of 128 rows -> turns: 16384 tokens with 64 / 8 heads 3966 -> 3640 us, 8192 with 32 / 8 525 -> 481, 4096 146 -> 133, 2048 + 2048 81 -> 79; 2048 + 2048 with
+    // 32 / 32 heads 80 -> 84.
     if (lora::kv_turns(kv.cfg.dtype, kv.cfg.head_dim)) {
-        int64_t n_tiles = 0, tokens = 0;
+        int64_t tokens = 0;
         for (size_t i = 0; i < g.seqs.size(); ++i) {
             const int64_t n = g.n_tokens[i], rows = n * grp, ctx = g.seqs[i]->n_tokens - n;
             if (rows > lora::KV_ROW_ITEM)
                 for (int64_t r = 0; r < rows; r += tile) tokens += tile_end(ctx, rows, r), ++n_tiles;
         }
-        cut.turns = n_tiles * n_kv >= 2 * kv.n_cu && tokens >= 1024 * n_tiles;
+        if (n_tiles * n_kv >= 2 * kv.n_cu && tokens >= 1024 * n_tiles) cut.way = lora::KV_TILES_TURNS;
     }
-    if (!cut.turns) tile = lora::KV_TILE;
+    if (cut.way != lora::KV_TILES_TURNS) tile = lora::KV_TILE;
+    n_tiles = 0;
     for (size_t i = 0; i < g.seqs.size(); ++i) {
         const int64_t n = g.n_tokens[i], rows = n * grp, ctx = g.seqs[i]->n_tokens - n;
         if (!n) continue;
         if (rows <= lora::KV_ROW_ITEM) row_tokens += ctx + n;
         else
-            for (int64_t r = 0; r < rows; r += tile) tile_tokens += tile_end(ctx, rows, r);
+            for (int64_t r = 0; r < rows; r += tile, ++n_tiles) {
+                const int64_t end = tile_end(ctx, rows, r);
+                tile_tokens += end;
+                longest = std::max(longest, end);
+            }
     }
     const auto at_least = [](int64_t tokens, int64_t least) { return (int32_t)std::min(std::max(tokens, least), (int64_t)LORA_KV_MAX_TOKENS); };
     int32_t row_piece = at_least(row_tokens * n_kv / ROW_BLOCKS, ROW_MIN_TOKENS);
     // A tile that takes longer than all of a compute unit's share is cut, into pieces of half of that: two at a time are worked on
     const int64_t share = tile_tokens * n_kv / kv.n_cu;
     int32_t tile_piece = at_least(share / 2, TILE_MIN_TOKENS), tile_whole = at_least(share, TILE_MIN_TOKENS);
+    // No more blocks than compute units and no tile of over 1024 tokens: for heads of 64, whose steps are mostly instructions of one wavefront after the other, two groups of
+    // wavefronts share a tile's tokens, and tiles stay whole (700 tokens with 32 heads 16.5 -> 12.5 us, with 32 / 8 heads 15.3 -> 12.3).  Longer ones, and heads of 128, do as well
+    // or better with pieces.
+    if (cut.way == lora::KV_TILES_PLAIN && lora::kv_pairs(kv.cfg.dtype, kv.cfg.head_dim) && n_tiles * n_kv <= kv.n_cu && longest <= 2 * TILE_MIN_TOKENS) {
+        cut.way = lora::KV_TILES_PAIRS;
+        tile_whole = 2 * TILE_MIN_TOKENS;
+    }
     for (;;) {
         cut.rows.clear();
         cut.tiles.clear();
@@ -365,10 +377,22 @@ void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
                 cut_block(it, end, end > tile_whole ? tile_piece : end, (it.n_rows + 31) & ~31, n_kv, cut.tiles, cut.tile_joins, part);
             }
         }
+        if (cut.way == lora::KV_TILES_PAIRS && (int64_t)(cut.tiles.size() + cut.rows.size()) * n_kv > kv.n_cu) {
+            cut.way = lora::KV_TILES_PLAIN;
+            tile_whole = at_least(share, TILE_MIN_TOKENS);
+            continue;
+        }
         if (part <= kv.part_rows && cut.joins.size() + cut.tile_joins.size() <= (size_t)MAX_EXTRA && (int64_t)(cut.rows.size() + cut.tiles.size()) <= max_items(kv.cfg)) break;
         row_piece = at_least((int64_t)row_piece * 2, 0);
         tile_piece = at_least((int64_t)tile_piece * 2, 0);
         tile_whole = std::max(tile_whole, tile_piece);
+    }
+    // Three blocks on a compute unit, where the tiles fill more than three for each, or more than two and are short (256 tokens in the mean): bf16 heads of 128, two blocks -> three,
+    // 8 x 500 tokens with 32 heads 42.6 -> 39.2 us, 6 x 300 24.4 -> 17.3; but 2048 with 40 heads 68.2 -> 74.5.
+    if (cut.way == lora::KV_TILES_PLAIN && lora::kv_many(kv.cfg.dtype, kv.cfg.head_dim)) {
+        int64_t blocks = (int64_t)cut.tiles.size() * n_kv, tokens = 0;
+        for (const AttnItem &t : cut.tiles) tokens += t.kv1 - t.kv0;
+        if (blocks > 3 * kv.n_cu || (blocks > 2 * kv.n_cu && tokens < 256 * (int64_t)cut.tiles.size())) cut.way = lora::KV_TILES_MANY;
     }
     // the longest first: what starts last is short
     const auto longer = [](const AttnItem &a, const AttnItem &b) { return a.kv1 - a.kv0 > b.kv1 - b.kv0; };
@@ -383,7 +407,7 @@ void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     // Tiles are worked on two at a time on a compute unit, block b beside block b + n_cu: the longest go with the shortest of the first two rounds
     // (2048 tokens with 32 / 8 heads: 70 -> 55 us).
     const size_t round = ((size_t)kv.n_cu + n_kv - 1) / n_kv;
-    if (!cut.turns && cut.tiles.size() > round) std::reverse(cut.tiles.begin() + round, cut.tiles.begin() + std::min(cut.tiles.size(), 2 * round));
+    if (cut.way != lora::KV_TILES_TURNS && cut.tiles.size() > round) std::reverse(cut.tiles.begin() + round, cut.tiles.begin() + std::min(cut.tiles.size(), 2 * round));
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -785,7 +809,7 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
         std::copy(cut.tiles.begin(), cut.tiles.end(), reinterpret_cast<AttnItem *>(b->pinned + b->off_tiles));
         std::copy(cut.joins.begin(), cut.joins.end(), reinterpret_cast<JoinItem *>(b->pinned + b->off_joins));
         std::copy(cut.tile_joins.begin(), cut.tile_joins.end(), reinterpret_cast<JoinItem *>(b->pinned + b->off_tile_joins));
-        b->turns = cut.turns;
+        b->way = cut.way;
         b->n_short = cut.n_short;
         b->n_joins = (int32_t)cut.joins.size(), b->n_tile_joins = (int32_t)cut.tile_joins.size();
         b->join_rows = 0;
@@ -885,7 +909,7 @@ int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const v
     a.n_tiles = batch->info.n_tile_items;
     a.n_rows = batch->info.n_row_items - batch->n_short;
     a.n_short = batch->n_short;
-    KV_TRY(lora::launch_attn(a, c.dtype, c.head_dim, batch->turns, kv->n_cu, st));
+    KV_TRY(lora::launch_attn(a, c.dtype, c.head_dim, batch->way, kv->n_cu, st));
     lora::JoinArgs j{};
     j.out = out, j.out_stride = out_stride;
     j.part_o = kv->part_o, j.part_ml = kv->part_ml;
@@ -897,7 +921,7 @@ int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const v
     }
     if (batch->n_tile_joins) {
         j.items = reinterpret_cast<const JoinItem *>(batch->dev + batch->off_tile_joins);
-        j.n_items = batch->n_tile_joins, j.max_rows = batch->turns ? lora::KV_TURNS_TILE : lora::KV_TILE;
+        j.n_items = batch->n_tile_joins, j.max_rows = batch->way == lora::KV_TILES_TURNS ? lora::KV_TURNS_TILE : lora::KV_TILE;
         KV_TRY(lora::launch_attn_join(j, c.dtype, c.head_dim, true, st));
     }
     return LORA_OK;

@@ -15,6 +15,11 @@ constexpr int KV_ROW_ITEM = 16;   // rows of a row item: the query side of one 1
 constexpr int KV_TILE = 128;      // rows of a tile item
 constexpr int KV_TURNS_TILE = 256; // ... where two groups of wavefronts take turns (attn_kernels.hip), which there is for
 constexpr bool kv_turns(int dtype, int dim) { return dtype == LORA_BF16 && dim == 128; }
+// How a batch's tiles are worked on (attn_kernels.hip): four wavefronts to a tile and two blocks on a compute unit, three blocks, or two groups of four wavefronts to a tile; all three
+// with tiles of KV_TILE rows; two groups in turns
+enum KvTiles { KV_TILES_PLAIN, KV_TILES_MANY, KV_TILES_PAIRS, KV_TILES_TURNS };
+constexpr bool kv_many(int dtype, int dim) { return dtype == LORA_BF16 && dim == 128; }
+constexpr bool kv_pairs(int dtype, int dim) { return dtype == LORA_BF16 && dim == 64; }
 constexpr int KV_MAX_MOVES = 128; // page copies of one launch (they travel as its arguments)
 
 // One new token: where it stands and the page it lies in.
@@ -85,7 +90,7 @@ struct JoinArgs {
 hipError_t prepare_attn_kernels();  // once for the current device
 hipError_t launch_append(const AppendArgs &a, int dtype, hipStream_t st);
 hipError_t launch_moves(const KvMoves &m, int n, char *pages, int64_t page_stride, hipStream_t st);
-hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, bool turns, int n_cu, hipStream_t st);
+hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, KvTiles way, int n_cu, hipStream_t st);
 hipError_t launch_attn_join(const JoinArgs &a, int dtype, int dim, bool tiles, hipStream_t st);
 
 }  // namespace lora

@@ -205,6 +205,48 @@ def test_long_prompts():
     _check([(0, 600)], 2, 1, 128, dtype="f32", seed=6)
 
 
+# Steps of 32 tokens, by one wavefront or two in turn: every number of them from one to nine, whole and broken, with tokens in the cache and without
+STEPS = [(0, 31), (0, 32), (1, 32), (5, 60), (0, 64), (32, 64), (0, 97), (64, 64), (100, 33), (0, 160), (97, 95), (193, 31), (200, 57), (255, 33)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,kv,dim,page", [(2, 2, 64, 32), (6, 2, 64, 128), (2, 1, 128, 32), (4, 4, 128, 256), (4, 1, 256, 32), (2, 2, 256, 64)])
+def test_prompts_of_every_number_of_steps(heads, kv, dim, page, dtype):
+    for part in (STEPS[:5], STEPS[5:10], STEPS[10:]):
+        _check(part, heads, kv, dim, page=page, dtype=dtype, seed=11, beyond=float("nan"))
+
+
+# Batches for each way of working on tiles: heads of 64 with few tiles, alone and beside single tokens, with a longer tile, with more tiles than compute units; heads of 128
+# with two blocks on a compute unit, with three (many tiles, and short ones), single tokens beside both
+@pytest.mark.parametrize("segs,heads,kv,dim", [
+    ([(0, 1000)], 4, 4, 64), ([(3, 700), (12, 1), (900, 1), (0, 2)], 8, 4, 64), ([(0, 1100)], 4, 4, 64), ([(0, 300), (70, 230), (0, 140)], 40, 40, 64),
+    ([(0, 900)], 40, 40, 128), ([(0, 129), (5, 130), (0, 200), (64, 150), (0, 100), (0, 1), (33, 250)], 48, 48, 128), ([(0, 40)] * 26, 32, 32, 128),
+    ([(500, 1)] * 9 + [(0, 310)], 64, 8, 128), ([(0, 400), (400, 300)], 32, 32, 256)])
+def test_tiles_few_and_many(segs, heads, kv, dim):
+    _check(segs, heads, kv, dim, seed=12)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [128, 256])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_scores_of_prompts_that_grow_along_the_cache(sign, dim, dtype):
+    """As below, for the other head sizes: the maximum moves beside products that are under way."""
+    s = Setup([(0, 333), (50, 130)], 4, 2, dim, dtype=dtype, seed=13)
+    try:
+        a = s.host.float().numpy()
+        for i, (c, n) in enumerate(s.segs):
+            for h in range(s.kv):
+                k, v = kv_plain.read(a, s.tables[i], 0, h, s.page, s.dim, s.u, c + n)
+                k = np.abs(k) * np.linspace(0.01, 4, c + n)[:, None]
+                kv_plain.write(a, s.tables[i], 0, h, s.page, s.dim, s.u, 0, k, v)
+        s.host = torch.from_numpy(a).to(s.dt)
+        s.cache.pages.copy_(s.host)
+        s.q = (s.q.float().abs() * sign).to(s.dt)
+        s.check()
+    finally:
+        s.close()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("fill,scale", [(30.0, 1.0), (1.0, 1e-6), (8.0, 0.5), (1e-20, 1.0)])
 def test_scores_of_every_size(fill, scale, dtype):
