@@ -13,33 +13,40 @@ template <typename E> struct alignas(16) Vals {
     E v[CHUNK<E>];
 };
 
-// 16 bytes past the caches: what is read once, and what is written here to be read when much else has been
+// 16 bytes, past the caches with PAST: what is read once, and what is written here to be read when much else has been
 typedef uint32_t Words __attribute__((ext_vector_type(4)));
-template <typename E> __device__ __forceinline__ Vals<E> load_once(const E *p)
+template <bool PAST, typename E> __device__ __forceinline__ Vals<E> load_once(const E *p)
 {
-    return __builtin_bit_cast(Vals<E>, __builtin_nontemporal_load(reinterpret_cast<const Words *>(p)));
+    if constexpr (PAST) return __builtin_bit_cast(Vals<E>, __builtin_nontemporal_load(reinterpret_cast<const Words *>(p)));
+    else return *reinterpret_cast<const Vals<E> *>(p);
 }
-template <typename E> __device__ __forceinline__ void store_past(E *p, const Vals<E> &v)
+template <bool PAST, typename E> __device__ __forceinline__ void store_past(E *p, const Vals<E> &v)
 {
-    __builtin_nontemporal_store(__builtin_bit_cast(Words, v), reinterpret_cast<Words *>(p));
+    if constexpr (PAST) __builtin_nontemporal_store(__builtin_bit_cast(Words, v), reinterpret_cast<Words *>(p));
+    else *reinterpret_cast<Vals<E> *>(p) = v;
 }
 
 }  // namespace
 
 // Keys and queries: a thread takes two chunks of one token whose values turn together (HALVES: chunk p and the one rope_dim / 2 values on;
 // NEIGHBOURS and unturned values: two chunks in a row), of HEADS heads: the position's cosines and sines are fetched once for
-// them (8 heads in large batches, 12900 tokens of 32 + 32 + 32 heads of 128: 172 us with 4, 161 with 8; 2 in small ones, 64 tokens 6.1 -> 5.1).  8 tokens go with a run of 8 threads: a token's key chunks lie page_tokens chunks apart in the page, the same chunk of
+// them.  8 tokens go with a run of 8 threads: a token's key chunks lie page_tokens chunks apart in the page, the same chunk of
 // the next token right beside, so that a prompt is read and written in runs of 128 bytes.
 // Values: a thread takes u values of a head of the tokens that share their chunks, turns the u x u square round in its registers,
 // and the wavefront hands the chunks round through LDS to store them 1 KB at a time; chunks that this group does not fill
 // are written value by value.
+//
+// Only bytes move.  Large batches: 8 heads a thread, past the caches, 12900 tokens of 32 + 32 + 32 heads of 128 (650 MB) in 160 us, 4.1 TB/s (172 with 4 heads).  Small ones, which stay in the
+// caches until the attention reads them: 2 heads a thread and no such hints, 64 tokens 6.1 -> 5.1 us of kernel time; 920 tokens of 32 + 32 + 32 heads with their attention, two layers, 108 -> 103.
+// From 16 MB of rows on the former is faster (6 x 300 tokens, two layers 138 -> 126).  Of batches of single tokens every key chunk is a piece of 16 bytes of a line of its own, every value one of 2.
 constexpr int APPEND_MANY_HEADS = 8, APPEND_FEW_HEADS = 2;
-constexpr int64_t APPEND_MANY = 1 << 17;  // tokens times heads from which a batch is a large one
+constexpr int64_t APPEND_MANY = 1 << 24;  // bytes of keys and queries from which a batch is a large one
 
 template <typename E, int APPEND_HEADS>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t key_blocks)
 {
     constexpr int U = CHUNK<E>;
+    constexpr bool PAST = APPEND_HEADS == APPEND_MANY_HEADS;
     const int page_tokens = 1 << a.page_shift;
     const size_t head_values = (size_t)a.dim << a.page_shift;  // of one half of a page
     if (blockIdx.x < key_blocks) {
@@ -65,8 +72,8 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t key_
 #pragma unroll
         for (int k = 0; k < APPEND_HEADS; ++k) {
             const E *src = source(min(h0 + k, heads - 1));
-            x[k] = load_once(src + c0 * U);
-            y[k] = load_once(src + c1 * U);
+            x[k] = load_once<PAST>(src + c0 * U);
+            y[k] = load_once<PAST>(src + c1 * U);
         }
         if (turn) {
             // HALVES: entries c0 U .. c0 U + U - 1 turn x with y; NEIGHBOURS: entries p U .. turn the pairs of x, then those of y
@@ -105,8 +112,8 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t key_
                 *reinterpret_cast<Vals<E> *>(page + ((size_t)c1 << a.page_shift) * U) = y[k];
             } else if (h < heads) {
                 E *to = static_cast<E *>(a.q_out) + t * a.q_out_stride + (h - a.n_kv) * a.dim;
-                store_past(to + c0 * U, x[k]);
-                store_past(to + c1 * U, y[k]);
+                store_past<PAST>(to + c0 * U, x[k]);
+                store_past<PAST>(to + c1 * U, y[k]);
             }
         }
         return;
@@ -127,7 +134,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t key_
     if (grp.n == U) {
         Vals<E> in[U];
 #pragma unroll
-        for (int t = 0; t < U; ++t) in[t] = load_once(src + t * a.v_stride);
+        for (int t = 0; t < U; ++t) in[t] = load_once<PAST>(src + t * a.v_stride);
 #pragma unroll
         for (int d = 0; d < U; ++d) {
             Vals<E> o;
@@ -137,7 +144,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t key_
         }
     } else {
         for (int t = 0; t < grp.n; ++t) {
-            const Vals<E> in = load_once(src + t * a.v_stride);
+            const Vals<E> in = load_once<PAST>(src + t * a.v_stride);
 #pragma unroll
             for (int d = 0; d < U; ++d) to[(c * U + d) * U + at % U + t] = in.v[d];
         }
@@ -151,7 +158,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t key_
         const bool whole = __builtin_amdgcn_readlane(grp.n, from) == U;
         const uint64_t there = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(base >> 32), from) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)base, from);
         const int first = __builtin_amdgcn_readlane(c, from) * U;
-        if (whole) store_past(reinterpret_cast<E *>(there) + (first + lane) * U, mine[owner * U + ((lane & (U - 1)) ^ (owner & (U - 1)))]);
+        if (whole) store_past<PAST>(reinterpret_cast<E *>(there) + (first + lane) * U, mine[owner * U + ((lane & (U - 1)) ^ (owner & (U - 1)))]);
     }
 }
 
@@ -159,7 +166,7 @@ hipError_t launch_append(const AppendArgs &a, int dtype, hipStream_t st)
 {
     const int u = dtype == LORA_BF16 ? 8 : 4;
     const int64_t heads = (a.q ? a.n_heads : 0) + a.n_kv;
-    const bool many = a.n_tokens * heads >= APPEND_MANY;
+    const bool many = a.n_tokens * heads * a.dim * (dtype == LORA_BF16 ? 2 : 4) >= APPEND_MANY;
     const int64_t each = many ? APPEND_MANY_HEADS : APPEND_FEW_HEADS;
     const int64_t keys = ((int64_t)(a.n_tokens + 7) / 8 * ((heads + each - 1) / each) * (a.dim / (2 * u)) * 8 + 255) / 256;
     const int64_t vals = ((int64_t)a.n_groups * a.n_kv * (a.dim / u) + 255) / 256;
@@ -175,7 +182,8 @@ hipError_t launch_append(const AppendArgs &a, int dtype, hipStream_t st)
     return hipGetLastError();
 }
 
-// A page's bytes, all layers, in pieces of 16 KB: a block each, 4 chunks of 16 bytes in flight per thread.
+// A page's bytes, all layers, in pieces of 16 KB: a block each, 4 chunks of 16 bytes in flight per thread.  4 pages of 34 MB that are copies
+// of one: 34 us, written past the caches at 3.9 TB/s and read from them.
 constexpr int MOVE_BYTES = 256 * 4 * 16;
 
 __global__ __launch_bounds__(256) void moves_kernel(KvMoves m, char *pages, int64_t page_stride)
