@@ -198,15 +198,18 @@ int refuse_capture(hipStream_t st)
     return cs == hipStreamCaptureStatusNone ? LORA_OK : LORA_E_STATE;
 }
 
-int copy_pages(lora_kv &kv, const std::vector<int32_t> &from, const std::vector<int32_t> &to, hipStream_t st)
+// Copies pages; `lists` (16-byte pieces, n may be 0) go up with the last of the launches, or in one of their own, which `done` is recorded with.
+int copy_pages(lora_kv &kv, const std::vector<int32_t> &from, const std::vector<int32_t> &to, hipStream_t st, const lora::KvLists &lists = {}, hipEvent_t done = nullptr)
 {
     for (size_t at = 0; at < from.size(); at += lora::KV_MAX_MOVES) {
         lora::KvMoves m;
         const int n = (int)std::min(from.size() - at, (size_t)lora::KV_MAX_MOVES);
         std::copy_n(from.begin() + at, n, m.from);
         std::copy_n(to.begin() + at, n, m.to);
-        KV_TRY(lora::launch_moves(m, n, kv.pages, (int64_t)kv.page_bytes, st));
+        const bool last = at + n == from.size();
+        KV_TRY(lora::launch_moves(m, n, kv.pages, (int64_t)kv.page_bytes, last ? lists : lora::KvLists{}, st, last ? done : nullptr));
     }
+    if (from.empty()) KV_TRY(lora::launch_upload(lists.to, lists.from, (size_t)lists.n * 16, st, done));
     return LORA_OK;
 }
 
@@ -815,9 +818,7 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
         b->join_rows = 0;
         for (const JoinItem &j : cut.joins) b->join_rows = std::max(b->join_rows, j.n_rows);
         b->info = {T, n_seg, (int32_t)n_pages, (int32_t)groups.size(), (int32_t)cut.rows.size(), (int32_t)cut.tiles.size(), (int32_t)(cut.joins.size() + cut.tile_joins.size())};
-        if (const int rc = copy_pages(*kv, g.from, g.to, st)) return rc;
-        KV_TRY(lora::launch_upload(b->dev, b->pinned_dev, at, st, nullptr));
-        KV_TRY(hipEventRecord(b->uploaded, st));
+        if (const int rc = copy_pages(*kv, g.from, g.to, st, {b->dev, b->pinned_dev, (uint32_t)((at + 15) / 16)}, b->uploaded)) return rc;
         b->upload_pending = true;
         b->stale = false;
         b->alive = true;

@@ -54,6 +54,13 @@ struct KvMoves {
     int32_t from[KV_MAX_MOVES], to[KV_MAX_MOVES];
 };
 
+// Lists on their way up from pinned memory: n pieces of 16 bytes
+struct KvLists {
+    void *to;
+    const void *from;
+    uint32_t n;
+};
+
 struct AppendArgs {
     const void *q, *k, *v;
     void *q_out;
@@ -89,7 +96,7 @@ struct JoinArgs {
 
 hipError_t prepare_attn_kernels();  // once for the current device
 hipError_t launch_append(const AppendArgs &a, int dtype, hipStream_t st);
-hipError_t launch_moves(const KvMoves &m, int n, char *pages, int64_t page_stride, hipStream_t st);
+hipError_t launch_moves(const KvMoves &m, int n, char *pages, int64_t page_stride, const KvLists &lists, hipStream_t st, hipEvent_t done);
 hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, KvTiles way, int n_cu, hipStream_t st);
 hipError_t launch_attn_join(const JoinArgs &a, int dtype, int dim, bool tiles, hipStream_t st);
 
