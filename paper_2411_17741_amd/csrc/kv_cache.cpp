@@ -33,7 +33,9 @@ constexpr int SPARE_BATCHES = 2;
 constexpr int ROW_BLOCKS = 512, ROW_MIN_TOKENS = 512;
 // Tokens times head_dim up to which a wavefront may have an item to itself.
 constexpr int ROW_SHORT_VALUES = 16384;
-constexpr int TILE_MIN_TOKENS = 512, TILE_LEAST_TOKENS = 256;  // the latter where there are few tiles
+// Tiles are cut into pieces of no fewer tokens than join work is worth -- fp32 products take 8 times as long --, or of half of that where there are few tiles.  Measured for fp32, 512 -> these:
+// prompts of 300, 1 and 77 tokens with 32 / 8 heads of 128, append and attention, 59 -> 42 us, with 6 / 2 58 -> 32, with 32 / 8 heads of 64 37 -> 32 us.
+constexpr int tile_min_tokens(const lora_kv_config_t &c) { return c.dtype == LORA_BF16 ? 512 : c.head_dim == 64 ? 256 : 128; }
 constexpr int PIECE_STEP = 64;  // pieces begin at multiples of it: a whole number of every kernel's steps, in one page or at the start of one
 constexpr int MAX_EXTRA = 2048;  // pieces beyond one for each block of rows
 
@@ -317,7 +319,7 @@ void cut_block(AttnItem base, int32_t kv_len, int32_t piece, int32_t rows, int32
 
 void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, Cut &cut)
 {
-    const int32_t grp = kv.group(), n_kv = kv.cfg.n_kv_heads;
+    const int32_t grp = kv.group(), n_kv = kv.cfg.n_kv_heads, tile_min = tile_min_tokens(kv.cfg);
     int64_t row_tokens = 0, tile_tokens = 0, n_tiles = 0, longest = 0, part = 0, tile = lora::KV_TURNS_TILE;
     const auto tile_end = [&tile, grp](int64_t ctx, int64_t rows, int64_t row0) {  // tokens that the tile's last row sees
         return (int32_t)(ctx + (std::min(rows, row0 + tile) - 1) / grp + 1);
@@ -351,19 +353,19 @@ void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     int32_t row_piece = at_least(row_tokens * n_kv / ROW_BLOCKS, ROW_MIN_TOKENS);
     // A tile that takes longer than all of a compute unit's share is cut, into pieces of half of that: two at a time are worked on
     const int64_t share = tile_tokens * n_kv / kv.n_cu;
-    int32_t tile_piece = at_least(share / 2, TILE_MIN_TOKENS), tile_whole = at_least(share, TILE_MIN_TOKENS);
+    int32_t tile_piece = at_least(share / 2, tile_min), tile_whole = at_least(share, tile_min);
     // No more blocks than compute units and no tile of over 1024 tokens: for heads of 64, whose steps are mostly instructions of one wavefront after the other, two groups of
     // wavefronts share a tile's tokens, and tiles stay whole (700 tokens with 32 heads 16.5 -> 12.5 us, with 32 / 8 heads 15.3 -> 12.3).  Longer ones, and heads of 128, do as well
     // or better with pieces.
-    if (cut.way == lora::KV_TILES_PLAIN && lora::kv_pairs(kv.cfg.dtype, kv.cfg.head_dim) && n_tiles * n_kv <= kv.n_cu && longest <= 2 * TILE_MIN_TOKENS) {
+    if (cut.way == lora::KV_TILES_PLAIN && lora::kv_pairs(kv.cfg.dtype, kv.cfg.head_dim) && n_tiles * n_kv <= kv.n_cu && longest <= 2 * tile_min) {
         cut.way = lora::KV_TILES_PAIRS;
-        tile_whole = 2 * TILE_MIN_TOKENS;
+        tile_whole = 2 * tile_min;
     }
     // Where tiles are cut anyway, and pieces of fewer tokens still find a compute unit each (a quarter more than the share: not all pieces are whole), the last is done earlier: 213 + 752 tokens
     // with 6 / 2 heads 18.6 -> 15.2 us, 1072 19.7 -> 18.5.
-    if (cut.way == lora::KV_TILES_PLAIN && longest > TILE_MIN_TOKENS) {
-        const int32_t piece = at_least(share * 5 / 4, TILE_LEAST_TOKENS);
-        if (piece < TILE_MIN_TOKENS) tile_piece = tile_whole = piece;
+    if (cut.way == lora::KV_TILES_PLAIN && longest > tile_min) {
+        const int32_t piece = at_least(share * 5 / 4, tile_min / 2);
+        if (piece < tile_min) tile_piece = tile_whole = piece;
     }
     for (;;) {
         cut.rows.clear();
@@ -388,7 +390,7 @@ void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
         }
         if (cut.way == lora::KV_TILES_PAIRS && (int64_t)(cut.tiles.size() + cut.rows.size()) * n_kv > kv.n_cu) {
             cut.way = lora::KV_TILES_PLAIN;
-            tile_whole = at_least(share, TILE_MIN_TOKENS);
+            tile_whole = at_least(share, tile_min);
             continue;
         }
         if (part <= kv.part_rows && cut.joins.size() + cut.tile_joins.size() <= (size_t)MAX_EXTRA && (int64_t)(cut.rows.size() + cut.tiles.size()) <= max_items(kv.cfg)) break;
