@@ -999,9 +999,11 @@ __global__ __launch_bounds__(256, 3) void attn_many_kernel(AttnArgs a)
     attn_tile_plain<E, D, 32>(a, it, blockIdx.x % a.n_kv, lds);
 }
 
-// Tiles, and the blocks of the row items behind them: one launch where all of them are on the machine at once anyway (64 / 8 heads of 128, prompts of 2 to 234
-// tokens 16.1 -> 11.7 us; 196 single tokens beside 3 prompts with 40 / 8 heads, two layers 107 -> 88).  Of larger batches a launch for each does better: here the rows
-// have the tiles' occupancy.
+// Tiles, and the blocks of the row items behind them in one launch, while there are no more than BOTH_ROUNDS times as many as are on the machine at once: rows wait for memory beside tiles' products.
+// Apart -> together: prompts of 2 to 234 tokens with 64 / 8 heads of 128 16.1 -> 11.7 us; 30 tokens of about 300 beside 100 + 200 with 40 heads 43.7 -> 36.4; 8 of 3000 beside 1500 with
+// 32 / 8 heads 67 -> 61; 20 of 8000 beside 900 + 700 147 -> 154.  Of larger batches nothing is gained, or lost where rows have fewer blocks on a compute unit this way (heads of 256, 100 tokens
+// of 500 beside 600: 109 -> 122).
+constexpr int BOTH_ROUNDS = 4;
 template <typename E, int D>
 __global__ __launch_bounds__(256, (TileShape<E, D>::BLOCKS)) void attn_both_kernel(AttnArgs a)
 {
@@ -1258,7 +1260,7 @@ hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, KvTiles way, int n
     return by_type(dtype, dim, [&](auto e, auto d) {
         typedef decltype(e) E;
         constexpr int D = decltype(d)::value;
-        if (n_tiles && n_rows && way == KV_TILES_PLAIN && n_tiles + n_rows <= TileShape<E, D>::BLOCKS * n_cu) {
+        if (n_tiles && n_rows && way == KV_TILES_PLAIN && n_tiles + n_rows <= BOTH_ROUNDS * TileShape<E, D>::BLOCKS * n_cu) {
             hipLaunchKernelGGL((attn_both_kernel<E, D>), dim3((unsigned)(n_tiles + n_rows)), dim3(256), (TileShape<E, D>::LDS), st, a);
             return;
         }
