@@ -251,7 +251,7 @@ __device__ __forceinline__ void put_row(const AttnArgs &a, const AttnItem &it, i
 #pragma unroll
         for (int j = 0; j < D / 64; ++j) {
             const int d = lane + 64 * j;
-            if (TILE) a.part_o[(at & ~(int64_t)31) * D + tile_part(r & 31, d)] = st.o[j];
+            if (TILE) a.part_o[(at - (r & 31)) * D + tile_part(r & 31, d)] = st.o[j];  // (32 rows' results begin wherever the pieces before them end)
             else a.part_o[at * D + d] = st.o[j];
         }
         if (lane == 0) a.part_ml[2 * at] = st.m, a.part_ml[2 * at + 1] = st.l;
