@@ -137,12 +137,18 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
                          lora_kv_batch_t **out);
 int lora_kv_batch_destroy(lora_kv_t *kv, lora_kv_batch_t *batch);
 
+/* How the attention works on tiles of rows: four wavefronts to a tile; the same, three tiles on a compute unit; two groups of four wavefronts to a
+ * tile; tiles of twice as many rows, two groups in turns. */
+enum { LORA_KV_TILES_PLAIN = 0, LORA_KV_TILES_MANY = 1, LORA_KV_TILES_PAIRS = 2, LORA_KV_TILES_TURNS = 3 };
+
 /* What the batch was cut into, for tests and tools. */
 typedef struct {
     int32_t n_tokens, n_segments, n_pages; /* n_pages: entries of the page lists */
     int32_t n_groups;                      /* pieces of the append */
     int32_t n_row_items, n_tile_items;     /* attention, per key-value head: pieces with up to 16 rows, tiles of rows */
     int32_t n_joins;                       /* row blocks whose pieces are joined afterwards */
+    int32_t n_short_items;                 /* of the row items: those that a wavefront has to itself */
+    int32_t tiles_way;                     /* LORA_KV_TILES_* */
 } lora_kv_batch_info_t;
 int lora_kv_batch_info(const lora_kv_batch_t *batch, lora_kv_batch_info_t *out);
 

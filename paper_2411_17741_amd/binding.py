@@ -26,6 +26,7 @@ LORA_CACHE_HOST_ONLY, LORA_CACHE_FUSED_GEMV, LORA_CACHE_SPLIT_GEMV, LORA_CACHE_D
 LORA_CACHE_SMALL_SCRATCH = 32
 LORA_KV_HOST_ONLY, LORA_KV_MAX_TOKENS = 1, 1 << 28
 LORA_ROPE_HALVES, LORA_ROPE_NEIGHBOURS = 0, 1
+LORA_KV_TILES_PLAIN, LORA_KV_TILES_MANY, LORA_KV_TILES_PAIRS, LORA_KV_TILES_TURNS = 0, 1, 2, 3
 LORA_MAX_RANK, LORA_TILE_TOKENS, LORA_MFMA_MIN_TOKENS, LORA_MFMA_MIN_TOKENS_MIXED = 128, 64, 16, 8
 
 
@@ -114,7 +115,7 @@ class lora_kv_stats_t(ctypes.Structure):
 
 
 class lora_kv_batch_info_t(ctypes.Structure):
-    _fields_ = [(n, c_int32) for n in ("n_tokens", "n_segments", "n_pages", "n_groups", "n_row_items", "n_tile_items", "n_joins")]
+    _fields_ = [(n, c_int32) for n in ("n_tokens", "n_segments", "n_pages", "n_groups", "n_row_items", "n_tile_items", "n_joins", "n_short_items", "tiles_way")]
 
 
 # lora_kv_append_t: k, v, k_stride, v_stride, q, q_out, q_stride, q_out_stride, rope, rope_positions, rope_dim, rope_pairs (packed: a ctypes structure of twelve fields

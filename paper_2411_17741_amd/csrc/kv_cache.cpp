@@ -56,8 +56,7 @@ struct lora_kv_batch {
     hipEvent_t uploaded = nullptr;
     lora_kv_batch_info_t info{};
     int32_t max_pos = -1;  // of the batch's tokens
-    int32_t n_joins = 0, n_tile_joins = 0, join_rows = 0, n_short = 0;  // join_rows: the most rows of a join of row items
-    lora::KvTiles way = lora::KV_TILES_PLAIN;
+    int32_t n_joins = 0, n_tile_joins = 0, join_rows = 0;  // join_rows: the most rows of a join of row items
     size_t off_tokens = 0, off_groups = 0, off_pages = 0, off_rows = 0, off_tiles = 0, off_joins = 0, off_tile_joins = 0;
     std::vector<uint8_t> member;  // by sequence slot
 };
@@ -820,12 +819,11 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
         std::copy(cut.tiles.begin(), cut.tiles.end(), reinterpret_cast<AttnItem *>(b->pinned + b->off_tiles));
         std::copy(cut.joins.begin(), cut.joins.end(), reinterpret_cast<JoinItem *>(b->pinned + b->off_joins));
         std::copy(cut.tile_joins.begin(), cut.tile_joins.end(), reinterpret_cast<JoinItem *>(b->pinned + b->off_tile_joins));
-        b->way = cut.way;
-        b->n_short = cut.n_short;
         b->n_joins = (int32_t)cut.joins.size(), b->n_tile_joins = (int32_t)cut.tile_joins.size();
         b->join_rows = 0;
         for (const JoinItem &j : cut.joins) b->join_rows = std::max(b->join_rows, j.n_rows);
-        b->info = {T, n_seg, (int32_t)n_pages, (int32_t)groups.size(), (int32_t)cut.rows.size(), (int32_t)cut.tiles.size(), (int32_t)(cut.joins.size() + cut.tile_joins.size())};
+        b->info = {T, n_seg, (int32_t)n_pages, (int32_t)groups.size(), (int32_t)cut.rows.size(), (int32_t)cut.tiles.size(), (int32_t)(cut.joins.size() + cut.tile_joins.size()),
+                   cut.n_short, (int32_t)cut.way};
         if (const int rc = copy_pages(*kv, g.from, g.to, st, {b->dev, b->pinned_dev, (uint32_t)((at + 15) / 16)}, b->uploaded)) return rc;
         b->upload_pending = true;
         b->stale = false;
@@ -916,9 +914,10 @@ int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const v
     a.tiles = reinterpret_cast<const AttnItem *>(batch->dev + batch->off_tiles);
     a.rows = reinterpret_cast<const AttnItem *>(batch->dev + batch->off_rows);
     a.n_tiles = batch->info.n_tile_items;
-    a.n_rows = batch->info.n_row_items - batch->n_short;
-    a.n_short = batch->n_short;
-    KV_TRY(lora::launch_attn(a, c.dtype, c.head_dim, batch->way, kv->n_cu, st));
+    a.n_rows = batch->info.n_row_items - batch->info.n_short_items;
+    a.n_short = batch->info.n_short_items;
+    const lora::KvTiles way = (lora::KvTiles)batch->info.tiles_way;
+    KV_TRY(lora::launch_attn(a, c.dtype, c.head_dim, way, kv->n_cu, st));
     lora::JoinArgs j{};
     j.out = out, j.out_stride = out_stride;
     j.part_o = kv->part_o, j.part_ml = kv->part_ml;
@@ -930,7 +929,7 @@ int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const v
     }
     if (batch->n_tile_joins) {
         j.items = reinterpret_cast<const JoinItem *>(batch->dev + batch->off_tile_joins);
-        j.n_items = batch->n_tile_joins, j.max_rows = batch->way == lora::KV_TILES_TURNS ? lora::KV_TURNS_TILE : lora::KV_TILE;
+        j.n_items = batch->n_tile_joins, j.max_rows = way == lora::KV_TILES_TURNS ? lora::KV_TURNS_TILE : lora::KV_TILE;
         KV_TRY(lora::launch_attn_join(j, c.dtype, c.head_dim, true, st));
     }
     return LORA_OK;

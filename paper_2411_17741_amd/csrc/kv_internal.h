@@ -17,7 +17,7 @@ constexpr int KV_TURNS_TILE = 256; // ... where two groups of wavefronts take tu
 constexpr bool kv_turns(int dtype, int dim) { return dtype == LORA_BF16 && dim == 128; }
 // How a batch's tiles are worked on (attn_kernels.hip): four wavefronts to a tile and two blocks on a compute unit, three blocks, or two groups of four wavefronts to a tile; all three
 // with tiles of KV_TILE rows; two groups in turns
-enum KvTiles { KV_TILES_PLAIN, KV_TILES_MANY, KV_TILES_PAIRS, KV_TILES_TURNS };
+enum KvTiles { KV_TILES_PLAIN = LORA_KV_TILES_PLAIN, KV_TILES_MANY = LORA_KV_TILES_MANY, KV_TILES_PAIRS = LORA_KV_TILES_PAIRS, KV_TILES_TURNS = LORA_KV_TILES_TURNS };
 constexpr bool kv_many(int dtype, int dim) { return dtype == LORA_BF16 && dim == 128; }
 constexpr bool kv_pairs(int dtype, int dim) { return dtype == LORA_BF16 && dim == 64; }
 constexpr int KV_MAX_MOVES = 128; // page copies of one launch (they travel as its arguments)

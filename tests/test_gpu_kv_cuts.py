@@ -64,3 +64,95 @@ def test_no_number_behind_a_token_of_a_cut_tile_beside_cut_rows(segs, which, at,
         check_beside_no_number(s, which, at, kv - 1)
     finally:
         s.close()
+
+
+def info_of(s):
+    from paper_2411_17741_amd import binding as B
+
+    rc, info = B.lora_kv_batch_info(s.batch)
+    assert rc == B.LORA_OK
+    return info
+
+
+PLAIN, MANY, PAIRS, TURNS = range(4)
+# Each way of working on tiles: whole tiles and cut ones (with `joins`), broken last tiles, cached context, pages of every size, beside single tokens that are cut themselves;
+# `which`, `at`: a token whose key and value can be no numbers
+WAYS = [
+    (TURNS, [(600, 1024)], 128, 16, 128, 32, 0, 0, 900),
+    (TURNS, [(0, 2048)], 64, 64, 128, 256, 0, 0, 2047),
+    (TURNS, [(611, 1013), (6000, 40)], 128, 16, 128, 64, 2, 1, 6003),
+    (TURNS, [(2500, 1), (311, 1700), (6000, 50), (30, 7)], 80, 16, 128, 32, 2, 2, 6011),
+    (TURNS, [(1000, 1), (2500, 300), (0, 1500)], 128, 8, 128, 128, 1, 1, 2600),
+    (MANY, [(0, 60)] * 30 + [(700, 90)], 32, 32, 128, 64, 0, 30, 731),
+    (MANY, [(0, 40)] * 30 + [(3600, 100), (2500, 1)], 32, 32, 128, 32, 2, 30, 3650),
+    (PAIRS, [(3, 700), (12, 1), (900, 1), (0, 2)], 8, 4, 64, 32, 1, 0, 400),
+    (PAIRS, [(2500, 1), (20, 1000), (0, 33)], 4, 4, 64, 128, 1, 1, 21),
+    (PLAIN, [(0, 300), (70, 230), (0, 140)], 40, 40, 64, 64, 0, 1, 150),
+    (PLAIN, [(2000, 900), (0, 900)], 6, 2, 128, 64, 2, 0, 2400),
+    (PLAIN, [(1500, 300), (40, 50)], 4, 2, 256, 64, 1, 0, 1600),
+]
+
+
+@pytest.mark.parametrize("way,segs,heads,kv,dim,page,joins,which,at", WAYS)
+def test_every_way_of_working_on_tiles(way, segs, heads, kv, dim, page, joins, which, at):
+    s = Setup(segs, heads, kv, dim, page=page, seed=22, beyond=float("nan"))
+    try:
+        info = info_of(s)
+        assert info.tiles_way == way and info.n_tile_items > 0 and info.n_joins >= joins
+        check(s)
+        first = s.run(0.1)
+        assert torch.equal(s.run(0.1), first)
+    finally:
+        s.close()
+
+
+@pytest.mark.parametrize("way,segs,heads,kv,dim,page,joins,which,at", WAYS)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_no_number_behind_a_token_of_every_way(way, segs, heads, kv, dim, page, joins, which, at, bad):
+    s = Setup(segs, heads, kv, dim, page=page, seed=23)
+    try:
+        assert info_of(s).tiles_way == way
+        check_beside_no_number(s, which, at, kv // 2, bad)
+    finally:
+        s.close()
+
+
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_scores_that_grow_along_prompts_in_turns(sign):
+    """The running maximum moves in every stage, or never after the first."""
+    s = Setup([(600, 1024)], 128, 16, 128, page=64, seed=24)
+    try:
+        assert info_of(s).tiles_way == TURNS
+        a = s.host.float().numpy()
+        for h in range(s.kv):
+            k, v = kv_plain.read(a, s.tables[0], 0, h, s.page, s.dim, s.u, 1624)
+            kv_plain.write(a, s.tables[0], 0, h, s.page, s.dim, s.u, 0, np.abs(k) * np.linspace(0.01, 4, 1624)[:, None], v)
+        s.host = torch.from_numpy(a).to(s.dt)
+        s.cache.pages.copy_(s.host)
+        s.q = (s.q.float().abs() * sign).to(s.dt)
+        check(s)
+    finally:
+        s.close()
+
+
+# More short items than blocks are on the machine: a wavefront has one to itself; beside longer ones and tiles, with several tokens, in every length up to the longest short one
+SHORT = [
+    ([(i % 128, 1) for i in range(130)], 8, 8, 128, 64, 5, 5),
+    ([(i % 120, 1 + i % 3) for i in range(80)] + [(300, 1), (0, 50), (2000, 1)], 32, 8, 128, 32, 77, 78),
+    ([(100 + i, 1) for i in range(156)] + [(200, 4)] * 5, 16, 4, 64, 64, 156, 202),
+    ([(i % 64, 1) for i in range(150)] + [(40, 3)], 4, 4, 256, 32, 150, 41),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("segs,heads,kv,dim,page,which,at", SHORT)
+def test_short_items(segs, heads, kv, dim, page, which, at, dtype):
+    s = Setup(segs, heads, kv, dim, page=page, dtype=dtype, seed=25, beyond=float("nan"))
+    try:
+        info = info_of(s)
+        assert info.n_short_items * kv > 512 and info.n_row_items - info.n_short_items < 10
+        check(s)
+        s.host = torch.nan_to_num(s.host)
+        check_beside_no_number(s, which, at, kv // 2)
+    finally:
+        s.close()
