@@ -921,7 +921,7 @@ __device__ __forceinline__ void attn_tile_plain(const AttnArgs &a, const AttnIte
     Rows t(a, it, kv_head, wave);
     // stages that there are, and of which the wavefront's rows see something
     const int n = (it.kv1 - it.kv0 + TK - 1) / TK, most = it.ctx + (it.row0 + min(wave * 32 + 31, it.n_rows - 1)) / a.group + 1;
-    const int mine = wave * 32 < it.n_rows ? min(n, (most - it.kv0 + TK - 1) / TK) : 0;
+    const int mine = wave * 32 < it.n_rows && most > it.kv0 ? min(n, (most - it.kv0 + TK - 1) / TK) : 0;
     t.wait_for_queries();
     int buf = 0, t0 = it.kv0;
     const auto next = [&](int i) {  // waits for stage i and requests the one behind it

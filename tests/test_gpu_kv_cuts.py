@@ -156,3 +156,18 @@ def test_short_items(segs, heads, kv, dim, page, which, at, dtype):
         check_beside_no_number(s, which, at, kv // 2)
     finally:
         s.close()
+
+
+@pytest.mark.parametrize("segs", [[(0, 60)] * 30 + [(4000, 128)], [(0, 100)] * 40 + [(3969, 128)], [(0, 60)] * 30 + [(4000, 100), (2000, 1)]])
+def test_a_last_piece_that_the_first_rows_of_its_tile_do_not_see(segs):
+    """Three tiles on a compute unit, one query head to a key-value head: rows of a tile stand up to 127 tokens apart, its last piece has 32, 1 and 4 tokens."""
+    s = Setup(segs, 32, 32, 128, seed=26, beyond=float("nan"))
+    try:
+        info = info_of(s)
+        assert info.tiles_way == MANY and info.n_joins > 0
+        check(s)
+        s.host = torch.nan_to_num(s.host)
+        which = next(i for i, (c, n) in enumerate(segs) if c and n > 1)
+        check_beside_no_number(s, which, segs[which][0] + segs[which][1] - 1, 3)
+    finally:
+        s.close()
