@@ -356,7 +356,7 @@ void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     // No more blocks than compute units and no tile of over 1024 tokens: for heads of 64, whose steps are mostly instructions of one wavefront after the other, two groups of
     // wavefronts share a tile's tokens, and tiles stay whole (700 tokens with 32 heads 16.5 -> 12.5 us, with 32 / 8 heads 15.3 -> 12.3).  Longer ones, and heads of 128, do as well
     // or better with pieces.
-    if (cut.way == lora::KV_TILES_PLAIN && lora::kv_pairs(kv.cfg.dtype, kv.cfg.head_dim) && n_tiles * n_kv <= kv.n_cu && longest <= 2 * tile_min) {
+    if (cut.way == lora::KV_TILES_PLAIN && lora::kv_pairs(kv.cfg.dtype, kv.cfg.head_dim) && n_tiles && n_tiles * n_kv <= kv.n_cu && longest <= 2 * tile_min) {
         cut.way = lora::KV_TILES_PAIRS;
         tile_whole = 2 * tile_min;
     }

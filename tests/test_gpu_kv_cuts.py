@@ -171,3 +171,16 @@ def test_a_last_piece_that_the_first_rows_of_its_tile_do_not_see(segs):
         check_beside_no_number(s, which, segs[which][0] + segs[which][1] - 1, 3)
     finally:
         s.close()
+
+
+@pytest.mark.parametrize("segs", [[(300, 1)], [(900, 1), (40, 2), (0, 1)], [(20, 0)]])
+def test_batches_without_tiles_take_no_way_of_theirs(segs):
+    """Heads of 64: two groups of wavefronts to a tile are for batches that have tiles."""
+    s = Setup(segs, 4, 4, 64, seed=27)
+    try:
+        info = info_of(s)
+        assert info.tiles_way == PLAIN and info.n_tile_items == 0
+        if s.T:
+            check(s)
+    finally:
+        s.close()
