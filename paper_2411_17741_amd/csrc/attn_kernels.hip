@@ -491,12 +491,12 @@ __global__ __launch_bounds__(64 * ROW_WAVES, 2) void attn_rows_kernel(AttnArgs a
 // it brings to LDS.
 template <typename E> __device__ __forceinline__ int key_of_row(int row) { return sizeof(E) == 2 ? (row & ~12) | (row & 4) << 1 | (row & 8) >> 1 : row; }
 
-// Requests of 4 wavefronts for stages of TK tokens to LDS, keys as [D / u][TK] chunks, values as [TK / u][D].  A wavefront's request brings 64
-// chunks: keys of 64 tokens (32 in a page, 32 perhaps in another) or two chunks of 32, values of u tokens (in one page).  The values are
+// Requests of 4 wavefronts for stages of 64 tokens to LDS, keys as [D / u][64] chunks, values as [64 / u][D].  A wavefront's request brings 64
+// chunks: keys of 64 tokens (32 in a page, 32 perhaps in another), values of u tokens (in one page).  The values are
 // asked for after the keys: their pages are the ones that the keys were in.  Past the last stage requests may go on: they
 // bring the last page's.
-template <typename E, int D, int TK> struct Stages {
-    static constexpr int U = CHUNK<E>, HALF = TK * D * (int)sizeof(E), PER = HALF / 4096;  // bytes of a stage's keys or values; a wavefront's requests for them
+template <typename E, int D> struct Stages {
+    static constexpr int TK = 64, U = CHUNK<E>, HALF = TK * D * (int)sizeof(E), PER = HALF / 4096;  // bytes of a stage's keys or values; a wavefront's requests for them
     PageList pages;
     const char *head, *k_lane;  // the head's keys in page 0, and the lane's first chunk of them
     uint32_t page_stride;
@@ -506,18 +506,18 @@ template <typename E, int D, int TK> struct Stages {
           loader(which_loader), lane(threadIdx.x & 63), values_at(((a.n_kv * D) << a.page_shift) * (int)sizeof(E)), at(0), t0(first)
     {
         head = a.pages + ((size_t)kv_head * D << a.page_shift) * sizeof(E);
-        const int slot = lane % TK, tok = (slot & 32) | key_of_row<E>(slot & 31), chunk = TK == 64 ? loader : 2 * loader + lane / 32;
-        k_lane = head + ((chunk << a.page_shift) + (a.page_shift == 5 ? tok & 31 : tok)) * 16;
+        const int tok = (lane & 32) | key_of_row<E>(lane & 31);
+        k_lane = head + ((loader << a.page_shift) + (a.page_shift == 5 ? tok & 31 : tok)) * 16;
         page[0] = page[1] = 0;
     }
     __device__ __forceinline__ void keys(unsigned char *to)  // of the next stage
     {
         page[0] = pages[t0 >> page_shift];
-        if (TK == 64) page[1] = pages[(t0 + 32) >> page_shift];
+        page[1] = pages[(t0 + 32) >> page_shift];
         at = t0 & ((1 << page_shift) - 1);
-        const char *const from = k_lane + (uint64_t)page_stride * (uint32_t)(TK == 32 || lane < 32 ? page[0] : page[1]) + at * 16;
+        const char *const from = k_lane + (uint64_t)page_stride * (uint32_t)(lane < 32 ? page[0] : page[1]) + at * 16;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) request16(reinterpret_cast<const __bf16 *>(from + (((TK == 64 ? 4 : 8) * i) << page_shift) * 16), to + loader * 1024 + i * 4096);
+        for (int i = 0; i < PER; ++i) request16(reinterpret_cast<const __bf16 *>(from + ((4 * i) << page_shift) * 16), to + loader * 1024 + i * 4096);
         t0 += TK;
     }
     __device__ __forceinline__ void values(unsigned char *to)  // of the stage whose keys were asked for last
@@ -532,7 +532,7 @@ template <typename E, int D, int TK> struct Stages {
     }
 };
 
-// The same for stages of 32 tokens, STRIDE tokens apart.  They lie in one page, their values in one run: what differs between lanes is the same for all stages.
+// Such requests for stages of 32 tokens, STRIDE tokens apart.  They lie in one page, their values in one run: what differs between lanes is the same for all stages.
 template <typename E, int D, int STRIDE> struct Steps {
     static constexpr int PER = 32 * D * (int)sizeof(E) / 4096;
     PageList pages;
@@ -1042,14 +1042,13 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 // before the first that needs them, so that a wavefront takes its first operands out of LDS before the barrier that starts its
 // products.
 // 8192 tokens with 32 / 8 heads: 480 us, 1.15 PFLOP/s; 16384 with 64 / 8 3640 us, 1.21.  Bound by power: the clock is at 1.75 GHz, the matrix units are busy 56 % of the cycles (tiles of 128 rows: 525 and 3966 us).
-constexpr int TURN_TOKENS = 64;
-constexpr int turn_lds(int dim) { return 6 * TURN_TOKENS * dim * 2; }
+constexpr int turn_lds(int dim) { return 6 * 64 * dim * 2; }
 
 template <int D>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_turns_kernel(AttnArgs a)
 {
     typedef __bf16 E;
-    constexpr int U = 8, TK = TURN_TOKENS, HALF = TK * D * 2, PER = Stages<E, D, TK>::PER, DJ = D / 32;
+    constexpr int U = 8, TK = Stages<E, D>::TK, HALF = Stages<E, D>::HALF, PER = Stages<E, D>::PER, DJ = D / 32;
     constexpr int AHEAD = 8, NV = 4 * DJ, NK = D / 8;  // products of values, of keys
     extern __shared__ __align__(16) unsigned char lds[];  // keys of three stages, values of three
     const AttnItem it = a.tiles[blockIdx.x / a.n_kv];
@@ -1058,7 +1057,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const bool second = wave >= 4;
     const int n = (it.kv1 - it.kv0 + TK - 1) / TK;
     const auto after = [](int place) { return place == 2 * HALF ? 0 : place + HALF; };
-    Stages<E, D, TK> stages(a, it, kv_head, wave & 3, it.kv0);
+    Stages<E, D> stages(a, it, kv_head, wave & 3, it.kv0);
     int put = 0, put_v = 0;
     const auto request_keys = [&] {
         stages.keys(lds + put);
