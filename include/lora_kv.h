@@ -175,8 +175,9 @@ int lora_kv_append(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const l
  * q_stride / out_stride values apart, 16-byte aligned; out may be q itself with the same stride; scale > 0.  Scores, sums and outputs are held in fp32 and outputs
  * rounded once; with LORA_BF16 the weights exp(score - max) are rounded to bf16 for the product with the values (of segments with up to 16
  * rows -- tokens times n_heads / n_kv_heads -- to 16 significant bits, which costs nothing there).  A key or value
- * beyond a token's position has no influence on its output, whatever it is.  The batch's parts are summed in an order that depends on the
- * batch alone: the same call gives the same bits. */
+ * beyond a token's position has no influence on its output, whatever it is.  Sums are kept in range: an output is finite where the scores and
+ * values that its token sees are, and infinite where one of the values is (if its weight is not 0).  The batch's parts are summed in an order
+ * that depends on the batch alone: the same call gives the same bits. */
 int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const void *q, int64_t q_stride, void *out,
                    int64_t out_stride, float scale, void *stream);
 

@@ -3,8 +3,8 @@
 // For the rows of an item -- query vectors q_r of one key-value head -- and tokens [kv0, kv1) of its sequence, one pass
 // over the tokens keeps, per row, the running maximum m of the scores (in units of log2: s = q.k * scale * log2 e), the
 // sum l of exp2(s - m) and the vector o = sum exp2(s - m) v; when m grows, l and o are scaled by exp2(m_old - m_new).  The row's
-// output is o / l.  Parts of a sequence join with M = max m_i as l = sum l_i exp2(m_i - M), o = sum o_i exp2(m_i - M).  A
-// token beyond the row's own position has weight 0 and its value is not multiplied at all.
+// output is o / l.  Parts of a sequence are kept as m, l and o / l and join with M = max m_i as l = sum l_i exp2(m_i - M), out = sum (o_i / l_i) (l_i exp2(m_i - M) / l):
+// means of values, which stay in range where the values do.  A token beyond the row's own position has weight 0 and its value is not multiplied at all.
 #include <cfloat>
 #include <type_traits>
 
@@ -35,7 +35,10 @@ __device__ __forceinline__ const E *half_page(const AttnArgs &a, int page, int k
     return reinterpret_cast<const E *>(a.pages + page * a.page_stride) + (((size_t)half * a.n_kv + kv_head) * D << a.page_shift);
 }
 
-// One row by one wavefront, a token a lane for the scores and D / 64 values of the output a lane.  Lane i holds values i, i + 64, ...
+// One row by one wavefront, a token a lane for the scores and D / 64 values of the output a lane.  Lane i holds values i, i + 64, ...  The weights, and their sum l, are
+// 2^28 times smaller than elsewhere: a sequence has no more tokens than that, so their sums with values of any size stay in range.
+constexpr float ROW_ROOM = 1 << 28;
+static_assert(LORA_KV_MAX_TOKENS <= 1 << 28, "the room of one_row's sums");
 template <typename E, int D> struct RowState {
     float m, l, o[D / 64];
 };
@@ -65,7 +68,7 @@ __device__ void one_row(const AttnArgs &a, const AttnItem &it, int kv_head, int 
         }
         s = s0 + lane < end ? s * a.scale_log2 : -INFINITY;
         const float m = fmaxf(st.m, wave_max(s)), fade = __builtin_amdgcn_exp2f(st.m - m);
-        const float p = s0 + lane < end ? __builtin_amdgcn_exp2f(s - m) : 0.f;
+        const float p = s0 + lane < end ? __builtin_amdgcn_exp2f(s - m) * (1.f / ROW_ROOM) : 0.f;
         st.m = m;
         st.l = st.l * fade + wave_sum(p);
 #pragma unroll
@@ -246,19 +249,19 @@ template <typename E, int D, bool TILE>
 __device__ __forceinline__ void put_row(const AttnArgs &a, const AttnItem &it, int kv_head, int r, const RowState<E, D> &st)
 {
     const int lane = threadIdx.x & 63;
+    const float f = st.l == 0.f ? 0.f : 1.f / st.l;
     if (it.part >= 0) {
         const int64_t at = it.part + (int64_t)kv_head * (TILE ? (it.n_rows + 31) & ~31 : it.n_rows) + r;
 #pragma unroll
         for (int j = 0; j < D / 64; ++j) {
             const int d = lane + 64 * j;
-            if (TILE) a.part_o[(at - (r & 31)) * D + tile_part(r & 31, d)] = st.o[j];  // (32 rows' results begin wherever the pieces before them end)
-            else a.part_o[at * D + d] = st.o[j];
+            if (TILE) a.part_o[(at - (r & 31)) * D + tile_part(r & 31, d)] = st.o[j] * f;  // (32 rows' results begin wherever the pieces before them end)
+            else a.part_o[at * D + d] = st.o[j] * f;
         }
-        if (lane == 0) a.part_ml[2 * at] = st.m, a.part_ml[2 * at + 1] = st.l;
+        if (lane == 0) a.part_ml[2 * at] = st.m, a.part_ml[2 * at + 1] = st.l * ROW_ROOM;
     } else {
         const int row = it.row0 + r;
         E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D;
-        const float f = st.l == 0.f ? 0.f : 1.f / st.l;
 #pragma unroll
         for (int j = 0; j < D / 64; ++j) out[lane + 64 * j] = (E)(st.o[j] * f);
     }
@@ -284,7 +287,7 @@ template <int D> struct RowsLds {
     static constexpr int DP = D < ROW_JOIN ? D : ROW_JOIN;  // columns joined in one go; padded against bank conflicts
     alignas(16) float o[ROW_WAVES][KV_ROW_ITEM][DP + 4];
     float m[ROW_WAVES][KV_ROW_ITEM], l[ROW_WAVES][KV_ROW_ITEM];
-    int redo;
+    int redo[ROW_WAVES];
 };
 
 template <typename E, int D, bool ALONE>
@@ -293,7 +296,6 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it,
     constexpr int U = CHUNK<E>, NT = U / 4, STEP = 16 * NT, KC = D / U / 4, VJ = D / 16, NW = ROW_WAVES, DP = RowsLds<D>::DP;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int in_page = (1 << a.page_shift) - 1;
-    if (!ALONE && threadIdx.x == 0) lds.redo = 0;
 
     const int row = it.row0 + min(r, it.n_rows - 1);
     const int end = it.ctx + row / a.group + 1;  // tokens that this lane's row sees
@@ -394,31 +396,23 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it,
         }
     }
     l = sum16(sum32(l));
-    // rows of several tokens: a value behind a row's own position had weight 0, but 0 times infinity is no number.  Such rows are done again
-    // without touching it
-    if ((it.row0 + it.n_rows - 1) / a.group != it.row0 / a.group) {
-        float none = 0.f;
+    // Outputs that are no numbers or infinite are worked out again: a value behind a row's own position had weight 0, but 0 times infinity is no number; an infinite value that
+    // the row sees has met what its weight lost, which may be 0 or less; and weights that are up to 2^SLACK may have taken a sum out of range
+    float none = 0.f;
 #pragma unroll
-        for (int j = 0; j < VJ; ++j)
+    for (int j = 0; j < VJ; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) none += o[j][i] * 0.f;
-        bool redo = __any(none != 0.f);
-        if constexpr (!ALONE) {
-            __syncthreads();
-            if (redo) lds.redo = 1;
-            __syncthreads();
-            redo = lds.redo;
+        for (int i = 0; i < 4; ++i) none += o[j][i] * 0.f;
+    const bool redo = __any(none != 0.f);
+    const auto again = [&](int from, int step) {
+        for (int i = from; i < it.n_rows; i += step) {
+            RowState<E, D> st;
+            one_row<E, D>(a, it, kv_head, it.row0 + i, it.kv0, it.kv1, st);
+            put_row<E, D, false>(a, it, kv_head, i, st);
         }
-        if (redo) {
-            for (int i = ALONE ? 0 : wave; i < it.n_rows; i += ALONE ? 1 : NW) {
-                RowState<E, D> st;
-                one_row<E, D>(a, it, kv_head, it.row0 + i, it.kv0, it.kv1, st);
-                put_row<E, D, false>(a, it, kv_head, i, st);
-            }
-            return;
-        }
-    }
+    };
     if constexpr (ALONE) {  // (items that one wavefront has to itself are whole)
+        if (redo) return again(0, 1);
         if (r >= it.n_rows) return;
         const float f = l == 0.f ? 0.f : 1.f / l;
         E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D;
@@ -427,9 +421,16 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it,
         return;
     }
     if (g == 0) lds.m[wave][r] = m, lds.l[wave][r] = l;
+    if (lane == 0) lds.redo[wave] = redo;
 #pragma unroll
     for (int pass = 0; pass < D / DP; ++pass) {
         __syncthreads();
+        if (pass == 0) {
+            int any = 0;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) any |= lds.redo[w];
+            if (any) return again(wave, NW);
+        }
 #pragma unroll
         for (int j = 0; j < DP / 16; ++j) *reinterpret_cast<floatx4 *>(&lds.o[wave][r][16 * j + 4 * g]) = o[pass * (DP / 16) + j];
         __syncthreads();
@@ -438,23 +439,24 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it,
             float top = lds.m[0][rr];
 #pragma unroll
             for (int w = 1; w < NW; ++w) top = fmaxf(top, lds.m[w][rr]);
-            float sum = 0.f;
-            floatx4 v = {0.f, 0.f, 0.f, 0.f};
+            float sum = 0.f, f[NW];
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
-                const float f = __builtin_amdgcn_exp2f(lds.m[w][rr] - top);
-                sum += lds.l[w][rr] * f;
-                v += *reinterpret_cast<const floatx4 *>(&lds.o[w][rr][d]) * f;
+                f[w] = __builtin_amdgcn_exp2f(lds.m[w][rr] - top);
+                sum += lds.l[w][rr] * f[w];
             }
+            const float each = sum == 0.f ? 0.f : 1.f / sum;
+            floatx4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < NW; ++w) v += *reinterpret_cast<const floatx4 *>(&lds.o[w][rr][d]) * (f[w] * each);
             if (it.part >= 0) {
                 const int64_t at = it.part + (int64_t)kv_head * it.n_rows + rr;
                 *reinterpret_cast<floatx4 *>(a.part_o + at * D + pass * DP + d) = v;
                 if (pass == 0 && d == 0) a.part_ml[2 * at] = top, a.part_ml[2 * at + 1] = sum;
             } else {
                 const int rw = it.row0 + rr;
-                const float f = sum == 0.f ? 0.f : 1.f / sum;
                 E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + rw / a.group) * a.out_stride + (kv_head * a.group + rw % a.group) * D + pass * DP + d;
-                put_four(out, v * f);
+                put_four(out, v);
             }
         }
     }
@@ -641,7 +643,7 @@ __device__ __forceinline__ void finish_tile(const AttnArgs &a, const AttnItem &i
     constexpr int DJ = D / 32;
     const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5, my = part * 32 + r, row = it.row0 + min(my, it.n_rows - 1);
     const float l = sum32(t.l);
-    // a value behind a row's own position had weight 0, but 0 times infinity is no number: such rows are done again without touching it
+    // a value behind a row's own position had weight 0, but 0 times infinity is no number, and weights of up to 2^SLACK may have taken a sum out of range: such rows are done again
     float none = 0.f;
 #pragma unroll
     for (int j = 0; j < DJ; ++j)
@@ -655,17 +657,17 @@ __device__ __forceinline__ void finish_tile(const AttnArgs &a, const AttnItem &i
         }
         return;
     }
+    const float f = l == 0.f ? 0.f : 1.f / l;
     if (it.part >= 0) {
         const int64_t at = it.part + (int64_t)kv_head * ((it.n_rows + 31) & ~31) + part * 32;
 #pragma unroll
         for (int j = 0; j < DJ; ++j)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                *reinterpret_cast<floatx4 *>(a.part_o + at * D + ((4 * j + k) * 64 + lane) * 4) = floatx4{t.o[j][4 * k], t.o[j][4 * k + 1], t.o[j][4 * k + 2], t.o[j][4 * k + 3]};
+                *reinterpret_cast<floatx4 *>(a.part_o + at * D + ((4 * j + k) * 64 + lane) * 4) = floatx4{t.o[j][4 * k], t.o[j][4 * k + 1], t.o[j][4 * k + 2], t.o[j][4 * k + 3]} * f;
         if (h == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * (at + r)) = make_float2(t.m, l);
         return;
     }
-    const float f = l == 0.f ? 0.f : 1.f / l;
     E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D;
 #pragma unroll
     for (int j = 0; j < DJ; ++j) {
@@ -1169,7 +1171,11 @@ __global__ __launch_bounds__(256) void attn_join_kernel(JoinArgs a)
     }
     l = wave_sum(l);
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    const auto weight = [&](int i) { return __builtin_amdgcn_exp2f(a.part_ml[2 * (first + (int64_t)i * it.stride)] - m); };
+    const float each = l == 0.f ? 0.f : 1.f / l;
+    const auto weight = [&](int i) {
+        const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (first + (int64_t)i * it.stride));
+        return ml.y * __builtin_amdgcn_exp2f(ml.x - m) * each;
+    };
 #pragma unroll
     for (int k = 0; k < AT_ONCE; ++k)
         if (g + k * GROUPS < it.n_parts) o += v[k] * weight(g + k * GROUPS);
@@ -1179,8 +1185,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(JoinArgs a)
     if (g == 0) {
         for (int i = 1; i < GROUPS; ++i) o += *reinterpret_cast<const floatx4 *>(&sums[i][d]);
         const int row = it.row0 + r;
-        const float f = l == 0.f ? 0.f : 1.f / l;
-        put_four(static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D + d, o * f);
+        put_four(static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D + d, o);
     }
 }
 
@@ -1216,25 +1221,28 @@ __global__ __launch_bounds__(256) void attn_join_tiles_kernel(JoinArgs a)
         float top = m;
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) top = fmaxf(top, x[j].x);
-        const float fade = __builtin_amdgcn_exp2f(m - top);
+        const float before = l * __builtin_amdgcn_exp2f(m - top);
         m = top;
-        l *= fade;
-#pragma unroll
-        for (int k = 0; k < N; ++k) o[k] *= fade;
+        l = before;
+        float w[AT_ONCE];
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) {
-            const float f = __builtin_amdgcn_exp2f(x[j].x - m);  // (of a part that is not there: times 0)
-            l += x[j].y * f;
-#pragma unroll
-            for (int k = 0; k < N; ++k) o[k] += v[j][k] * f;
+            w[j] = x[j].y * __builtin_amdgcn_exp2f(x[j].x - m);  // (of a part that is not there: 0)
+            l += w[j];
         }
+        const float each = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int k = 0; k < N; ++k) o[k] *= before * each;
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j)
+#pragma unroll
+            for (int k = 0; k < N; ++k) o[k] += v[j][k] * (w[j] * each);
     }
     if (group * 32 + r >= it.n_rows) return;
     const int row = it.row0 + group * 32 + r;
-    const float f = l == 0.f ? 0.f : 1.f / l;
     E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D;
 #pragma unroll
-    for (int k = 0; k < N; ++k) put_four(out + (k * 4 + threadIdx.x / 64) * 8 + lane / 32 * 4, o[k] * f);
+    for (int k = 0; k < N; ++k) put_four(out + (k * 4 + threadIdx.x / 64) * 8 + lane / 32 * 4, o[k]);
 }
 
 namespace {

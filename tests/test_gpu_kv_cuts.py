@@ -184,3 +184,55 @@ def test_batches_without_tiles_take_no_way_of_theirs(segs):
             check(s)
     finally:
         s.close()
+
+
+# Batches whose single tokens, short segments and tiles are worked on and joined in every way
+LARGE = [
+    ([(5, 1), (300, 1), (0, 1), (40, 5)], 4, 2, 64, 0), ([(2500, 1), (4000, 2), (77, 1)], 8, 2, 128, 2), ([(1300, 1), (600, 3)], 2, 1, 256, 1),
+    ([(i % 60, 1) for i in range(140)], 4, 4, 256, 0), ([(0, 70), (10, 200)], 4, 4, 64, 0), ([(2500, 60), (1800, 1)], 6, 2, 128, 2), ([(1500, 90)], 4, 2, 256, 1),
+    ([(0, 60)] * 30 + [(1700, 100)], 32, 32, 128, 1), ([(600, 1024)], 128, 16, 128, 0), ([(2500, 1), (311, 1700), (6000, 50)], 80, 16, 128, 2),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [1e33, 1e36, 2e37, 3e38])
+@pytest.mark.parametrize("segs,heads,kv,dim,joins", LARGE)
+def test_values_near_the_types_largest(segs, heads, kv, dim, joins, size, dtype):
+    """Outputs are means of values: finite where those are, however close to the end of the type's range."""
+    s = Setup(segs, heads, kv, dim, dtype=dtype, seed=28)
+    try:
+        assert info_of(s).n_joins >= joins
+        host = s.host.float()
+        sign = torch.where(torch.arange(dim) % 3 == 0, -1.0, 1.0).repeat_interleave(s.u).repeat(s.page // s.u)  # the values of a place have one sign: their sums grow
+        host[:, :, 1] = (0.1 + 0.9 * torch.rand(host[:, :, 1].shape, generator=torch.Generator().manual_seed(1))) * size * sign
+        s.host = host.to(s.dt)
+        s.cache.pages.copy_(s.host)
+        check(s)
+    finally:
+        s.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("segs,heads,kv,dim,joins", LARGE[:8])
+def test_an_infinite_value_that_a_token_sees(segs, heads, kv, dim, joins, dtype):
+    """One value of one token of each segment: that place of the outputs that see it is infinite, all others are as they were."""
+    s = Setup(segs, heads, kv, dim, dtype=dtype, seed=29)
+    try:
+        scale, g = 1.0 / math.sqrt(dim), heads // kv
+        out, mass, reach = definition(s, scale)
+        a, inf = s.host.float().numpy(), np.zeros(out.shape, bool)
+        for i, (c, n) in enumerate(segs):
+            at, d, sign = (c + n) * 2 // 3, i % dim, 1 - 2 * (i % 2)
+            k, v = kv_plain.read(a, s.tables[i], 0, kv - 1, s.page, dim, s.u, c + n)
+            v[at, d] = sign * np.inf
+            kv_plain.write(a, s.tables[i], 0, kv - 1, s.page, dim, s.u, 0, k, v)
+            rows = slice(int(s.offsets[i]) + max(at - c, 0), int(s.offsets[i + 1]))
+            inf[rows, (kv - 1) * g :, d] = True
+            out[rows, (kv - 1) * g :, d] = sign * np.inf
+        s.cache.pages.copy_(torch.from_numpy(a).to(s.dt))
+        got = s.run(scale).float().cpu().numpy()
+        assert np.array_equal(got[inf], out[inf])
+        over = np.where(inf, 0, np.abs(np.where(inf, 0, got) - np.where(inf, 0, out)) - s.bound(np.where(inf, 0, out), mass, reach))
+        assert np.isfinite(got[~inf]).all() and (over <= 0).all()
+    finally:
+        s.close()
