@@ -4,7 +4,8 @@
 // over the tokens keeps, per row, the running maximum m of the scores (in units of log2: s = q.k * scale * log2 e), the
 // sum l of exp2(s - m) and the vector o = sum exp2(s - m) v; when m grows, l and o are scaled by exp2(m_old - m_new).  The row's
 // output is o / l.  Parts of a sequence are kept as m, l and o / l and join with M = max m_i as l = sum l_i exp2(m_i - M), out = sum (o_i / l_i) (l_i exp2(m_i - M) / l):
-// means of values, which stay in range where the values do.  A token beyond the row's own position has weight 0 and its value is not multiplied at all.
+// means of values, which stay in range where the values do.  A part without a token that the row sees counts for nothing (l = 0); a row all of whose scores are -inf has no
+// softmax, and its output is no number.  A token beyond the row's own position has weight 0 and its value is not multiplied at all.
 #include <cfloat>
 #include <type_traits>
 
@@ -249,7 +250,7 @@ template <typename E, int D, bool TILE>
 __device__ __forceinline__ void put_row(const AttnArgs &a, const AttnItem &it, int kv_head, int r, const RowState<E, D> &st)
 {
     const int lane = threadIdx.x & 63;
-    const float f = st.l == 0.f ? 0.f : 1.f / st.l;
+    const float f = it.part >= 0 && st.l == 0.f ? 0.f : 1.f / st.l;
     if (it.part >= 0) {
         const int64_t at = it.part + (int64_t)kv_head * (TILE ? (it.n_rows + 31) & ~31 : it.n_rows) + r;
 #pragma unroll
@@ -414,7 +415,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it,
     if constexpr (ALONE) {  // (items that one wavefront has to itself are whole)
         if (redo) return again(0, 1);
         if (r >= it.n_rows) return;
-        const float f = l == 0.f ? 0.f : 1.f / l;
+        const float f = 1.f / l;
         E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D;
 #pragma unroll
         for (int j = 0; j < VJ; ++j) put_four(out + 16 * j + 4 * g, o[j] * f);
@@ -445,7 +446,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it,
                 f[w] = __builtin_amdgcn_exp2f(lds.m[w][rr] - top);
                 sum += lds.l[w][rr] * f[w];
             }
-            const float each = sum == 0.f ? 0.f : 1.f / sum;
+            const float each = it.part >= 0 && sum == 0.f ? 0.f : 1.f / sum;
             floatx4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < NW; ++w) v += *reinterpret_cast<const floatx4 *>(&lds.o[w][rr][d]) * (f[w] * each);
@@ -657,7 +658,7 @@ __device__ __forceinline__ void finish_tile(const AttnArgs &a, const AttnItem &i
         }
         return;
     }
-    const float f = l == 0.f ? 0.f : 1.f / l;
+    const float f = it.part >= 0 && l == 0.f ? 0.f : 1.f / l;
     if (it.part >= 0) {
         const int64_t at = it.part + (int64_t)kv_head * ((it.n_rows + 31) & ~31) + part * 32;
 #pragma unroll
@@ -1171,7 +1172,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(JoinArgs a)
     }
     l = wave_sum(l);
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    const float each = l == 0.f ? 0.f : 1.f / l;
+    const float each = 1.f / l;
     const auto weight = [&](int i) {
         const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (first + (int64_t)i * it.stride));
         return ml.y * __builtin_amdgcn_exp2f(ml.x - m) * each;
@@ -1242,7 +1243,7 @@ __global__ __launch_bounds__(256) void attn_join_tiles_kernel(JoinArgs a)
     const int row = it.row0 + group * 32 + r;
     E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D;
 #pragma unroll
-    for (int k = 0; k < N; ++k) put_four(out + (k * 4 + threadIdx.x / 64) * 8 + lane / 32 * 4, o[k]);
+    for (int k = 0; k < N; ++k) put_four(out + (k * 4 + threadIdx.x / 64) * 8 + lane / 32 * 4, l == 0.f ? o[k] / l : o[k]);
 }
 
 namespace {

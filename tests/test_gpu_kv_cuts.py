@@ -236,3 +236,32 @@ def test_an_infinite_value_that_a_token_sees(segs, heads, kv, dim, joins, dtype)
         assert np.isfinite(got[~inf]).all() and (over <= 0).all()
     finally:
         s.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("segs,heads,kv,dim,joins", LARGE)
+def test_rows_all_of_whose_scores_are_minus_infinity(segs, heads, kv, dim, joins, dtype):
+    """They have no softmax: no number, as the formula has it.  Rows that see one finite score are as if the others were not there."""
+    s = Setup(segs, heads, kv, dim, dtype=dtype, seed=30)
+    try:
+        s.q, scale, g = s.q.abs() + 0.01, 1.0 / math.sqrt(dim), heads // kv
+        a, none = s.host.float().numpy(), np.zeros((s.T, heads), bool)
+        for i, (c, n) in enumerate(segs):
+            upto = c + n // 2 if n > 1 else c + i % 2  # tokens of -inf: of half of a prompt's tokens, and of every other single token, all that they see
+            k, v = kv_plain.read(a, s.tables[i], 0, 0, s.page, dim, s.u, c + n)
+            k[:upto] = -np.inf
+            kv_plain.write(a, s.tables[i], 0, 0, s.page, dim, s.u, 0, k, v)
+            none[int(s.offsets[i]) : int(s.offsets[i]) + max(upto - c, 0), :g] = True
+        s.host = torch.from_numpy(a).to(s.dt)
+        s.cache.pages.copy_(s.host)
+        got = s.run(scale).float().cpu().numpy()
+        finite = s.host.clone()
+        finite[torch.isneginf(finite)] = -1e4  # a weight of 0 too, and a bound on rounding that is a number
+        s.host = finite
+        out, mass, _reach = definition(s, scale)
+        reach = np.full(none.shape, 6.0 * math.sqrt(dim))
+        assert none.any() and np.isnan(got[none]).all()
+        over = np.where(none[..., None], 0, np.abs(got - out) - s.bound(out, mass, reach))
+        assert np.isfinite(got[~none]).all() and (over <= 0).all()
+    finally:
+        s.close()
