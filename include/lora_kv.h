@@ -88,7 +88,8 @@ int lora_kv_seq_add(lora_kv_t *kv, int32_t n, const int64_t *ids);
 int lora_kv_seq_fork(lora_kv_t *kv, int64_t parent, int32_t n, const int64_t *ids, int32_t n_tokens);
 
 /* Add n_tokens[i] tokens to sequence ids[i] whose keys and values the caller puts into the pages himself (restored from
- * elsewhere, say): takes pages -- the free ones with the lowest numbers --, copies a shared page that the tokens begin in.
+ * elsewhere, say) by work on `stream`, which waits for the cache's earlier work on other streams: takes pages -- the free ones with the lowest
+ * numbers --, copies a shared page that the tokens begin in.
  * Batches with a sequence whose page was copied can't be used any more.  LORA_E_NOMEM if there are too few pages, LORA_E_NOTFOUND,
  * LORA_E_INVAL (a sequence named twice, a negative count), LORA_E_STATE on a stream that is captured. */
 int lora_kv_seq_extend(lora_kv_t *kv, int32_t n, const int64_t *ids, const int32_t *n_tokens, void *stream);
@@ -111,8 +112,8 @@ int lora_kv_seq_pages(const lora_kv_t *kv, int64_t id, int32_t *pages, int32_t c
 /* ---- pages ------------------------------------------------------------------------------- */
 
 /* Move pages so that the ones in use are the lowest numbers (the highest ones are copied, all layers, into the holes).  *moved
- * receives how many.  All batches that are alive can't be used any more if any page moved.  LORA_E_STATE on a stream that is
- * captured. */
+ * receives how many.  All batches that are alive can't be used any more if any page moved.  Work on `stream` after the call comes after all
+ * earlier work on the pages, also if none moved: it may put those that are free behind a limit to another use.  LORA_E_STATE on a stream that is captured. */
 int lora_kv_compact(lora_kv_t *kv, void *stream, int32_t *moved);
 
 /* Pages with numbers from `limit` on are not handed out (limit up to n_pages; the memory behind them is the caller's to use).

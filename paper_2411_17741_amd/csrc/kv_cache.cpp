@@ -578,13 +578,13 @@ int lora_kv_seq_extend(lora_kv_t *kv, int32_t n, const int64_t *ids, const int32
     return guarded([&]() -> int {
         Growth g;
         if (const int rc = check_growth(*kv, n, ids, n_tokens, nullptr, g)) return rc;
-        if (!kv->host_only)
-            if (const int rc = refuse_capture(st)) return rc;
         reserve(*kv, g);
+        if (!kv->host_only) {
+            if (const int rc = refuse_capture(st)) return rc;
+            if (const int rc = in_order(*kv, st)) return rc;  // (also where nothing is copied: what the caller puts into the pages must not overtake work that reads them)
+        }
         grow(*kv, g);
-        if (kv->host_only || g.from.empty()) return LORA_OK;
-        if (const int rc = in_order(*kv, st)) return rc;
-        return copy_pages(*kv, g.from, g.to, st);
+        return g.from.empty() || kv->host_only ? LORA_OK : copy_pages(*kv, g.from, g.to, st);
     });
 }
 
@@ -669,13 +669,14 @@ int lora_kv_compact(lora_kv_t *kv, void *stream, int32_t *moved)
             from.push_back(p);
             to.push_back(hole++);
         }
-        if (from.empty()) return LORA_OK;
         std::vector<int32_t> where(kv->cfg.n_pages);
         if (!kv->host_only) {
             if (const int rc = refuse_capture(st)) return rc;
-            if (const int rc = in_order(*kv, st)) return rc;
-            if (const int rc = copy_pages(*kv, from, to, st)) return rc;
+            if (const int rc = in_order(*kv, st)) return rc;  // (also where nothing moves: the free pages may be put to another use next, behind a limit)
         }
+        if (from.empty()) return LORA_OK;
+        if (!kv->host_only)
+            if (const int rc = copy_pages(*kv, from, to, st)) return rc;
         for (int32_t p = 0; p < kv->cfg.n_pages; ++p) where[p] = p;
         const auto mark = [&](int32_t p, bool is_free) {
             const uint64_t bit = (uint64_t)1 << (p & 63);

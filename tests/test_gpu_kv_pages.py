@@ -174,3 +174,43 @@ def test_a_captured_stream_takes_no_batch():
         assert bool((x == 1).all())
     finally:
         cache.close()
+
+
+def test_pages_are_given_out_behind_the_work_that_reads_them():
+    """A request ends while its attention is still to come on one stream; its pages are filled for another request, or put to another use behind a limit, on a second stream."""
+    from paper_2411_17741_amd.kv import KvCache
+
+    cache = KvCache(1, 4, 2, 64, 20, page_tokens=32, max_seqs=4, max_batch_seqs=2, max_batch_tokens=8)
+    try:
+        one, two = torch.cuda.Stream(), torch.cuda.Stream()
+        q = torch.randn(1, 4, 64, device="cuda").bfloat16()
+        for use in ("extend", "compact"):
+            cache.pages.normal_()
+            cache.add([0])
+            cache.extend([0], [600])
+            batch = cache.batch([0], [0, 1])
+            want, out = torch.empty_like(q), torch.empty_like(q)
+            cache.attend(batch, 0, q, want, 0.1)
+            torch.cuda.synchronize()
+            with torch.cuda.stream(one):
+                torch.cuda._sleep(20_000_000)
+            cache.attend(batch, 0, q, out, 0.1, stream=one)
+            cache.batch_destroy(batch)
+            cache.free([0])
+            if use == "extend":
+                cache.add([1])
+                cache.extend([1], [640], stream=two)
+                taken = torch.from_numpy(cache.pages_of(1).astype("int64")).cuda()
+                cache.free([1])
+            else:
+                assert cache.compact(stream=two) == 0
+                cache.set_limit(0)
+                taken = torch.arange(20, device="cuda")
+                cache.set_limit(20)
+            with torch.cuda.stream(two):
+                two.wait_stream(torch.cuda.default_stream())
+                cache.pages[taken] = float("nan")
+            torch.cuda.synchronize()
+            assert torch.equal(out, want), use
+    finally:
+        cache.close()
