@@ -176,7 +176,8 @@ size_t list_bytes(const lora_kv_config_t &c)
            align_up((size_t)max_items(c) * sizeof(AttnItem)) + align_up((size_t)MAX_EXTRA * sizeof(JoinItem)) + 3 * ALIGN;
 }
 
-// Work of a call on a stream waits for the work of the one before it on another.
+// Work of a call on a stream waits for the work of the one before it on another; asked for before a call changes anything.  Nothing can wait for a stream that is
+// being captured without becoming part of the capture, so calls on others are refused meanwhile.
 int in_order(lora_kv &kv, hipStream_t st)
 {
     if (kv.any_stream && kv.last == st) return LORA_OK;
@@ -184,6 +185,8 @@ int in_order(lora_kv &kv, hipStream_t st)
     KV_TRY(hipStreamIsCapturing(st, &cs));
     if (cs != hipStreamCaptureStatusNone) return LORA_OK;  // the caller's to order
     if (kv.any_stream) {
+        KV_TRY(hipStreamIsCapturing(kv.last, &cs));
+        if (cs != hipStreamCaptureStatusNone) return LORA_E_STATE;
         KV_TRY(hipEventRecord(kv.order_ev, kv.last));
         KV_TRY(hipStreamWaitEvent(st, kv.order_ev, 0));
     }
@@ -755,11 +758,11 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
         cut.page0.resize(n_seg);
         cut.rows.reserve(n_seg + MAX_EXTRA);
         cut.joins.reserve(MAX_EXTRA);
+        if (const int rc = in_order(*kv, st)) return rc;
         if (b->upload_pending) {
             KV_TRY(hipEventSynchronize(b->uploaded));
             b->upload_pending = false;
         }
-        if (const int rc = in_order(*kv, st)) return rc;
 
         std::vector<KvGroup> groups;
         groups.reserve((size_t)T / kv->chunk() + 2 * (size_t)n_seg);

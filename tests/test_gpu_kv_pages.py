@@ -214,3 +214,47 @@ def test_pages_are_given_out_behind_the_work_that_reads_them():
             assert torch.equal(out, want), use
     finally:
         cache.close()
+
+
+def test_no_call_joins_a_capture_of_another_stream():
+    """The latest call's stream is being captured: a call on another cannot wait for it, and is refused before it changes anything."""
+    from paper_2411_17741_amd import binding as B
+    from paper_2411_17741_amd.kv import KvCache
+
+    cache = KvCache(1, 4, 2, 64, 20, page_tokens=32, max_seqs=4, max_batch_seqs=3, max_batch_tokens=100)
+    try:
+        cache.pages.normal_()
+        q = torch.randn(3, 4, 64, device="cuda").bfloat16()
+        out, other_out, k = torch.zeros_like(q), torch.zeros_like(q), torch.randn(3, 2, 64, device="cuda").bfloat16()
+        graph, stream, other = torch.cuda.CUDAGraph(), torch.cuda.Stream(), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        cache.add([0, 1])
+        cache.extend([0, 1], [70, 70], stream=stream)
+        cache.fork(1, [2])
+        cache.free([0])  # (something to move)
+        batch = cache.batch([1, 2], [0, 1, 3], stream=stream)
+        cache.attend(batch, 0, q, out, 0.1, stream=stream)
+        pages, before, row, h, o = [cache.pages_of(i).tolist() for i in (1, 2)], cache.stats(), 4 * 64, cache.handle, other.cuda_stream
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            cache.attend(batch, 0, q, out, 0.1, stream=stream)
+            got = [B.lora_kv_batch_create(h, [1], [0, 1], o)[0], B.lora_kv_seq_extend(h, [1, 2], [40, 1], o), B.lora_kv_compact(h, o)[0],
+                   B.lora_kv_append(h, batch, 0, k.data_ptr(), k.data_ptr(), 128, 128, stream=o),
+                   B.lora_kv_attend(h, batch, 0, q.data_ptr(), row, other_out.data_ptr(), row, 0.1, o)]
+        assert got == [B.LORA_E_STATE] * 5
+        after = cache.stats()
+        assert [cache.pages_of(i).tolist() for i in (1, 2)] == pages and all(getattr(after, n) == getattr(before, n) for n, _t in before._fields_)
+        assert cache.length(1) == 71 and cache.length(2) == 72
+        # afterwards they go through, and the graph holds its own call alone
+        cache.attend(batch, 0, q, other_out, 0.1, stream=other)
+        torch.cuda.synchronize()
+        want = other_out.clone()
+        for _ in range(3):
+            out.zero_(), other_out.zero_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want) and not other_out.any()
+        assert B.lora_kv_batch_create(h, [1], [0, 1], o)[0] == B.LORA_OK and cache.compact(stream=other) > 0
+    finally:
+        cache.close()
