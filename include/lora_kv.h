@@ -42,7 +42,7 @@ extern "C" {
 #endif
 
 typedef struct lora_kv lora_kv_t;             /* opaque */
-typedef struct lora_kv_batch lora_kv_batch_t; /* opaque: device-resident lists of one batch */
+typedef struct lora_kv_batch lora_kv_batch_t; /* opaque: device-resident lists of one batch; a handle never comes back, that of a destroyed batch is refused */
 
 enum { LORA_KV_HOST_ONLY = 1 }; /* flags: sequences and pages only, no device work */
 

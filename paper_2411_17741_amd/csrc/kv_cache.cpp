@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <mutex>
 #include <new>
 #include <unordered_map>
 #include <vector>
@@ -46,10 +47,10 @@ struct Seq {
     std::vector<int32_t> pages;
 };
 
-}  // namespace
-
-struct lora_kv_batch {
-    bool alive = false, stale = false, upload_pending = false;
+// A batch's lists, of which a cache has n_batches and a few; `name` is what the caller holds of a batch, 0 if the lists are nobody's.
+struct Batch {
+    uint64_t name = 0;
+    bool stale = false, upload_pending = false;
     int64_t freed_at = 0;  // order in which lists became free
     char *dev = nullptr, *pinned = nullptr;
     const char *pinned_dev = nullptr;
@@ -59,7 +60,18 @@ struct lora_kv_batch {
     int32_t n_joins = 0, n_tile_joins = 0, join_rows = 0;  // join_rows: the most rows of a join of row items
     size_t off_tokens = 0, off_groups = 0, off_pages = 0, off_rows = 0, off_tiles = 0, off_joins = 0, off_tile_joins = 0;
     std::vector<uint8_t> member;  // by sequence slot
+    bool alive() const { return name != 0; }
 };
+
+// Batches are known by numbers that are given once in the life of the process: which lists of their cache, below, and a count.  So a batch that was destroyed, or is another
+// cache's, is never taken for one that is alive.  The lock guards the count, the list of caches and the names and infos of their batches for lora_kv_batch_info, which is told
+// no cache.
+constexpr int NAME_BITS = 11;
+std::mutex g_lock;
+uint64_t g_names = 0;
+lora_kv *g_caches = nullptr;
+
+}  // namespace
 
 struct lora_kv {
     lora_kv_config_t cfg{};
@@ -81,7 +93,8 @@ struct lora_kv {
     std::vector<uint32_t> seen;  // by sequence slot: the call that named it last
     uint32_t call = 0;
 
-    std::vector<lora_kv_batch> batches;
+    std::vector<Batch> batches;
+    lora_kv *next = nullptr, *before = nullptr;  // in g_caches
     int64_t tick = 0;
     int32_t alive_batches = 0;
 
@@ -133,7 +146,7 @@ struct lora_kv {
     void drop_batches_with(const Seq &s)
     {
         for (auto &b : batches)
-            if (b.alive && b.member[slot(s)]) b.stale = true;
+            if (b.alive() && b.member[slot(s)]) b.stale = true;
     }
 };
 
@@ -143,6 +156,14 @@ using lora::AttnItem;
 using lora::JoinItem;
 using lora::KvGroup;
 using lora::KvToken;
+
+static_assert(1024 + SPARE_BATCHES <= 1 << NAME_BITS, "the most batches of a cache");
+
+Batch *find_batch(lora_kv &kv, const lora_kv_batch_t *handle)
+{
+    const uint64_t name = reinterpret_cast<uintptr_t>(handle), at = name & ((1 << NAME_BITS) - 1);
+    return name && at < kv.batches.size() && kv.batches[at].name == name ? &kv.batches[at] : nullptr;
+}
 
 size_t elem_bytes(int32_t dtype) { return dtype == LORA_BF16 ? 2 : 4; }
 
@@ -502,6 +523,12 @@ int lora_kv_create(const lora_kv_config_t *cfg, void *dev_pages, size_t pages_by
             kv->part_o = reinterpret_cast<float *>(at);
             kv->part_ml = kv->part_o + kv->part_rows * cfg->head_dim;
         }
+        {
+            std::lock_guard<std::mutex> lock(g_lock);
+            kv->next = g_caches;
+            if (g_caches) g_caches->before = kv;
+            g_caches = kv;
+        }
         guard.kv = nullptr;
         *out = kv;
         return LORA_OK;
@@ -511,6 +538,12 @@ int lora_kv_create(const lora_kv_config_t *cfg, void *dev_pages, size_t pages_by
 int lora_kv_destroy(lora_kv_t *kv)
 {
     if (!kv) return LORA_E_INVAL;
+    {
+        std::lock_guard<std::mutex> lock(g_lock);
+        if (kv->next) kv->next->before = kv->before;
+        if (kv->before) kv->before->next = kv->next;
+        else if (g_caches == kv) g_caches = kv->next;
+    }
     for (auto &b : kv->batches) {
         if (b.pinned) (void)hipHostFree(b.pinned);
         if (b.uploaded) (void)hipEventDestroy(b.uploaded);
@@ -694,7 +727,7 @@ int lora_kv_compact(lora_kv_t *kv, void *stream, int32_t *moved)
         }
         for (auto &s : kv->seqs)
             for (int32_t &p : s.pages) p = where[p];
-        for (auto &b : kv->batches) b.stale = b.stale || b.alive;
+        for (auto &b : kv->batches) b.stale = b.stale || b.alive();
         kv->free_from = 0;
         kv->copied += (int64_t)from.size();
         if (moved) *moved = (int32_t)from.size();
@@ -750,9 +783,9 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
         if (const int rc = refuse_capture(st)) return rc;
 
         // the lists that have been free for longest: their last upload is over or nearly so
-        lora_kv_batch *b = nullptr;
+        Batch *b = nullptr;
         for (auto &x : kv->batches)
-            if (!x.alive && (!b || x.freed_at < b->freed_at)) b = &x;
+            if (!x.alive() && (!b || x.freed_at < b->freed_at)) b = &x;
         reserve(*kv, g);
         Cut cut;
         cut.page0.resize(n_seg);
@@ -826,42 +859,46 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
         b->n_joins = (int32_t)cut.joins.size(), b->n_tile_joins = (int32_t)cut.tile_joins.size();
         b->join_rows = 0;
         for (const JoinItem &j : cut.joins) b->join_rows = std::max(b->join_rows, j.n_rows);
-        b->info = {T, n_seg, (int32_t)n_pages, (int32_t)groups.size(), (int32_t)cut.rows.size(), (int32_t)cut.tiles.size(), (int32_t)(cut.joins.size() + cut.tile_joins.size()),
-                   cut.n_short, (int32_t)cut.way};
         if (const int rc = copy_pages(*kv, g.from, g.to, st, {b->dev, b->pinned_dev, (uint32_t)((at + 15) / 16)}, b->uploaded)) return rc;
         b->upload_pending = true;
         b->stale = false;
-        b->alive = true;
         ++kv->alive_batches;
-        *out = b;
+        std::lock_guard<std::mutex> lock(g_lock);
+        b->info = {T, n_seg, (int32_t)n_pages, (int32_t)groups.size(), (int32_t)cut.rows.size(), (int32_t)cut.tiles.size(), (int32_t)(cut.joins.size() + cut.tile_joins.size()),
+                   cut.n_short, (int32_t)cut.way};
+        b->name = ++g_names << NAME_BITS | (uint64_t)(b - kv->batches.data());
+        *out = reinterpret_cast<lora_kv_batch_t *>((uintptr_t)b->name);
         return LORA_OK;
     });
 }
 
-static bool of(const lora_kv_t *kv, const lora_kv_batch_t *b)
+int lora_kv_batch_destroy(lora_kv_t *kv, lora_kv_batch_t *handle)
 {
-    return b >= kv->batches.data() && b < kv->batches.data() + kv->batches.size() && b->alive;
-}
-
-int lora_kv_batch_destroy(lora_kv_t *kv, lora_kv_batch_t *batch)
-{
-    if (!kv || !batch || !of(kv, batch)) return LORA_E_INVAL;
-    batch->alive = false;
+    Batch *const batch = kv ? find_batch(*kv, handle) : nullptr;
+    if (!batch) return LORA_E_INVAL;
     batch->freed_at = ++kv->tick;
     --kv->alive_batches;
+    std::lock_guard<std::mutex> lock(g_lock);
+    batch->name = 0;
     return LORA_OK;
 }
 
-int lora_kv_batch_info(const lora_kv_batch_t *batch, lora_kv_batch_info_t *out)
+int lora_kv_batch_info(const lora_kv_batch_t *handle, lora_kv_batch_info_t *out)
 {
-    if (!batch || !out) return LORA_E_INVAL;
-    *out = batch->info;
-    return LORA_OK;
+    if (!handle || !out) return LORA_E_INVAL;
+    std::lock_guard<std::mutex> lock(g_lock);
+    for (lora_kv *kv = g_caches; kv; kv = kv->next)
+        if (const Batch *const batch = find_batch(*kv, handle)) {
+            *out = batch->info;
+            return LORA_OK;
+        }
+    return LORA_E_INVAL;
 }
 
-int lora_kv_append(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const lora_kv_append_t *a, void *stream)
+int lora_kv_append(lora_kv_t *kv, lora_kv_batch_t *handle, int32_t layer, const lora_kv_append_t *a, void *stream)
 {
-    if (!kv || !batch || !a || !of(kv, batch) || layer < 0 || layer >= kv->cfg.n_layers) return LORA_E_INVAL;
+    Batch *const batch = kv ? find_batch(*kv, handle) : nullptr;
+    if (!batch || !a || layer < 0 || layer >= kv->cfg.n_layers) return LORA_E_INVAL;
     if (batch->stale) return LORA_E_STATE;
     const lora_kv_config_t &c = kv->cfg;
     const int64_t row = (int64_t)c.n_kv_heads * c.head_dim, q_row = (int64_t)c.n_heads * c.head_dim, u = kv->chunk();
@@ -893,10 +930,11 @@ int lora_kv_append(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const l
     return LORA_OK;
 }
 
-int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride, float scale,
+int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *handle, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride, float scale,
                    void *stream)
 {
-    if (!kv || !batch || !of(kv, batch) || layer < 0 || layer >= kv->cfg.n_layers) return LORA_E_INVAL;
+    Batch *const batch = kv ? find_batch(*kv, handle) : nullptr;
+    if (!batch || layer < 0 || layer >= kv->cfg.n_layers) return LORA_E_INVAL;
     if (batch->stale) return LORA_E_STATE;
     const lora_kv_config_t &c = kv->cfg;
     const float scale_log2 = scale * 1.44269504088896340736f;

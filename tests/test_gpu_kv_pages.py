@@ -258,3 +258,40 @@ def test_no_call_joins_a_capture_of_another_stream():
         assert B.lora_kv_batch_create(h, [1], [0, 1], o)[0] == B.LORA_OK and cache.compact(stream=other) > 0
     finally:
         cache.close()
+
+
+def test_a_destroyed_batch_stays_one():
+    """Its lists serve other batches later; its handle is refused for good, and does nothing to them."""
+    from paper_2411_17741_amd import binding as B
+    from paper_2411_17741_amd.kv import KvCache
+
+    make = lambda: KvCache(1, 2, 2, 64, 10, page_tokens=32, max_seqs=4, n_batches=2)  # noqa: E731
+    cache, other = make(), make()
+    try:
+        q = torch.zeros(1, 2, 64, device="cuda").bfloat16()
+        k, out, h = torch.zeros_like(q), torch.zeros_like(q), cache.handle
+        for c in (cache, other):
+            c.add([1])
+        first = other.batch([1], [0, 1])
+        old = []
+        for i in range(12):
+            batch = cache.batch([1], [0, 1])
+            for b in old[-9:] + [first]:
+                assert B.lora_kv_batch_destroy(h, b) == B.LORA_E_INVAL
+                assert B.lora_kv_attend(h, b, 0, q.data_ptr(), 128, out.data_ptr(), 128, 0.1) == B.LORA_E_INVAL
+                assert B.lora_kv_append(h, b, 0, k.data_ptr(), k.data_ptr(), 128, 128) == B.LORA_E_INVAL
+            assert all(B.lora_kv_batch_info(b)[0] == B.LORA_E_INVAL for b in old)
+            rc, info = B.lora_kv_batch_info(batch)
+            assert rc == 0 and info.n_tokens == 1 and B.lora_kv_batch_info(first)[0] == 0
+            cache.append(batch, 0, k, k)
+            cache.attend(batch, 0, q, out, 0.1)
+            cache.batch_destroy(batch)
+            old.append(batch)
+        torch.cuda.synchronize()
+        assert cache.length(1) == 12
+        assert B.lora_kv_batch_info(None)[0] == B.LORA_E_INVAL
+        other.batch_destroy(first)
+    finally:
+        cache.close()
+        other.close()
+    assert all(B.lora_kv_batch_info(b)[0] == B.LORA_E_INVAL for b in old + [first])
