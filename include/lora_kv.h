@@ -24,7 +24,8 @@
  *
  * Conventions are those of lora_cache.h: every function returns LORA_OK or a negative lora_status, nothing aborts or
  * throws; device memory is the caller's; streams are hipStream_t as void* (NULL = the default stream); calls only
- * enqueue work.  One lora_kv_t is driven by one host thread at a time.  Calls that enqueue work wait, on the device,
+ * enqueue work.  A cache belongs to the device that is current when it is created: its buffers, tensors and streams are that
+ * device's (calls make it current for themselves).  One lora_kv_t is driven by one host thread at a time.  Calls that enqueue work wait, on the device,
  * for the latest earlier call's stream if theirs is another one (that stream has to exist still; while it is being captured
  * calls on others return LORA_E_STATE; an ordering between captured calls and others is the caller's).  Lists of sequences
  * are checked before anything changes: a call that returns an error has changed nothing, except LORA_E_HIP.

@@ -80,7 +80,7 @@ struct lora_kv {
     size_t layer_bytes = 0, page_bytes = 0, list_cap = 0;
     float *part_o = nullptr, *part_ml = nullptr;
     int64_t part_rows = 0;
-    int page_shift = 0, n_cu = 256;
+    int page_shift = 0, n_cu = 256, device = 0;
 
     std::vector<Seq> seqs;
     std::vector<int32_t> free_seqs;
@@ -196,6 +196,23 @@ size_t list_bytes(const lora_kv_config_t &c)
     return align_up(T * sizeof(KvToken)) + align_up(T * sizeof(KvGroup)) + align_up((size_t)c.max_batch_pages * 4) +
            align_up((size_t)max_items(c) * sizeof(AttnItem)) + align_up((size_t)MAX_EXTRA * sizeof(JoinItem)) + 3 * ALIGN;
 }
+
+// The cache's device is the current one as long as this lives: events, the default stream and kernels are the current device's.
+class OnDevice {
+    int back_ = -1;
+
+public:
+    explicit OnDevice(const lora_kv &kv)
+    {
+        int now = 0;
+        if (!kv.host_only && hipGetDevice(&now) == hipSuccess && now != kv.device && hipSetDevice(kv.device) == hipSuccess) back_ = now;
+    }
+    ~OnDevice()
+    {
+        if (back_ >= 0) (void)hipSetDevice(back_);
+    }
+    OnDevice(const OnDevice &) = delete;
+};
 
 // Work of a call on a stream waits for the work of the one before it on another; asked for before a call changes anything.  Nothing can wait for a stream that is
 // being captured without becoming part of the capture, so calls on others are refused meanwhile.
@@ -505,9 +522,9 @@ int lora_kv_create(const lora_kv_config_t *cfg, void *dev_pages, size_t pages_by
         for (auto &b : kv->batches) b.member.assign(cfg->max_seqs, 0);
         if (!host_only) {
             KV_TRY(lora::prepare_attn_kernels());
-            int device = 0, n = 0;
-            KV_TRY(hipGetDevice(&device));
-            KV_TRY(hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, device));
+            int n = 0;
+            KV_TRY(hipGetDevice(&kv->device));
+            KV_TRY(hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, kv->device));
             if (n > 0) kv->n_cu = n;
             char *at = kv->work;
             for (auto &b : kv->batches) {
@@ -612,6 +629,7 @@ int lora_kv_seq_extend(lora_kv_t *kv, int32_t n, const int64_t *ids, const int32
     if (!kv || n < 0 || (n && (!ids || !n_tokens))) return LORA_E_INVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
     return guarded([&]() -> int {
+        const OnDevice on(*kv);
         Growth g;
         if (const int rc = check_growth(*kv, n, ids, n_tokens, nullptr, g)) return rc;
         reserve(*kv, g);
@@ -697,6 +715,7 @@ int lora_kv_compact(lora_kv_t *kv, void *stream, int32_t *moved)
     if (moved) *moved = 0;
     hipStream_t st = static_cast<hipStream_t>(stream);
     return guarded([&]() -> int {
+        const OnDevice on(*kv);
         std::vector<int32_t> from, to;
         int32_t hole = 0;
         for (int32_t p = kv->used_pages; p < kv->limit; ++p) {
@@ -773,6 +792,7 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
     if (T > kv->cfg.max_batch_tokens) return LORA_E_NOMEM;
     hipStream_t st = static_cast<hipStream_t>(stream);
     return guarded([&]() -> int {
+        const OnDevice on(*kv);
         if (kv->alive_batches >= kv->cfg.n_batches) return LORA_E_NOMEM;
         Growth g;
         if (const int rc = check_growth(*kv, n_seg, seg_seq, nullptr, seg_offsets, g)) return rc;
@@ -913,6 +933,7 @@ int lora_kv_append(lora_kv_t *kv, lora_kv_batch_t *handle, int32_t layer, const 
     if (a->rope && a->rope_pairs != LORA_ROPE_HALVES && a->rope_pairs != LORA_ROPE_NEIGHBOURS) return LORA_E_INVAL;
     if (!batch->info.n_tokens) return LORA_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
+    const OnDevice on(*kv);
     if (const int rc = in_order(*kv, st)) return rc;
     lora::AppendArgs k{};
     k.q = a->q, k.k = a->k, k.v = a->v, k.q_out = a->q_out;
@@ -944,6 +965,7 @@ int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *handle, int32_t layer, const 
     const auto bad = [&](const void *p, int64_t stride) { return !p || !aligned16(p) || stride < row || stride % u || stride > ((int64_t)1 << 40); };
     if (bad(q, q_stride) || bad(out, out_stride) || (q == out && q_stride != out_stride)) return LORA_E_INVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
+    const OnDevice on(*kv);
     if (const int rc = in_order(*kv, st)) return rc;
     lora::AttnArgs a{};
     a.q = q, a.out = out, a.q_stride = q_stride, a.out_stride = out_stride;

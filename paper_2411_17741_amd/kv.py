@@ -22,8 +22,9 @@ class KvCache:
                  dtype: int = B.LORA_BF16, device: str = "cuda:0", pages: Optional[torch.Tensor] = None):
         if not torch.cuda.is_available():
             raise RuntimeError("KvCache needs a GPU: the library has no CPU path")
-        self.device = torch.device(device)
-        self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
+        index = torch.device(device).index
+        self._index = index if index is not None else torch.cuda.current_device()
+        self.device = torch.device("cuda", self._index)
         self.n_heads, self.n_kv_heads, self.head_dim, self.dtype = n_heads, n_kv_heads, head_dim, _dtype(dtype)
         # (forks share pages: the sequences of a batch may name more pages than there are)
         max_batch_pages = max_batch_pages or min(max_batch_seqs * n_pages, 4 * n_pages + 65536)
@@ -35,11 +36,12 @@ class KvCache:
         shape = (n_pages, n_layers, 2, n_kv_heads, page_tokens * head_dim)
         if pages is None:
             pages = torch.empty(shape, dtype=self.dtype, device=self.device)
-        if tuple(pages.shape) != shape or pages.dtype != self.dtype or not pages.is_cuda or not pages.is_contiguous():
-            raise ValueError(f"pages: a contiguous {self.dtype} GPU tensor of shape {shape} is wanted")
+        if tuple(pages.shape) != shape or pages.dtype != self.dtype or pages.get_device() != self._index or not pages.is_contiguous():
+            raise ValueError(f"pages: a contiguous {self.dtype} tensor of shape {shape} on {self.device} is wanted")
         self.pages = pages
         self.work = torch.empty(work + 256, dtype=torch.uint8, device=self.device)
-        rc, self.handle = B.lora_kv_create(self.cfg, pages.data_ptr(), n_bytes, (self.work.data_ptr() + 255) // 256 * 256, work)
+        with torch.cuda.device(self._index):  # the cache belongs to the device that is current now
+            rc, self.handle = B.lora_kv_create(self.cfg, pages.data_ptr(), n_bytes, (self.work.data_ptr() + 255) // 256 * 256, work)
         B.check(rc, "lora_kv_create")
 
     def close(self) -> None:
@@ -114,8 +116,8 @@ class KvCache:
         flat = len(shape) == 2 and shape[1] == heads * d and stride[1] == 1
         if not (flat or (len(shape) == 3 and shape[1] == heads and shape[2] == d and stride[2] == 1 and (stride[1] == d or heads == 1))):
             raise ValueError(f"{name}: [{n}][{heads}][{d}] with the heads of a token in a row is wanted, got {tuple(shape)}, strides {stride}")
-        if shape[0] != n or t.dtype is not self.dtype or not t.is_cuda:
-            raise ValueError(f"{name}: {n} tokens of {self.dtype} on the GPU are wanted, got {tuple(shape)} of {t.dtype} on {t.device}")
+        if shape[0] != n or t.dtype is not self.dtype or t.get_device() != self._index:
+            raise ValueError(f"{name}: {n} tokens of {self.dtype} on {self.device} are wanted, got {tuple(shape)} of {t.dtype} on {t.device}")
         return t.data_ptr(), stride[0] if n > 1 else heads * d
 
     def append(self, batch, layer: int, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
@@ -132,8 +134,8 @@ class KvCache:
             raise ValueError("q_out without q")
         rp = rn = rd = 0
         if rope is not None:
-            if rope.dim() != 2 or rope.dtype != torch.float32 or not rope.is_cuda or not rope.is_contiguous():
-                raise ValueError("rope: a contiguous fp32 GPU tensor [positions][rope_dim] is wanted")
+            if rope.dim() != 2 or rope.dtype != torch.float32 or rope.get_device() != self._index or not rope.is_contiguous():
+                raise ValueError(f"rope: a contiguous fp32 tensor [positions][rope_dim] on {self.device} is wanted")
             rp, (rn, rd) = rope.data_ptr(), rope.shape
         B.check(B.lora_kv_append(self.handle, batch, layer, kp, vp, ks, vs, qp, op, qs, os_, rp, min(rn, 2**31 - 1), rd,
                                  B.LORA_ROPE_NEIGHBOURS if neighbours else B.LORA_ROPE_HALVES, self._stream(stream)), "lora_kv_append")

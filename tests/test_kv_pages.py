@@ -208,3 +208,44 @@ def test_handles_and_lists_are_checked():
     with pytest.raises(ValueError):
         B.lora_kv_batch_create(h, [5], [0])
     B.lora_kv_destroy(h)
+
+
+def test_tensors_of_another_gpu_are_refused(monkeypatch):
+    """Keys, values, queries, outputs and tables of angles have to lie on the cache's device: any other's address means nothing there.  Host only: tensors that
+    say where they lie, and calls that say that they were made."""
+    torch = pytest.importorskip("torch")
+    from types import SimpleNamespace
+
+    from paper_2411_17741_amd.kv import KvCache
+
+    class On:
+        def __init__(self, device, *shape, dtype=torch.bfloat16):
+            t = torch.empty(shape, dtype=dtype)
+            self.shape, self.dtype, self.is_cuda, self.device = t.shape, dtype, True, torch.device("cuda", device)
+            self.stride, self.dim, self.is_contiguous = t.stride, t.dim, t.is_contiguous
+
+        def get_device(self):
+            return self.device.index
+
+        def data_ptr(self):
+            return 4096
+
+    calls = []
+    for name in ("lora_kv_append", "lora_kv_attend"):
+        monkeypatch.setattr(B, name, lambda *a, name=name, **kw: calls.append(name) or 0)
+    cache = KvCache.__new__(KvCache)
+    cache.handle, cache.device, cache._index = None, torch.device("cuda", 0), 0
+    cache.n_heads, cache.n_kv_heads, cache.head_dim, cache.dtype = 4, 2, 64, torch.bfloat16
+    batch, stream = SimpleNamespace(n_tokens=3), SimpleNamespace(cuda_stream=0)
+
+    def call(**other):
+        on = lambda name: other.get(name, 0)  # noqa: E731
+        cache.append(batch, 0, On(on("k"), 3, 2, 64), On(on("v"), 3, 2, 64), q=On(on("q"), 3, 4, 64), q_out=On(on("q_out"), 3, 4, 64), rope=On(on("rope"), 9, 64, dtype=torch.float32), stream=stream)
+        cache.attend(batch, 0, On(on("aq"), 3, 4, 64), On(on("out"), 3, 4, 64), 0.1, stream=stream)
+
+    call()
+    assert calls == ["lora_kv_append", "lora_kv_attend"]
+    for name in ("k", "v", "q", "q_out", "rope", "aq", "out"):
+        with pytest.raises(ValueError, match="cuda:0"):
+            call(**{name: 1})
+    cache.handle = None
