@@ -15,7 +15,10 @@ def _dtype(dtype: int) -> torch.dtype:
 
 class KvCache:
     """Owns the cache handle and, unless the caller brings them, the pages' memory: a tensor
-    [n_pages][n_layers][2][n_kv_heads][page_tokens * head_dim] (see the header for what lies where in it)."""
+    [n_pages][n_layers][2][n_kv_heads][page_tokens * head_dim] (see the header for what lies where in it).
+
+    max_batch_pages: pages that the sequences of a batch may have together, one that they share counted for each; a batch with more is refused.  By default
+    whatever max_batch_seqs sequences can have, up to 4 million or 4 times the pages there are."""
 
     def __init__(self, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, n_pages: int, page_tokens: int = 64, max_seqs: int = 512,
                  max_batch_tokens: int = 4096, max_batch_seqs: int = 512, max_batch_pages: int = 0, n_batches: int = 2,
@@ -26,8 +29,8 @@ class KvCache:
         self._index = index if index is not None else torch.cuda.current_device()
         self.device = torch.device("cuda", self._index)
         self.n_heads, self.n_kv_heads, self.head_dim, self.dtype = n_heads, n_kv_heads, head_dim, _dtype(dtype)
-        # (forks share pages: the sequences of a batch may name more pages than there are)
-        max_batch_pages = max_batch_pages or min(max_batch_seqs * n_pages, 4 * n_pages + 65536)
+        # Forks share pages: the sequences of a batch may name more pages than there are.  Every sequence may name all of them, up to a list of 16 MB for each batch
+        max_batch_pages = max_batch_pages or min(max_batch_seqs * n_pages, max(4 * n_pages, 1 << 22))
         self.cfg = B.make_kv_config(n_layers, n_heads, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs, max_batch_seqs, max_batch_tokens,
                                     max_batch_pages, n_batches, dtype)
         n_bytes, work = B.lora_kv_pages_bytes(self.cfg), B.lora_kv_work_bytes(self.cfg)

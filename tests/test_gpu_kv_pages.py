@@ -295,3 +295,34 @@ def test_a_destroyed_batch_stays_one():
         cache.close()
         other.close()
     assert all(B.lora_kv_batch_info(b)[0] == B.LORA_E_INVAL for b in old + [first])
+
+
+def test_a_batch_of_many_forks_of_a_long_prefix():
+    """Its sequences name each page of the prefix: many times as many as there are, all of which are there."""
+    from paper_2411_17741_amd import binding as B
+    from paper_2411_17741_amd.kv import KvCache
+
+    n, prefix, page = 50, 2048, 32
+    cache = KvCache(1, 1, 1, 64, prefix + n + 2, page_tokens=page, max_seqs=n + 1, max_batch_tokens=n)
+    try:
+        cache.pages.normal_()
+        ids = np.arange(1, n + 1)
+        cache.add(0)
+        cache.extend(0, prefix * page - 5)
+        cache.fork(0, ids)
+        batch = cache.batch(ids, np.arange(n + 1))
+        assert B.lora_kv_batch_info(batch)[1].n_pages == n * prefix
+        q = torch.randn(1, 1, 64, device="cuda").bfloat16().expand(n, 1, 64).contiguous()
+        k = torch.randn(1, 1, 64, device="cuda").bfloat16().expand(n, 1, 64).contiguous()
+        out = torch.empty_like(q)
+        cache.append(batch, 0, k, k)
+        cache.attend(batch, 0, q, out, 0.125)
+        torch.cuda.synchronize()
+        host, table, total = cache.pages.float().cpu().numpy(), cache.pages_of(n), prefix * page - 4
+        keys, vals = kv_plain.read(host, table, 0, 0, page, 64, 8, total)
+        want, mass, _reach = kv_plain.attend(q[:1, 0].float().cpu().numpy(), keys, vals, total - 1, 0.125)
+        got = out.float().cpu().numpy()
+        # weights of 16 significant bits, one rounding of the output to 8
+        assert (np.abs(got[:, 0] - want) <= 2.0**-8 * np.abs(want) + 2.0**-12 * mass).all() and all(np.array_equal(g, got[0]) for g in got)
+    finally:
+        cache.close()
