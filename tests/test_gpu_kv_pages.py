@@ -326,3 +326,35 @@ def test_a_batch_of_many_forks_of_a_long_prefix():
         assert (np.abs(got[:, 0] - want) <= 2.0**-8 * np.abs(want) + 2.0**-12 * mass).all() and all(np.array_equal(g, got[0]) for g in got)
     finally:
         cache.close()
+
+
+def test_pages_that_move_are_the_ones_that_were_kept():
+    """More moves than one launch takes; every kept page is told apart by its bits, and none of them is a NaN."""
+    from paper_2411_17741_amd.kv import KvCache
+
+    n = 600
+    cache = KvCache(2, 1, 1, 64, 2 * n + 10, page_tokens=32, max_seqs=n + 1, max_batch_seqs=n, max_batch_tokens=n)
+    try:
+        ids = np.arange(1, n + 1)
+        cache.add(0)
+        cache.extend(0, 50)
+        cache.fork(0, ids)
+        batch = cache.batch(ids, np.arange(n + 1))
+        cache.batch_destroy(batch)
+        torch.cuda.synchronize()
+        cache.pages.copy_(torch.randn(cache.pages.shape, generator=torch.Generator().manual_seed(1)))
+        before = cache.pages.clone()
+        tables = {int(i): cache.pages_of(int(i)) for i in ids}
+        cache.free(ids[0::2])
+        cache.pages[torch.as_tensor([int(tables[int(i)][1]) for i in ids[0::2]], device="cuda")] = float("nan")  # what was given back
+        torch.cuda.synchronize()
+        moved = cache.compact()
+        torch.cuda.synchronize()
+        st = cache.stats()
+        assert moved > 128 and st.pages_end == st.pages_used == 2 + n // 2
+        assert not torch.isnan(cache.pages[: st.pages_end]).any()
+        for i in ids[1::2].tolist():
+            now = cache.pages_of(i)
+            assert all(torch.equal(cache.pages[int(a)], before[int(b)]) for a, b in zip(now, tables[i]))
+    finally:
+        cache.close()
