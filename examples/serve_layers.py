@@ -86,7 +86,9 @@ def main(argv=None):
         ap.add_argument("--" + name, type=int, default=value)
     a = ap.parse_args(argv)
     rng = np.random.default_rng(1)
-    model = Layers(a.layers, a.heads, a.kv_heads, a.dim, adapters=4)
+    # room for prompts of up to 300 tokens, a token in each iteration after that, and the continuations
+    seqs, each = a.requests + 3, 300 + a.iterations
+    model = Layers(a.layers, a.heads, a.kv_heads, a.dim, adapters=4, max_tokens=max(4096, 300 * seqs), max_seqs=max(64, seqs), n_pages=max(512, seqs * (each // 64 + 1) + 64))
     try:
         gen = torch.Generator(device="cuda").manual_seed(2)
         token = lambda n: torch.randn(n, model.hidden, generator=gen, device="cuda").bfloat16()  # noqa: E731
@@ -103,7 +105,7 @@ def main(argv=None):
                 for i in ended:
                     del lengths[i], adapter[i]
                 moved, used = model.cache.compact(), model.cache.stats()
-                model.cache.set_limit(used.pages_end + 64)
+                model.cache.set_limit(min(used.limit, used.pages_end + len(lengths) * (a.iterations // 64 + 2) + 64))
                 print(f"{len(ended)} requests ended, {moved} pages moved, {used.pages_used} in use, {used.pages_shared} of them shared")
             ids = list(lengths)
             lens = [lengths[i] for i in ids]

@@ -107,3 +107,10 @@ def test_the_example_runs():
 
     stats = S.main(["--layers", "2", "--heads", "8", "--kv-heads", "2", "--dim", "64", "--requests", "5", "--iterations", "4"])
     assert stats.pages_used > 0 and stats.seqs == 6
+
+
+def test_the_example_runs_with_many_requests():
+    import serve_layers as S
+
+    stats = S.main(["--layers", "1", "--heads", "4", "--kv-heads", "2", "--dim", "64", "--requests", "70", "--iterations", "3"])
+    assert stats.seqs == 38
