@@ -179,7 +179,9 @@ __device__ __forceinline__ float sum16(float v)
     return v + o;
 }
 
-// a chunk of weights: rounded to the values' type (8 weights to nearest bf16, the product's operand type; 4 fp32 weights as they are)
+// A chunk of weights, in the values' type: 4 fp32 weights as they are, 8 weights rounded to nearest bf16, the type of the product's operands.  Rows make up for what is lost with a second product;
+// tiles, which are bound by their products and instructions, do not: it would be half as many products again.  Their outputs are off by 2.0e-3 of their norm where rounding the outputs
+// alone makes 1.6e-3 (bf16, 8192 tokens).
 __device__ __forceinline__ uint4 weights(const float (&p)[8])
 {
     bf16x8 v;
@@ -280,7 +282,7 @@ __device__ __forceinline__ void put_row(const AttnArgs &a, const AttnItem &it, i
 // (O^T = V^T P^T) wants them, with no exchange at all: lane group g = lane / 16 holds tokens u g .. u g + u - 1 of the step, a chunk
 // of values (u = 8 with bf16, where two products of 16 tokens make a step: row 4 g + i of product t is token 8 g + 4 t + i).
 // Bound by memory: 512 tokens of about 1000 cached ones with 32 / 8 heads of 128, 2.6 GB, in 387 us, 6.75 TB/s (439 us with loads through the caches, which nothing here reads again); one token of
-// 131071 with 64 / 8 heads, cut into 64 pieces, 79 us, 6.8 TB/s.  With 16 rows an item's 16 x 16 products are mostly its own; the matrix units are busy 7 % of the time.
+// 131071 with 64 / 8 heads, cut into 64 pieces, 79 us, 6.8 TB/s; fp32, 512 of about 1000 790 us, 6.6 TB/s.  With 16 rows an item's 16 x 16 products are mostly its own; the matrix units are busy 7 % of the time.
 template <typename E, int D> constexpr bool ROWS_AHEAD = D <= 128;  // else two steps' registers are too many
 constexpr int ROW_WAVES = 4, ROW_JOIN = 128;  // ROW_JOIN: columns that go through LDS at a time
 
@@ -698,7 +700,8 @@ __device__ __forceinline__ void finish_tile(const AttnArgs &a, const AttnItem &i
 // Keys and values are requested DEEP steps ahead, values of stage t together with keys of stage t + 1, which the step of stage t waits for.  The keys of a stage are read in one step,
 // its values in that and the next: there are DEEP + 1 places for keys in LDS, DEEP + 2 for values.
 // A step of a wavefront alone on its SIMD takes 0.50 us with heads of 128, 0.9 with 256, 0.45 with 64, where its products are 0.27, 0.53 and 0.13: the rest are its other instructions,
-// one after the other, and the barrier.  5000 tokens with 32 / 8 heads of 256: 431 us, 0.95 PFLOP/s (585 with products and exponentials in turns); 8000 with heads of 64: 297 us.
+// one after the other, and the barrier.  5000 tokens with 32 / 8 heads of 256: 444 us, 0.92 PFLOP/s (585 with products and exponentials in turns); 8000 with 32 / 8 heads of 64: 305 us, 0.86.
+// fp32, 4096 tokens: 32 / 8 heads of 128 1117 us, 123 TFLOP/s, of 64 539 us, 128; 16 / 4 of 256 1438 us, 96.
 template <typename E, int D> struct TileShape {
     static constexpr int TK = 32, PLACE = TK * D * (int)sizeof(E);
     static constexpr int BLOCKS = PLACE <= 8192 ? 2 : 1;  // on a compute unit
@@ -1003,9 +1006,10 @@ __global__ __launch_bounds__(256, 3) void attn_many_kernel(AttnArgs a)
 }
 
 // Tiles, and the blocks of the row items behind them in one launch, while there are no more than BOTH_ROUNDS times as many as are on the machine at once: rows wait for memory beside tiles' products.
-// Apart -> together: prompts of 2 to 234 tokens with 64 / 8 heads of 128 16.1 -> 11.7 us; 30 tokens of about 300 beside 100 + 200 with 40 heads 43.7 -> 36.4; 8 of 3000 beside 1500 with
-// 32 / 8 heads 67 -> 61; 20 of 8000 beside 900 + 700 147 -> 154.  Of larger batches nothing is gained, or lost where rows have fewer blocks on a compute unit this way (heads of 256, 100 tokens
-// of 500 beside 600: 109 -> 122).
+// Apart -> together, heads of 128: prompts of 2 to 234 tokens with 64 / 8 heads 16.1 -> 11.7 us; 30 tokens of about 300 beside 100 + 200 with 40 heads 42.2 -> 37.0; 8 of 3000 beside 1500 with
+// 32 / 8 heads 64.9 -> 56.5; 100 of 1000 beside 300 82.2 -> 73.3; 4 of 30000 beside 500 102.5 -> 96.8.  The rule counts blocks alone, and loses where the rows' bytes are most of the
+// time: 20 of 3000 beside 900 + 700 72.0 -> 74.2, 20 of 8000 135.1 -> 145.7; 30 of 2000 beside 700 with 40 heads 203 -> 219.  Of larger batches nothing is gained, or lost where rows have
+// fewer blocks on a compute unit this way (heads of 256, 100 tokens of 500 beside 600: 109 -> 122).
 constexpr int BOTH_ROUNDS = 4;
 template <typename E, int D>
 __global__ __launch_bounds__(256, (TileShape<E, D>::BLOCKS)) void attn_both_kernel(AttnArgs a)
@@ -1044,7 +1048,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 // slot 2 j - 4 (their places were last read by group 1 in slot 2 j - 5); they have come when slot 2 j - 2 ends, a slot
 // before the first that needs them, so that a wavefront takes its first operands out of LDS before the barrier that starts its
 // products.
-// 8192 tokens with 32 / 8 heads: 480 us, 1.15 PFLOP/s; 16384 with 64 / 8 3640 us, 1.21.  Bound by power: the clock is at 1.75 GHz, the matrix units are busy 56 % of the cycles (tiles of 128 rows: 525 and 3966 us).
+// 8192 tokens with 32 / 8 heads: 480 to 499 us over runs, 1.10 to 1.15 PFLOP/s; 16384 with 64 / 8 3650 us, 1.20.  Bound by power: the clock is at 1.75 GHz, the matrix units are busy 56 % of the cycles (tiles of 128 rows: 537 and
+// 3985 us).
 constexpr int turn_lds(int dim) { return 6 * 64 * dim * 2; }
 
 template <int D>

@@ -35,7 +35,7 @@ constexpr int ROW_BLOCKS = 512, ROW_MIN_TOKENS = 512;
 // Tokens times head_dim up to which a wavefront may have an item to itself.
 constexpr int ROW_SHORT_VALUES = 16384;
 // Tiles are cut into pieces of no fewer tokens than join work is worth -- fp32 products take 8 times as long --, or of half of that where there are few tiles.  Measured for fp32, 512 -> these:
-// prompts of 300, 1 and 77 tokens with 32 / 8 heads of 128, append and attention, 59 -> 42 us, with 6 / 2 58 -> 32, with 32 / 8 heads of 64 37 -> 32 us.
+// prompts of 300, 1 and 77 tokens with 32 / 8 heads of 128, append and attention of two layers, 111 -> 76 us, with 6 / 2 108 -> 56, with 32 / 8 heads of 64 65 -> 56.
 constexpr int tile_min_tokens(const lora_kv_config_t &c) { return c.dtype == LORA_BF16 ? 512 : c.head_dim == 64 ? 256 : 128; }
 constexpr int PIECE_STEP = 64;  // pieces begin at multiples of it: a whole number of every kernel's steps, in one page or at the start of one
 constexpr int MAX_EXTRA = 2048;  // pieces beyond one for each block of rows
@@ -365,8 +365,8 @@ void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
         return (int32_t)(ctx + (std::min(rows, row0 + tile) - 1) / grp + 1);
     };
     // Two groups of wavefronts in turns, 256 rows at a time, where every compute unit gets two such blocks at least and they are long (1024 tokens in the
-    // mean).  Measured, tiles of 128 rows -> turns: 16384 tokens with 64 / 8 heads 3966 -> 3640 us, 8192 with 32 / 8 525 -> 481, 4096 146 -> 133, 2048 + 2048 81 -> 79; 2048 + 2048 with
-    // 32 / 32 heads 80 -> 84.
+    // mean).  Measured, tiles of 128 rows -> turns: 16384 tokens with 64 / 8 heads 3985 -> 3650 us, 8192 with 32 / 8 537 -> 499, 4096 150 -> 136, 2048 + 2048 81.3 -> 76.9, 4096 with 32 / 32
+    // heads 152 -> 143.  The rule does not ask for a gain where it takes few rounds of blocks: 2048 + 2048 with 32 / 32 heads 85.1 -> 85.5, 3 x 1500 behind 600 with 40 / 40 155.5 -> 160.
     if (lora::kv_turns(kv.cfg.dtype, kv.cfg.head_dim)) {
         int64_t tokens = 0;
         for (size_t i = 0; i < g.seqs.size(); ++i) {
@@ -402,7 +402,7 @@ void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
         tile_whole = 2 * tile_min;
     }
     // Where tiles are cut anyway, and pieces of fewer tokens still find a compute unit each (a quarter more than the share: not all pieces are whole), the last is done earlier: 213 + 752 tokens
-    // with 6 / 2 heads 18.6 -> 15.2 us, 1072 19.7 -> 18.5.
+    // with 6 / 2 heads 17.6 -> 13.9 us, 1072 18.6 -> 16.8, 1000 with 8 / 1 heads of 256 29.1 -> 24.5.
     if (cut.way == lora::KV_TILES_PLAIN && longest > tile_min) {
         const int32_t piece = at_least(share * 5 / 4, tile_min / 2);
         if (piece < tile_min) tile_piece = tile_whole = piece;

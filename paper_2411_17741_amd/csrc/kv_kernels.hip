@@ -40,8 +40,8 @@ template <bool PAST, typename E> __device__ __forceinline__ void store_past(E *p
 // are written value by value.
 //
 // Only bytes move.  Large batches: 8 heads a thread, past the caches, 12900 tokens of 32 + 32 + 32 heads of 128 (650 MB) in 160 us, 4.1 TB/s (172 with 4 heads).  Small ones, which stay in the
-// caches until the attention reads them: 2 heads a thread and no such hints, 64 tokens 6.1 -> 5.1 us of kernel time; 920 tokens of 32 + 32 + 32 heads with their attention, two layers, 108 -> 103.
-// From 16 MB of rows on the former is faster (6 x 300 tokens, two layers 138 -> 126).  Of batches of single tokens every key chunk is a piece of 16 bytes of a line of its own, every value one of 2.
+// caches until the attention reads them: 2 heads a thread and no such hints, 920 tokens of 32 + 32 + 32 heads 19.9 -> 18.5 us, with their attention, two layers, 187 -> 182; 64 tokens 5.9 us of kernel time.
+// From 16 MB of rows on the former is faster (6 x 300 tokens, 2 -> 8 heads a thread 26.0 -> 23.3, two layers with their attention 99.7 -> 85.4).  Of batches of single tokens every key chunk is a piece of 16 bytes of a line of its own, every value one of 2.
 constexpr int APPEND_MANY_HEADS = 8, APPEND_FEW_HEADS = 2;
 constexpr int64_t APPEND_MANY = 1 << 24;  // bytes of keys and queries from which a batch is a large one
 
@@ -189,7 +189,7 @@ hipError_t launch_append(const AppendArgs &a, int dtype, hipStream_t st)
 // of one: 34 us, written past the caches at 3.9 TB/s and read from them.
 constexpr int MOVE_BYTES = 256 * 4 * 16;
 
-// A batch's lists go up with its copies (row n of the grid): a launch less, forks of a request of 487 tokens with 6 / 2 heads 16.4 -> 11.8 us.
+// A batch's lists go up with its copies (row n of the grid): a launch less, 8 forks of a request of 487 tokens with 6 / 2 heads, 8 layers, 12.6 -> 10.2 us.
 __global__ __launch_bounds__(256) void moves_kernel(KvMoves m, int n, char *pages, int64_t page_stride, KvLists lists)
 {
     if ((int)blockIdx.y == n) {
