@@ -22,6 +22,13 @@
  * [page_tokens / u][head_dim][u tokens]: both as the matrix instructions take them, a chunk to a lane.  What lies
  * beyond a sequence's last token is never used, whatever its bits are.
  *
+ * Pages of 8 bits (LORA_KV_PAGES_E4M3, with LORA_BF16).  Keys and values are held as e4m3 (4 bits of exponent, 3 behind the leading one, up to
+ * 448, no infinities): as above in chunks of u = 16.  Behind the two halves of a page's layer lie its exponents, bytes [2][n_kv_heads][page_tokens]:
+ * a value of token p and head h stands for value * 2^(exponent - 127).  lora_kv_append stores the smallest exponent, of 10 to 247, with which
+ * no finite value of the token's head is over 448, and of each value the nearest of 8 bits (halves to even); what is infinite or no number
+ * is stored as no number.  All that is stored that way is exact in bf16, which is what attention and lora_kv_seq_read work with.  Exponents that the caller puts
+ * there himself are 1 to 254.
+ *
  * Conventions are those of lora_cache.h: every function returns LORA_OK or a negative lora_status, nothing aborts or
  * throws; device memory is the caller's; streams are hipStream_t as void* (NULL = the default stream); calls only
  * enqueue work.  A cache belongs to the device that is current when it is created: its buffers, tensors and streams are that
@@ -45,7 +52,11 @@ extern "C" {
 typedef struct lora_kv lora_kv_t;             /* opaque */
 typedef struct lora_kv_batch lora_kv_batch_t; /* opaque: device-resident lists of one batch; a handle never comes back, that of a destroyed batch is refused */
 
-enum { LORA_KV_HOST_ONLY = 1 }; /* flags: sequences and pages only, no device work */
+/* flags */
+enum {
+    LORA_KV_HOST_ONLY = 1,  /* sequences and pages only, no device work */
+    LORA_KV_PAGES_E4M3 = 4, /* pages of 8-bit values (see above); dtype, which is LORA_BF16 then, is that of q, k, v and out alone */
+};
 
 #define LORA_KV_MAX_TOKENS (1 << 28) /* of one sequence */
 
@@ -60,7 +71,7 @@ typedef struct {
     int32_t max_batch_tokens;    /* tokens of a batch; times n_heads / n_kv_heads at most LORA_KV_MAX_TOKENS */
     int32_t max_batch_pages;     /* pages of all sequences of a batch together (a shared page counts for each) */
     int32_t n_batches;           /* batches alive at once */
-    int32_t dtype;               /* LORA_F32 | LORA_BF16: q, k, v, out and the pages */
+    int32_t dtype;               /* LORA_F32 | LORA_BF16: q, k, v, out and (without LORA_KV_PAGES_E4M3) the pages */
     int32_t flags;
 } lora_kv_config_t;
 
@@ -109,6 +120,12 @@ int lora_kv_seq_info(const lora_kv_t *kv, int64_t id, lora_kv_seq_info_t *out);
 
 /* The sequence's pages in order; *n receives how many there are, `pages` (may be NULL) up to cap of them. */
 int lora_kv_seq_pages(const lora_kv_t *kv, int64_t id, int32_t *pages, int32_t cap, int32_t *n);
+
+/* Keys and values of one layer out of the pages, turned as they were stored: tokens [first[i], first[i] + n_tokens[i]) of sequence ids[i], one sequence's
+ * behind the other's, as rows [n_kv_heads][head_dim] of the cache's dtype, k_stride / v_stride values apart, 16-byte aligned.  A sequence may be named more than once.
+ * The pages are those of the time of the call (that a captured call reads again).  LORA_E_NOTFOUND, LORA_E_INVAL (tokens that a sequence has not, bad arguments). */
+int lora_kv_seq_read(lora_kv_t *kv, int32_t n, const int64_t *ids, const int32_t *first, const int32_t *n_tokens, int32_t layer, void *k, int64_t k_stride,
+                     void *v, int64_t v_stride, void *stream);
 
 /* ---- pages ------------------------------------------------------------------------------- */
 
@@ -172,6 +189,17 @@ typedef struct {
  * LORA_E_INVAL on bad arguments (a position of the batch beyond rope_positions among them), LORA_E_STATE if the batch can't be
  * used any more. */
 int lora_kv_append(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const lora_kv_append_t *a, void *stream);
+
+/* Norms of heads on their way: each query or key vector x of a head becomes x * w / sqrt(mean of x^2 + eps) before it is turned. */
+typedef struct {
+    const float *q, *k;         /* device, weights w: head_dim values, 16-byte aligned; or NULL: queries / keys get no norm */
+    int32_t q_stride, k_stride; /* values from one head's weights to the next one's: 0 (all heads have the same), or from head_dim on a multiple of 4 */
+    float eps;                  /* > 0 */
+} lora_kv_norm_t;
+
+/* lora_kv_append with the norms of `norm` (NULL: none), in the same pass: sums of squares and factors are held in 64 bits, the rest in fp32 (keys for pages of 8 bits
+ * in 64 bits as a whole), and what is stored is rounded once.  Errors as lora_kv_append; LORA_E_INVAL on a bad norm, on weights for queries without queries. */
+int lora_kv_append_norm(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const lora_kv_append_t *a, const lora_kv_norm_t *norm, void *stream);
 
 /* Attention of the batch's tokens over their sequences' pages in one layer, causal: q and out device [T][n_heads][head_dim], tokens
  * q_stride / out_stride values apart, 16-byte aligned; out may be q itself with the same stride; scale > 0.  Scores, sums and outputs are held in fp32 and outputs

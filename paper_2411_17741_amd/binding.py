@@ -24,7 +24,7 @@ LORA_F32, LORA_BF16 = 0, 1
 LORA_SLOT_EMPTY, LORA_SLOT_FILLING, LORA_SLOT_READY = 0, 1, 2
 LORA_CACHE_HOST_ONLY, LORA_CACHE_FUSED_GEMV, LORA_CACHE_SPLIT_GEMV, LORA_CACHE_DIRECT_FILL, LORA_CACHE_NO_OVERLAP = 1, 2, 4, 8, 16
 LORA_CACHE_SMALL_SCRATCH = 32
-LORA_KV_HOST_ONLY, LORA_KV_MAX_TOKENS = 1, 1 << 28
+LORA_KV_HOST_ONLY, LORA_KV_PAGES_E4M3, LORA_KV_MAX_TOKENS = 1, 4, 1 << 28
 LORA_ROPE_HALVES, LORA_ROPE_NEIGHBOURS = 0, 1
 LORA_KV_TILES_PLAIN, LORA_KV_TILES_MANY, LORA_KV_TILES_PAIRS, LORA_KV_TILES_TURNS = 0, 1, 2, 3
 LORA_MAX_RANK, LORA_TILE_TOKENS, LORA_MFMA_MIN_TOKENS, LORA_MFMA_MIN_TOKENS_MIXED = 128, 64, 16, 8
@@ -121,6 +121,7 @@ class lora_kv_batch_info_t(ctypes.Structure):
 # lora_kv_append_t: k, v, k_stride, v_stride, q, q_out, q_stride, q_out_stride, rope, rope_positions, rope_dim, rope_pairs (packed: a ctypes structure of twelve fields
 # costs a call 1 us more)
 _kv_append_t = struct.Struct("=QQqqQQqqQiii4x")
+_kv_norm_t = struct.Struct("=QQiif4x")  # lora_kv_norm_t: q, k, q_stride, k_stride, eps
 
 
 if not os.path.exists(LIB_PATH):
@@ -202,6 +203,8 @@ _SIGS = {
     "lora_kv_batch_destroy": (c_int, [c_void_p, c_void_p]),
     "lora_kv_batch_info": (c_int, [c_void_p, POINTER(lora_kv_batch_info_t)]),
     "lora_kv_append": (c_int, [c_void_p, c_void_p, c_int32, c_char_p, c_void_p]),
+    "lora_kv_append_norm": (c_int, [c_void_p, c_void_p, c_int32, c_char_p, c_char_p, c_void_p]),
+    "lora_kv_seq_read": (c_int, [c_void_p, c_int32, _i64a, _i32a, _i32a, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p]),
     "lora_kv_attend": (c_int, [c_void_p, c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_float, c_void_p]),
     "lora_strerror": (c_char_p, [c_int]),
     "lora_last_hip_error": (c_int, []),
@@ -712,6 +715,19 @@ def lora_kv_append(kv, batch, layer: int, k: int, v: int, k_stride: int, v_strid
                    q_out_stride: int = 0, rope: int = 0, rope_positions: int = 0, rope_dim: int = 0, rope_pairs: int = 0, stream: int = 0) -> int:
     a = _kv_append_t.pack(k, v, k_stride, v_stride, q, q_out, q_stride, q_out_stride, rope, rope_positions, rope_dim, rope_pairs)
     return _lib.lora_kv_append(kv, batch, layer, a, stream)
+
+
+def lora_kv_append_norm(kv, batch, layer: int, k: int, v: int, k_stride: int, v_stride: int, q: int = 0, q_out: int = 0, q_stride: int = 0,
+                        q_out_stride: int = 0, rope: int = 0, rope_positions: int = 0, rope_dim: int = 0, rope_pairs: int = 0, q_norm: int = 0, k_norm: int = 0,
+                        q_norm_stride: int = 0, k_norm_stride: int = 0, eps: float = 1e-6, stream: int = 0) -> int:
+    a = _kv_append_t.pack(k, v, k_stride, v_stride, q, q_out, q_stride, q_out_stride, rope, rope_positions, rope_dim, rope_pairs)
+    return _lib.lora_kv_append_norm(kv, batch, layer, a, _kv_norm_t.pack(q_norm, k_norm, q_norm_stride, k_norm_stride, eps), stream)
+
+
+def lora_kv_seq_read(kv, ids, first, n_tokens, layer: int, k: int, k_stride: int, v: int, v_stride: int, stream: int = 0) -> int:
+    a, n = _ids_and_counts(ids, n_tokens)
+    _, f = _ids_and_counts(ids, first)
+    return _lib.lora_kv_seq_read(kv, a.size, _ptr(a), _ptr(f), _ptr(n), layer, k, k_stride, v, v_stride, stream)
 
 
 def lora_kv_attend(kv, batch, layer: int, q: int, q_stride: int, out: int, out_stride: int, scale: float, stream: int = 0) -> int:

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblora_cache.so")
 
 SOURCES = ["lora_cache.cpp", "indexer.cpp", "scheduler.cpp", "gemv_kernels.hip", "mfma_kernels.hip", "linear_kernels.hip", "fill_kernels.hip",
-           "kv_cache.cpp", "kv_kernels.hip", "attn_kernels.hip"]
+           "kv_cache.cpp", "kv_kernels.hip", "attn_kernels.hip", "attn_e4m3_kernels.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950",

@@ -102,7 +102,9 @@ struct lora_kv {
     hipStream_t last = nullptr;
     hipEvent_t order_ev = nullptr;
 
-    int chunk() const { return cfg.dtype == LORA_BF16 ? 8 : 4; }
+    bool e4m3() const { return cfg.flags & LORA_KV_PAGES_E4M3; }
+    int row_chunk() const { return cfg.dtype == LORA_BF16 ? 8 : 4; }  // values of 16 bytes: of queries, keys, values and outputs,
+    int chunk() const { return e4m3() ? 16 : row_chunk(); }          // ... and of the pages
     int group() const { return cfg.n_heads / cfg.n_kv_heads; }
     bool page_free(int32_t p) const { return (free_bits[(size_t)p >> 6] >> (p & 63)) & 1; }
     void give_back(int32_t p)
@@ -169,7 +171,11 @@ size_t elem_bytes(int32_t dtype) { return dtype == LORA_BF16 ? 2 : 4; }
 
 constexpr size_t MAX_PAGE_BYTES = ((size_t)1 << 32) - 1;  // the kernels multiply a page's number by 32 bits
 
-size_t layer_bytes(const lora_kv_config_t &c) { return (size_t)2 * c.n_kv_heads * c.page_tokens * c.head_dim * elem_bytes(c.dtype); }
+size_t layer_bytes(const lora_kv_config_t &c)
+{
+    const size_t rows = (size_t)2 * c.n_kv_heads * c.page_tokens;
+    return c.flags & LORA_KV_PAGES_E4M3 ? rows * (c.head_dim + 1) : rows * c.head_dim * elem_bytes(c.dtype);
+}
 
 bool good(const lora_kv_config_t *c)
 {
@@ -180,7 +186,8 @@ bool good(const lora_kv_config_t *c)
         return false;
     if ((int64_t)c->max_batch_tokens * (c->n_heads / c->n_kv_heads) > LORA_KV_MAX_TOKENS) return false;
     if (c->n_heads > 4096 || c->n_layers > 65536 || c->n_batches > 1024 || c->max_batch_tokens > LORA_KV_MAX_TOKENS) return false;
-    if ((c->dtype != LORA_BF16 && c->dtype != LORA_F32) || (c->flags & ~LORA_KV_HOST_ONLY)) return false;
+    if ((c->dtype != LORA_BF16 && c->dtype != LORA_F32) || (c->flags & ~(LORA_KV_HOST_ONLY | LORA_KV_PAGES_E4M3))) return false;
+    if ((c->flags & LORA_KV_PAGES_E4M3) && c->dtype != LORA_BF16) return false;
     return layer_bytes(*c) <= MAX_PAGE_BYTES / (size_t)c->n_layers;
 }
 
@@ -707,6 +714,47 @@ int lora_kv_seq_pages(const lora_kv_t *kv, int64_t id, int32_t *pages, int32_t c
     return LORA_OK;
 }
 
+int lora_kv_seq_read(lora_kv_t *kv, int32_t n, const int64_t *ids, const int32_t *first, const int32_t *n_tokens, int32_t layer, void *k, int64_t k_stride, void *v, int64_t v_stride,
+                     void *stream)
+{
+    if (!kv || n < 0 || (n && (!ids || !first || !n_tokens)) || layer < 0 || layer >= kv->cfg.n_layers) return LORA_E_INVAL;
+    if (kv->host_only) return LORA_E_STATE;
+    const lora_kv_config_t &c = kv->cfg;
+    int64_t tokens = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        const Seq *s = kv->find(ids[i]);
+        if (!s) return LORA_E_NOTFOUND;
+        if (first[i] < 0 || n_tokens[i] < 0 || (int64_t)first[i] + n_tokens[i] > s->n_tokens) return LORA_E_INVAL;
+        tokens += n_tokens[i];
+    }
+    if (!tokens) return LORA_OK;
+    const int64_t row = (int64_t)c.n_kv_heads * c.head_dim, u = kv->row_chunk();
+    const auto bad = [&](const void *p, int64_t stride) { return !p || !aligned16(p) || stride < row || stride % u || stride > ((int64_t)1 << 40); };
+    if (bad(k, k_stride) || bad(v, v_stride)) return LORA_E_INVAL;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const OnDevice on(*kv);
+    if (const int rc = in_order(*kv, st)) return rc;
+    lora::ReadArgs a;
+    a.pages = kv->pages + kv->layer_bytes * layer;
+    a.page_stride = (int64_t)kv->page_bytes;
+    a.k = k, a.v = v, a.k_stride = k_stride, a.v_stride = v_stride;
+    a.n_kv = c.n_kv_heads, a.dim = c.head_dim, a.page_shift = kv->page_shift, a.n_reads = 0;
+    int64_t at = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        const Seq *s = kv->find(ids[i]);
+        for (int32_t pos = first[i], end = first[i] + n_tokens[i]; pos < end;) {
+            const int32_t off = pos & (c.page_tokens - 1), m = std::min(end - pos, c.page_tokens - off);
+            a.reads[a.n_reads++] = {at, s->pages[pos >> kv->page_shift], (int16_t)off, (int16_t)m};
+            at += m, pos += m;
+            if (a.n_reads == lora::KV_MAX_READS || at == tokens) {
+                KV_TRY(lora::launch_read(a, c.dtype, kv->e4m3(), st));
+                a.n_reads = 0;
+            }
+        }
+    }
+    return LORA_OK;
+}
+
 // ---- pages ---------------------------------------------------------------------------------
 
 int lora_kv_compact(lora_kv_t *kv, void *stream, int32_t *moved)
@@ -915,13 +963,15 @@ int lora_kv_batch_info(const lora_kv_batch_t *handle, lora_kv_batch_info_t *out)
     return LORA_E_INVAL;
 }
 
-int lora_kv_append(lora_kv_t *kv, lora_kv_batch_t *handle, int32_t layer, const lora_kv_append_t *a, void *stream)
+int lora_kv_append(lora_kv_t *kv, lora_kv_batch_t *handle, int32_t layer, const lora_kv_append_t *a, void *stream) { return lora_kv_append_norm(kv, handle, layer, a, nullptr, stream); }
+
+int lora_kv_append_norm(lora_kv_t *kv, lora_kv_batch_t *handle, int32_t layer, const lora_kv_append_t *a, const lora_kv_norm_t *norm, void *stream)
 {
     Batch *const batch = kv ? find_batch(*kv, handle) : nullptr;
     if (!batch || !a || layer < 0 || layer >= kv->cfg.n_layers) return LORA_E_INVAL;
     if (batch->stale) return LORA_E_STATE;
     const lora_kv_config_t &c = kv->cfg;
-    const int64_t row = (int64_t)c.n_kv_heads * c.head_dim, q_row = (int64_t)c.n_heads * c.head_dim, u = kv->chunk();
+    const int64_t row = (int64_t)c.n_kv_heads * c.head_dim, q_row = (int64_t)c.n_heads * c.head_dim, u = kv->row_chunk();
     const auto bad = [&](const void *p, int64_t stride, int64_t least) { return !p || !aligned16(p) || stride < least || stride % u || stride > ((int64_t)1 << 40); };
     if (batch->info.n_tokens) {
         if (bad(a->k, a->k_stride, row) || bad(a->v, a->v_stride, row)) return LORA_E_INVAL;
@@ -929,7 +979,10 @@ int lora_kv_append(lora_kv_t *kv, lora_kv_batch_t *handle, int32_t layer, const 
         if (a->q && a->q == a->q_out && a->q_stride != a->q_out_stride) return LORA_E_INVAL;
         if (a->rope && (!aligned16(a->rope) || a->rope_dim < 16 || a->rope_dim > c.head_dim || a->rope_dim % 16 || a->rope_positions <= batch->max_pos))
             return LORA_E_INVAL;
+        const auto bad_weights = [&](const float *w, int32_t stride) { return w && (!aligned16(w) || stride % 4 || (stride && stride < c.head_dim)); };
+        if (norm && (bad_weights(norm->q, norm->q_stride) || bad_weights(norm->k, norm->k_stride) || (norm->q && !a->q))) return LORA_E_INVAL;
     }
+    if (norm && !(norm->eps > 0.f && std::isfinite(norm->eps))) return LORA_E_INVAL;
     if (a->rope && a->rope_pairs != LORA_ROPE_HALVES && a->rope_pairs != LORA_ROPE_NEIGHBOURS) return LORA_E_INVAL;
     if (!batch->info.n_tokens) return LORA_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -947,7 +1000,13 @@ int lora_kv_append(lora_kv_t *kv, lora_kv_batch_t *handle, int32_t layer, const 
     k.groups = reinterpret_cast<const KvGroup *>(batch->dev + batch->off_groups);
     k.n_tokens = batch->info.n_tokens, k.n_groups = batch->info.n_groups;
     k.n_heads = c.n_heads, k.n_kv = c.n_kv_heads, k.dim = c.head_dim, k.page_shift = kv->page_shift;
-    KV_TRY(lora::launch_append(k, c.dtype, st));
+    if (kv->e4m3() || (norm && (norm->q || norm->k))) {
+        lora::AppendHeadsArgs h{k, nullptr, nullptr, 0, 0, 1.0};
+        if (norm) h = {k, norm->q, norm->k, norm->q_stride, norm->k_stride, norm->eps};
+        KV_TRY(lora::launch_append_heads(h, c.dtype, kv->e4m3(), st));
+    } else {
+        KV_TRY(lora::launch_append(k, c.dtype, st));
+    }
     return LORA_OK;
 }
 
@@ -961,7 +1020,7 @@ int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *handle, int32_t layer, const 
     const float scale_log2 = scale * 1.44269504088896340736f;
     if (!(scale > 0.f) || !std::isfinite(scale_log2)) return LORA_E_INVAL;
     if (!batch->info.n_tokens) return LORA_OK;
-    const int64_t row = (int64_t)c.n_heads * c.head_dim, u = kv->chunk();
+    const int64_t row = (int64_t)c.n_heads * c.head_dim, u = kv->row_chunk();
     const auto bad = [&](const void *p, int64_t stride) { return !p || !aligned16(p) || stride < row || stride % u || stride > ((int64_t)1 << 40); };
     if (bad(q, q_stride) || bad(out, out_stride) || (q == out && q_stride != out_stride)) return LORA_E_INVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -981,7 +1040,8 @@ int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *handle, int32_t layer, const 
     a.n_rows = batch->info.n_row_items - batch->info.n_short_items;
     a.n_short = batch->info.n_short_items;
     const lora::KvTiles way = (lora::KvTiles)batch->info.tiles_way;
-    KV_TRY(lora::launch_attn(a, c.dtype, c.head_dim, way, kv->n_cu, st));
+    if (kv->e4m3()) KV_TRY(lora::launch_attn_e4m3(a, c.head_dim, way, kv->n_cu, st));
+    else KV_TRY(lora::launch_attn(a, c.dtype, c.head_dim, way, kv->n_cu, st));
     lora::JoinArgs j{};
     j.out = out, j.out_stride = out_stride;
     j.part_o = kv->part_o, j.part_ml = kv->part_ml;

@@ -21,6 +21,9 @@ enum KvTiles { KV_TILES_PLAIN = LORA_KV_TILES_PLAIN, KV_TILES_MANY = LORA_KV_TIL
 constexpr bool kv_many(int dtype, int dim) { return dtype == LORA_BF16 && dim == 128; }
 constexpr bool kv_pairs(int dtype, int dim) { return dtype == LORA_BF16 && dim == 64; }
 constexpr int KV_MAX_MOVES = 128; // page copies of one launch (they travel as its arguments)
+constexpr int KV_MAX_READS = 192; // pages read back by one launch (likewise)
+// Pages of 8 bits: exponents are held with this added, and lie from -117 (the smallest value above 0 is normal in bf16) to 120 (of the largest fp32 values)
+constexpr int KV_EXP_BIAS = 127, KV_EXP_MIN = -117, KV_EXP_MAX = 120;
 
 // One new token: where it stands and the page it lies in.
 struct KvToken {
@@ -73,6 +76,30 @@ struct AppendArgs {
     int32_t n_tokens, n_groups, n_heads, n_kv, dim, page_shift, rope_dim, neighbours;
 };
 
+// ... with norms of heads; weights may be null
+struct AppendHeadsArgs {
+    AppendArgs a;
+    const float *q_norm, *k_norm;
+    int32_t q_norm_stride, k_norm_stride;
+    double eps;
+};
+
+// Tokens off .. off + n - 1 of a page: rows row .. of what is read
+struct KvRead {
+    int64_t row;
+    int32_t page;
+    int16_t off, n;
+};
+
+struct ReadArgs {
+    const char *pages;  // of this layer
+    int64_t page_stride;
+    void *k, *v;
+    int64_t k_stride, v_stride;
+    int32_t n_kv, dim, page_shift, n_reads;
+    KvRead reads[KV_MAX_READS];
+};
+
 struct AttnArgs {
     const void *q;
     void *out;
@@ -96,8 +123,11 @@ struct JoinArgs {
 
 hipError_t prepare_attn_kernels();  // once for the current device
 hipError_t launch_append(const AppendArgs &a, int dtype, hipStream_t st);
+hipError_t launch_append_heads(const AppendHeadsArgs &a, int dtype, bool e4m3, hipStream_t st);
+hipError_t launch_read(const ReadArgs &a, int dtype, bool e4m3, hipStream_t st);
 hipError_t launch_moves(const KvMoves &m, int n, char *pages, int64_t page_stride, const KvLists &lists, hipStream_t st, hipEvent_t done);
 hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, KvTiles way, int n_cu, hipStream_t st);
+hipError_t launch_attn_e4m3(const AttnArgs &a, int dim, KvTiles way, int n_cu, hipStream_t st);
 hipError_t launch_attn_join(const JoinArgs &a, int dtype, int dim, bool tiles, hipStream_t st);
 
 }  // namespace lora

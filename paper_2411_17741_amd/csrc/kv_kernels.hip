@@ -1,7 +1,10 @@
-// The paged key-value cache's writes (gfx950): new keys and values into the pages with their positions turned, and
-// pages copied to others.  Both only move bytes; the layout of the pages is in include/lora_kv.h.
+// The paged key-value cache's writes (gfx950): new keys and values into the pages with their positions turned, with norms of their
+// heads and as 8-bit values where that is asked for, and pages copied to others; and what the pages hold read back.  All of it only moves bytes; the
+// layout of the pages is in include/lora_kv.h.
 #include <algorithm>
+#include <type_traits>
 
+#include "kv_e4m3.h"
 #include "kv_internal.h"
 #include "lora_device.h"
 #include "lora_internal.h"
@@ -44,6 +47,55 @@ template <bool PAST, typename E> __device__ __forceinline__ void store_past(E *p
 // From 16 MB of rows on the former is faster (6 x 300 tokens, 2 -> 8 heads a thread 26.0 -> 23.3, two layers with their attention 99.7 -> 85.4).  Of batches of single tokens every key chunk is a piece of 16 bytes of a line of its own, every value one of 2.
 constexpr int APPEND_MANY_HEADS = 8, APPEND_FEW_HEADS = 2;
 constexpr int64_t APPEND_MANY = 1 << 24;  // bytes of keys and queries from which a batch is a large one
+
+// A block's share of the values; `mine`: 64 u chunks of LDS for the wavefront
+template <typename E, bool PAST>
+__device__ __forceinline__ void append_values(const AppendArgs &a, uint32_t block, Vals<E> *mine)
+{
+    constexpr int U = CHUNK<E>;
+    const int page_tokens = 1 << a.page_shift;
+    const size_t head_values = (size_t)a.dim << a.page_shift;  // of one half of a page
+    const int n_chunks = a.dim / U, lane = threadIdx.x & 63;
+    uint32_t i = block * 256u + threadIdx.x;
+    const int c = i % n_chunks;
+    i /= n_chunks;
+    const int h = i % a.n_kv;
+    const int g = i / a.n_kv;
+    KvGroup grp{0, 0, 0, 0};
+    if (g < a.n_groups) grp = a.groups[g];
+    const E *src = static_cast<const E *>(a.v) + (int64_t)grp.tok * a.v_stride + h * a.dim + c * U;
+    const int at = grp.pos & (page_tokens - 1);
+    E *to = reinterpret_cast<E *>(a.pages + grp.page * a.page_stride) + (a.n_kv + h) * head_values + (size_t)(at / U) * a.dim * U;  // the chunks of value 0, 1, ... of the head
+    if (grp.n == U) {
+        Vals<E> in[U];
+#pragma unroll
+        for (int t = 0; t < U; ++t) in[t] = load_once<PAST>(src + t * a.v_stride);
+#pragma unroll
+        for (int d = 0; d < U; ++d) {
+            Vals<E> o;
+#pragma unroll
+            for (int t = 0; t < U; ++t) o.v[t] = in[t].v[d];
+            mine[lane * U + (d ^ (lane & (U - 1)))] = o;  // (a lane's chunks in an order of its own: the lanes' banks differ)
+        }
+    } else {
+        for (int t = 0; t < grp.n; ++t) {
+            const Vals<E> in = load_once<PAST>(src + t * a.v_stride);
+#pragma unroll
+            for (int d = 0; d < U; ++d) to[(c * U + d) * U + at % U + t] = in.v[d];
+        }
+    }
+    __builtin_amdgcn_wave_barrier();
+    // chunk n of the wavefront's 64 u is lane n / u's; the 64 / u lanes of a store belong to one group and head (dim is a multiple of 64)
+    const uint64_t base = reinterpret_cast<uint64_t>(to);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        const int from = k * (64 / U), owner = from + lane / U;
+        const bool whole = __builtin_amdgcn_readlane(grp.n, from) == U;
+        const uint64_t there = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(base >> 32), from) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)base, from);
+        const int first = __builtin_amdgcn_readlane(c, from) * U;
+        if (whole) store_past<PAST>(reinterpret_cast<E *>(there) + (first + lane) * U, mine[owner * U + ((lane & (U - 1)) ^ (owner & (U - 1)))]);
+    }
+}
 
 template <typename E, int APPEND_HEADS>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t key_blocks)
@@ -122,47 +174,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a, uint32_t key_
         return;
     }
     __shared__ Vals<E> turned[4][64 * U];
-    const int n_chunks = a.dim / U, lane = threadIdx.x & 63;
-    uint32_t i = (blockIdx.x - key_blocks) * 256u + threadIdx.x;
-    const int c = i % n_chunks;
-    i /= n_chunks;
-    const int h = i % a.n_kv;
-    const int g = i / a.n_kv;
-    KvGroup grp{0, 0, 0, 0};
-    if (g < a.n_groups) grp = a.groups[g];
-    const E *src = static_cast<const E *>(a.v) + (int64_t)grp.tok * a.v_stride + h * a.dim + c * U;
-    const int at = grp.pos & (page_tokens - 1);
-    E *to = reinterpret_cast<E *>(a.pages + grp.page * a.page_stride) + (a.n_kv + h) * head_values + (size_t)(at / U) * a.dim * U;  // the chunks of value 0, 1, ... of the head
-    Vals<E> *const mine = turned[threadIdx.x >> 6];
-    if (grp.n == U) {
-        Vals<E> in[U];
-#pragma unroll
-        for (int t = 0; t < U; ++t) in[t] = load_once<PAST>(src + t * a.v_stride);
-#pragma unroll
-        for (int d = 0; d < U; ++d) {
-            Vals<E> o;
-#pragma unroll
-            for (int t = 0; t < U; ++t) o.v[t] = in[t].v[d];
-            mine[lane * U + (d ^ (lane & (U - 1)))] = o;  // (a lane's chunks in an order of its own: the lanes' banks differ)
-        }
-    } else {
-        for (int t = 0; t < grp.n; ++t) {
-            const Vals<E> in = load_once<PAST>(src + t * a.v_stride);
-#pragma unroll
-            for (int d = 0; d < U; ++d) to[(c * U + d) * U + at % U + t] = in.v[d];
-        }
-    }
-    __builtin_amdgcn_wave_barrier();
-    // chunk n of the wavefront's 64 u is lane n / u's; the 64 / u lanes of a store belong to one group and head (dim is a multiple of 64)
-    const uint64_t base = reinterpret_cast<uint64_t>(to);
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-        const int from = k * (64 / U), owner = from + lane / U;
-        const bool whole = __builtin_amdgcn_readlane(grp.n, from) == U;
-        const uint64_t there = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(base >> 32), from) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)base, from);
-        const int first = __builtin_amdgcn_readlane(c, from) * U;
-        if (whole) store_past<PAST>(reinterpret_cast<E *>(there) + (first + lane) * U, mine[owner * U + ((lane & (U - 1)) ^ (owner & (U - 1)))]);
-    }
+    append_values<E, PAST>(a, blockIdx.x - key_blocks, turned[threadIdx.x >> 6]);
 }
 
 hipError_t launch_append(const AppendArgs &a, int dtype, hipStream_t st)
@@ -182,6 +194,351 @@ hipError_t launch_append(const AppendArgs &a, int dtype, hipStream_t st)
         if (many) hipLaunchKernelGGL((append_kernel<float, APPEND_MANY_HEADS>), grid, dim3(256), 0, st, a, (uint32_t)keys);
         else hipLaunchKernelGGL((append_kernel<float, APPEND_FEW_HEADS>), grid, dim3(256), 0, st, a, (uint32_t)keys);
     }
+    return hipGetLastError();
+}
+
+// The same with norms of the heads, and into pages of 8-bit values.  A token's part of a head is dim / (2 u) threads' of one wavefront, which find the
+// sum of its squares, or the largest of its values, between them by a few exchanges.
+//
+// 8 bits: a value that is beside a border between two of them goes the wrong way if what it is made of was rounded before, and is off by 2^-4 of itself then:
+// keys are normed and turned in 64 bits (their products with 24-bit cosines and sines are exact there), and rounded to the nearest of 8 bits by way of fp32
+// values that are rounded to odd -- towards zero, with the last bit set if anything was lost --, which leaves the second rounding what it has to know.
+__device__ __forceinline__ float to_odd(double d)
+{
+    const float f = (float)d;
+    const double lost = d - (double)f;
+    uint32_t b = __float_as_uint(f);
+    if ((lost < 0. || lost > 0.) && !(b & 1) && f != 0.f) b += (lost > 0.) == (f > 0.f) ? 1 : -1;
+    return __uint_as_float(b);
+}
+
+// the largest |value| of those that are finite
+__device__ __forceinline__ float larger(float top, float v)
+{
+    const float size = fabsf(v);
+    return size < INFINITY && size > top ? size : top;
+}
+
+// The smallest e with top <= 448 * 2^e: 448 is 1.75 * 2^8, so a fraction over 1.75 takes one more
+__device__ __forceinline__ int exponent_for(float top)
+{
+    return min(max((int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 127 - 8, KV_EXP_MIN), KV_EXP_MAX);
+}
+
+// a value for the conversion to 8 bits: 448 at most, or no number
+__device__ __forceinline__ float scaled(float v, float unit)
+{
+    v *= unit;
+    return fabsf(v) <= 448.f ? v : NAN;
+}
+
+// ... four of them
+__device__ __forceinline__ uint32_t four_e4m3(float a, float b, float c, float d)
+{
+    const int low = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, low, true);
+}
+
+// x and y of a thread, U values each, turned: the same roundings whatever is compiled beside it, and append_kernel's
+__device__ __forceinline__ float fused(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
+__device__ __forceinline__ double fused(double a, double b, double c) { return __builtin_fma(a, b, c); }
+template <typename T, int U>
+__device__ __forceinline__ void turn_pairs(T (&x)[U], T (&y)[U], const float (&c)[U], const float (&s)[U], bool halves)
+{
+    if (halves) {
+#pragma unroll
+        for (int e = 0; e < U; ++e) {
+            const T u = x[e], w = y[e];
+            x[e] = fused(u, (T)c[e], -(w * s[e]));
+            y[e] = fused(w, (T)c[e], u * s[e]);
+        }
+    } else {
+        const auto pairs = [&](T(&z)[U], int first) {
+#pragma unroll
+            for (int e = 0; e < U; e += 2) {
+                const T u = z[e], w = z[e + 1];
+                z[e] = fused(u, (T)c[first + e / 2], -(w * s[first + e / 2]));
+                z[e + 1] = fused(w, (T)c[first + e / 2], u * s[first + e / 2]);
+            }
+        };
+        pairs(x, 0), pairs(y, U / 2);
+    }
+}
+
+// A block's share of the values into pages of 8 bits: a thread takes 8 values of a head of up to 16 tokens that share their chunks
+__device__ __forceinline__ void append_values_e4m3(const AppendArgs &a, uint32_t block)
+{
+    constexpr int U = 8, N = 16;
+    const int n_chunks = a.dim / U;
+    uint32_t i = block * 256u + threadIdx.x;
+    const int c = i % n_chunks;
+    i /= n_chunks;
+    const int h = i % a.n_kv;
+    const int g = i / a.n_kv;
+    KvGroup grp{0, 0, 0, 0};
+    if (g < a.n_groups) grp = a.groups[g];
+    const __bf16 *src = static_cast<const __bf16 *>(a.v) + (int64_t)grp.tok * a.v_stride + h * a.dim + c * U;
+    const int at = grp.pos & ((1 << a.page_shift) - 1);
+    char *const page = a.pages + grp.page * a.page_stride;
+    const size_t head_values = (size_t)a.dim << a.page_shift;
+    uint8_t *to = reinterpret_cast<uint8_t *>(page) + (a.n_kv + h) * head_values + (size_t)(at / N) * a.dim * N + c * U * N;
+    uint8_t *exps = reinterpret_cast<uint8_t *>(page) + 2 * a.n_kv * head_values + ((size_t)(a.n_kv + h) << a.page_shift) + at;
+    Vals<__bf16> in[N];
+    float unit[N];
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+        float top = 0.f;
+        if (t < grp.n) {
+            in[t] = *reinterpret_cast<const Vals<__bf16> *>(src + t * a.v_stride);
+#pragma unroll
+            for (int e = 0; e < U; ++e) top = larger(top, (float)in[t].v[e]);
+        }
+        for (int m = 1; m < n_chunks; m <<= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
+        const int e = exponent_for(top);
+        unit[t] = unit_of(KV_EXP_BIAS - e);
+        if (t < grp.n && c == 0) exps[t] = (uint8_t)(e + KV_EXP_BIAS);
+    }
+    if (grp.n == N) {
+#pragma unroll
+        for (int d = 0; d < U; ++d) {
+            const auto four = [&](int t) {
+                return four_e4m3(scaled((float)in[t].v[d], unit[t]), scaled((float)in[t + 1].v[d], unit[t + 1]), scaled((float)in[t + 2].v[d], unit[t + 2]),
+                                 scaled((float)in[t + 3].v[d], unit[t + 3]));
+            };
+            *reinterpret_cast<uint4 *>(to + d * N) = make_uint4(four(0), four(4), four(8), four(12));
+        }
+    } else {
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+            if (t < grp.n) {
+#pragma unroll
+                for (int d = 0; d < U; ++d) to[d * N + at % N + t] = (uint8_t)four_e4m3(scaled((float)in[t].v[d], unit[t]), 0.f, 0.f, 0.f);
+            }
+    }
+}
+
+template <typename E, bool E8, bool NORM, int APPEND_HEADS>
+__global__ __launch_bounds__(256) void append_heads_kernel(AppendHeadsArgs n, uint32_t key_blocks)
+{
+    constexpr int U = CHUNK<E>;
+    constexpr bool PAST = APPEND_HEADS == APPEND_MANY_HEADS;
+    const AppendArgs &a = n.a;
+    if (blockIdx.x >= key_blocks) {
+        if constexpr (E8) {
+            append_values_e4m3(a, blockIdx.x - key_blocks);
+        } else {
+            __shared__ Vals<E> turned[4][64 * U];
+            append_values<E, PAST>(a, blockIdx.x - key_blocks, turned[threadIdx.x >> 6]);
+        }
+        return;
+    }
+    const int page_tokens = 1 << a.page_shift;
+    const size_t head_values = (size_t)a.dim << a.page_shift;  // of one half of a page
+    const int n_pairs = a.dim / (2 * U), tokens = 64 / n_pairs, lane = threadIdx.x & 63;  // of a wavefront
+    const int heads = (a.q ? a.n_heads : 0) + a.n_kv, head_groups = (heads + APPEND_HEADS - 1) / APPEND_HEADS;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4u + (threadIdx.x >> 6));
+    const int h0 = wave % head_groups * APPEND_HEADS, first = (int)(wave / head_groups) * tokens;
+    if (first >= a.n_tokens) return;
+    // lanes behind the last token work on it with the others, and store nothing
+    const int p = lane / tokens, t = min(first + lane % tokens, a.n_tokens - 1);
+    const bool there = first + lane % tokens < a.n_tokens;
+    const KvToken tok = a.tokens[t];
+    const int turned = a.rope_dim / (2 * U);  // pairs of chunks that turn
+    const bool turn = p < turned, halves = turn && !a.neighbours;
+    const int c0 = halves ? p : 2 * p, c1 = halves ? p + turned : 2 * p + 1;
+    // keys come first, then queries
+    const auto source = [&](int h) {
+        return h < a.n_kv ? static_cast<const E *>(a.k) + t * a.k_stride + h * a.dim : static_cast<const E *>(a.q) + t * a.q_stride + (h - a.n_kv) * a.dim;
+    };
+    Vals<E> x[APPEND_HEADS], y[APPEND_HEADS];
+#pragma unroll
+    for (int k = 0; k < APPEND_HEADS; ++k) {
+        const E *src = source(min(h0 + k, heads - 1));
+        x[k] = load_once<PAST>(src + c0 * U);
+        y[k] = load_once<PAST>(src + c1 * U);
+    }
+    float c[U], s[U];
+    if (turn) {
+        const float *cs = a.rope + (size_t)tok.pos * a.rope_dim + p * U, *sn = cs + a.rope_dim / 2;
+#pragma unroll
+        for (int e = 0; e < U; ++e) c[e] = cs[e], s[e] = sn[e];
+    }
+#pragma unroll
+    for (int k = 0; k < APPEND_HEADS; ++k) {
+        const int h = h0 + k;
+        if (h >= heads) break;
+        const bool key = h < a.n_kv;
+        const float *w = nullptr;
+        double factor = 1.;
+        if constexpr (NORM) {
+            w = key ? n.k_norm : n.q_norm;
+            if (w) {
+                w += (int64_t)(key ? h : h - a.n_kv) * (key ? n.k_norm_stride : n.q_norm_stride);
+                double sum = 0.;
+#pragma unroll
+                for (int e = 0; e < U; ++e) {
+                    const double u = (double)(float)x[k].v[e], v = (double)(float)y[k].v[e];
+                    sum += u * u;
+                    sum += v * v;
+                }
+                for (int m = tokens; m < 64; m <<= 1) sum += __shfl_xor(sum, m, 64);
+                factor = 1. / sqrt(sum / a.dim + n.eps);
+            }
+        }
+        if (E8 && key) {
+            double u[U], v[U];
+#pragma unroll
+            for (int e = 0; e < U; ++e) u[e] = (double)(float)x[k].v[e], v[e] = (double)(float)y[k].v[e];
+            if (w) {
+#pragma unroll
+                for (int e = 0; e < U; ++e) u[e] *= factor * (double)w[c0 * U + e], v[e] *= factor * (double)w[c1 * U + e];
+            }
+            if (turn) turn_pairs(u, v, c, s, halves);
+            float f[U], g[U], top = 0.f;
+#pragma unroll
+            for (int e = 0; e < U; ++e) {
+                f[e] = to_odd(u[e]), g[e] = to_odd(v[e]);
+                top = larger(larger(top, f[e]), g[e]);
+            }
+            for (int m = tokens; m < 64; m <<= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
+            const int e = exponent_for(top);
+            const float unit = unit_of(KV_EXP_BIAS - e);
+            if (there) {
+                if constexpr (U == 8) {
+                    uint8_t *const page = reinterpret_cast<uint8_t *>(a.pages + tok.page * a.page_stride);
+                    uint8_t *const to = page + h * head_values + (size_t)(tok.pos & (page_tokens - 1)) * 16;
+                    const auto put = [&](int chunk, const float(&z)[U]) {
+                        *reinterpret_cast<uint2 *>(to + ((size_t)(chunk >> 1) << a.page_shift) * 16 + (chunk & 1) * 8) =
+                            make_uint2(four_e4m3(scaled(z[0], unit), scaled(z[1], unit), scaled(z[2], unit), scaled(z[3], unit)),
+                                       four_e4m3(scaled(z[4], unit), scaled(z[5], unit), scaled(z[6], unit), scaled(z[7], unit)));
+                    };
+                    put(c0, f), put(c1, g);
+                    if (p == 0) page[2 * a.n_kv * head_values + ((size_t)h << a.page_shift) + (tok.pos & (page_tokens - 1))] = (uint8_t)(e + KV_EXP_BIAS);
+                }
+            }
+            continue;
+        }
+        if (w || turn) {
+            float u[U], v[U];
+#pragma unroll
+            for (int e = 0; e < U; ++e) u[e] = (float)x[k].v[e], v[e] = (float)y[k].v[e];
+            if (w) {
+                const float by = (float)factor;
+#pragma unroll
+                for (int e = 0; e < U; ++e) u[e] *= by * w[c0 * U + e], v[e] *= by * w[c1 * U + e];
+            }
+            if (turn) turn_pairs(u, v, c, s, halves);
+#pragma unroll
+            for (int e = 0; e < U; ++e) x[k].v[e] = (E)u[e], y[k].v[e] = (E)v[e];
+        }
+        if (!there) continue;
+        if (key) {
+            E *page = reinterpret_cast<E *>(a.pages + tok.page * a.page_stride) + h * head_values + (size_t)(tok.pos & (page_tokens - 1)) * U;
+            *reinterpret_cast<Vals<E> *>(page + ((size_t)c0 << a.page_shift) * U) = x[k];
+            *reinterpret_cast<Vals<E> *>(page + ((size_t)c1 << a.page_shift) * U) = y[k];
+        } else {
+            E *to = static_cast<E *>(a.q_out) + t * a.q_out_stride + (h - a.n_kv) * a.dim;
+            store_past<PAST>(to + c0 * U, x[k]);
+            store_past<PAST>(to + c1 * U, y[k]);
+        }
+    }
+}
+
+hipError_t launch_append_heads(const AppendHeadsArgs &n, int dtype, bool e4m3, hipStream_t st)
+{
+    const AppendArgs &a = n.a;
+    const int u = dtype == LORA_BF16 ? 8 : 4;
+    const int64_t heads = (a.q ? a.n_heads : 0) + a.n_kv, tokens = 64 / (a.dim / (2 * u));
+    const bool many = a.n_tokens * heads * a.dim * (dtype == LORA_BF16 ? 2 : 4) >= APPEND_MANY, norm = n.q_norm || n.k_norm;
+    const int64_t each = many ? APPEND_MANY_HEADS : APPEND_FEW_HEADS;
+    const int64_t keys = ((a.n_tokens + tokens - 1) / tokens * ((heads + each - 1) / each) + 3) / 4;
+    const int64_t vals = ((int64_t)a.n_groups * a.n_kv * (a.dim / u) + 255) / 256;
+    if (keys * 256 > UINT32_MAX || vals * 256 > UINT32_MAX || keys + vals > INT32_MAX) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)(keys + vals));
+    const auto launch = [&](auto e, auto e8, auto with) {
+        typedef decltype(e) E;
+        constexpr bool E8 = decltype(e8)::value, NORM = decltype(with)::value;
+        if (many) hipLaunchKernelGGL((append_heads_kernel<E, E8, NORM, APPEND_MANY_HEADS>), grid, dim3(256), 0, st, n, (uint32_t)keys);
+        else hipLaunchKernelGGL((append_heads_kernel<E, E8, NORM, APPEND_FEW_HEADS>), grid, dim3(256), 0, st, n, (uint32_t)keys);
+    };
+    if (dtype == LORA_F32) launch(float{}, std::false_type{}, std::true_type{});
+    else if (!e4m3) launch(__bf16{}, std::false_type{}, std::true_type{});
+    else if (norm) launch(__bf16{}, std::true_type{}, std::true_type{});
+    else launch(__bf16{}, std::true_type{}, std::false_type{});
+    return hipGetLastError();
+}
+
+// What pages hold, as rows: block row y takes a piece of a page.  Keys: a thread takes a chunk of one token; 8 tokens go with a run of 8 threads, so that the page is read in runs of
+// 128 bytes, and 8 threads beside each other in a row's.  Values: a thread takes 16 bytes of a row of all tokens that share their chunks.
+template <typename E, typename P>
+__global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
+{
+    constexpr int U = CHUNK<P>, W = CHUNK<E>;  // values of 16 bytes of a page, of a row
+    const KvRead r = a.reads[blockIdx.y];
+    const char *const page = a.pages + r.page * a.page_stride;
+    const size_t head_values = (size_t)a.dim << a.page_shift;
+    const P *const values = reinterpret_cast<const P *>(page);
+    const uint8_t *const exps = reinterpret_cast<const uint8_t *>(page) + 2 * a.n_kv * head_values;  // (pages of 8 bits)
+    uint32_t i = blockIdx.x * 256u + threadIdx.x;
+    const uint32_t n_keys = (uint32_t)(a.dim / U * a.n_kv) << a.page_shift;
+    if (i < n_keys) {
+        const int t8 = i & 7;
+        i >>= 3;
+        const int c = i % (a.dim / U);
+        i /= a.dim / U;
+        const int h = i % a.n_kv, t = i / a.n_kv * 8 + t8;
+        if (t < r.off || t >= r.off + r.n) return;
+        const Vals<P> in = *reinterpret_cast<const Vals<P> *>(values + h * head_values + (((size_t)c << a.page_shift) + t) * U);
+        E *const to = static_cast<E *>(a.k) + (r.row + t - r.off) * a.k_stride + h * a.dim + c * U;
+        if constexpr (sizeof(P) == sizeof(E)) {
+            *reinterpret_cast<Vals<P> *>(to) = in;
+        } else {
+            const float unit = unit_of(exps[((size_t)h << a.page_shift) + t]);
+#pragma unroll
+            for (int k = 0; k < U / W; ++k) {
+                Vals<E> out;
+#pragma unroll
+                for (int e = 0; e < W; ++e) out.v[e] = (E)(value_of(in.v[k * W + e]) * unit);
+                *reinterpret_cast<Vals<E> *>(to + k * W) = out;
+            }
+        }
+        return;
+    }
+    i -= n_keys;
+    const int c = i % (a.dim / W);
+    i /= a.dim / W;
+    const int h = i % a.n_kv, t0 = i / a.n_kv * U;
+    if (t0 + U <= r.off || t0 >= r.off + r.n) return;  // (of blocks beyond the page, too: t0 is no token of it)
+    Vals<P> in[W];
+#pragma unroll
+    for (int e = 0; e < W; ++e) in[e] = *reinterpret_cast<const Vals<P> *>(values + (a.n_kv + h) * head_values + ((size_t)(t0 / U) * a.dim + c * W + e) * U);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        const int t = t0 + k;
+        if (t < r.off || t >= r.off + r.n) continue;
+        Vals<E> out;
+        if constexpr (sizeof(P) == sizeof(E)) {
+#pragma unroll
+            for (int e = 0; e < W; ++e) out.v[e] = in[e].v[k];
+        } else {
+            const float unit = unit_of(exps[((size_t)(a.n_kv + h) << a.page_shift) + t]);
+#pragma unroll
+            for (int e = 0; e < W; ++e) out.v[e] = (E)(value_of(in[e].v[k]) * unit);
+        }
+        *reinterpret_cast<Vals<E> *>(static_cast<E *>(a.v) + (r.row + t - r.off) * a.v_stride + h * a.dim + c * W) = out;
+    }
+}
+
+hipError_t launch_read(const ReadArgs &a, int dtype, bool e4m3, hipStream_t st)
+{
+    const int64_t u = e4m3 ? 16 : dtype == LORA_BF16 ? 8 : 4, w = dtype == LORA_BF16 ? 8 : 4;
+    const int64_t threads = ((int64_t)(a.dim / u) * a.n_kv << a.page_shift) + (int64_t)(a.dim / w) * a.n_kv * ((1 << a.page_shift) / u);
+    const int64_t blocks = (threads + 255) / 256;
+    if (blocks > INT32_MAX || a.n_reads > KV_MAX_READS) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)blocks, (unsigned)a.n_reads);
+    if (dtype == LORA_F32) hipLaunchKernelGGL((read_kernel<float, float>), grid, dim3(256), 0, st, a);
+    else if (!e4m3) hipLaunchKernelGGL((read_kernel<__bf16, __bf16>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((read_kernel<__bf16, E4m3>), grid, dim3(256), 0, st, a);
     return hipGetLastError();
 }
 

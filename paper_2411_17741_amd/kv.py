@@ -4,6 +4,7 @@ from __future__ import annotations
 
 from typing import Optional
 
+import numpy as np
 import torch
 
 from . import binding as B
@@ -17,12 +18,16 @@ class KvCache:
     """Owns the cache handle and, unless the caller brings them, the pages' memory: a tensor
     [n_pages][n_layers][2][n_kv_heads][page_tokens * head_dim] (see the header for what lies where in it).
 
+    e4m3: keys and values are held in 8 bits, with an exponent for each token and head.  The pages are bytes then, a tensor
+    [n_pages][n_layers][2 * n_kv_heads * page_tokens * (head_dim + 1)]; queries, keys, values and outputs of the calls are bf16 as before.
+
     max_batch_pages: pages that the sequences of a batch may have together, one that they share counted for each; a batch with more is refused.  By default
     whatever max_batch_seqs sequences can have, up to 4 million or 4 times the pages there are."""
 
     def __init__(self, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, n_pages: int, page_tokens: int = 64, max_seqs: int = 512,
                  max_batch_tokens: int = 4096, max_batch_seqs: int = 512, max_batch_pages: int = 0, n_batches: int = 2,
-                 dtype: int = B.LORA_BF16, device: str = "cuda:0", pages: Optional[torch.Tensor] = None):
+                 dtype: int = B.LORA_BF16, device: str = "cuda:0", pages: Optional[torch.Tensor] = None,
+                 e4m3: bool = False):
         if not torch.cuda.is_available():
             raise RuntimeError("KvCache needs a GPU: the library has no CPU path")
         index = torch.device(device).index
@@ -32,15 +37,18 @@ class KvCache:
         # Forks share pages: the sequences of a batch may name more pages than there are.  Every sequence may name all of them, up to a list of 16 MB for each batch
         max_batch_pages = max_batch_pages or min(max_batch_seqs * n_pages, max(4 * n_pages, 1 << 22))
         self.cfg = B.make_kv_config(n_layers, n_heads, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs, max_batch_seqs, max_batch_tokens,
-                                    max_batch_pages, n_batches, dtype)
+                                    max_batch_pages, n_batches, dtype, B.LORA_KV_PAGES_E4M3 if e4m3 else 0)
         n_bytes, work = B.lora_kv_pages_bytes(self.cfg), B.lora_kv_work_bytes(self.cfg)
         if n_bytes == 0:
             raise B.LoraError(B.LORA_E_INVAL, "lora_kv_pages_bytes")
-        shape = (n_pages, n_layers, 2, n_kv_heads, page_tokens * head_dim)
+        if e4m3:
+            shape, held = (n_pages, n_layers, 2 * n_kv_heads * page_tokens * (head_dim + 1)), torch.uint8
+        else:
+            shape, held = (n_pages, n_layers, 2, n_kv_heads, page_tokens * head_dim), self.dtype
         if pages is None:
-            pages = torch.empty(shape, dtype=self.dtype, device=self.device)
-        if tuple(pages.shape) != shape or pages.dtype != self.dtype or pages.get_device() != self._index or not pages.is_contiguous():
-            raise ValueError(f"pages: a contiguous {self.dtype} tensor of shape {shape} on {self.device} is wanted")
+            pages = torch.empty(shape, dtype=held, device=self.device)
+        if tuple(pages.shape) != shape or pages.dtype != held or pages.get_device() != self._index or not pages.is_contiguous():
+            raise ValueError(f"pages: a contiguous {held} tensor of shape {shape} on {self.device} is wanted")
         self.pages = pages
         self.work = torch.empty(work + 256, dtype=torch.uint8, device=self.device)
         with torch.cuda.device(self._index):  # the cache belongs to the device that is current now
@@ -79,6 +87,17 @@ class KvCache:
     def free(self, ids) -> None:
         B.check(B.lora_kv_seq_free(self.handle, ids), "lora_kv_seq_free")
 
+    def read(self, ids, layer: int, k: torch.Tensor, v: torch.Tensor, first=None, n_tokens=None, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """Keys and values of tokens [first[i], first[i] + n_tokens[i]) of each sequence -- all there are, if not given -- out of the pages: k and v
+        [tokens of all of them][n_kv_heads][head_dim], one sequence's behind the other's."""
+        ids = np.asarray(ids, np.int64).reshape(-1)
+        first = np.zeros(ids.size, np.int32) if first is None else np.asarray(first, np.int32).reshape(-1)
+        n_tokens = np.asarray([self.length(int(i)) for i in ids], np.int32) - first if n_tokens is None else np.asarray(n_tokens, np.int32).reshape(-1)
+        n = int(n_tokens.sum(dtype=np.int64))
+        kp, ks = self._rows(k, "k", n, self.n_kv_heads)
+        vp, vs = self._rows(v, "v", n, self.n_kv_heads)
+        B.check(B.lora_kv_seq_read(self.handle, ids, first, n_tokens, layer, kp, ks, vp, vs, self._stream(stream)), "lora_kv_seq_read")
+
     def length(self, seq: int) -> int:
         rc, info = B.lora_kv_seq_info(self.handle, seq)
         B.check(rc, "lora_kv_seq_info")
@@ -113,9 +132,9 @@ class KvCache:
     def batch_destroy(self, batch) -> None:
         B.check(B.lora_kv_batch_destroy(self.handle, batch), "lora_kv_batch_destroy")
 
-    def _rows(self, t: torch.Tensor, name: str, batch, heads: int):
-        """(address, values between tokens) of [T][heads][head_dim] or [T][heads * head_dim], the heads of a token one after the other"""
-        d, n, shape, stride = self.head_dim, batch.n_tokens, t.shape, t.stride()
+    def _rows(self, t: torch.Tensor, name: str, n: int, heads: int):
+        """(address, values between tokens) of [n][heads][head_dim] or [n][heads * head_dim], the heads of a token one after the other"""
+        d, shape, stride = self.head_dim, t.shape, t.stride()
         flat = len(shape) == 2 and shape[1] == heads * d and stride[1] == 1
         if not (flat or (len(shape) == 3 and shape[1] == heads and shape[2] == d and stride[2] == 1 and (stride[1] == d or heads == 1))):
             raise ValueError(f"{name}: [{n}][{heads}][{d}] with the heads of a token in a row is wanted, got {tuple(shape)}, strides {stride}")
@@ -124,15 +143,17 @@ class KvCache:
         return t.data_ptr(), stride[0] if n > 1 else heads * d
 
     def append(self, batch, layer: int, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
-               rope: Optional[torch.Tensor] = None, neighbours: bool = False, stream: Optional[torch.cuda.Stream] = None) -> None:
-        """rope: [positions][rope_dim] fp32, the cosines of a position and then its sines.  q_out: q itself if not given."""
+               rope: Optional[torch.Tensor] = None, neighbours: bool = False, stream: Optional[torch.cuda.Stream] = None,
+               q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6) -> None:
+        """rope: [positions][rope_dim] fp32, the cosines of a position and then its sines.  q_out: q itself if not given.  q_norm, k_norm: the weights, fp32, of norms
+        of every head of the queries and keys before they turn: [head_dim], or [heads][head_dim] with weights of each head's own."""
         rows = self._rows
-        kp, ks = rows(k, "k", batch, self.n_kv_heads)
-        vp, vs = rows(v, "v", batch, self.n_kv_heads)
+        kp, ks = rows(k, "k", batch.n_tokens, self.n_kv_heads)
+        vp, vs = rows(v, "v", batch.n_tokens, self.n_kv_heads)
         qp = qs = op = os_ = 0
         if q is not None:
-            qp, qs = rows(q, "q", batch, self.n_heads)
-            op, os_ = (qp, qs) if q_out is None else rows(q_out, "q_out", batch, self.n_heads)
+            qp, qs = rows(q, "q", batch.n_tokens, self.n_heads)
+            op, os_ = (qp, qs) if q_out is None else rows(q_out, "q_out", batch.n_tokens, self.n_heads)
         elif q_out is not None:
             raise ValueError("q_out without q")
         rp = rn = rd = 0
@@ -140,10 +161,26 @@ class KvCache:
             if rope.dim() != 2 or rope.dtype != torch.float32 or rope.get_device() != self._index or not rope.is_contiguous():
                 raise ValueError(f"rope: a contiguous fp32 tensor [positions][rope_dim] on {self.device} is wanted")
             rp, (rn, rd) = rope.data_ptr(), rope.shape
-        B.check(B.lora_kv_append(self.handle, batch, layer, kp, vp, ks, vs, qp, op, qs, os_, rp, min(rn, 2**31 - 1), rd,
-                                 B.LORA_ROPE_NEIGHBOURS if neighbours else B.LORA_ROPE_HALVES, self._stream(stream)), "lora_kv_append")
+        args = (self.handle, batch, layer, kp, vp, ks, vs, qp, op, qs, os_, rp, min(rn, 2**31 - 1), rd, B.LORA_ROPE_NEIGHBOURS if neighbours else B.LORA_ROPE_HALVES)
+        if q_norm is None and k_norm is None:
+            B.check(B.lora_kv_append(*args, self._stream(stream)), "lora_kv_append")
+            return
+        if q_norm is not None and q is None:
+            raise ValueError("q_norm without q")
+        qw, qws = self._weights(q_norm, "q_norm", self.n_heads)
+        kw, kws = self._weights(k_norm, "k_norm", self.n_kv_heads)
+        B.check(B.lora_kv_append_norm(*args, qw, kw, qws, kws, eps, self._stream(stream)), "lora_kv_append_norm")
+
+    def _weights(self, w: Optional[torch.Tensor], name: str, heads: int):
+        """(address, values between heads) of a norm's weights [head_dim] or [heads][head_dim]"""
+        if w is None:
+            return 0, 0
+        d, shape = self.head_dim, tuple(w.shape)
+        if shape not in ((d,), (heads, d)) or w.dtype != torch.float32 or w.get_device() != self._index or w.stride(-1) != 1:
+            raise ValueError(f"{name}: fp32 weights [{d}] or [{heads}][{d}] on {self.device} are wanted, got {shape} of {w.dtype} on {w.device}")
+        return w.data_ptr(), w.stride(0) if len(shape) == 2 and heads > 1 else 0
 
     def attend(self, batch, layer: int, q: torch.Tensor, out: torch.Tensor, scale: float, stream: Optional[torch.cuda.Stream] = None) -> None:
-        qp, qs = self._rows(q, "q", batch, self.n_heads)
-        op, os_ = self._rows(out, "out", batch, self.n_heads)
+        qp, qs = self._rows(q, "q", batch.n_tokens, self.n_heads)
+        op, os_ = self._rows(out, "out", batch.n_tokens, self.n_heads)
         B.check(B.lora_kv_attend(self.handle, batch, layer, qp, qs, op, os_, scale, self._stream(stream)), "lora_kv_attend")
