@@ -154,6 +154,11 @@ int lora_kv_stats(const lora_kv_t *kv, lora_kv_stats_t *out);
  * alive), LORA_E_STATE on a stream that is captured. */
 int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, const int32_t *seg_offsets, void *stream,
                          lora_kv_batch_t **out);
+/* The same for requests that begin alike (forks of a long prompt, say): where segments of few rows -- tokens times n_heads / n_kv_heads, fewer than 128 -- share pages
+ * that are full, attention reads those once, for the rows of all of them together, and joins the result with that of each one's own tokens.  Prefixes may branch: what some of
+ * the segments share beyond what all do is a prefix of its own.  Which pages are shared is seen from the books (pages with the same keys and values that were appended twice are not).  A
+ * prefix too short to gain by it is left to the segments, and so are all if the pieces' results have no room.  Outputs are those of lora_kv_batch_create up to the rounding of sums. */
+int lora_kv_batch_create_shared(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, const int32_t *seg_offsets, void *stream, lora_kv_batch_t **out);
 int lora_kv_batch_destroy(lora_kv_t *kv, lora_kv_batch_t *batch);
 
 /* How the attention works on tiles of rows: four wavefronts to a tile; the same, three tiles on a compute unit; two groups of four wavefronts to a
@@ -170,6 +175,13 @@ typedef struct {
     int32_t tiles_way;                     /* LORA_KV_TILES_* */
 } lora_kv_batch_info_t;
 int lora_kv_batch_info(const lora_kv_batch_t *batch, lora_kv_batch_info_t *out);
+
+/* What its segments share: prefixes, segments that have one, tokens of all prefixes together, pieces of attention over them. */
+typedef struct {
+    int32_t n_prefixes, n_segments, n_row_items, n_tile_items;
+    int64_t n_tokens;
+} lora_kv_prefix_info_t;
+int lora_kv_batch_prefixes(const lora_kv_batch_t *batch, lora_kv_prefix_info_t *out);
 
 enum { LORA_ROPE_HALVES = 0, LORA_ROPE_NEIGHBOURS = 1 };
 

@@ -118,6 +118,10 @@ class lora_kv_batch_info_t(ctypes.Structure):
     _fields_ = [(n, c_int32) for n in ("n_tokens", "n_segments", "n_pages", "n_groups", "n_row_items", "n_tile_items", "n_joins", "n_short_items", "tiles_way")]
 
 
+class lora_kv_prefix_info_t(ctypes.Structure):
+    _fields_ = [(n, c_int32) for n in ("n_prefixes", "n_segments", "n_row_items", "n_tile_items")] + [("n_tokens", c_int64)]
+
+
 # lora_kv_append_t: k, v, k_stride, v_stride, q, q_out, q_stride, q_out_stride, rope, rope_positions, rope_dim, rope_pairs (packed: a ctypes structure of twelve fields
 # costs a call 1 us more)
 _kv_append_t = struct.Struct("=QQqqQQqqQiii4x")
@@ -200,6 +204,8 @@ _SIGS = {
     "lora_kv_set_limit": (c_int, [c_void_p, c_int32]),
     "lora_kv_stats": (c_int, [c_void_p, POINTER(lora_kv_stats_t)]),
     "lora_kv_batch_create": (c_int, [c_void_p, c_int32, _i64a, _i32a, c_void_p, POINTER(c_void_p)]),
+    "lora_kv_batch_create_shared": (c_int, [c_void_p, c_int32, _i64a, _i32a, c_void_p, POINTER(c_void_p)]),
+    "lora_kv_batch_prefixes": (c_int, [c_void_p, POINTER(lora_kv_prefix_info_t)]),
     "lora_kv_batch_destroy": (c_int, [c_void_p, c_void_p]),
     "lora_kv_batch_info": (c_int, [c_void_p, POINTER(lora_kv_batch_info_t)]),
     "lora_kv_append": (c_int, [c_void_p, c_void_p, c_int32, c_char_p, c_void_p]),
@@ -690,14 +696,30 @@ def lora_kv_stats(kv):
     return rc, st
 
 
-def lora_kv_batch_create(kv, seg_seq, seg_offsets, stream: int = 0):
-    """-> (status, batch handle)"""
+def _kv_batch(create, kv, seg_seq, seg_offsets, stream: int):
     ids, off = _i64(seg_seq), _i32(seg_offsets).reshape(-1)
     if off.size != ids.size + 1:
         raise ValueError(f"{ids.size} segments, {off.size} offsets")
     b = c_void_p()
-    rc = _lib.lora_kv_batch_create(kv, ids.size, _ptr(ids), _ptr(off), c_void_p(stream or None), ctypes.byref(b))
+    rc = create(kv, ids.size, _ptr(ids), _ptr(off), c_void_p(stream or None), ctypes.byref(b))
     return rc, b
+
+
+def lora_kv_batch_create(kv, seg_seq, seg_offsets, stream: int = 0):
+    """-> (status, batch handle)"""
+    return _kv_batch(_lib.lora_kv_batch_create, kv, seg_seq, seg_offsets, stream)
+
+
+def lora_kv_batch_create_shared(kv, seg_seq, seg_offsets, stream: int = 0):
+    """-> (status, batch handle)"""
+    return _kv_batch(_lib.lora_kv_batch_create_shared, kv, seg_seq, seg_offsets, stream)
+
+
+def lora_kv_batch_prefixes(batch):
+    """-> (status, lora_kv_prefix_info_t)"""
+    info = lora_kv_prefix_info_t()
+    rc = _lib.lora_kv_batch_prefixes(batch, ctypes.byref(info))
+    return rc, info
 
 
 def lora_kv_batch_destroy(kv, batch) -> int:

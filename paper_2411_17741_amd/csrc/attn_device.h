@@ -46,6 +46,9 @@ __device__ __forceinline__ const uint8_t *exponents(const AttnArgs &a, int page,
     return reinterpret_cast<const uint8_t *>(a.pages + page * a.page_stride) + ((size_t)(2 * a.n_kv * D + half * a.n_kv + kv_head) << a.page_shift);
 }
 
+// The token in the packed batch of an item's rows t * group, t * group + 1, ...
+__device__ __forceinline__ int token_of(const AttnArgs &a, const AttnItem &it, int t) { return it.ctx == KV_SHARED ? a.row_tokens[it.tok0 + t] : it.tok0 + t; }
+
 // One row by one wavefront, a token a lane for the scores and D / 64 values of the output a lane.  Lane i holds values i, i + 64, ...  The weights, and their sum l, are
 // 2^28 times smaller than elsewhere: a sequence has no more tokens than that, so their sums with values of any size stay in range.
 constexpr float ROW_ROOM = 1 << 28;
@@ -61,7 +64,7 @@ __device__ void one_row(const AttnArgs &a, const AttnItem &it, int kv_head, int 
     constexpr int U = CHUNK<P>;
     const int lane = threadIdx.x & 63;
     const int t = row / a.group, head = kv_head * a.group + row % a.group;
-    const E *q = static_cast<const E *>(a.q) + (int64_t)(it.tok0 + t) * a.q_stride + head * D;
+    const E *q = static_cast<const E *>(a.q) + (int64_t)token_of(a, it, t) * a.q_stride + head * D;
     const int end = min(kv1, it.ctx + t + 1);
     const int in_page = (1 << a.page_shift) - 1;
     st.m = -FLT_MAX;
@@ -328,7 +331,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it,
     const int end = it.ctx + row / a.group + 1;  // tokens that this lane's row sees
     uint4 q[KC];
     {
-        const E *p = static_cast<const E *>(a.q) + (int64_t)(it.tok0 + row / a.group) * a.q_stride + (kv_head * a.group + row % a.group) * D;
+        const E *p = static_cast<const E *>(a.q) + (int64_t)token_of(a, it, row / a.group) * a.q_stride + (kv_head * a.group + row % a.group) * D;
 #pragma unroll
         for (int c = 0; c < KC; ++c) q[c] = *reinterpret_cast<const uint4 *>(p + (4 * c + g) * U);
     }
@@ -607,7 +610,7 @@ template <typename E, int D, int TK> struct TileRows {
         const int t = row / a.group;
         end = it.ctx + t + 1;
         least = it.ctx + (it.row0 + min(part * 32, it.n_rows - 1)) / a.group + 1;
-        const E *p = static_cast<const E *>(a.q) + (int64_t)(it.tok0 + t) * a.q_stride + (kv_head * a.group + row - t * a.group) * D;
+        const E *p = static_cast<const E *>(a.q) + (int64_t)token_of(a, it, t) * a.q_stride + (kv_head * a.group + row - t * a.group) * D;
 #pragma unroll
         for (int c = 0; c < QC; ++c) q[c] = *reinterpret_cast<const uint4 *>(p + (2 * c + h) * U);
         m = -FLT_MAX;
@@ -1273,6 +1276,44 @@ __global__ __launch_bounds__(256) void attn_join_tiles_kernel(JoinArgs a)
     E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D;
 #pragma unroll
     for (int k = 0; k < N; ++k) put_four(out + (k * 4 + threadIdx.x / 64) * 8 + lane / 32 * 4, l == 0.f ? o[k] / l : o[k]);
+}
+
+// Joins the parts of rows whose segments share prefixes: a wavefront to a row, a lane to a part for their maxima and sums, then D / 4 lanes to a part's values.
+template <typename E, int D>
+__global__ __launch_bounds__(256) void shared_join_kernel(SharedJoinArgs a)
+{
+    constexpr int PER = D / 4, AT_ONCE = 64 / PER;  // lanes of a part's values; parts that the lanes have at a time
+    const SharedJoin it = a.items[blockIdx.x / a.n_kv];
+    const int kv_head = blockIdx.x % a.n_kv, r = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (r >= it.n_rows) return;
+    const int mine = lane / PER, d = lane % PER * 4;
+    float m = -FLT_MAX, l = 0.f;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < it.n_sources; ++k) {
+        const SharedSource src = a.sources[it.source0 + k];
+        const SharedBlock blk = a.blocks[src.block0 + (src.row0 + r) / src.rows];
+        const int rr = (src.row0 + r) % src.rows;
+        const int64_t first = blk.part + (int64_t)kv_head * (src.tile ? (blk.n_rows + 31) & ~31 : blk.n_rows) + rr;
+        const float *from = a.part_o + (src.tile ? (first - (rr & 31)) * D + tile_part(rr & 31, d) : first * D + d);
+        for (int i0 = 0; i0 < blk.n_parts; i0 += 64) {
+            const int n = min(blk.n_parts - i0, 64);
+            const float2 ml = lane < n ? *reinterpret_cast<const float2 *>(a.part_ml + 2 * (first + (int64_t)(i0 + lane) * blk.stride)) : make_float2(-FLT_MAX, 0.f);
+            const float top = fmaxf(m, wave_max(ml.x)), before = l * __builtin_amdgcn_exp2f(m - top), w = ml.y * __builtin_amdgcn_exp2f(ml.x - top);
+            m = top;
+            l = before + wave_sum(w);
+            const float each = l == 0.f ? 0.f : 1.f / l;
+            o *= before * each;
+            for (int i = 0; i < n; i += AT_ONCE) {
+                const float f = __shfl(w, i + mine, 64) * each;  // (of a part that is not there: 0)
+                if (i + mine < n) o += *reinterpret_cast<const floatx4 *>(from + (int64_t)(i0 + i + mine) * blk.stride * D) * f;
+            }
+        }
+    }
+#pragma unroll
+    for (int off = 32; off >= PER; off >>= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], off, 64);
+    if (mine == 0) put_four(static_cast<E *>(a.out) + (int64_t)(it.tok0 + r / a.group) * a.out_stride + (kv_head * a.group + r % a.group) * D + d, l == 0.f ? o / l : o);
 }
 
 }  // namespace lora

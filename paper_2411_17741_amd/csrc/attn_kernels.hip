@@ -89,4 +89,14 @@ hipError_t launch_attn_join(const JoinArgs &a, int dtype, int dim, bool tiles, h
     });
 }
 
+hipError_t launch_shared_join(const SharedJoinArgs &a, int dtype, int dim, hipStream_t st)
+{
+    if ((int64_t)a.n_items * a.n_kv > INT32_MAX) return hipErrorInvalidValue;
+    return by_type(dtype, dim, [&](auto e, auto d) {
+        typedef decltype(e) E;
+        constexpr int D = decltype(d)::value;
+        hipLaunchKernelGGL((shared_join_kernel<E, D>), dim3(a.n_items * a.n_kv, (a.max_rows + 3) / 4), dim3(256), 0, st, a);
+    });
+}
+
 }  // namespace lora

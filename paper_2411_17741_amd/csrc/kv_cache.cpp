@@ -39,6 +39,8 @@ constexpr int ROW_SHORT_VALUES = 16384;
 constexpr int tile_min_tokens(const lora_kv_config_t &c) { return c.dtype == LORA_BF16 ? 512 : c.head_dim == 64 ? 256 : 128; }
 constexpr int PIECE_STEP = 64;  // pieces begin at multiples of it: a whole number of every kernel's steps, in one page or at the start of one
 constexpr int MAX_EXTRA = 2048;  // pieces beyond one for each block of rows
+// Prefixes: tokens from which sharing one is worth the join, of how many prefixes of prefixes a segment may have a part, tokens' places in all of them together (times max_batch_tokens)
+constexpr int SHARED_MIN_TOKENS = 256, SHARED_DEPTH = 7, SHARED_TOKENS = 2;
 
 struct Seq {
     int64_t id = 0;
@@ -58,6 +60,9 @@ struct Batch {
     lora_kv_batch_info_t info{};
     int32_t max_pos = -1;  // of the batch's tokens
     int32_t n_joins = 0, n_tile_joins = 0, join_rows = 0;  // join_rows: the most rows of a join of row items
+    int32_t n_shared_joins = 0, shared_rows = 0;  // segments with prefixes; the most rows of one
+    lora_kv_prefix_info_t prefixes{};
+    size_t off_row_tokens = 0, off_sources = 0, off_blocks = 0, off_shared_joins = 0;
     size_t off_tokens = 0, off_groups = 0, off_pages = 0, off_rows = 0, off_tiles = 0, off_joins = 0, off_tile_joins = 0;
     std::vector<uint8_t> member;  // by sequence slot
     bool alive() const { return name != 0; }
@@ -158,6 +163,9 @@ using lora::AttnItem;
 using lora::JoinItem;
 using lora::KvGroup;
 using lora::KvToken;
+using lora::SharedBlock;
+using lora::SharedJoin;
+using lora::SharedSource;
 
 static_assert(1024 + SPARE_BATCHES <= 1 << NAME_BITS, "the most batches of a cache");
 
@@ -201,7 +209,9 @@ size_t list_bytes(const lora_kv_config_t &c)
 {
     const size_t T = c.max_batch_tokens;
     return align_up(T * sizeof(KvToken)) + align_up(T * sizeof(KvGroup)) + align_up((size_t)c.max_batch_pages * 4) +
-           align_up((size_t)max_items(c) * sizeof(AttnItem)) + align_up((size_t)MAX_EXTRA * sizeof(JoinItem)) + 3 * ALIGN;
+           align_up((size_t)max_items(c) * sizeof(AttnItem)) + align_up((size_t)MAX_EXTRA * sizeof(JoinItem)) + 3 * ALIGN +
+           align_up(T * SHARED_TOKENS * 4) + align_up((size_t)max_items(c) * sizeof(SharedBlock)) + align_up((size_t)c.max_batch_seqs * (SHARED_DEPTH + 1) * sizeof(SharedSource)) +
+           align_up((size_t)c.max_batch_seqs * sizeof(SharedJoin));
 }
 
 // The cache's device is the current one as long as this lives: events, the default stream and kernels are the current device's.
@@ -332,8 +342,22 @@ void reserve(const lora_kv &kv, Growth &g)
     g.to.reserve(g.seqs.size());
 }
 
+// A prefix: entries [from, to) of the page lists of its segments, which they have in common, and as many rows as the segments have together.
+struct Prefix {
+    int32_t from, to;
+    std::vector<int32_t> segs;
+    int64_t rows;
+};
+
 // How the attention of a batch is cut up.
 struct Cut {
+    std::vector<Prefix> prefixes;
+    std::vector<int32_t> own;  // by segment: the pages that are its prefixes' (empty: none has one)
+    std::vector<int32_t> row_tokens;
+    std::vector<SharedSource> sources;
+    std::vector<SharedBlock> blocks;
+    std::vector<SharedJoin> shared_joins;
+    int32_t prefix_row_items = 0, prefix_tile_items = 0;
     lora::KvTiles way = lora::KV_TILES_PLAIN;
     int32_t n_short = 0;  // of the rows' items, at the list's end
     std::vector<AttnItem> rows, tiles;
@@ -364,8 +388,76 @@ void cut_block(AttnItem base, int32_t kv_len, int32_t piece, int32_t rows, int32
     }
 }
 
-void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, Cut &cut)
+// What segments of few rows have in common.  Larger ones fill tiles of their own: the products take as long, and there is nothing to join.  (Called before the
+// sequences grow: pages that are full by then stay as they are.)
+void find_prefixes(const lora_kv &kv, const Growth &g, Cut &cut)
 {
+    const int32_t grp = kv.group();
+    struct Set {
+        int32_t at, base, depth;  // pages that the segments have in common; those of them that are in prefixes already; how many these are
+        std::vector<int32_t> segs;
+    };
+    const auto full = [&](int32_t i) { return g.seqs[i]->n_tokens >> kv.page_shift; };
+    const auto page = [&](int32_t i, int32_t at) { return g.seqs[i]->pages[at]; };
+    std::vector<Set> sets(1);
+    for (size_t i = 0; i < g.seqs.size(); ++i)
+        if (g.n_tokens[i] && (int64_t)g.n_tokens[i] * grp < lora::KV_TILE) sets[0].segs.push_back((int32_t)i);
+    sets[0].at = sets[0].base = sets[0].depth = 0;
+    cut.own.assign(g.seqs.size(), 0);
+    int64_t room = (int64_t)kv.cfg.max_batch_tokens * SHARED_TOKENS;
+    while (!sets.empty()) {
+        Set set = std::move(sets.back());
+        sets.pop_back();
+        if (set.depth == SHARED_DEPTH) continue;
+        std::vector<int32_t> &segs = set.segs;
+        segs.erase(std::remove_if(segs.begin(), segs.end(), [&](int32_t i) { return full(i) <= set.at || kv.refs[page(i, set.at)] < 2; }), segs.end());
+        std::sort(segs.begin(), segs.end(), [&](int32_t a, int32_t b) { return page(a, set.at) != page(b, set.at) ? page(a, set.at) < page(b, set.at) : a < b; });
+        for (size_t first = 0, last; first < segs.size(); first = last) {
+            for (last = first + 1; last < segs.size() && page(segs[last], set.at) == page(segs[first], set.at);) ++last;
+            if (last - first < 2) continue;
+            Set part{full(segs[first]), set.base, set.depth, {segs.begin() + first, segs.begin() + last}};
+            const int32_t *const p = g.seqs[segs[first]]->pages.data();
+            int64_t tokens = 0;
+            for (const int32_t i : part.segs) {
+                part.at = std::min(part.at, full(i));
+                part.at = (int32_t)(std::mismatch(p + set.at, p + part.at, g.seqs[i]->pages.data() + set.at).first - p);
+                tokens += g.n_tokens[i];
+            }
+            if (((int64_t)(part.at - part.base) << kv.page_shift) >= SHARED_MIN_TOKENS) {
+                if (tokens > room) continue;
+                room -= tokens;
+                cut.prefixes.push_back({part.base, part.at, part.segs, tokens * grp});
+                for (const int32_t i : part.segs) cut.own[i] = part.at;
+                part.base = part.at;
+                ++part.depth;
+            }
+            sets.push_back(std::move(part));
+        }
+    }
+    if (cut.prefixes.empty()) cut.own.clear();
+}
+
+// The same into pieces whose results are always joined, from token `from` on; where they lie is noted as a block of rows
+void cut_shared(AttnItem base, int32_t from, int32_t to, int32_t piece, int32_t rows, int32_t n_kv, std::vector<AttnItem> &items, std::vector<SharedBlock> &blocks, int64_t &part)
+{
+    int32_t n = std::max((to - from + piece - 1) / piece, 1);
+    const int32_t each = ((to - from + n - 1) / n + PIECE_STEP - 1) / PIECE_STEP * PIECE_STEP, stride = rows * n_kv;
+    n = (to - from + each - 1) / each;
+    blocks.push_back({(int32_t)part, n, stride, base.n_rows});
+    for (int32_t i = 0; i < n; ++i) {
+        base.kv0 = from + i * each;
+        base.kv1 = std::min(to, from + (i + 1) * each);
+        base.part = (int32_t)part;
+        part += stride;
+        items.push_back(base);
+    }
+}
+
+// false: the results of the prefixes' pieces have no room
+bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, Cut &cut)
+{
+    const auto from_of = [&](size_t i) { return cut.own.empty() ? (int64_t)0 : (int64_t)cut.own[i] << kv.page_shift; };
+    const auto tokens_of = [&](const Prefix &p) { return (int64_t)(p.to - p.from) << kv.page_shift; };
     const int32_t grp = kv.group(), n_kv = kv.cfg.n_kv_heads, tile_min = tile_min_tokens(kv.cfg);
     int64_t row_tokens = 0, tile_tokens = 0, n_tiles = 0, longest = 0, part = 0, tile = lora::KV_TURNS_TILE;
     const auto tile_end = [&tile, grp](int64_t ctx, int64_t rows, int64_t row0) {  // tokens that the tile's last row sees
@@ -379,8 +471,10 @@ void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
         for (size_t i = 0; i < g.seqs.size(); ++i) {
             const int64_t n = g.n_tokens[i], rows = n * grp, ctx = g.seqs[i]->n_tokens - n;
             if (rows > lora::KV_ROW_ITEM)
-                for (int64_t r = 0; r < rows; r += tile) tokens += tile_end(ctx, rows, r), ++n_tiles;
+                for (int64_t r = 0; r < rows; r += tile) tokens += tile_end(ctx, rows, r) - from_of(i), ++n_tiles;
         }
+        for (const Prefix &p : cut.prefixes)
+            if (p.rows > lora::KV_ROW_ITEM) tokens += (p.rows + tile - 1) / tile * tokens_of(p), n_tiles += (p.rows + tile - 1) / tile;
         if (n_tiles * n_kv >= 2 * kv.n_cu && tokens >= 1024 * n_tiles) cut.way = lora::KV_TILES_TURNS;
     }
     if (cut.way != lora::KV_TILES_TURNS) tile = lora::KV_TILE;
@@ -388,13 +482,23 @@ void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     for (size_t i = 0; i < g.seqs.size(); ++i) {
         const int64_t n = g.n_tokens[i], rows = n * grp, ctx = g.seqs[i]->n_tokens - n;
         if (!n) continue;
-        if (rows <= lora::KV_ROW_ITEM) row_tokens += ctx + n;
+        if (rows <= lora::KV_ROW_ITEM) row_tokens += ctx + n - from_of(i);
         else
             for (int64_t r = 0; r < rows; r += tile, ++n_tiles) {
-                const int64_t end = tile_end(ctx, rows, r);
+                const int64_t end = tile_end(ctx, rows, r) - from_of(i);
                 tile_tokens += end;
                 longest = std::max(longest, end);
             }
+    }
+    for (const Prefix &p : cut.prefixes) {
+        if (p.rows <= lora::KV_ROW_ITEM) {
+            row_tokens += tokens_of(p);
+            continue;
+        }
+        const int64_t tiles = (p.rows + tile - 1) / tile;
+        n_tiles += tiles;
+        tile_tokens += tiles * tokens_of(p);
+        longest = std::max(longest, tokens_of(p));
     }
     const auto at_least = [](int64_t tokens, int64_t least) { return (int32_t)std::min(std::max(tokens, least), (int64_t)LORA_KV_MAX_TOKENS); };
     int32_t row_piece = at_least(row_tokens * n_kv / ROW_BLOCKS, ROW_MIN_TOKENS);
@@ -404,7 +508,7 @@ void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     // No more blocks than compute units and no tile of over 1024 tokens: for heads of 64, whose steps are mostly instructions of one wavefront after the other, two groups of
     // wavefronts share a tile's tokens, and tiles stay whole (700 tokens with 32 heads 16.5 -> 12.5 us, with 32 / 8 heads 15.3 -> 12.3).  Longer ones, and heads of 128, do as well
     // or better with pieces.
-    if (cut.way == lora::KV_TILES_PLAIN && lora::kv_pairs(kv.cfg.dtype, kv.cfg.head_dim) && n_tiles && n_tiles * n_kv <= kv.n_cu && longest <= 2 * tile_min) {
+    if (cut.way == lora::KV_TILES_PLAIN && cut.prefixes.empty() && lora::kv_pairs(kv.cfg.dtype, kv.cfg.head_dim) && n_tiles && n_tiles * n_kv <= kv.n_cu && longest <= 2 * tile_min) {
         cut.way = lora::KV_TILES_PAIRS;
         tile_whole = 2 * tile_min;
     }
@@ -419,11 +523,45 @@ void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
         cut.tiles.clear();
         cut.joins.clear();
         cut.tile_joins.clear();
+        cut.row_tokens.clear();
+        cut.sources.clear();
+        cut.blocks.clear();
+        cut.shared_joins.clear();
         part = 0;
+        // prefixes first, then the segments' own tokens: what of a prefix a segment's rows are, by prefix and segment
+        std::vector<std::vector<SharedSource>> of_segment(cut.own.size());
+        for (const Prefix &p : cut.prefixes) {
+            const bool tiles = p.rows > lora::KV_ROW_ITEM;
+            const int32_t rows_of = tiles ? (int32_t)tile : lora::KV_ROW_ITEM, block0 = (int32_t)cut.blocks.size(), list0 = (int32_t)cut.row_tokens.size();
+            int64_t row = 0;
+            for (const int32_t i : p.segs) {
+                of_segment[i].push_back({(int32_t)row, block0, rows_of, tiles});
+                for (int32_t t = 0; t < g.n_tokens[i]; ++t) cut.row_tokens.push_back(offsets[i] + t);
+                row += (int64_t)g.n_tokens[i] * grp;
+            }
+            AttnItem it{list0, lora::KV_SHARED, cut.page0[p.segs[0]], 0, 0, 0, 0, -1};
+            for (int64_t r = 0; r < p.rows; r += rows_of) {
+                it.row0 = (int32_t)r;
+                it.n_rows = (int32_t)std::min(p.rows - r, (int64_t)rows_of);
+                cut_shared(it, p.from << kv.page_shift, p.to << kv.page_shift, tiles ? tile_piece : row_piece, tiles ? (it.n_rows + 31) & ~31 : it.n_rows, n_kv, tiles ? cut.tiles : cut.rows,
+                           cut.blocks, part);
+            }
+        }
+        cut.prefix_row_items = (int32_t)cut.rows.size();
+        cut.prefix_tile_items = (int32_t)cut.tiles.size();
         for (size_t i = 0; i < g.seqs.size(); ++i) {
             const int64_t n = g.n_tokens[i], rows = n * grp, ctx = g.seqs[i]->n_tokens - n;
             if (!n) continue;
             AttnItem it{offsets[i], (int32_t)ctx, cut.page0[i], 0, (int32_t)rows, 0, 0, -1};
+            if (from_of(i)) {  // (fewer rows than a tile has)
+                const bool tiles = rows > lora::KV_ROW_ITEM;
+                of_segment[i].push_back({0, (int32_t)cut.blocks.size(), lora::KV_TILE, tiles});
+                cut_shared(it, (int32_t)from_of(i), (int32_t)(ctx + n), tiles ? tile_piece : row_piece, tiles ? (it.n_rows + 31) & ~31 : it.n_rows, n_kv, tiles ? cut.tiles : cut.rows, cut.blocks,
+                           part);
+                cut.shared_joins.push_back({offsets[i], (int32_t)rows, (int32_t)cut.sources.size(), (int32_t)of_segment[i].size()});
+                cut.sources.insert(cut.sources.end(), of_segment[i].begin(), of_segment[i].end());
+                continue;
+            }
             if (rows <= lora::KV_ROW_ITEM) {
                 cut_block(it, (int32_t)(ctx + n), row_piece, it.n_rows, n_kv, cut.rows, cut.joins, part);
                 continue;
@@ -441,6 +579,7 @@ void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
             continue;
         }
         if (part <= kv.part_rows && cut.joins.size() + cut.tile_joins.size() <= (size_t)MAX_EXTRA && (int64_t)(cut.rows.size() + cut.tiles.size()) <= max_items(kv.cfg)) break;
+        if (!cut.prefixes.empty() && row_piece == LORA_KV_MAX_TOKENS && tile_piece == LORA_KV_MAX_TOKENS) return false;
         row_piece = at_least((int64_t)row_piece * 2, 0);
         tile_piece = at_least((int64_t)tile_piece * 2, 0);
         tile_whole = std::max(tile_whole, tile_piece);
@@ -466,6 +605,7 @@ void cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     // (2048 tokens with 32 / 8 heads: 70 -> 55 us).
     const size_t round = ((size_t)kv.n_cu + n_kv - 1) / n_kv;
     if (cut.way != lora::KV_TILES_TURNS && cut.tiles.size() > round) std::reverse(cut.tiles.begin() + round, cut.tiles.begin() + std::min(cut.tiles.size(), 2 * round));
+    return true;
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -827,7 +967,7 @@ int lora_kv_stats(const lora_kv_t *kv, lora_kv_stats_t *out)
 
 // ---- batches --------------------------------------------------------------------------------
 
-int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, const int32_t *seg_offsets, void *stream, lora_kv_batch_t **out)
+static int create_batch(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, const int32_t *seg_offsets, void *stream, bool shared, lora_kv_batch_t **out)
 {
     if (!out) return LORA_E_INVAL;
     *out = nullptr;
@@ -872,10 +1012,16 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
             cut.page0[i] = page0;
             if (g.n_tokens[i]) page0 += (int32_t)(((int64_t)g.seqs[i]->n_tokens + g.n_tokens[i] + kv->cfg.page_tokens - 1) >> kv->page_shift);
         }
+        if (shared) find_prefixes(*kv, g, cut);
         // cut_attention sees the lengths after the growth; they are put back if it runs out of host memory
         for (int32_t i = 0; i < n_seg; ++i) g.seqs[i]->n_tokens += g.n_tokens[i];
         try {
-            cut_attention(*kv, g, seg_offsets, cut);
+            if (!cut_attention(*kv, g, seg_offsets, cut)) {
+                cut.prefixes.clear();
+                cut.own.clear();
+                cut.way = lora::KV_TILES_PLAIN;
+                (void)cut_attention(*kv, g, seg_offsets, cut);
+            }
         } catch (...) {
             for (int32_t i = 0; i < n_seg; ++i) g.seqs[i]->n_tokens -= g.n_tokens[i];
             throw;
@@ -896,6 +1042,10 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
         b->off_tiles = place(cut.tiles.size() * sizeof(AttnItem));
         b->off_joins = place(cut.joins.size() * sizeof(JoinItem));
         b->off_tile_joins = place(cut.tile_joins.size() * sizeof(JoinItem));
+        b->off_row_tokens = place(cut.row_tokens.size() * 4);
+        b->off_sources = place(cut.sources.size() * sizeof(SharedSource));
+        b->off_blocks = place(cut.blocks.size() * sizeof(SharedBlock));
+        b->off_shared_joins = place(cut.shared_joins.size() * sizeof(SharedJoin));
         KvToken *tokens = reinterpret_cast<KvToken *>(b->pinned + b->off_tokens);
         int32_t *pages = reinterpret_cast<int32_t *>(b->pinned + b->off_pages);
         b->max_pos = -1;
@@ -924,6 +1074,12 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
         std::copy(cut.tiles.begin(), cut.tiles.end(), reinterpret_cast<AttnItem *>(b->pinned + b->off_tiles));
         std::copy(cut.joins.begin(), cut.joins.end(), reinterpret_cast<JoinItem *>(b->pinned + b->off_joins));
         std::copy(cut.tile_joins.begin(), cut.tile_joins.end(), reinterpret_cast<JoinItem *>(b->pinned + b->off_tile_joins));
+        std::copy(cut.row_tokens.begin(), cut.row_tokens.end(), reinterpret_cast<int32_t *>(b->pinned + b->off_row_tokens));
+        std::copy(cut.sources.begin(), cut.sources.end(), reinterpret_cast<SharedSource *>(b->pinned + b->off_sources));
+        std::copy(cut.blocks.begin(), cut.blocks.end(), reinterpret_cast<SharedBlock *>(b->pinned + b->off_blocks));
+        std::copy(cut.shared_joins.begin(), cut.shared_joins.end(), reinterpret_cast<SharedJoin *>(b->pinned + b->off_shared_joins));
+        b->n_shared_joins = (int32_t)cut.shared_joins.size(), b->shared_rows = 0;
+        for (const SharedJoin &j : cut.shared_joins) b->shared_rows = std::max(b->shared_rows, j.n_rows);
         b->n_joins = (int32_t)cut.joins.size(), b->n_tile_joins = (int32_t)cut.tile_joins.size();
         b->join_rows = 0;
         for (const JoinItem &j : cut.joins) b->join_rows = std::max(b->join_rows, j.n_rows);
@@ -934,10 +1090,22 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
         std::lock_guard<std::mutex> lock(g_lock);
         b->info = {T, n_seg, (int32_t)n_pages, (int32_t)groups.size(), (int32_t)cut.rows.size(), (int32_t)cut.tiles.size(), (int32_t)(cut.joins.size() + cut.tile_joins.size()),
                    cut.n_short, (int32_t)cut.way};
+        b->prefixes = {(int32_t)cut.prefixes.size(), b->n_shared_joins, cut.prefix_row_items, cut.prefix_tile_items, 0};
+        for (const Prefix &p : cut.prefixes) b->prefixes.n_tokens += (int64_t)(p.to - p.from) << kv->page_shift;
         b->name = ++g_names << NAME_BITS | (uint64_t)(b - kv->batches.data());
         *out = reinterpret_cast<lora_kv_batch_t *>((uintptr_t)b->name);
         return LORA_OK;
     });
+}
+
+int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, const int32_t *seg_offsets, void *stream, lora_kv_batch_t **out)
+{
+    return create_batch(kv, n_seg, seg_seq, seg_offsets, stream, false, out);
+}
+
+int lora_kv_batch_create_shared(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, const int32_t *seg_offsets, void *stream, lora_kv_batch_t **out)
+{
+    return create_batch(kv, n_seg, seg_seq, seg_offsets, stream, true, out);
 }
 
 int lora_kv_batch_destroy(lora_kv_t *kv, lora_kv_batch_t *handle)
@@ -958,6 +1126,18 @@ int lora_kv_batch_info(const lora_kv_batch_t *handle, lora_kv_batch_info_t *out)
     for (lora_kv *kv = g_caches; kv; kv = kv->next)
         if (const Batch *const batch = find_batch(*kv, handle)) {
             *out = batch->info;
+            return LORA_OK;
+        }
+    return LORA_E_INVAL;
+}
+
+int lora_kv_batch_prefixes(const lora_kv_batch_t *handle, lora_kv_prefix_info_t *out)
+{
+    if (!handle || !out) return LORA_E_INVAL;
+    std::lock_guard<std::mutex> lock(g_lock);
+    for (lora_kv *kv = g_caches; kv; kv = kv->next)
+        if (const Batch *const batch = find_batch(*kv, handle)) {
+            *out = batch->prefixes;
             return LORA_OK;
         }
     return LORA_E_INVAL;
@@ -1031,6 +1211,7 @@ int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *handle, int32_t layer, const 
     a.pages = kv->pages + kv->layer_bytes * layer;
     a.page_stride = (int64_t)kv->page_bytes;
     a.page_list = reinterpret_cast<const int32_t *>(batch->dev + batch->off_pages);
+    a.row_tokens = reinterpret_cast<const int32_t *>(batch->dev + batch->off_row_tokens);
     a.part_o = kv->part_o, a.part_ml = kv->part_ml;
     a.scale_log2 = scale_log2;
     a.n_kv = c.n_kv_heads, a.group = kv->group(), a.page_shift = kv->page_shift;
@@ -1055,6 +1236,16 @@ int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *handle, int32_t layer, const 
         j.items = reinterpret_cast<const JoinItem *>(batch->dev + batch->off_tile_joins);
         j.n_items = batch->n_tile_joins, j.max_rows = way == lora::KV_TILES_TURNS ? lora::KV_TURNS_TILE : lora::KV_TILE;
         KV_TRY(lora::launch_attn_join(j, c.dtype, c.head_dim, true, st));
+    }
+    if (batch->n_shared_joins) {
+        lora::SharedJoinArgs h{};
+        h.out = out, h.out_stride = out_stride;
+        h.items = reinterpret_cast<const SharedJoin *>(batch->dev + batch->off_shared_joins);
+        h.sources = reinterpret_cast<const SharedSource *>(batch->dev + batch->off_sources);
+        h.blocks = reinterpret_cast<const SharedBlock *>(batch->dev + batch->off_blocks);
+        h.part_o = kv->part_o, h.part_ml = kv->part_ml;
+        h.n_items = batch->n_shared_joins, h.n_kv = c.n_kv_heads, h.group = kv->group(), h.max_rows = batch->shared_rows;
+        KV_TRY(lora::launch_shared_join(h, c.dtype, c.head_dim, st));
     }
     return LORA_OK;
 }

@@ -39,13 +39,27 @@ struct KvGroup {
 // One piece of the attention, for every key-value head: rows row0 .. row0 + n_rows - 1 of a segment over tokens kv0 .. kv1 - 1 of its
 // sequence.  Row r is query head kv_head * g + r % g of the segment's token r / g.
 struct AttnItem {
-    int32_t tok0;   // the segment's first token in the packed batch
-    int32_t ctx;    // its position
+    int32_t tok0;   // the segment's first token in the packed batch; of rows that share a prefix: where their tokens are listed
+    int32_t ctx;    // its position; KV_SHARED: the rows of several segments, which see all the tokens
     int32_t page0;  // the sequence's first entry of the page list
     int32_t row0, n_rows;
     int32_t kv0, kv1;
     int32_t part;   // -1: writes its rows of the output; else where its partial results go, in rows: head h, row r at part + h * n_rows + r (of a
                     // tile n_rows rounded up to 32)
+};
+
+constexpr int KV_SHARED = LORA_KV_MAX_TOKENS;  // (no segment's first token stands there)
+
+// Segments with shared prefixes: every part of what a row attends to -- prefixes, the segment's own tokens -- is a source of partial results, which lie in
+// blocks of rows: row r of the segment is row (row0 + r) % rows of block block0 + (row0 + r) / rows.
+struct SharedSource {
+    int32_t row0, block0, rows, tile;  // tile: laid out as a tile's
+};
+struct SharedBlock {
+    int32_t part, n_parts, stride, n_rows;
+};
+struct SharedJoin {
+    int32_t tok0, n_rows, source0, n_sources;
 };
 
 // Rows whose pieces are joined: n_parts pieces, `stride` rows of partial results apart.
@@ -106,7 +120,7 @@ struct AttnArgs {
     int64_t q_stride, out_stride;
     const char *pages;  // of this layer
     int64_t page_stride;
-    const int32_t *page_list;
+    const int32_t *page_list, *row_tokens;
     const AttnItem *tiles, *rows;
     float *part_o, *part_ml;
     float scale_log2;  // scale * log2(e)
@@ -121,6 +135,16 @@ struct JoinArgs {
     int32_t n_items, n_kv, group, max_rows;
 };
 
+struct SharedJoinArgs {
+    void *out;
+    int64_t out_stride;
+    const SharedJoin *items;
+    const SharedSource *sources;
+    const SharedBlock *blocks;
+    const float *part_o, *part_ml;
+    int32_t n_items, n_kv, group, max_rows;
+};
+
 hipError_t prepare_attn_kernels();  // once for the current device
 hipError_t launch_append(const AppendArgs &a, int dtype, hipStream_t st);
 hipError_t launch_append_heads(const AppendHeadsArgs &a, int dtype, bool e4m3, hipStream_t st);
@@ -129,5 +153,7 @@ hipError_t launch_moves(const KvMoves &m, int n, char *pages, int64_t page_strid
 hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, KvTiles way, int n_cu, hipStream_t st);
 hipError_t launch_attn_e4m3(const AttnArgs &a, int dim, KvTiles way, int n_cu, hipStream_t st);
 hipError_t launch_attn_join(const JoinArgs &a, int dtype, int dim, bool tiles, hipStream_t st);
+
+hipError_t launch_shared_join(const SharedJoinArgs &a, int dtype, int dim, hipStream_t st);
 
 }  // namespace lora

@@ -123,9 +123,10 @@ class KvCache:
         return st
 
     # -- batches --------------------------------------------------------------------------
-    def batch(self, seg_seq, seg_offsets, stream: Optional[torch.cuda.Stream] = None):
-        rc, b = B.lora_kv_batch_create(self.handle, seg_seq, seg_offsets, self._stream(stream))
-        B.check(rc, "lora_kv_batch_create")
+    def batch(self, seg_seq, seg_offsets, stream: Optional[torch.cuda.Stream] = None, shared: bool = False):
+        """shared: attention reads pages that sequences of the batch share once for all of them, where that is worth it"""
+        rc, b = (B.lora_kv_batch_create_shared if shared else B.lora_kv_batch_create)(self.handle, seg_seq, seg_offsets, self._stream(stream))
+        B.check(rc, "lora_kv_batch_create_shared" if shared else "lora_kv_batch_create")
         b.n_tokens = int(seg_offsets[-1])
         return b
 
