@@ -227,7 +227,7 @@ template <typename E> __device__ __forceinline__ uint4 first_values(const uint4 
     Vals<E> x = __builtin_bit_cast(Vals<E>, v);
 #pragma unroll
     for (int e = 0; e < CHUNK<E>; ++e)
-        if (e >= n) x.v[e] = (E)0.f;
+        if (e >= n) x.v[e] = E{};
     return __builtin_bit_cast(uint4, x);
 }
 
@@ -320,10 +320,84 @@ template <int D> struct RowsLds {
     int redo[ROW_WAVES];
 };
 
+// The end of a wavefront's share of an item: rows r = lane % 16, of whose outputs lane group g = lane / 16 holds values 16 j + 4 g + i in o[j][i]
+template <typename E, int D, bool ALONE, typename P>
+__device__ __forceinline__ void finish_rows(const AttnArgs &a, const AttnItem &it, int kv_head, RowsLds<D> &lds, float m, float l, const floatx4 (&o)[D / 16])
+{
+    constexpr int VJ = D / 16, NW = ROW_WAVES, DP = RowsLds<D>::DP;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int row = it.row0 + min(r, it.n_rows - 1);
+    l = sum16(sum32(l));
+    // Outputs that are no numbers or infinite are worked out again: a value behind a row's own position had weight 0, but 0 times infinity is no number; an infinite value that
+    // the row sees has met what its weight lost, which may be 0 or less; and weights that are up to 2^SLACK may have taken a sum out of range
+    float none = 0.f;
+#pragma unroll
+    for (int j = 0; j < VJ; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) none += o[j][i] * 0.f;
+    const bool redo = __any(none != 0.f);
+    const auto again = [&](int from, int step) {
+        for (int i = from; i < it.n_rows; i += step) {
+            RowState<E, D> st;
+            one_row<E, D, P>(a, it, kv_head, it.row0 + i, it.kv0, it.kv1, st);
+            put_row<E, D, false>(a, it, kv_head, i, st);
+        }
+    };
+    if constexpr (ALONE) {  // (items that one wavefront has to itself are whole)
+        if (redo) return again(0, 1);
+        if (r >= it.n_rows) return;
+        const float f = 1.f / l;
+        E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D;
+#pragma unroll
+        for (int j = 0; j < VJ; ++j) put_four(out + 16 * j + 4 * g, o[j] * f);
+        return;
+    }
+    if (g == 0) lds.m[wave][r] = m, lds.l[wave][r] = l;
+    if (lane == 0) lds.redo[wave] = redo;
+#pragma unroll
+    for (int pass = 0; pass < D / DP; ++pass) {
+        __syncthreads();
+        if (pass == 0) {
+            int any = 0;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) any |= lds.redo[w];
+            if (any) return again(wave, NW);
+        }
+#pragma unroll
+        for (int j = 0; j < DP / 16; ++j) *reinterpret_cast<floatx4 *>(&lds.o[wave][r][16 * j + 4 * g]) = o[pass * (DP / 16) + j];
+        __syncthreads();
+        for (int i = threadIdx.x; i < it.n_rows * (DP / 4); i += 64 * NW) {
+            const int rr = i / (DP / 4), d = i % (DP / 4) * 4;
+            float top = lds.m[0][rr];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) top = fmaxf(top, lds.m[w][rr]);
+            float sum = 0.f, f[NW];
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                f[w] = __builtin_amdgcn_exp2f(lds.m[w][rr] - top);
+                sum += lds.l[w][rr] * f[w];
+            }
+            const float each = it.part >= 0 && sum == 0.f ? 0.f : 1.f / sum;
+            floatx4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < NW; ++w) v += *reinterpret_cast<const floatx4 *>(&lds.o[w][rr][d]) * (f[w] * each);
+            if (it.part >= 0) {
+                const int64_t at = it.part + (int64_t)kv_head * it.n_rows + rr;
+                *reinterpret_cast<floatx4 *>(a.part_o + at * D + pass * DP + d) = v;
+                if (pass == 0 && d == 0) a.part_ml[2 * at] = top, a.part_ml[2 * at + 1] = sum;
+            } else {
+                const int rw = it.row0 + rr;
+                E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + rw / a.group) * a.out_stride + (kv_head * a.group + rw % a.group) * D + pass * DP + d;
+                put_four(out, v);
+            }
+        }
+    }
+}
+
 template <typename E, int D, bool ALONE>
 __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it, int kv_head, RowsLds<D> &lds)
 {
-    constexpr int U = CHUNK<E>, NT = U / 4, STEP = 16 * NT, KC = D / U / 4, VJ = D / 16, NW = ROW_WAVES, DP = RowsLds<D>::DP;
+    constexpr int U = CHUNK<E>, NT = U / 4, STEP = 16 * NT, KC = D / U / 4, VJ = D / 16, NW = ROW_WAVES;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int in_page = (1 << a.page_shift) - 1;
 
@@ -425,94 +499,168 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it,
             }
         }
     }
-    l = sum16(sum32(l));
-    // Outputs that are no numbers or infinite are worked out again: a value behind a row's own position had weight 0, but 0 times infinity is no number; an infinite value that
-    // the row sees has met what its weight lost, which may be 0 or less; and weights that are up to 2^SLACK may have taken a sum out of range
-    float none = 0.f;
+    finish_rows<E, D, ALONE, E>(a, it, kv_head, lds, m, l, o);
+}
+
+// Up to 16 rows over pages of 8-bit values.  As above with steps of 64 tokens: a 16-byte chunk is 16 values, and so two operands.  The keys' chunks are turned into
+// bf16 with their tokens' units at once, which is exact; a chunk of values is of 16 tokens, and the weights take their units.  The tokens of a step may lie in two
+// pages (of 32).
+template <int D, bool ALONE>
+__device__ __forceinline__ void attn_rows_e4m3(const AttnArgs &a, const AttnItem &it, int kv_head, RowsLds<D> &lds)
+{
+    constexpr int U = 16, NT = 4, STEP = 64, KC = D / 64, VJ = D / 16, NW = ROW_WAVES;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const bool two_pages = a.page_shift == 5;
+    const int in_page = (1 << a.page_shift) - 1;
+
+    const int row = it.row0 + min(r, it.n_rows - 1);
+    const int end = it.ctx + row / a.group + 1;  // tokens that this lane's row sees
+    uint4 q[2 * KC];
+    {
+        const __bf16 *p = static_cast<const __bf16 *>(a.q) + (int64_t)token_of(a, it, row / a.group) * a.q_stride + (kv_head * a.group + row % a.group) * D;
 #pragma unroll
-    for (int j = 0; j < VJ; ++j)
+        for (int c = 0; c < 2 * KC; ++c) q[c] = *reinterpret_cast<const uint4 *>(p + (4 * (c / 2) + g) * U + c % 2 * 8);
+    }
+
+    const int steps = (it.kv1 - it.kv0 + STEP - 1) / STEP, per_wave = (steps + NW - 1) / NW;
+    const int first = ALONE ? it.kv0 : it.kv0 + wave * per_wave * STEP, last = ALONE ? it.kv1 : min(it.kv1, first + per_wave * STEP);
+    PageList pages(a.page_list + it.page0, (it.kv1 - 1) >> a.page_shift, min(first, it.kv1 - 1) >> a.page_shift);
+
+    struct Step {
+        uint4 k[NT][KC], v[VJ], k_units, v_units;
+    };
+    const size_t half = (size_t)a.n_kv * D << a.page_shift, units = 2 * half;  // bytes of a half of a page's layer; where its exponents begin
+    const int k_lane = U * (r >> 2) + (r & 3);  // product t's row r is token k_lane + 4 t of the step
+    const auto load = [&](Step &s, int pos) {
+        const int page0 = pages[pos >> a.page_shift], page1 = two_pages ? pages[(pos + 32) >> a.page_shift] : page0, at = pos & in_page;
+        const char *const k_page = a.pages + (r < 8 ? page0 : page1) * a.page_stride, *const v_page = a.pages + (g < 2 ? page0 : page1) * a.page_stride;
+        const int k_at = (at + U * (r >> 2)) & in_page, v_at = (at + U * g) & in_page;
+        const char *const kp = k_page + ((size_t)kv_head * D << a.page_shift) + (k_at + (r & 3)) * U, *const vp = v_page + half + ((size_t)kv_head * D << a.page_shift) + (size_t)v_at * D;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) none += o[j][i] * 0.f;
-    const bool redo = __any(none != 0.f);
-    const auto again = [&](int from, int step) {
-        for (int i = from; i < it.n_rows; i += step) {
-            RowState<E, D> st;
-            one_row<E, D>(a, it, kv_head, it.row0 + i, it.kv0, it.kv1, st);
-            put_row<E, D, false>(a, it, kv_head, i, st);
+        for (int c = 0; c < KC; ++c)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) s.k[t][c] = load_once(kp + (((size_t)(4 * c + g) << a.page_shift) + 4 * t) * U);
+        s.k_units = *reinterpret_cast<const uint4 *>(k_page + units + ((size_t)kv_head << a.page_shift) + k_at);
+        s.v_units = *reinterpret_cast<const uint4 *>(v_page + units + ((size_t)(a.n_kv + kv_head) << a.page_shift) + v_at);
+#pragma unroll
+        for (int j = 0; j < VJ; ++j) s.v[j] = load_once(vp + (16 * j + r) * U);
+    };
+
+    float m = -FLT_MAX, l = 0.f;
+    floatx4 o[VJ];
+#pragma unroll
+    for (int j = 0; j < VJ; ++j) o[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+    const auto use = [&](Step &s, int pos) {
+        const uint32_t ku[4] = {s.k_units.x, s.k_units.y, s.k_units.z, s.k_units.w}, vu[4] = {s.v_units.x, s.v_units.y, s.v_units.z, s.v_units.w};
+        float p[U];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const float unit = unit_of(ku[t] >> 8 * (r & 3) & 255);
+            floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+                mma16<__bf16>(acc, eight_bf16(s.k[t][c].x, s.k[t][c].y, unit), q[2 * c]);
+                mma16<__bf16>(acc, eight_bf16(s.k[t][c].z, s.k[t][c].w, unit), q[2 * c + 1]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[4 * t + i] = pos + U * g + 4 * t + i < end ? acc[i] * a.scale_log2 : -INFINITY;
+        }
+        float top = p[0];
+#pragma unroll
+        for (int e = 1; e < U; ++e) top = fmaxf(top, p[e]);
+        top = max16(max32(top));
+        if (__any(top > m + SLACK)) {
+            const float now = fmaxf(m, top), fade = __builtin_amdgcn_exp2f(m - now);
+            m = now;
+            l *= fade;
+#pragma unroll
+            for (int j = 0; j < VJ; ++j) o[j] *= fade;
+        }
+        const int there = it.kv1 - pos - U * g;  // of the lane's tokens: behind the sequence's last one, whatever is there is no value, and no exponent
+#pragma unroll
+        for (int e = 0; e < U; ++e) {
+            p[e] = __builtin_amdgcn_exp2f(p[e] - m);
+            l += p[e];
+            p[e] *= unit_of(vu[e / 4] >> 8 * (e % 4) & 255);
+        }
+        if (pos + STEP > it.kv1) {
+#pragma unroll
+            for (int e = 0; e < U; ++e) p[e] = e < there ? p[e] : 0.f;
+#pragma unroll
+            for (int j = 0; j < VJ; ++j) s.v[j] = first_values<E4m3>(s.v[j], there);
+        }
+        // what the weights lose when they are rounded goes through a second product, as above
+        uint4 w[2], rest[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = p[8 * k + e];
+            w[k] = weights(x);
+            const Vals<__bf16> rounded = __builtin_bit_cast(Vals<__bf16>, w[k]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] -= (float)rounded.v[e];
+            rest[k] = weights(x);
+        }
+#pragma unroll
+        for (int j = 0; j < VJ; ++j) {
+            const uint4 lo = eight_bf16(s.v[j].x, s.v[j].y, 1.f), hi = eight_bf16(s.v[j].z, s.v[j].w, 1.f);
+            mma16<__bf16>(o[j], lo, w[0]);
+            mma16<__bf16>(o[j], hi, w[1]);
+            mma16<__bf16>(o[j], lo, rest[0]);
+            mma16<__bf16>(o[j], hi, rest[1]);
         }
     };
-    if constexpr (ALONE) {  // (items that one wavefront has to itself are whole)
-        if (redo) return again(0, 1);
-        if (r >= it.n_rows) return;
-        const float f = 1.f / l;
-        E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D;
-#pragma unroll
-        for (int j = 0; j < VJ; ++j) put_four(out + 16 * j + 4 * g, o[j] * f);
-        return;
-    }
-    if (g == 0) lds.m[wave][r] = m, lds.l[wave][r] = l;
-    if (lane == 0) lds.redo[wave] = redo;
-#pragma unroll
-    for (int pass = 0; pass < D / DP; ++pass) {
-        __syncthreads();
-        if (pass == 0) {
-            int any = 0;
-#pragma unroll
-            for (int w = 0; w < NW; ++w) any |= lds.redo[w];
-            if (any) return again(wave, NW);
-        }
-#pragma unroll
-        for (int j = 0; j < DP / 16; ++j) *reinterpret_cast<floatx4 *>(&lds.o[wave][r][16 * j + 4 * g]) = o[pass * (DP / 16) + j];
-        __syncthreads();
-        for (int i = threadIdx.x; i < it.n_rows * (DP / 4); i += 64 * NW) {
-            const int rr = i / (DP / 4), d = i % (DP / 4) * 4;
-            float top = lds.m[0][rr];
-#pragma unroll
-            for (int w = 1; w < NW; ++w) top = fmaxf(top, lds.m[w][rr]);
-            float sum = 0.f, f[NW];
-#pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                f[w] = __builtin_amdgcn_exp2f(lds.m[w][rr] - top);
-                sum += lds.l[w][rr] * f[w];
+
+    if (first < last) {
+        if constexpr (ROWS_AHEAD<__bf16, D>) {
+            Step s0, s1;
+            load(s0, first);
+            for (int pos = first;; pos += 2 * STEP) {
+                if (pos + STEP < last) load(s1, pos + STEP);
+                use(s0, pos);
+                if (pos + STEP >= last) break;
+                if (pos + 2 * STEP < last) load(s0, pos + 2 * STEP);
+                use(s1, pos + STEP);
+                if (pos + 2 * STEP >= last) break;
             }
-            const float each = it.part >= 0 && sum == 0.f ? 0.f : 1.f / sum;
-            floatx4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int w = 0; w < NW; ++w) v += *reinterpret_cast<const floatx4 *>(&lds.o[w][rr][d]) * (f[w] * each);
-            if (it.part >= 0) {
-                const int64_t at = it.part + (int64_t)kv_head * it.n_rows + rr;
-                *reinterpret_cast<floatx4 *>(a.part_o + at * D + pass * DP + d) = v;
-                if (pass == 0 && d == 0) a.part_ml[2 * at] = top, a.part_ml[2 * at + 1] = sum;
-            } else {
-                const int rw = it.row0 + rr;
-                E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + rw / a.group) * a.out_stride + (kv_head * a.group + rw % a.group) * D + pass * DP + d;
-                put_four(out, v);
+        } else {
+            Step s;
+            for (int pos = first; pos < last; pos += STEP) {
+                load(s, pos);
+                use(s, pos);
             }
         }
     }
+    finish_rows<__bf16, D, ALONE, E4m3>(a, it, kv_head, lds, m, l, o);
 }
 
 // Block b of the row items: the first n_rows of the list have a block for each key-value head; the others, n_short of them, are short and a wavefront does one
-template <typename E, int D>
+template <typename E, int D, typename P = E>
 __device__ __forceinline__ void attn_rows_block(const AttnArgs &a, uint32_t b, RowsLds<D> &lds)
 {
+    const auto work = [&](const AttnItem &it, int kv_head, auto alone) {
+        if constexpr (std::is_same_v<P, E4m3>) attn_rows_e4m3<D, decltype(alone)::value>(a, it, kv_head, lds);
+        else attn_rows<E, D, decltype(alone)::value>(a, it, kv_head, lds);
+    };
     const uint32_t blocks = (uint32_t)a.n_rows * a.n_kv;
     if (b < blocks) {
         const AttnItem it = a.rows[b / a.n_kv];
-        attn_rows<E, D, false>(a, it, b % a.n_kv, lds);
+        work(it, b % a.n_kv, std::false_type{});
     } else {
         const uint32_t n = (b - blocks) * ROW_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         if (n >= (uint32_t)a.n_short * a.n_kv) return;
         const AttnItem it = a.rows[a.n_rows + n / a.n_kv];
-        attn_rows<E, D, true>(a, it, n % a.n_kv, lds);
+        work(it, n % a.n_kv, std::true_type{});
     }
 }
 
-template <typename E, int D>
+template <typename E, int D, typename P = E>
 __global__ __launch_bounds__(64 * ROW_WAVES, 2) void attn_rows_kernel(AttnArgs a)
 {
     __shared__ RowsLds<D> lds;
-    attn_rows_block<E, D>(a, blockIdx.x, lds);
+    attn_rows_block<E, D, P>(a, blockIdx.x, lds);
 }
 
 // Tiles of rows of one key-value head (its query heads token by token): wavefronts of 32 rows share the keys and values, which go through
