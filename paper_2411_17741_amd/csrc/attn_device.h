@@ -744,6 +744,98 @@ template <typename E, int D, int STRIDE> struct Steps {
     }
 };
 
+// The same for pages of 8-bit values, whose way to LDS leads through registers, where they become bf16 with their tokens' units: what a call brings to LDS was asked for by the one
+// before it.  Keys: a thread has a chunk of 16 values of a token.  Values: 16 tokens of one value, the same tokens for all of a wavefront, whose units are scalars.
+// (Heads of 64 have chunks for half the threads each: two wavefronts bring keys, two values.)
+template <int D, int STRIDE> struct StepsE4m3 {
+    static constexpr int N = D < 128 ? 1 : D / 128;
+    PageList pages;
+    const char *head, *units;  // the head's keys in page 0; the exponents of its keys
+    uint32_t page_stride, k_lane, v_lane, v_units_at;
+    int page_shift, loader, row, values_at, units_at, t0, k_page, k_at;
+    uint4 k[N], v[N], v_units[N == 2 ? 2 : 1];
+    uint32_t k_unit;
+    __device__ __forceinline__ StepsE4m3(const AttnArgs &a, const AttnItem &it, int kv_head, int which_loader, int first)
+        : pages(a.page_list + it.page0, (it.kv1 - 1) >> a.page_shift, it.kv0 >> a.page_shift), page_stride((uint32_t)a.page_stride), page_shift(a.page_shift), loader(which_loader),
+          values_at((a.n_kv * D) << a.page_shift), units_at(a.n_kv << a.page_shift), t0(first)
+    {
+        const int lane = threadIdx.x & 63;
+        row = lane & 31;
+        head = a.pages + ((size_t)kv_head * D << a.page_shift);
+        units = a.pages + (((size_t)2 * a.n_kv * D + kv_head) << a.page_shift);
+        const int tok = key_of_row<__bf16>(row), w = D < 128 ? loader & 1 : loader;
+        k_lane = (((2 * w + lane / 32) << a.page_shift) + tok) * 16;
+        v_lane = (D == 128 ? (w >> 1) * D + (w & 1) * 64 + lane : w * 64 + lane) * 16;
+        v_units_at = D == 128 ? (w >> 1) * 16 : D < 128 ? w * 16 : 0;
+        ask_keys();
+        ask_values();
+    }
+    __device__ __forceinline__ bool has_keys() const { return D >= 128 || loader < 2; }
+    __device__ __forceinline__ bool has_values() const { return D >= 128 || loader >= 2; }
+    __device__ __forceinline__ void ask_keys()
+    {
+        k_page = pages[t0 >> page_shift];
+        k_at = t0 & ((1 << page_shift) - 1);
+        t0 += STRIDE;
+        if (!has_keys()) return;
+        const char *const from = head + (uint64_t)page_stride * (uint32_t)k_page + k_at * 16 + k_lane;
+#pragma unroll
+        for (int i = 0; i < N; ++i) k[i] = *reinterpret_cast<const uint4 *>(from + ((8 * i) << page_shift) * 16);
+        k_unit = *reinterpret_cast<const uint8_t *>(units + (uint64_t)page_stride * (uint32_t)k_page + k_at + key_of_row<__bf16>(row));
+    }
+    __device__ __forceinline__ void ask_values()  // of the stage whose keys were asked for last
+    {
+        if (!has_values()) return;
+        const uint64_t page = (uint64_t)page_stride * (uint32_t)k_page;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = *reinterpret_cast<const uint4 *>(head + values_at + page + k_at * D + v_lane + i * D * 16);
+            v_units[i] = *reinterpret_cast<const uint4 *>(units + units_at + page + k_at + v_units_at + i * 16);
+        }
+    }
+    __device__ __forceinline__ void put_keys(unsigned char *to)
+    {
+        const float unit = unit_of(k_unit);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            unsigned char *const at = to + ((2 * (2 * (D < 128 ? loader & 1 : loader) + (int)(threadIdx.x & 63) / 32 + 8 * i)) * 32 + row) * 16;
+            *reinterpret_cast<uint4 *>(at) = eight_bf16(k[i].x, k[i].y, unit);
+            *reinterpret_cast<uint4 *>(at + 512) = eight_bf16(k[i].z, k[i].w, unit);
+        }
+    }
+    __device__ __forceinline__ void put_values(unsigned char *to)
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int s = D == 128 ? loader >> 1 : D < 128 ? loader & 1 : i, d = D == 128 ? (loader & 1) * 64 + lane : D < 128 ? lane : loader * 64 + lane;
+            const uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w}, u[4] = {v_units[i].x, v_units[i].y, v_units[i].z, v_units[i].w};
+            bf16x8 y[2];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t us = __builtin_amdgcn_readfirstlane(u[w]);
+                const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(x[w], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(x[w], true);
+                y[w / 2][w % 2 * 4] = (__bf16)(lo[0] * unit_of(us & 255));
+                y[w / 2][w % 2 * 4 + 1] = (__bf16)(lo[1] * unit_of(us >> 8 & 255));
+                y[w / 2][w % 2 * 4 + 2] = (__bf16)(hi[0] * unit_of(us >> 16 & 255));
+                y[w / 2][w % 2 * 4 + 3] = (__bf16)(hi[1] * unit_of(us >> 24));
+            }
+            *reinterpret_cast<bf16x8 *>(to + (2 * s * D + d) * 16) = y[0];
+            *reinterpret_cast<bf16x8 *>(to + ((2 * s + 1) * D + d) * 16) = y[1];
+        }
+    }
+    __device__ __forceinline__ void keys(unsigned char *to)  // of the next stage
+    {
+        if (has_keys()) put_keys(to);
+        ask_keys();
+    }
+    __device__ __forceinline__ void values(unsigned char *to)  // of the stage before the one whose keys were asked for last
+    {
+        if (has_values()) put_values(to);
+        ask_values();
+    }
+};
+
 // 32 rows of a wavefront: lane r + 32 h has row r's queries (chunks 2 c + h), its maximum, half of its weights and outputs.  s: scores of
 // the stage; w: its weights; o[j][4 k + i]: value 32 j + 8 k + 4 h + i
 template <typename E, int D, int TK> struct TileRows {
@@ -815,7 +907,7 @@ template <typename E, int D, int TK> struct TileRows {
 };
 
 // The end of a wavefront's 32 rows
-template <typename E, int D, int TK>
+template <typename E, int D, int TK, typename P = E>
 __device__ __forceinline__ void finish_tile(const AttnArgs &a, const AttnItem &it, int kv_head, int part, const TileRows<E, D, TK> &t)
 {
     constexpr int DJ = D / 32;
@@ -830,7 +922,7 @@ __device__ __forceinline__ void finish_tile(const AttnArgs &a, const AttnItem &i
     if (__any(none != 0.f)) {
         for (int i = part * 32; i < min(it.n_rows, part * 32 + 32); ++i) {
             RowState<E, D> st;
-            one_row<E, D>(a, it, kv_head, it.row0 + i, it.kv0, it.kv1, st);
+            one_row<E, D, P>(a, it, kv_head, it.row0 + i, it.kv0, it.kv1, st);
             put_row<E, D, true>(a, it, kv_head, i, st);
         }
         return;
@@ -877,23 +969,28 @@ __device__ __forceinline__ void finish_tile(const AttnArgs &a, const AttnItem &i
 // A step of a wavefront alone on its SIMD takes 0.50 us with heads of 128, 0.9 with 256, 0.45 with 64, where its products are 0.27, 0.53 and 0.13: the rest are its other instructions,
 // one after the other, and the barrier.  5000 tokens with 32 / 8 heads of 256: 444 us, 0.92 PFLOP/s (585 with products and exponentials in turns); 8000 with 32 / 8 heads of 64: 305 us, 0.86.
 // fp32, 4096 tokens: 32 / 8 heads of 128 1117 us, 123 TFLOP/s, of 64 539 us, 128; 16 / 4 of 256 1438 us, 96.
-template <typename E, int D> struct TileShape {
+template <typename E, int D, typename P = E> struct TileShape {
     static constexpr int TK = 32, PLACE = TK * D * (int)sizeof(E);
     static constexpr int BLOCKS = PLACE <= 8192 ? 2 : 1;  // on a compute unit
-    static constexpr int DEEP = PLACE <= 16384 ? 3 : 1;
+    static constexpr int DEEP = PLACE <= 16384 && std::is_same_v<P, E> ? 3 : 1;  // (what goes through registers has been asked for a step before that)
     static constexpr int LDS = (2 * DEEP + 3) * PLACE;
 };
 
-template <typename E, int D, int GROUPS>
+template <typename E, int D, int GROUPS, typename P = E>
 __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it, int kv_head, unsigned char *all_lds)
 {
-    typedef TileShape<E, D> Shape;
+    typedef TileShape<E, D, P> Shape;
+    constexpr bool AS_IS = std::is_same_v<P, E>;  // pages hold what the products take
     constexpr int TK = Shape::TK, PLACE = Shape::PLACE, DEEP = Shape::DEEP, K_END = (DEEP + 1) * PLACE, V_END = (DEEP + 2) * PLACE;
     constexpr int U = CHUNK<E>;
     typedef TileRows<E, D, TK> Rows;
     constexpr int QC = Rows::QC, DJ = Rows::DJ, PK = Rows::PK, NV = PK * DJ, AHEAD = NV < 8 ? NV : 8, STRIDE = GROUPS * TK;
-    typedef Steps<E, D, STRIDE> Requests;
-    constexpr int PER = Requests::PER;
+    typedef std::conditional_t<AS_IS, Steps<E, D, STRIDE>, StepsE4m3<D, STRIDE>> Requests;
+    // up to `steps` steps' requests are still on their way
+    const auto wait = [](auto steps) {
+        if constexpr (AS_IS) wait_requests<decltype(steps)::value * 2 * Steps<E, D, STRIDE>::PER>();
+        else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    };
     static_assert(NV % AHEAD == 0 && QC % AHEAD == 0, "the operands' ring");
     const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = id & 3, group = id >> 2, r = lane & 31, h = lane >> 5;
     unsigned char *const lds = all_lds + group * Shape::LDS;
@@ -917,7 +1014,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it,
         __builtin_amdgcn_sched_barrier(0);
     };
     const auto next = [&] {  // a step begins: its operands have come, and nobody reads any more what its requests will overwrite
-        wait_requests<(DEEP - 1) * 2 * PER>();
+        wait(std::integral_constant<int, DEEP - 1>{});
         meet();
         v_last = v;
         v = after(v, V_END);
@@ -1012,7 +1109,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it,
         t0 += STRIDE;
     };
     t.wait_for_queries();
-    wait_requests<DEEP * 2 * PER>();
+    wait(std::integral_constant<int, DEEP>{});
     meet();
     if (mine) {
         floatx16 s0, s1;
@@ -1057,7 +1154,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it,
         next();
         request();
     }
-    wait_requests<0>();  // none is on its way to LDS when the block ends
+    wait(std::integral_constant<int, 0>{});  // none is on its way to LDS when the block ends
     if constexpr (GROUPS == 2) {  // the second group's maxima, sums and outputs go to the first through LDS
         meet();
         floatx4 *const other = reinterpret_cast<floatx4 *>(all_lds) + wave * DJ * 4 * 64 + lane;
@@ -1084,7 +1181,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it,
                 for (int e = 0; e < 4; ++e) t.o[j][4 * i + e] = t.o[j][4 * i + e] * f0 + x[e] * f1;
             }
     }
-    if (wave * 32 < it.n_rows) finish_tile<E, D, TK>(a, it, kv_head, wave, t);
+    if (wave * 32 < it.n_rows) finish_tile<E, D, TK, P>(a, it, kv_head, wave, t);
 }
 
 // Without the steps' overlap, whose registers would leave room for two blocks on a compute unit, for three: their wavefronts' products and exponentials fall beside each other's, and
@@ -1163,12 +1260,12 @@ __device__ __forceinline__ void attn_tile_plain(const AttnArgs &a, const AttnIte
     if (wave * 32 < it.n_rows) finish_tile<E, D, TK>(a, it, kv_head, wave, t);
 }
 
-template <typename E, int D>
+template <typename E, int D, typename P = E>
 __global__ __launch_bounds__(256, (TileShape<E, D>::BLOCKS)) void attn_tiles_kernel(AttnArgs a)
 {
     extern __shared__ __align__(16) unsigned char lds[];
     const AttnItem it = a.tiles[blockIdx.x / a.n_kv];
-    attn_tile<E, D, 1>(a, it, blockIdx.x % a.n_kv, lds);
+    attn_tile<E, D, 1, P>(a, it, blockIdx.x % a.n_kv, lds);
 }
 
 template <typename E, int D> constexpr int MANY_LDS = 4 * 32 * D * (int)sizeof(E);
@@ -1186,17 +1283,17 @@ __global__ __launch_bounds__(256, 3) void attn_many_kernel(AttnArgs a)
 // time: 20 of 3000 beside 900 + 700 72.0 -> 74.2, 20 of 8000 135.1 -> 145.7; 30 of 2000 beside 700 with 40 heads 203 -> 219.  Of larger batches nothing is gained, or lost where rows have
 // fewer blocks on a compute unit this way (heads of 256, 100 tokens of 500 beside 600: 109 -> 122).
 constexpr int BOTH_ROUNDS = 4;
-template <typename E, int D>
+template <typename E, int D, typename P = E>
 __global__ __launch_bounds__(256, (TileShape<E, D>::BLOCKS)) void attn_both_kernel(AttnArgs a)
 {
     extern __shared__ __align__(16) unsigned char lds[];
-    static_assert(TileShape<E, D>::LDS >= (int)sizeof(RowsLds<D>), "the rows' LDS is the tiles'");
+    static_assert(TileShape<E, D, P>::LDS >= (int)sizeof(RowsLds<D>), "the rows' LDS is the tiles'");
     const uint32_t tiles = (uint32_t)a.n_tiles * a.n_kv;
     if (blockIdx.x < tiles) {
         const AttnItem it = a.tiles[blockIdx.x / a.n_kv];
-        attn_tile<E, D, 1>(a, it, blockIdx.x % a.n_kv, lds);
+        attn_tile<E, D, 1, P>(a, it, blockIdx.x % a.n_kv, lds);
     } else {
-        attn_rows_block<E, D>(a, blockIdx.x - tiles, *reinterpret_cast<RowsLds<D> *>(lds));
+        attn_rows_block<E, D, P>(a, blockIdx.x - tiles, *reinterpret_cast<RowsLds<D> *>(lds));
     }
 }
 

@@ -1,33 +1,50 @@
-// Attention over pages of 8-bit values (gfx950).
+// Attention over the paged key-value cache (gfx950): the kernels of attn_device.h for pages of 8-bit values, and their launchers.
 #include "attn_device.h"
 
 namespace lora {
 
-// A wavefront to a row
-template <int D, bool TILE>
-__global__ __launch_bounds__(256) void attn_each_kernel(AttnArgs a, const AttnItem *items)
+namespace {
+
+template <typename F>
+hipError_t by_dim(int dim, F f)
 {
-    const AttnItem it = items[blockIdx.x / a.n_kv];
-    for (int r = threadIdx.x >> 6; r < it.n_rows; r += 4) {
-        RowState<__bf16, D> st;
-        one_row<__bf16, D, E4m3>(a, it, blockIdx.x % a.n_kv, it.row0 + r, it.kv0, it.kv1, st);
-        put_row<__bf16, D, TILE>(a, it, blockIdx.x % a.n_kv, r, st);
-    }
+    if (dim == 64) f(std::integral_constant<int, 64>{});
+    else if (dim == 128) f(std::integral_constant<int, 128>{});
+    else f(std::integral_constant<int, 256>{});
+    return hipGetLastError();
 }
 
-hipError_t launch_attn_e4m3(const AttnArgs &a, int dim, KvTiles, int, hipStream_t st)
+}  // namespace
+
+hipError_t prepare_attn_e4m3_kernels()
+{
+    hipError_t e = hipSuccess;
+    const auto allow = [&](const void *kernel, int lds) {
+        if (e == hipSuccess) e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    };
+    for (int dim : {64, 128, 256})
+        (void)by_dim(dim, [&](auto d) {
+            constexpr int D = decltype(d)::value, LDS = TileShape<__bf16, D, E4m3>::LDS;
+            allow(reinterpret_cast<const void *>(&attn_tiles_kernel<__bf16, D, E4m3>), LDS);
+            allow(reinterpret_cast<const void *>(&attn_both_kernel<__bf16, D, E4m3>), LDS);
+        });
+    return e;
+}
+
+hipError_t launch_attn_e4m3(const AttnArgs &a, int dim, KvTiles way, int n_cu, hipStream_t st)
 {
     const int64_t n_tiles = (int64_t)a.n_tiles * a.n_kv, n_rows = (int64_t)a.n_rows * a.n_kv + ((int64_t)a.n_short * a.n_kv + ROW_WAVES - 1) / ROW_WAVES;
     if (n_tiles > INT32_MAX || n_rows > INT32_MAX) return hipErrorInvalidValue;
-    const auto launch = [&](auto d) {
-        constexpr int D = decltype(d)::value;
-        if (n_tiles) hipLaunchKernelGGL((attn_each_kernel<D, true>), dim3((unsigned)n_tiles), dim3(256), 0, st, a, a.tiles);
-        if (n_rows) hipLaunchKernelGGL((attn_rows_kernel<__bf16, D, E4m3>), dim3((unsigned)n_rows), dim3(64 * ROW_WAVES), 0, st, a);
-    };
-    if (dim == 64) launch(std::integral_constant<int, 64>{});
-    else if (dim == 128) launch(std::integral_constant<int, 128>{});
-    else launch(std::integral_constant<int, 256>{});
-    return hipGetLastError();
+    const dim3 tiles((unsigned)n_tiles), rows((unsigned)n_rows);
+    return by_dim(dim, [&](auto d) {
+        constexpr int D = decltype(d)::value, LDS = TileShape<__bf16, D, E4m3>::LDS;
+        if (n_tiles && n_rows && way == KV_TILES_PLAIN && n_tiles + n_rows <= BOTH_ROUNDS * TileShape<__bf16, D>::BLOCKS * n_cu) {
+            hipLaunchKernelGGL((attn_both_kernel<__bf16, D, E4m3>), dim3((unsigned)(n_tiles + n_rows)), dim3(256), LDS, st, a);
+            return;
+        }
+        if (n_tiles) hipLaunchKernelGGL((attn_tiles_kernel<__bf16, D, E4m3>), tiles, dim3(256), LDS, st, a);
+        if (n_rows) hipLaunchKernelGGL((attn_rows_kernel<__bf16, D, E4m3>), rows, dim3(64 * ROW_WAVES), 0, st, a);
+    });
 }
 
 }  // namespace lora

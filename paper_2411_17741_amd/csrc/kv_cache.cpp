@@ -423,12 +423,13 @@ void find_prefixes(const lora_kv &kv, const Growth &g, Cut &cut)
                 part.at = (int32_t)(std::mismatch(p + set.at, p + part.at, g.seqs[i]->pages.data() + set.at).first - p);
                 tokens += g.n_tokens[i];
             }
-            if (((int64_t)(part.at - part.base) << kv.page_shift) >= SHARED_MIN_TOKENS) {
+            const int32_t to = part.at & ~(std::max(PIECE_STEP >> kv.page_shift, 1) - 1);  // (what is behind a prefix begins where pieces may)
+            if (((int64_t)(to - part.base) << kv.page_shift) >= SHARED_MIN_TOKENS) {
                 if (tokens > room) continue;
                 room -= tokens;
-                cut.prefixes.push_back({part.base, part.at, part.segs, tokens * grp});
-                for (const int32_t i : part.segs) cut.own[i] = part.at;
-                part.base = part.at;
+                cut.prefixes.push_back({part.base, to, part.segs, tokens * grp});
+                for (const int32_t i : part.segs) cut.own[i] = to;
+                part.base = to;
                 ++part.depth;
             }
             sets.push_back(std::move(part));
@@ -466,7 +467,7 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     // Two groups of wavefronts in turns, 256 rows at a time, where every compute unit gets two such blocks at least and they are long (1024 tokens in the
     // mean).  Measured, tiles of 128 rows -> turns: 16384 tokens with 64 / 8 heads 3985 -> 3650 us, 8192 with 32 / 8 537 -> 499, 4096 150 -> 136, 2048 + 2048 81.3 -> 76.9, 4096 with 32 / 32
     // heads 152 -> 143.  The rule does not ask for a gain where it takes few rounds of blocks: 2048 + 2048 with 32 / 32 heads 85.1 -> 85.5, 3 x 1500 behind 600 with 40 / 40 155.5 -> 160.
-    if (lora::kv_turns(kv.cfg.dtype, kv.cfg.head_dim)) {
+    if (!kv.e4m3() && lora::kv_turns(kv.cfg.dtype, kv.cfg.head_dim)) {
         int64_t tokens = 0;
         for (size_t i = 0; i < g.seqs.size(); ++i) {
             const int64_t n = g.n_tokens[i], rows = n * grp, ctx = g.seqs[i]->n_tokens - n;
@@ -508,7 +509,7 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     // No more blocks than compute units and no tile of over 1024 tokens: for heads of 64, whose steps are mostly instructions of one wavefront after the other, two groups of
     // wavefronts share a tile's tokens, and tiles stay whole (700 tokens with 32 heads 16.5 -> 12.5 us, with 32 / 8 heads 15.3 -> 12.3).  Longer ones, and heads of 128, do as well
     // or better with pieces.
-    if (cut.way == lora::KV_TILES_PLAIN && cut.prefixes.empty() && lora::kv_pairs(kv.cfg.dtype, kv.cfg.head_dim) && n_tiles && n_tiles * n_kv <= kv.n_cu && longest <= 2 * tile_min) {
+    if (cut.way == lora::KV_TILES_PLAIN && cut.prefixes.empty() && !kv.e4m3() && lora::kv_pairs(kv.cfg.dtype, kv.cfg.head_dim) && n_tiles && n_tiles * n_kv <= kv.n_cu && longest <= 2 * tile_min) {
         cut.way = lora::KV_TILES_PAIRS;
         tile_whole = 2 * tile_min;
     }
@@ -586,7 +587,7 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     }
     // Three blocks on a compute unit, where the tiles fill more than three for each, or more than two and are short (256 tokens in the mean): bf16 heads of 128, two blocks -> three,
     // 8 x 500 tokens with 32 heads 42.6 -> 39.2 us, 6 x 300 24.4 -> 17.3; but 2048 with 40 heads 68.2 -> 74.5.
-    if (cut.way == lora::KV_TILES_PLAIN && lora::kv_many(kv.cfg.dtype, kv.cfg.head_dim)) {
+    if (cut.way == lora::KV_TILES_PLAIN && !kv.e4m3() && lora::kv_many(kv.cfg.dtype, kv.cfg.head_dim)) {
         int64_t blocks = (int64_t)cut.tiles.size() * n_kv, tokens = 0;
         for (const AttnItem &t : cut.tiles) tokens += t.kv1 - t.kv0;
         if (blocks > 3 * kv.n_cu || (blocks > 2 * kv.n_cu && tokens < 256 * (int64_t)cut.tiles.size())) cut.way = lora::KV_TILES_MANY;
@@ -669,6 +670,7 @@ int lora_kv_create(const lora_kv_config_t *cfg, void *dev_pages, size_t pages_by
         for (auto &b : kv->batches) b.member.assign(cfg->max_seqs, 0);
         if (!host_only) {
             KV_TRY(lora::prepare_attn_kernels());
+            KV_TRY(lora::prepare_attn_e4m3_kernels());
             int n = 0;
             KV_TRY(hipGetDevice(&kv->device));
             KV_TRY(hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, kv->device));

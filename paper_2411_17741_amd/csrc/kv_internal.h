@@ -146,6 +146,7 @@ struct SharedJoinArgs {
 };
 
 hipError_t prepare_attn_kernels();  // once for the current device
+hipError_t prepare_attn_e4m3_kernels();
 hipError_t launch_append(const AppendArgs &a, int dtype, hipStream_t st);
 hipError_t launch_append_heads(const AppendHeadsArgs &a, int dtype, bool e4m3, hipStream_t st);
 hipError_t launch_read(const ReadArgs &a, int dtype, bool e4m3, hipStream_t st);

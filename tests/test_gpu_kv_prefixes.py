@@ -358,6 +358,7 @@ def test_what_is_shared():
     assert info(forks(2, 640, lambda i: 1, lambda i: 64)) == (0, 0, 0)  # tiles of their own
     assert info(forks(2, 640, lambda i: 1, lambda i: 63)) == (1, 2, 640)
     assert info(forks(5, 640, lambda i: 1), shared=False) == (0, 0, 0)
+    assert info(forks(2, 352, lambda i: 5), page=32) == (1, 2, 320)   # 11 pages of 32: pieces begin at multiples of 64
     assert info([(None, -1, 640, 1), (0, -1, 0, 1)]) == (1, 2, 640)   # a parent in the batch
     assert info([(None, -1, 700, 1), (None, -1, 700, 1)]) == (0, 0, 0)
     assert info([(None, -1, 320, 0), (0, -1, 320, 0)] + [(1, -1, i, 1) for i in range(3)] + [(0, -1, i, 1) for i in range(3)]) == (2, 6, 640)
