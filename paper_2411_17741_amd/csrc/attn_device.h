@@ -744,94 +744,103 @@ template <typename E, int D, int STRIDE> struct Steps {
     }
 };
 
-// The same for pages of 8-bit values, whose way to LDS leads through registers, where they become bf16 with their tokens' units: what a call brings to LDS was asked for by the one
-// before it.  Keys: a thread has a chunk of 16 values of a token.  Values: 16 tokens of one value, the same tokens for all of a wavefront, whose units are scalars.
-// (Heads of 64 have chunks for half the threads each: two wavefronts bring keys, two values.)
-template <int D, int STRIDE> struct StepsE4m3 {
-    static constexpr int N = D < 128 ? 1 : D / 128;
+// The same for pages of 8-bit values, for stages of TK tokens, STRIDE apart, by 4 wavefronts.  Their way to LDS leads through registers, where they become bf16 with their tokens' units:
+// what comes to LDS was asked for a step before.  A thread has N chunks of keys, 16 values of a token each, and N chunks of values, 16 tokens of one value; the tokens of the
+// latter are the same for all of a wavefront, their units scalars.  (Heads of 64 have chunks for half the threads: two wavefronts bring keys, two values.)  The work
+// is done in pieces that fall beside the products of the step.
+template <int D, int TK, int STRIDE> struct StagesE4m3 {
+    static constexpr int ALL = D * TK / 16, N = ALL < 256 ? 1 : ALL / 256, PIECES = 6 * N;
+    static constexpr bool HALVES = ALL < 256;
     PageList pages;
-    const char *head, *units;  // the head's keys in page 0; the exponents of its keys
-    uint32_t page_stride, k_lane, v_lane, v_units_at;
-    int page_shift, loader, row, values_at, units_at, t0, k_page, k_at;
-    uint4 k[N], v[N], v_units[N == 2 ? 2 : 1];
+    const char *keys_at, *values_at;  // the head's in page 0, and the thread's first chunk of them
+    const char *k_units_at, *v_units_at;
+    uint32_t page_stride;
+    int page_shift, loader, w, row, tok, t0, page[2], at;
+    uint4 k[N], v[N], units[N], out;
     uint32_t k_unit;
-    __device__ __forceinline__ StepsE4m3(const AttnArgs &a, const AttnItem &it, int kv_head, int which_loader, int first)
+    __device__ __forceinline__ StagesE4m3(const AttnArgs &a, const AttnItem &it, int kv_head, int which_loader, int first)
         : pages(a.page_list + it.page0, (it.kv1 - 1) >> a.page_shift, it.kv0 >> a.page_shift), page_stride((uint32_t)a.page_stride), page_shift(a.page_shift), loader(which_loader),
-          values_at((a.n_kv * D) << a.page_shift), units_at(a.n_kv << a.page_shift), t0(first)
+          w(HALVES ? which_loader & 1 : which_loader), t0(first), at(0)
     {
         const int lane = threadIdx.x & 63;
-        row = lane & 31;
-        head = a.pages + ((size_t)kv_head * D << a.page_shift);
-        units = a.pages + (((size_t)2 * a.n_kv * D + kv_head) << a.page_shift);
-        const int tok = key_of_row<__bf16>(row), w = D < 128 ? loader & 1 : loader;
-        k_lane = (((2 * w + lane / 32) << a.page_shift) + tok) * 16;
-        v_lane = (D == 128 ? (w >> 1) * D + (w & 1) * 64 + lane : w * 64 + lane) * 16;
-        v_units_at = D == 128 ? (w >> 1) * 16 : D < 128 ? w * 16 : 0;
+        row = lane % TK;
+        tok = (row & 32) | key_of_row<__bf16>(row & 31);
+        if (a.page_shift == 5) tok &= 31;
+        const size_t head = (size_t)kv_head * D << a.page_shift, half = (size_t)a.n_kv * D << a.page_shift;
+        keys_at = a.pages + head + (size_t)((((w * 64 + lane) / TK) << a.page_shift) + tok) * 16;
+        values_at = a.pages + half + head + (w * 64 + lane) % D * 16;
+        k_units_at = a.pages + 2 * half + ((size_t)kv_head << a.page_shift) + tok;
+        v_units_at = a.pages + 2 * half + ((size_t)(a.n_kv + kv_head) << a.page_shift);
+        page[0] = page[1] = 0;
         ask_keys();
         ask_values();
     }
-    __device__ __forceinline__ bool has_keys() const { return D >= 128 || loader < 2; }
-    __device__ __forceinline__ bool has_values() const { return D >= 128 || loader >= 2; }
-    __device__ __forceinline__ void ask_keys()
+    __device__ __forceinline__ bool has_keys() const { return !HALVES || loader < 2; }
+    __device__ __forceinline__ bool has_values() const { return !HALVES || loader >= 2; }
+    __device__ __forceinline__ int step_of(int i) const { return (i * 256 + w * 64) / D; }  // of the wavefront's chunks of values: which 16 tokens of the stage
+    __device__ __forceinline__ void ask_keys()  // of the next stage
     {
-        k_page = pages[t0 >> page_shift];
-        k_at = t0 & ((1 << page_shift) - 1);
+        page[0] = pages[t0 >> page_shift];
+        if constexpr (TK == 64) page[1] = pages[(t0 + 32) >> page_shift];
+        at = t0 & ((1 << page_shift) - 1);
         t0 += STRIDE;
         if (!has_keys()) return;
-        const char *const from = head + (uint64_t)page_stride * (uint32_t)k_page + k_at * 16 + k_lane;
+        const uint64_t there = (uint64_t)page_stride * (uint32_t)(TK == 32 || row < 32 ? page[0] : page[1]) + at;
 #pragma unroll
-        for (int i = 0; i < N; ++i) k[i] = *reinterpret_cast<const uint4 *>(from + ((8 * i) << page_shift) * 16);
-        k_unit = *reinterpret_cast<const uint8_t *>(units + (uint64_t)page_stride * (uint32_t)k_page + k_at + key_of_row<__bf16>(row));
+        for (int i = 0; i < N; ++i) k[i] = *reinterpret_cast<const uint4 *>(keys_at + there + at * 15 + ((i * (256 / TK)) << page_shift) * 16);
+        k_unit = *reinterpret_cast<const uint8_t *>(k_units_at + there);
     }
     __device__ __forceinline__ void ask_values()  // of the stage whose keys were asked for last
     {
         if (!has_values()) return;
-        const uint64_t page = (uint64_t)page_stride * (uint32_t)k_page;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            v[i] = *reinterpret_cast<const uint4 *>(head + values_at + page + k_at * D + v_lane + i * D * 16);
-            v_units[i] = *reinterpret_cast<const uint4 *>(units + units_at + page + k_at + v_units_at + i * 16);
+            const int s = step_of(i), in_page = (at + 16 * s) & ((1 << page_shift) - 1);
+            const uint64_t there = (uint64_t)page_stride * (uint32_t)(TK == 32 || s < 2 ? page[0] : page[1]);
+            v[i] = *reinterpret_cast<const uint4 *>(values_at + there + in_page * D);
+            units[i] = *reinterpret_cast<const uint4 *>(v_units_at + there + in_page);
         }
     }
-    __device__ __forceinline__ void put_keys(unsigned char *to)
+    // piece p of the work that brings to LDS the next stage's keys, and the values of the stage before it
+    __device__ __forceinline__ void piece(int p, unsigned char *values_to, unsigned char *keys_to)
     {
-        const float unit = unit_of(k_unit);
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            unsigned char *const at = to + ((2 * (2 * (D < 128 ? loader & 1 : loader) + (int)(threadIdx.x & 63) / 32 + 8 * i)) * 32 + row) * 16;
-            *reinterpret_cast<uint4 *>(at) = eight_bf16(k[i].x, k[i].y, unit);
-            *reinterpret_cast<uint4 *>(at + 512) = eight_bf16(k[i].z, k[i].w, unit);
-        }
-    }
-    __device__ __forceinline__ void put_values(unsigned char *to)
-    {
-        const int lane = threadIdx.x & 63;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int s = D == 128 ? loader >> 1 : D < 128 ? loader & 1 : i, d = D == 128 ? (loader & 1) * 64 + lane : D < 128 ? lane : loader * 64 + lane;
-            const uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w}, u[4] = {v_units[i].x, v_units[i].y, v_units[i].z, v_units[i].w};
-            bf16x8 y[2];
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const uint32_t us = __builtin_amdgcn_readfirstlane(u[w]);
-                const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(x[w], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(x[w], true);
-                y[w / 2][w % 2 * 4] = (__bf16)(lo[0] * unit_of(us & 255));
-                y[w / 2][w % 2 * 4 + 1] = (__bf16)(lo[1] * unit_of(us >> 8 & 255));
-                y[w / 2][w % 2 * 4 + 2] = (__bf16)(hi[0] * unit_of(us >> 16 & 255));
-                y[w / 2][w % 2 * 4 + 3] = (__bf16)(hi[1] * unit_of(us >> 24));
+        const int i = p / 6, n = p % 6, lane = threadIdx.x & 63;
+        if (n < 4) {
+            if (!has_values()) return;
+            const uint32_t x = n == 0 ? v[i].x : n == 1 ? v[i].y : n == 2 ? v[i].z : v[i].w;
+            const uint32_t u = __builtin_amdgcn_readfirstlane(n == 0 ? units[i].x : n == 1 ? units[i].y : n == 2 ? units[i].z : units[i].w);
+            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(x, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(x, true);
+            const bf16x2 y = {(__bf16)(lo[0] * unit_of(u & 255)), (__bf16)(lo[1] * unit_of(u >> 8 & 255))};
+            const bf16x2 z = {(__bf16)(hi[0] * unit_of(u >> 16 & 255)), (__bf16)(hi[1] * unit_of(u >> 24))};
+            if (n % 2 == 0) {
+                out.x = __builtin_bit_cast(uint32_t, y), out.y = __builtin_bit_cast(uint32_t, z);
+            } else {
+                out.z = __builtin_bit_cast(uint32_t, y), out.w = __builtin_bit_cast(uint32_t, z);
+                *reinterpret_cast<uint4 *>(values_to + ((2 * step_of(i) + n / 2) * D + (w * 64 + lane) % D) * 16) = out;
             }
-            *reinterpret_cast<bf16x8 *>(to + (2 * s * D + d) * 16) = y[0];
-            *reinterpret_cast<bf16x8 *>(to + ((2 * s + 1) * D + d) * 16) = y[1];
+        } else {
+            if (!has_keys()) return;
+            const int c = (i * 256 + w * 64 + lane) / TK * 2 + n - 4;
+            *reinterpret_cast<uint4 *>(keys_to + (c * TK + row) * 16) = n == 4 ? eight_bf16(k[i].x, k[i].y, unit_of(k_unit)) : eight_bf16(k[i].z, k[i].w, unit_of(k_unit));
         }
+    }
+    __device__ __forceinline__ void ask()
+    {
+        ask_values();
+        ask_keys();
     }
     __device__ __forceinline__ void keys(unsigned char *to)  // of the next stage
     {
-        if (has_keys()) put_keys(to);
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p)
+            if (p % 6 >= 4) piece(p, nullptr, to);
         ask_keys();
     }
     __device__ __forceinline__ void values(unsigned char *to)  // of the stage before the one whose keys were asked for last
     {
-        if (has_values()) put_values(to);
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p)
+            if (p % 6 < 4) piece(p, to, nullptr);
         ask_values();
     }
 };
@@ -985,7 +994,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it,
     constexpr int U = CHUNK<E>;
     typedef TileRows<E, D, TK> Rows;
     constexpr int QC = Rows::QC, DJ = Rows::DJ, PK = Rows::PK, NV = PK * DJ, AHEAD = NV < 8 ? NV : 8, STRIDE = GROUPS * TK;
-    typedef std::conditional_t<AS_IS, Steps<E, D, STRIDE>, StepsE4m3<D, STRIDE>> Requests;
+    typedef std::conditional_t<AS_IS, Steps<E, D, STRIDE>, StagesE4m3<D, 32, STRIDE>> Requests;
     // up to `steps` steps' requests are still on their way
     const auto wait = [](auto steps) {
         if constexpr (AS_IS) wait_requests<decltype(steps)::value * 2 * Steps<E, D, STRIDE>::PER>();
@@ -1026,6 +1035,21 @@ __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it,
         stages.keys(lds + put_k);
         put_v = after(put_v, V_END);
         put_k = after(put_k, K_END);
+    };
+    const auto beside = [&](int i) {  // the same beside product i of a step
+        if constexpr (AS_IS) {
+            if (i == 1) request();
+        } else {
+            constexpr int FROM = 1, OVER = NV + QC - 2, PIECES = Requests::PIECES;
+            if (i < FROM) return;
+#pragma unroll
+            for (int p = (i - FROM) * PIECES / OVER; p < (i + 1 - FROM) * PIECES / OVER && p < PIECES; ++p) stages.piece(p, lds + K_END + put_v, lds + put_k);
+            if (i == FROM + OVER - 1) {
+                stages.ask();
+                put_v = after(put_v, V_END);
+                put_k = after(put_k, K_END);
+            }
+        }
     };
     uint4 fk[AHEAD], fv[AHEAD];
     const unsigned char *const my_keys = lds + (h * TK + r) * 16, *const my_values = lds + K_END + (h * D + r) * 16;
@@ -1088,7 +1112,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it,
 #pragma unroll
                     for (int i = (e - NV / 2) * 16 / NV; i < (e + 1 - NV / 2) * 16 / NV; ++i) top = max3(top, s[2 * i], s[2 * i + 1]);
                 }
-                if (e == 1) request();  // (beside the products)
+                beside(e);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -1104,6 +1128,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it,
                 for (int j = i * 2 * AHEAD / QC; j < (i + 1) * 2 * AHEAD / QC; ++j) fv[j] = value(j, v);
             }
             weigh(s, i * 8 / QC, (i + 1) * 8 / QC);
+            if constexpr (!FIRST) beside(NV + i);
         }
         __builtin_amdgcn_sched_barrier(0);
         t0 += STRIDE;
@@ -1324,10 +1349,12 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 // 3985 us).
 constexpr int turn_lds(int dim) { return 6 * 64 * dim * 2; }
 
-template <int D>
+template <int D, typename P = __bf16>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_turns_kernel(AttnArgs a)
 {
     typedef __bf16 E;
+    constexpr bool AS_IS = std::is_same_v<P, E>;  // pages hold what the products take
+    typedef std::conditional_t<AS_IS, Stages<E, D>, StagesE4m3<D, 64, 64>> Requests;
     constexpr int U = 8, TK = Stages<E, D>::TK, HALF = Stages<E, D>::HALF, PER = Stages<E, D>::PER, DJ = D / 32;
     constexpr int AHEAD = 8, NV = 4 * DJ, NK = D / 8;  // products of values, of keys
     extern __shared__ __align__(16) unsigned char lds[];  // keys of three stages, values of three
@@ -1337,7 +1364,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const bool second = wave >= 4;
     const int n = (it.kv1 - it.kv0 + TK - 1) / TK;
     const auto after = [](int place) { return place == 2 * HALF ? 0 : place + HALF; };
-    Stages<E, D> stages(a, it, kv_head, wave & 3, it.kv0);
+    Requests stages(a, it, kv_head, wave & 3, it.kv0);
     int put = 0, put_v = 0;
     const auto request_keys = [&] {
         stages.keys(lds + put);
@@ -1349,6 +1376,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_barrier" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto wait = [] {  // up to a stage's requests are still on their way (of group 0: the others have none)
+        if constexpr (AS_IS) wait_requests<2 * PER>();
+        else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
     if (!second) {
         request_keys();
@@ -1379,11 +1410,29 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             else if (i - NV < 2) mma32_first<E>(t.s[(i - NV) % 2], f[n_f], t.q[(i - NV) / 2]);
             else mma32<E>(t.s[(i - NV) % 2], f[n_f], t.q[(i - NV) / 2]);
             if (i + AHEAD < TO) f[n_f] = operand(i + AHEAD, v, k);
-            if (i == FROM + 2) {  // (beside the products)
-                __builtin_amdgcn_sched_barrier(0);
-                if (!second) {
-                    request_values();
-                    request_keys();
+            // (beside the products)
+            if constexpr (AS_IS) {
+                if (i == FROM + 2) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (!second) {
+                        request_values();
+                        request_keys();
+                    }
+                }
+            } else {
+                constexpr int PIECES = Requests::PIECES, OVER = TO - FROM - 3;
+                const int n = i - FROM - 2;
+                if (n >= 0 && n <= OVER) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (!second) {
+#pragma unroll
+                        for (int p = n * PIECES / OVER; p < (n + 1) * PIECES / OVER && p < PIECES; ++p) stages.piece(p, lds + 3 * HALF + put_v, lds + put);
+                        if (n == OVER) {
+                            stages.ask();
+                            put_v = put;
+                            put = after(put);
+                        }
+                    }
                 }
             }
         }
@@ -1393,12 +1442,12 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     typedef std::integral_constant<int, NV> Keys;
 
     int v = 0, k = 0, t0 = it.kv0;  // places of the stage's values and the next one's keys
-    wait_requests<2 * PER>();       // (of group 0: the others have none)
-    turn_over();                    // the keys of the first stage have come
+    wait();
+    turn_over();  // the keys of the first stage have come
     if (second) turn_over();
     fetch_first(0, 0, Keys{});
     products(0, 0, Keys{});
-    if (!second) wait_requests<2 * PER>();
+    if (!second) wait();
     turn_over();
     for (int i = 0; i + 1 < n; ++i) {
         t.weigh(t0, a.scale_log2);
@@ -1410,7 +1459,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         products(v, k, All{});
         __builtin_amdgcn_s_setprio(0);
         v = after(v);
-        if (!second) wait_requests<2 * PER>();
+        if (!second) wait();
         turn_over();
     }
     t.weigh(t0, a.scale_log2);
@@ -1419,7 +1468,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
     for (int i = 0; i < NV; ++i) mma32<E>(t.o[i % DJ], first_values<E>(operand(i, v, 0), it.kv1 - t0 - (2 * (i / DJ) + h) * U), t.w[i / DJ]);
     wait_requests<0>();  // none is on its way to LDS when the block ends
-    if (wave * 32 < it.n_rows) finish_tile<E, D, TK>(a, it, kv_head, wave, t);
+    if (wave * 32 < it.n_rows) finish_tile<E, D, TK, P>(a, it, kv_head, wave, t);
 }
 
 // A block joins the parts of one row: each wavefront finds the joined maximum and weight from all parts', then groups of D / 4 threads add

@@ -28,6 +28,7 @@ hipError_t prepare_attn_e4m3_kernels()
             allow(reinterpret_cast<const void *>(&attn_tiles_kernel<__bf16, D, E4m3>), LDS);
             allow(reinterpret_cast<const void *>(&attn_both_kernel<__bf16, D, E4m3>), LDS);
         });
+    allow(reinterpret_cast<const void *>(&attn_turns_kernel<128, E4m3>), turn_lds(128));
     return e;
 }
 
@@ -42,7 +43,13 @@ hipError_t launch_attn_e4m3(const AttnArgs &a, int dim, KvTiles way, int n_cu, h
             hipLaunchKernelGGL((attn_both_kernel<__bf16, D, E4m3>), dim3((unsigned)(n_tiles + n_rows)), dim3(256), LDS, st, a);
             return;
         }
-        if (n_tiles) hipLaunchKernelGGL((attn_tiles_kernel<__bf16, D, E4m3>), tiles, dim3(256), LDS, st, a);
+        bool done = n_tiles == 0;
+        if constexpr (kv_turns(LORA_BF16, D))
+            if (!done && way == KV_TILES_TURNS) {
+                hipLaunchKernelGGL((attn_turns_kernel<D, E4m3>), tiles, dim3(512), turn_lds(D), st, a);
+                done = true;
+            }
+        if (!done) hipLaunchKernelGGL((attn_tiles_kernel<__bf16, D, E4m3>), tiles, dim3(256), LDS, st, a);
         if (n_rows) hipLaunchKernelGGL((attn_rows_kernel<__bf16, D, E4m3>), rows, dim3(64 * ROW_WAVES), 0, st, a);
     });
 }

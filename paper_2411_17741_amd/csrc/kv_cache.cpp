@@ -467,7 +467,7 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     // Two groups of wavefronts in turns, 256 rows at a time, where every compute unit gets two such blocks at least and they are long (1024 tokens in the
     // mean).  Measured, tiles of 128 rows -> turns: 16384 tokens with 64 / 8 heads 3985 -> 3650 us, 8192 with 32 / 8 537 -> 499, 4096 150 -> 136, 2048 + 2048 81.3 -> 76.9, 4096 with 32 / 32
     // heads 152 -> 143.  The rule does not ask for a gain where it takes few rounds of blocks: 2048 + 2048 with 32 / 32 heads 85.1 -> 85.5, 3 x 1500 behind 600 with 40 / 40 155.5 -> 160.
-    if (!kv.e4m3() && lora::kv_turns(kv.cfg.dtype, kv.cfg.head_dim)) {
+    if (lora::kv_turns(kv.cfg.dtype, kv.cfg.head_dim)) {
         int64_t tokens = 0;
         for (size_t i = 0; i < g.seqs.size(); ++i) {
             const int64_t n = g.n_tokens[i], rows = n * grp, ctx = g.seqs[i]->n_tokens - n;

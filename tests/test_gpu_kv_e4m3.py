@@ -385,3 +385,28 @@ def test_exponents_from_end_to_end():
         s.check()
     finally:
         s.close()
+
+
+@pytest.mark.parametrize("page", [32, 64])
+def test_large_tiles(page):
+    """Prompts long enough for tiles of 256 rows, in pages of less than their stages' 64 tokens too: the last rows of some heads, whose lengths end inside everything."""
+    B, _K = _mods()
+    segs, heads, kv, dim = [(0, 2500), (700, 1700), (0, 2111)], 64, 8, 128
+    s = Setup(segs, heads, kv, dim, page=page, seed=13)
+    try:
+        assert B.lora_kv_batch_info(s.batch)[1].tiles_way == B.LORA_KV_TILES_TURNS
+        out = torch.full(s.q.shape, float("nan"), dtype=torch.bfloat16, device="cuda")
+        s.cache.attend(s.batch, 0, s.q.cuda(), out, 1.0 / math.sqrt(dim))
+        torch.cuda.synchronize()
+        got, q, pages = out.float().cpu().numpy(), s.q.float().numpy(), s.host.numpy()
+        assert np.isfinite(got).all()
+        for i, (c, n) in enumerate(segs):
+            for h in (0, 13, 63):
+                k, v = plain.read(pages, s.tables[i], 0, h // 8, kv, page, dim, c + n)
+                for t in (0, 1, 31, 32, 63, 100, n - 33, n - 2, n - 1):
+                    at = int(s.offsets[i]) + t
+                    want, mass, _r = kv_plain.attend(q[at : at + 1, h], k[: c + t + 1], v[: c + t + 1], c + t, 1.0 / math.sqrt(dim))
+                    # every weight is off by 2^-8 of itself, the output by half a step; what fp32 loses is 2^-12 at these lengths
+                    assert (np.abs(got[at, h] - want[0]) <= (2.0**-7 + 2.0**-12) * mass[0]).all(), (i, h, t)
+    finally:
+        s.close()
