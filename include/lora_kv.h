@@ -121,11 +121,12 @@ int lora_kv_seq_info(const lora_kv_t *kv, int64_t id, lora_kv_seq_info_t *out);
 /* The sequence's pages in order; *n receives how many there are, `pages` (may be NULL) up to cap of them. */
 int lora_kv_seq_pages(const lora_kv_t *kv, int64_t id, int32_t *pages, int32_t cap, int32_t *n);
 
-/* Keys and values of one layer out of the pages, turned as they were stored: tokens [first[i], first[i] + n_tokens[i]) of sequence ids[i], one sequence's
- * behind the other's, as rows [n_kv_heads][head_dim] of the cache's dtype, k_stride / v_stride values apart, 16-byte aligned.  A sequence may be named more than once.
- * The pages are those of the time of the call (that a captured call reads again).  LORA_E_NOTFOUND, LORA_E_INVAL (tokens that a sequence has not, bad arguments). */
+/* Keys and values of one layer out of the pages, turned as they were stored: tokens [first[i], first[i] + n_tokens[i]) of sequence ids[i] -- from 0 on if first is NULL, up to
+ * the last one there is if n_tokens is --, one sequence's behind the other's, as n_rows rows [n_kv_heads][head_dim] of the cache's dtype, k_stride / v_stride values apart, 16-byte aligned.
+ * A sequence may be named more than once.  The pages are those of the time of the call (that a captured call reads again).  LORA_E_NOTFOUND, LORA_E_INVAL (tokens
+ * that a sequence has not, another number of rows than of tokens, bad arguments). */
 int lora_kv_seq_read(lora_kv_t *kv, int32_t n, const int64_t *ids, const int32_t *first, const int32_t *n_tokens, int32_t layer, void *k, int64_t k_stride,
-                     void *v, int64_t v_stride, void *stream);
+                     void *v, int64_t v_stride, int64_t n_rows, void *stream);
 
 /* ---- pages ------------------------------------------------------------------------------- */
 

@@ -210,7 +210,7 @@ _SIGS = {
     "lora_kv_batch_info": (c_int, [c_void_p, POINTER(lora_kv_batch_info_t)]),
     "lora_kv_append": (c_int, [c_void_p, c_void_p, c_int32, c_char_p, c_void_p]),
     "lora_kv_append_norm": (c_int, [c_void_p, c_void_p, c_int32, c_char_p, c_char_p, c_void_p]),
-    "lora_kv_seq_read": (c_int, [c_void_p, c_int32, _i64a, _i32a, _i32a, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p]),
+    "lora_kv_seq_read": (c_int, [c_void_p, c_int32, _i64a, _i32a, _i32a, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_int64, c_void_p]),
     "lora_kv_attend": (c_int, [c_void_p, c_void_p, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_float, c_void_p]),
     "lora_strerror": (c_char_p, [c_int]),
     "lora_last_hip_error": (c_int, []),
@@ -746,10 +746,11 @@ def lora_kv_append_norm(kv, batch, layer: int, k: int, v: int, k_stride: int, v_
     return _lib.lora_kv_append_norm(kv, batch, layer, a, _kv_norm_t.pack(q_norm, k_norm, q_norm_stride, k_norm_stride, eps), stream)
 
 
-def lora_kv_seq_read(kv, ids, first, n_tokens, layer: int, k: int, k_stride: int, v: int, v_stride: int, stream: int = 0) -> int:
-    a, n = _ids_and_counts(ids, n_tokens)
-    _, f = _ids_and_counts(ids, first)
-    return _lib.lora_kv_seq_read(kv, a.size, _ptr(a), _ptr(f), _ptr(n), layer, k, k_stride, v, v_stride, stream)
+def lora_kv_seq_read(kv, ids, first, n_tokens, layer: int, k: int, k_stride: int, v: int, v_stride: int, n_rows: int, stream: int = 0) -> int:
+    """first, n_tokens: arrays as long as ids, or None"""
+    a = _i64(ids)
+    f, n = (None if c is None else _ids_and_counts(a, c)[1] for c in (first, n_tokens))
+    return _lib.lora_kv_seq_read(kv, a.size, _ptr(a), None if f is None else _ptr(f), None if n is None else _ptr(n), layer, k, k_stride, v, v_stride, n_rows, stream)
 
 
 def lora_kv_attend(kv, batch, layer: int, q: int, q_stride: int, out: int, out_stride: int, scale: float, stream: int = 0) -> int:

@@ -744,13 +744,14 @@ template <typename E, int D, int STRIDE> struct Steps {
     }
 };
 
-// The same for pages of 8-bit values, for stages of TK tokens, STRIDE apart, by 4 wavefronts.  Their way to LDS leads through registers, where they become bf16 with their tokens' units:
+// The same for pages of 8-bit values, for stages of TK tokens, STRIDE apart, by LOADERS wavefronts.  Their way to LDS leads through registers, where they become bf16 with their tokens' units:
 // what comes to LDS was asked for a step before.  A thread has N chunks of keys, 16 values of a token each, and N chunks of values, 16 tokens of one value; the tokens of the
 // latter are the same for all of a wavefront, their units scalars.  (Heads of 64 have chunks for half the threads: two wavefronts bring keys, two values.)  The work
 // is done in pieces that fall beside the products of the step.
-template <int D, int TK, int STRIDE> struct StagesE4m3 {
-    static constexpr int ALL = D * TK / 16, N = ALL < 256 ? 1 : ALL / 256, PIECES = 6 * N;
-    static constexpr bool HALVES = ALL < 256;
+template <int D, int TK, int STRIDE, int LOADERS = 4> struct StagesE4m3 {
+    static constexpr int ALL = D * TK / 16, THREADS = 64 * LOADERS, N = ALL < THREADS ? 1 : ALL / THREADS, PIECES = 6 * N;
+    static constexpr bool HALVES = ALL < THREADS;
+    static_assert(HALVES ? ALL * 2 == THREADS && LOADERS == 4 : ALL % THREADS == 0, "the threads' chunks");
     PageList pages;
     const char *keys_at, *values_at;  // the head's in page 0, and the thread's first chunk of them
     const char *k_units_at, *v_units_at;
@@ -777,7 +778,7 @@ template <int D, int TK, int STRIDE> struct StagesE4m3 {
     }
     __device__ __forceinline__ bool has_keys() const { return !HALVES || loader < 2; }
     __device__ __forceinline__ bool has_values() const { return !HALVES || loader >= 2; }
-    __device__ __forceinline__ int step_of(int i) const { return (i * 256 + w * 64) / D; }  // of the wavefront's chunks of values: which 16 tokens of the stage
+    __device__ __forceinline__ int step_of(int i) const { return (i * THREADS + w * 64) / D; }  // of the wavefront's chunks of values: which 16 tokens of the stage
     __device__ __forceinline__ void ask_keys()  // of the next stage
     {
         page[0] = pages[t0 >> page_shift];
@@ -787,7 +788,7 @@ template <int D, int TK, int STRIDE> struct StagesE4m3 {
         if (!has_keys()) return;
         const uint64_t there = (uint64_t)page_stride * (uint32_t)(TK == 32 || row < 32 ? page[0] : page[1]) + at;
 #pragma unroll
-        for (int i = 0; i < N; ++i) k[i] = *reinterpret_cast<const uint4 *>(keys_at + there + at * 15 + ((i * (256 / TK)) << page_shift) * 16);
+        for (int i = 0; i < N; ++i) k[i] = *reinterpret_cast<const uint4 *>(keys_at + there + at * 15 + ((i * (THREADS / TK)) << page_shift) * 16);
         k_unit = *reinterpret_cast<const uint8_t *>(k_units_at + there);
     }
     __device__ __forceinline__ void ask_values()  // of the stage whose keys were asked for last
@@ -820,7 +821,7 @@ template <int D, int TK, int STRIDE> struct StagesE4m3 {
             }
         } else {
             if (!has_keys()) return;
-            const int c = (i * 256 + w * 64 + lane) / TK * 2 + n - 4;
+            const int c = (i * THREADS + w * 64 + lane) / TK * 2 + n - 4;
             *reinterpret_cast<uint4 *>(keys_to + (c * TK + row) * 16) = n == 4 ? eight_bf16(k[i].x, k[i].y, unit_of(k_unit)) : eight_bf16(k[i].z, k[i].w, unit_of(k_unit));
         }
     }
@@ -1354,7 +1355,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 {
     typedef __bf16 E;
     constexpr bool AS_IS = std::is_same_v<P, E>;  // pages hold what the products take
-    typedef std::conditional_t<AS_IS, Stages<E, D>, StagesE4m3<D, 64, 64>> Requests;
+    typedef std::conditional_t<AS_IS, Stages<E, D>, StagesE4m3<D, 64, 64, 8>> Requests;
     constexpr int U = 8, TK = Stages<E, D>::TK, HALF = Stages<E, D>::HALF, PER = Stages<E, D>::PER, DJ = D / 32;
     constexpr int AHEAD = 8, NV = 4 * DJ, NK = D / 8;  // products of values, of keys
     extern __shared__ __align__(16) unsigned char lds[];  // keys of three stages, values of three
@@ -1364,7 +1365,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const bool second = wave >= 4;
     const int n = (it.kv1 - it.kv0 + TK - 1) / TK;
     const auto after = [](int place) { return place == 2 * HALF ? 0 : place + HALF; };
-    Requests stages(a, it, kv_head, wave & 3, it.kv0);
+    Requests stages(a, it, kv_head, AS_IS ? wave & 3 : wave, it.kv0);
+    const bool loads = !AS_IS || !second;  // conversions are shared out over all wavefronts, each beside its own products
     int put = 0, put_v = 0;
     const auto request_keys = [&] {
         stages.keys(lds + put);
@@ -1381,7 +1383,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         if constexpr (AS_IS) wait_requests<2 * PER>();
         else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     };
-    if (!second) {
+    if (loads) {
         request_keys();
         request_values();
         request_keys();
@@ -1424,14 +1426,12 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                 const int n = i - FROM - 2;
                 if (n >= 0 && n <= OVER) {
                     __builtin_amdgcn_sched_barrier(0);
-                    if (!second) {
 #pragma unroll
-                        for (int p = n * PIECES / OVER; p < (n + 1) * PIECES / OVER && p < PIECES; ++p) stages.piece(p, lds + 3 * HALF + put_v, lds + put);
-                        if (n == OVER) {
-                            stages.ask();
-                            put_v = put;
-                            put = after(put);
-                        }
+                    for (int p = n * PIECES / OVER; p < (n + 1) * PIECES / OVER && p < PIECES; ++p) stages.piece(p, lds + 3 * HALF + put_v, lds + put);
+                    if (n == OVER) {
+                        stages.ask();
+                        put_v = put;
+                        put = after(put);
                     }
                 }
             }
@@ -1447,7 +1447,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     if (second) turn_over();
     fetch_first(0, 0, Keys{});
     products(0, 0, Keys{});
-    if (!second) wait();
+    if (loads) wait();
     turn_over();
     for (int i = 0; i + 1 < n; ++i) {
         t.weigh(t0, a.scale_log2);
@@ -1459,7 +1459,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         products(v, k, All{});
         __builtin_amdgcn_s_setprio(0);
         v = after(v);
-        if (!second) wait();
+        if (loads) wait();
         turn_over();
     }
     t.weigh(t0, a.scale_log2);

@@ -857,44 +857,55 @@ int lora_kv_seq_pages(const lora_kv_t *kv, int64_t id, int32_t *pages, int32_t c
 }
 
 int lora_kv_seq_read(lora_kv_t *kv, int32_t n, const int64_t *ids, const int32_t *first, const int32_t *n_tokens, int32_t layer, void *k, int64_t k_stride, void *v, int64_t v_stride,
-                     void *stream)
+                     int64_t n_rows, void *stream)
 {
-    if (!kv || n < 0 || (n && (!ids || !first || !n_tokens)) || layer < 0 || layer >= kv->cfg.n_layers) return LORA_E_INVAL;
+    if (!kv || n < 0 || (n && !ids) || layer < 0 || layer >= kv->cfg.n_layers || n_rows < 0 || n_rows > INT32_MAX) return LORA_E_INVAL;
     if (kv->host_only) return LORA_E_STATE;
     const lora_kv_config_t &c = kv->cfg;
-    int64_t tokens = 0;
-    for (int32_t i = 0; i < n; ++i) {
-        const Seq *s = kv->find(ids[i]);
-        if (!s) return LORA_E_NOTFOUND;
-        if (first[i] < 0 || n_tokens[i] < 0 || (int64_t)first[i] + n_tokens[i] > s->n_tokens) return LORA_E_INVAL;
-        tokens += n_tokens[i];
-    }
-    if (!tokens) return LORA_OK;
-    const int64_t row = (int64_t)c.n_kv_heads * c.head_dim, u = kv->row_chunk();
-    const auto bad = [&](const void *p, int64_t stride) { return !p || !aligned16(p) || stride < row || stride % u || stride > ((int64_t)1 << 40); };
-    if (bad(k, k_stride) || bad(v, v_stride)) return LORA_E_INVAL;
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    const OnDevice on(*kv);
-    if (const int rc = in_order(*kv, st)) return rc;
-    lora::ReadArgs a;
-    a.pages = kv->pages + kv->layer_bytes * layer;
-    a.page_stride = (int64_t)kv->page_bytes;
-    a.k = k, a.v = v, a.k_stride = k_stride, a.v_stride = v_stride;
-    a.n_kv = c.n_kv_heads, a.dim = c.head_dim, a.page_shift = kv->page_shift, a.n_reads = 0;
-    int64_t at = 0;
-    for (int32_t i = 0; i < n; ++i) {
-        const Seq *s = kv->find(ids[i]);
-        for (int32_t pos = first[i], end = first[i] + n_tokens[i]; pos < end;) {
-            const int32_t off = pos & (c.page_tokens - 1), m = std::min(end - pos, c.page_tokens - off);
-            a.reads[a.n_reads++] = {at, s->pages[pos >> kv->page_shift], (int16_t)off, (int16_t)m};
-            at += m, pos += m;
-            if (a.n_reads == lora::KV_MAX_READS || at == tokens) {
-                KV_TRY(lora::launch_read(a, c.dtype, kv->e4m3(), st));
-                a.n_reads = 0;
-            }
+    return guarded([&]() -> int {
+        struct Part {
+            const Seq *seq;
+            int32_t pos, end;
+        };
+        std::vector<Part> parts(n);
+        int64_t tokens = 0;
+        for (int32_t i = 0; i < n; ++i) {
+            const Seq *s = kv->find(ids[i]);
+            if (!s) return LORA_E_NOTFOUND;
+            const int64_t pos = first ? first[i] : 0, end = n_tokens ? pos + n_tokens[i] : s->n_tokens;
+            if (pos < 0 || end < pos || end > s->n_tokens) return LORA_E_INVAL;
+            parts[i] = {s, (int32_t)pos, (int32_t)end};
+            tokens += end - pos;
         }
-    }
-    return LORA_OK;
+        if (tokens != n_rows) return LORA_E_INVAL;
+        if (!tokens) return LORA_OK;
+        const int64_t row = (int64_t)c.n_kv_heads * c.head_dim, u = kv->row_chunk();
+        const auto bad = [&](const void *p, int64_t stride) { return !p || !aligned16(p) || stride < row || stride % u || stride > ((int64_t)1 << 40); };
+        if (bad(k, k_stride) || bad(v, v_stride)) return LORA_E_INVAL;
+        hipStream_t st = static_cast<hipStream_t>(stream);
+        const OnDevice on(*kv);
+        if (const int rc = in_order(*kv, st)) return rc;
+        lora::ReadArgs a;
+        a.pages = kv->pages + kv->layer_bytes * layer;
+        a.page_stride = (int64_t)kv->page_bytes;
+        a.k = k, a.v = v, a.k_stride = k_stride, a.v_stride = v_stride;
+        a.n_kv = c.n_kv_heads, a.dim = c.head_dim, a.page_shift = kv->page_shift, a.n_reads = 0;
+        int32_t at = 0;
+        for (const Part &p : parts)
+            for (int32_t pos = p.pos; pos < p.end;) {
+                const int32_t off = pos & (c.page_tokens - 1), m = std::min(p.end - pos, c.page_tokens - off);
+                a.page[a.n_reads] = p.seq->pages[pos >> kv->page_shift];
+                a.off[a.n_reads] = (uint8_t)off;
+                a.row[a.n_reads] = at;
+                a.row[++a.n_reads] = at += m;
+                pos += m;
+                if (a.n_reads == lora::KV_MAX_READS || at == tokens) {
+                    KV_TRY(lora::launch_read(a, c.dtype, kv->e4m3(), st));
+                    a.n_reads = 0;
+                }
+            }
+        return LORA_OK;
+    });
 }
 
 // ---- pages ---------------------------------------------------------------------------------

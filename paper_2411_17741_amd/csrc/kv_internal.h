@@ -21,7 +21,7 @@ enum KvTiles { KV_TILES_PLAIN = LORA_KV_TILES_PLAIN, KV_TILES_MANY = LORA_KV_TIL
 constexpr bool kv_many(int dtype, int dim) { return dtype == LORA_BF16 && dim == 128; }
 constexpr bool kv_pairs(int dtype, int dim) { return dtype == LORA_BF16 && dim == 64; }
 constexpr int KV_MAX_MOVES = 128; // page copies of one launch (they travel as its arguments)
-constexpr int KV_MAX_READS = 192; // pages read back by one launch (likewise)
+constexpr int KV_MAX_READS = 440; // pages read back by one launch (likewise)
 // Pages of 8 bits: exponents are held with this added, and lie from -117 (the smallest value above 0 is normal in bf16) to 120 (of the largest fp32 values)
 constexpr int KV_EXP_BIAS = 127, KV_EXP_MIN = -117, KV_EXP_MAX = 120;
 
@@ -98,21 +98,17 @@ struct AppendHeadsArgs {
     double eps;
 };
 
-// Tokens off .. off + n - 1 of a page: rows row .. of what is read
-struct KvRead {
-    int64_t row;
-    int32_t page;
-    int16_t off, n;
-};
-
 struct ReadArgs {
     const char *pages;  // of this layer
     int64_t page_stride;
     void *k, *v;
     int64_t k_stride, v_stride;
     int32_t n_kv, dim, page_shift, n_reads;
-    KvRead reads[KV_MAX_READS];
+    // read i: tokens off[i] .. of page page[i], rows row[i] .. row[i + 1] - 1
+    int32_t page[KV_MAX_READS], row[KV_MAX_READS + 1];
+    uint8_t off[KV_MAX_READS];
 };
+static_assert(sizeof(ReadArgs) <= 4096, "a kernel's arguments");
 
 struct AttnArgs {
     const void *q;

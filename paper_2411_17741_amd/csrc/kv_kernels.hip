@@ -225,14 +225,7 @@ __device__ __forceinline__ int exponent_for(float top)
     return min(max((int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 127 - 8, KV_EXP_MIN), KV_EXP_MAX);
 }
 
-// a value for the conversion to 8 bits: 448 at most, or no number
-__device__ __forceinline__ float scaled(float v, float unit)
-{
-    v *= unit;
-    return fabsf(v) <= 448.f ? v : NAN;
-}
-
-// ... four of them
+// Four values of 448 at most to 8 bits (what is infinite or no number becomes no number)
 __device__ __forceinline__ uint32_t four_e4m3(float a, float b, float c, float d)
 {
     const int low = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
@@ -265,63 +258,137 @@ __device__ __forceinline__ void turn_pairs(T (&x)[U], T (&y)[U], const float (&c
     }
 }
 
-// A block's share of the values into pages of 8 bits: a thread takes 8 values of a head of up to 16 tokens that share their chunks
+// The largest of two tokens' values each, over the lanes that have the other values of the head (`lanes` beside each other: 16, 32 or 64)
+typedef unsigned short Sizes __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ Sizes largest(Sizes v, int lanes)
+{
+    const auto with = [&](auto ctrl) {
+        v = __builtin_elementwise_max(v, __builtin_bit_cast(Sizes, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(ctrl)::value, 0xF, 0xF, true)));
+    };
+    with(std::integral_constant<int, 0xB1>{});   // the neighbour
+    with(std::integral_constant<int, 0x4E>{});   // two lanes on
+    with(std::integral_constant<int, 0x141>{});  // the other four of eight
+    with(std::integral_constant<int, 0x140>{});  // the other eight of 16
+    const auto far = [&](int off) { v = __builtin_elementwise_max(v, __builtin_bit_cast(Sizes, __shfl_xor(__builtin_bit_cast(int, v), off, 64))); };
+    if (lanes > 16) far(16);
+    if (lanes > 32) far(32);
+    return v;
+}
+
+// A block's share of the values into pages of 8 bits: a thread takes 4 values of a head of up to 16 tokens that share their chunks (8 values: 185 registers instead of 100 and half the
+// wavefronts).  bf16 values compare as whole numbers without their sign, two tokens at a time.
+constexpr int VALUES_E4M3 = 4;
 __device__ __forceinline__ void append_values_e4m3(const AppendArgs &a, uint32_t block)
 {
-    constexpr int U = 8, N = 16;
-    const int n_chunks = a.dim / U;
+    constexpr int U = VALUES_E4M3, N = 16;
+    const int lanes = a.dim / U;  // that have a head's values
     uint32_t i = block * 256u + threadIdx.x;
-    const int c = i % n_chunks;
-    i /= n_chunks;
+    const int c = i % lanes;
+    i /= lanes;
     const int h = i % a.n_kv;
     const int g = i / a.n_kv;
     KvGroup grp{0, 0, 0, 0};
     if (g < a.n_groups) grp = a.groups[g];
     const __bf16 *src = static_cast<const __bf16 *>(a.v) + (int64_t)grp.tok * a.v_stride + h * a.dim + c * U;
-    const int at = grp.pos & ((1 << a.page_shift) - 1);
+    const int at = grp.pos & ((1 << a.page_shift) - 1), first = at % N;
     char *const page = a.pages + grp.page * a.page_stride;
     const size_t head_values = (size_t)a.dim << a.page_shift;
     uint8_t *to = reinterpret_cast<uint8_t *>(page) + (a.n_kv + h) * head_values + (size_t)(at / N) * a.dim * N + c * U * N;
     uint8_t *exps = reinterpret_cast<uint8_t *>(page) + 2 * a.n_kv * head_values + ((size_t)(a.n_kv + h) << a.page_shift) + at;
-    Vals<__bf16> in[N];
-    float unit[N];
+    const auto size = [](uint32_t two) {  // of two values; of those that are infinite or no number 0
+        Sizes v = __builtin_bit_cast(Sizes, two & 0x7fff7fffu);
+        v[0] = v[0] < 0x7f80 ? v[0] : 0, v[1] = v[1] < 0x7f80 ? v[1] : 0;
+        return v;
+    };
+    const auto top_of = [&](const uint2 &x) {
+        const Sizes m = __builtin_elementwise_max(size(x.x), size(x.y));
+        return m[0] > m[1] ? m[0] : m[1];
+    };
+    const auto exponent = [](unsigned short top) { return exponent_for(__uint_as_float((uint32_t)top << 16)); };
+    const auto value = [](const uint2 &x, int d) { return d == 0 ? bf_lo(x.x) : d == 1 ? bf_hi(x.x) : d == 2 ? bf_lo(x.y) : bf_hi(x.y); };
+    // Groups of more than a token or two: all tokens at once, by their places in the chunks.  What is not theirs in a chunk stays what it is (nobody else writes there now).
+    if (__any(grp.n > 2)) {
+        uint2 in[N];
+        float unit[N];
+        uint32_t e4[N / 4] = {};
 #pragma unroll
-    for (int t = 0; t < N; ++t) {
-        float top = 0.f;
-        if (t < grp.n) {
-            in[t] = *reinterpret_cast<const Vals<__bf16> *>(src + t * a.v_stride);
-#pragma unroll
-            for (int e = 0; e < U; ++e) top = larger(top, (float)in[t].v[e]);
+        for (int t = 0; t < N; ++t) {
+            in[t] = make_uint2(0, 0);
+            if (t >= first && t < first + grp.n) in[t] = *reinterpret_cast<const uint2 *>(src + (t - first) * a.v_stride);
         }
-        for (int m = 1; m < n_chunks; m <<= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
-        const int e = exponent_for(top);
-        unit[t] = unit_of(KV_EXP_BIAS - e);
-        if (t < grp.n && c == 0) exps[t] = (uint8_t)(e + KV_EXP_BIAS);
-    }
-    if (grp.n == N) {
+#pragma unroll
+        for (int t = 0; t < N; t += 2) {
+            const Sizes top = largest(Sizes{top_of(in[t]), top_of(in[t + 1])}, lanes);
+            const int e0 = exponent(top[0]), e1 = exponent(top[1]);
+            unit[t] = unit_of(KV_EXP_BIAS - e0), unit[t + 1] = unit_of(KV_EXP_BIAS - e1);
+            e4[t / 4] |= (uint32_t)(e0 + KV_EXP_BIAS | (e1 + KV_EXP_BIAS) << 8) << t % 4 * 8;
+        }
+        if (!grp.n) return;
+        const bool whole = grp.n == N;
+        uint4 chunk[U];
 #pragma unroll
         for (int d = 0; d < U; ++d) {
             const auto four = [&](int t) {
-                return four_e4m3(scaled((float)in[t].v[d], unit[t]), scaled((float)in[t + 1].v[d], unit[t + 1]), scaled((float)in[t + 2].v[d], unit[t + 2]),
-                                 scaled((float)in[t + 3].v[d], unit[t + 3]));
+                return four_e4m3(value(in[t], d) * unit[t], value(in[t + 1], d) * unit[t + 1], value(in[t + 2], d) * unit[t + 2], value(in[t + 3], d) * unit[t + 3]);
             };
-            *reinterpret_cast<uint4 *>(to + d * N) = make_uint4(four(0), four(4), four(8), four(12));
+            chunk[d] = make_uint4(four(0), four(4), four(8), four(12));
         }
-    } else {
+        uint4 e = make_uint4(e4[0], e4[1], e4[2], e4[3]), *const e_to = reinterpret_cast<uint4 *>(exps - first);
+        if (!whole) {
+            // the bytes of dword w that are the group's
+            const auto mine = [&](int w) {
+                const int from = min(max(first - 4 * w, 0), 4), to = min(max(first + grp.n - 4 * w, 0), 4);
+                const auto below = [](int n) { return n == 4 ? ~0u : (1u << n * 8) - 1u; };
+                return below(to) & ~below(from);
+            };
+            const uint32_t m[4] = {mine(0), mine(1), mine(2), mine(3)};
+            const auto merge = [&](uint4 &v, const uint4 &before) {
+                v = make_uint4((v.x & m[0]) | (before.x & ~m[0]), (v.y & m[1]) | (before.y & ~m[1]), (v.z & m[2]) | (before.z & ~m[2]), (v.w & m[3]) | (before.w & ~m[3]));
+            };
+            uint4 old[U], old_e = make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int t = 0; t < N; ++t)
-            if (t < grp.n) {
+            for (int d = 0; d < U; ++d) old[d] = *reinterpret_cast<const uint4 *>(to + d * N);
+            if (c == 0) old_e = *e_to;
 #pragma unroll
-                for (int d = 0; d < U; ++d) to[d * N + at % N + t] = (uint8_t)four_e4m3(scaled((float)in[t].v[d], unit[t]), 0.f, 0.f, 0.f);
-            }
+            for (int d = 0; d < U; ++d) merge(chunk[d], old[d]);
+            merge(e, old_e);
+        }
+#pragma unroll
+        for (int d = 0; d < U; ++d) *reinterpret_cast<uint4 *>(to + d * N) = chunk[d];
+        if (c == 0) *e_to = e;
+        return;
+    }
+#pragma unroll 1
+    for (int t = 0; t < grp.n; ++t) {
+        const uint2 x = *reinterpret_cast<const uint2 *>(src + t * a.v_stride);
+        const int e = exponent(largest(Sizes{top_of(x), 0}, lanes)[0]);
+        const float unit = unit_of(KV_EXP_BIAS - e);
+        if (c == 0) exps[t] = (uint8_t)(e + KV_EXP_BIAS);
+        const uint32_t v = four_e4m3(value(x, 0) * unit, value(x, 1) * unit, value(x, 2) * unit, value(x, 3) * unit);
+#pragma unroll
+        for (int d = 0; d < U; ++d) to[d * N + first + t] = (uint8_t)(v >> d * 8);
     }
 }
 
-template <typename E, bool E8, bool NORM, int APPEND_HEADS>
+// The sum over lanes `tokens` (2, 4, 8 or 16) apart
+__device__ __forceinline__ float over_pairs(float v, int tokens)
+{
+    const auto row = [&](auto ctrl) { v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(ctrl)::value, 0xF, 0xF, true)); };
+    if (tokens < 16) row(std::integral_constant<int, 0x128>{});  // 16 lanes turned by 8
+    if (tokens < 8) row(std::integral_constant<int, 0x124>{});
+    if (tokens < 4) row(std::integral_constant<int, 0x122>{});
+    const auto near = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(near[0]) + __uint_as_float(near[1]);
+    const auto far = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(far[0]) + __uint_as_float(far[1]);
+}
+
+constexpr int NORM_MANY_HEADS = 4, NORM_FEW_HEADS = 1;  // of a thread, all of whose values are on their way at once
+template <typename E, bool E8, bool NORM, int HEADS>
 __global__ __launch_bounds__(256) void append_heads_kernel(AppendHeadsArgs n, uint32_t key_blocks)
 {
     constexpr int U = CHUNK<E>;
-    constexpr bool PAST = APPEND_HEADS == APPEND_MANY_HEADS;
+    constexpr bool PAST = HEADS > 1;
     const AppendArgs &a = n.a;
     if (blockIdx.x >= key_blocks) {
         if constexpr (E8) {
@@ -335,9 +402,9 @@ __global__ __launch_bounds__(256) void append_heads_kernel(AppendHeadsArgs n, ui
     const int page_tokens = 1 << a.page_shift;
     const size_t head_values = (size_t)a.dim << a.page_shift;  // of one half of a page
     const int n_pairs = a.dim / (2 * U), tokens = 64 / n_pairs, lane = threadIdx.x & 63;  // of a wavefront
-    const int heads = (a.q ? a.n_heads : 0) + a.n_kv, head_groups = (heads + APPEND_HEADS - 1) / APPEND_HEADS;
+    const int heads = (a.q ? a.n_heads : 0) + a.n_kv, head_groups = (heads + HEADS - 1) / HEADS;
     const uint32_t wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4u + (threadIdx.x >> 6));
-    const int h0 = wave % head_groups * APPEND_HEADS, first = (int)(wave / head_groups) * tokens;
+    const int h0 = wave % head_groups * HEADS, first = (int)(wave / head_groups) * tokens;
     if (first >= a.n_tokens) return;
     // lanes behind the last token work on it with the others, and store nothing
     const int p = lane / tokens, t = min(first + lane % tokens, a.n_tokens - 1);
@@ -350,23 +417,23 @@ __global__ __launch_bounds__(256) void append_heads_kernel(AppendHeadsArgs n, ui
     const auto source = [&](int h) {
         return h < a.n_kv ? static_cast<const E *>(a.k) + t * a.k_stride + h * a.dim : static_cast<const E *>(a.q) + t * a.q_stride + (h - a.n_kv) * a.dim;
     };
-    Vals<E> x[APPEND_HEADS], y[APPEND_HEADS];
+    const auto fetch = [&](Vals<E> &x, Vals<E> &y, int h) {
+        const E *src = source(min(h, heads - 1));
+        x = load_once<PAST>(src + c0 * U);
+        y = load_once<PAST>(src + c1 * U);
+    };
+    Vals<E> x[HEADS], y[HEADS];
 #pragma unroll
-    for (int k = 0; k < APPEND_HEADS; ++k) {
-        const E *src = source(min(h0 + k, heads - 1));
-        x[k] = load_once<PAST>(src + c0 * U);
-        y[k] = load_once<PAST>(src + c1 * U);
-    }
+    for (int k = 0; k < HEADS; ++k) fetch(x[k], y[k], h0 + k);
     float c[U], s[U];
     if (turn) {
         const float *cs = a.rope + (size_t)tok.pos * a.rope_dim + p * U, *sn = cs + a.rope_dim / 2;
 #pragma unroll
         for (int e = 0; e < U; ++e) c[e] = cs[e], s[e] = sn[e];
     }
-#pragma unroll
-    for (int k = 0; k < APPEND_HEADS; ++k) {
-        const int h = h0 + k;
-        if (h >= heads) break;
+    const float *held = nullptr;  // the weights that are in wx, wy
+    float wx[U], wy[U];
+    const auto work = [&](Vals<E> &x, Vals<E> &y, int h) {
         const bool key = h < a.n_kv;
         const float *w = nullptr;
         double factor = 1.;
@@ -374,24 +441,47 @@ __global__ __launch_bounds__(256) void append_heads_kernel(AppendHeadsArgs n, ui
             w = key ? n.k_norm : n.q_norm;
             if (w) {
                 w += (int64_t)(key ? h : h - a.n_kv) * (key ? n.k_norm_stride : n.q_norm_stride);
-                double sum = 0.;
+                if (w != held) {
+                    held = w;
 #pragma unroll
-                for (int e = 0; e < U; ++e) {
-                    const double u = (double)(float)x[k].v[e], v = (double)(float)y[k].v[e];
-                    sum += u * u;
-                    sum += v * v;
+                    for (int e = 0; e < U; ++e) wx[e] = w[c0 * U + e], wy[e] = w[c1 * U + e];
                 }
-                for (int m = tokens; m < 64; m <<= 1) sum += __shfl_xor(sum, m, 64);
-                factor = 1. / sqrt(sum / a.dim + n.eps);
+                const auto exactly = [&] {
+                    double sum = 0.;
+#pragma unroll
+                    for (int e = 0; e < U; ++e) {
+                        const double u = (double)(float)x.v[e], v = (double)(float)y.v[e];
+                        sum += u * u;
+                        sum += v * v;
+                    }
+                    for (int m = tokens; m < 64; m <<= 1) sum += __shfl_xor(sum, m, 64);
+                    return 1. / sqrt(sum / a.dim + n.eps);
+                };
+                if (sizeof(E) == 4 || (E8 && key)) {
+                    factor = exactly();
+                } else if constexpr (sizeof(E) == 2) {
+                    // the squares are exact in fp32, and so are sums of 16 of them to 2^-20; where they leave its range, 64 bits hold them
+                    const uint4 xw = __builtin_bit_cast(uint4, x), yw = __builtin_bit_cast(uint4, y);
+                    float sum = 0.f;
+                    const auto add = [&](uint32_t two) { sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, two), sum, false); };
+                    add(xw.x), add(xw.y), add(xw.z), add(xw.w), add(yw.x), add(yw.y), add(yw.z), add(yw.w);
+                    sum = over_pairs(sum, tokens);
+                    const bool far = !(sum < 1e37f);
+                    factor = (double)__builtin_amdgcn_rsqf(sum / (float)a.dim + (float)n.eps);
+                    if (__any(far)) {
+                        const double f = exactly();
+                        factor = far ? f : factor;
+                    }
+                }
             }
         }
         if (E8 && key) {
             double u[U], v[U];
 #pragma unroll
-            for (int e = 0; e < U; ++e) u[e] = (double)(float)x[k].v[e], v[e] = (double)(float)y[k].v[e];
+            for (int e = 0; e < U; ++e) u[e] = (double)(float)x.v[e], v[e] = (double)(float)y.v[e];
             if (w) {
 #pragma unroll
-                for (int e = 0; e < U; ++e) u[e] *= factor * (double)w[c0 * U + e], v[e] *= factor * (double)w[c1 * U + e];
+                for (int e = 0; e < U; ++e) u[e] *= factor * (double)wx[e], v[e] *= factor * (double)wy[e];
             }
             if (turn) turn_pairs(u, v, c, s, halves);
             float f[U], g[U], top = 0.f;
@@ -409,39 +499,42 @@ __global__ __launch_bounds__(256) void append_heads_kernel(AppendHeadsArgs n, ui
                     uint8_t *const to = page + h * head_values + (size_t)(tok.pos & (page_tokens - 1)) * 16;
                     const auto put = [&](int chunk, const float(&z)[U]) {
                         *reinterpret_cast<uint2 *>(to + ((size_t)(chunk >> 1) << a.page_shift) * 16 + (chunk & 1) * 8) =
-                            make_uint2(four_e4m3(scaled(z[0], unit), scaled(z[1], unit), scaled(z[2], unit), scaled(z[3], unit)),
-                                       four_e4m3(scaled(z[4], unit), scaled(z[5], unit), scaled(z[6], unit), scaled(z[7], unit)));
+                            make_uint2(four_e4m3(z[0] * unit, z[1] * unit, z[2] * unit, z[3] * unit),
+                                       four_e4m3(z[4] * unit, z[5] * unit, z[6] * unit, z[7] * unit));
                     };
                     put(c0, f), put(c1, g);
                     if (p == 0) page[2 * a.n_kv * head_values + ((size_t)h << a.page_shift) + (tok.pos & (page_tokens - 1))] = (uint8_t)(e + KV_EXP_BIAS);
                 }
             }
-            continue;
+            return;
         }
         if (w || turn) {
             float u[U], v[U];
 #pragma unroll
-            for (int e = 0; e < U; ++e) u[e] = (float)x[k].v[e], v[e] = (float)y[k].v[e];
+            for (int e = 0; e < U; ++e) u[e] = (float)x.v[e], v[e] = (float)y.v[e];
             if (w) {
                 const float by = (float)factor;
 #pragma unroll
-                for (int e = 0; e < U; ++e) u[e] *= by * w[c0 * U + e], v[e] *= by * w[c1 * U + e];
+                for (int e = 0; e < U; ++e) u[e] *= by * wx[e], v[e] *= by * wy[e];
             }
             if (turn) turn_pairs(u, v, c, s, halves);
 #pragma unroll
-            for (int e = 0; e < U; ++e) x[k].v[e] = (E)u[e], y[k].v[e] = (E)v[e];
+            for (int e = 0; e < U; ++e) x.v[e] = (E)u[e], y.v[e] = (E)v[e];
         }
-        if (!there) continue;
+        if (!there) return;
         if (key) {
             E *page = reinterpret_cast<E *>(a.pages + tok.page * a.page_stride) + h * head_values + (size_t)(tok.pos & (page_tokens - 1)) * U;
-            *reinterpret_cast<Vals<E> *>(page + ((size_t)c0 << a.page_shift) * U) = x[k];
-            *reinterpret_cast<Vals<E> *>(page + ((size_t)c1 << a.page_shift) * U) = y[k];
+            *reinterpret_cast<Vals<E> *>(page + ((size_t)c0 << a.page_shift) * U) = x;
+            *reinterpret_cast<Vals<E> *>(page + ((size_t)c1 << a.page_shift) * U) = y;
         } else {
             E *to = static_cast<E *>(a.q_out) + t * a.q_out_stride + (h - a.n_kv) * a.dim;
-            store_past<PAST>(to + c0 * U, x[k]);
-            store_past<PAST>(to + c1 * U, y[k]);
+            store_past<PAST>(to + c0 * U, x);
+            store_past<PAST>(to + c1 * U, y);
         }
-    }
+    };
+#pragma unroll
+    for (int k = 0; k < HEADS; ++k)
+        if (h0 + k < heads) work(x[k], y[k], h0 + k);
 }
 
 hipError_t launch_append_heads(const AppendHeadsArgs &n, int dtype, bool e4m3, hipStream_t st)
@@ -450,16 +543,16 @@ hipError_t launch_append_heads(const AppendHeadsArgs &n, int dtype, bool e4m3, h
     const int u = dtype == LORA_BF16 ? 8 : 4;
     const int64_t heads = (a.q ? a.n_heads : 0) + a.n_kv, tokens = 64 / (a.dim / (2 * u));
     const bool many = a.n_tokens * heads * a.dim * (dtype == LORA_BF16 ? 2 : 4) >= APPEND_MANY, norm = n.q_norm || n.k_norm;
-    const int64_t each = many ? APPEND_MANY_HEADS : APPEND_FEW_HEADS;
+    const int64_t each = many ? NORM_MANY_HEADS : NORM_FEW_HEADS;
     const int64_t keys = ((a.n_tokens + tokens - 1) / tokens * ((heads + each - 1) / each) + 3) / 4;
-    const int64_t vals = ((int64_t)a.n_groups * a.n_kv * (a.dim / u) + 255) / 256;
+    const int64_t vals = ((int64_t)a.n_groups * a.n_kv * (a.dim / (e4m3 ? VALUES_E4M3 : u)) + 255) / 256;
     if (keys * 256 > UINT32_MAX || vals * 256 > UINT32_MAX || keys + vals > INT32_MAX) return hipErrorInvalidValue;
     const dim3 grid((unsigned)(keys + vals));
     const auto launch = [&](auto e, auto e8, auto with) {
         typedef decltype(e) E;
         constexpr bool E8 = decltype(e8)::value, NORM = decltype(with)::value;
-        if (many) hipLaunchKernelGGL((append_heads_kernel<E, E8, NORM, APPEND_MANY_HEADS>), grid, dim3(256), 0, st, n, (uint32_t)keys);
-        else hipLaunchKernelGGL((append_heads_kernel<E, E8, NORM, APPEND_FEW_HEADS>), grid, dim3(256), 0, st, n, (uint32_t)keys);
+        if (many) hipLaunchKernelGGL((append_heads_kernel<E, E8, NORM, NORM_MANY_HEADS>), grid, dim3(256), 0, st, n, (uint32_t)keys);
+        else hipLaunchKernelGGL((append_heads_kernel<E, E8, NORM, NORM_FEW_HEADS>), grid, dim3(256), 0, st, n, (uint32_t)keys);
     };
     if (dtype == LORA_F32) launch(float{}, std::false_type{}, std::true_type{});
     else if (!e4m3) launch(__bf16{}, std::false_type{}, std::true_type{});
@@ -474,8 +567,10 @@ template <typename E, typename P>
 __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
 {
     constexpr int U = CHUNK<P>, W = CHUNK<E>;  // values of 16 bytes of a page, of a row
-    const KvRead r = a.reads[blockIdx.y];
-    const char *const page = a.pages + r.page * a.page_stride;
+    // tokens off .. off + n - 1 of a page are rows row ..
+    const int at = blockIdx.y, off = a.off[at], n = a.row[at + 1] - a.row[at];
+    const int64_t row = a.row[at];
+    const char *const page = a.pages + a.page[at] * a.page_stride;
     const size_t head_values = (size_t)a.dim << a.page_shift;
     const P *const values = reinterpret_cast<const P *>(page);
     const uint8_t *const exps = reinterpret_cast<const uint8_t *>(page) + 2 * a.n_kv * head_values;  // (pages of 8 bits)
@@ -487,9 +582,9 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
         const int c = i % (a.dim / U);
         i /= a.dim / U;
         const int h = i % a.n_kv, t = i / a.n_kv * 8 + t8;
-        if (t < r.off || t >= r.off + r.n) return;
+        if (t < off || t >= off + n) return;
         const Vals<P> in = *reinterpret_cast<const Vals<P> *>(values + h * head_values + (((size_t)c << a.page_shift) + t) * U);
-        E *const to = static_cast<E *>(a.k) + (r.row + t - r.off) * a.k_stride + h * a.dim + c * U;
+        E *const to = static_cast<E *>(a.k) + (row + t - off) * a.k_stride + h * a.dim + c * U;
         if constexpr (sizeof(P) == sizeof(E)) {
             *reinterpret_cast<Vals<P> *>(to) = in;
         } else {
@@ -508,14 +603,14 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
     const int c = i % (a.dim / W);
     i /= a.dim / W;
     const int h = i % a.n_kv, t0 = i / a.n_kv * U;
-    if (t0 + U <= r.off || t0 >= r.off + r.n) return;  // (of blocks beyond the page, too: t0 is no token of it)
+    if (t0 + U <= off || t0 >= off + n) return;  // (of blocks beyond the page, too: t0 is no token of it)
     Vals<P> in[W];
 #pragma unroll
     for (int e = 0; e < W; ++e) in[e] = *reinterpret_cast<const Vals<P> *>(values + (a.n_kv + h) * head_values + ((size_t)(t0 / U) * a.dim + c * W + e) * U);
 #pragma unroll
     for (int k = 0; k < U; ++k) {
         const int t = t0 + k;
-        if (t < r.off || t >= r.off + r.n) continue;
+        if (t < off || t >= off + n) continue;
         Vals<E> out;
         if constexpr (sizeof(P) == sizeof(E)) {
 #pragma unroll
@@ -525,7 +620,7 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
 #pragma unroll
             for (int e = 0; e < W; ++e) out.v[e] = (E)(value_of(in[e].v[k]) * unit);
         }
-        *reinterpret_cast<Vals<E> *>(static_cast<E *>(a.v) + (r.row + t - r.off) * a.v_stride + h * a.dim + c * W) = out;
+        *reinterpret_cast<Vals<E> *>(static_cast<E *>(a.v) + (row + t - off) * a.v_stride + h * a.dim + c * W) = out;
     }
 }
 

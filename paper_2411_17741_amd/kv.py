@@ -4,7 +4,6 @@ from __future__ import annotations
 
 from typing import Optional
 
-import numpy as np
 import torch
 
 from . import binding as B
@@ -88,15 +87,12 @@ class KvCache:
         B.check(B.lora_kv_seq_free(self.handle, ids), "lora_kv_seq_free")
 
     def read(self, ids, layer: int, k: torch.Tensor, v: torch.Tensor, first=None, n_tokens=None, stream: Optional[torch.cuda.Stream] = None) -> None:
-        """Keys and values of tokens [first[i], first[i] + n_tokens[i]) of each sequence -- all there are, if not given -- out of the pages: k and v
+        """Keys and values of tokens [first[i], first[i] + n_tokens[i]) of each sequence -- from the first one on, up to the last, if not given -- out of the pages: k and v
         [tokens of all of them][n_kv_heads][head_dim], one sequence's behind the other's."""
-        ids = np.asarray(ids, np.int64).reshape(-1)
-        first = np.zeros(ids.size, np.int32) if first is None else np.asarray(first, np.int32).reshape(-1)
-        n_tokens = np.asarray([self.length(int(i)) for i in ids], np.int32) - first if n_tokens is None else np.asarray(n_tokens, np.int32).reshape(-1)
-        n = int(n_tokens.sum(dtype=np.int64))
+        n = k.shape[0]
         kp, ks = self._rows(k, "k", n, self.n_kv_heads)
         vp, vs = self._rows(v, "v", n, self.n_kv_heads)
-        B.check(B.lora_kv_seq_read(self.handle, ids, first, n_tokens, layer, kp, ks, vp, vs, self._stream(stream)), "lora_kv_seq_read")
+        B.check(B.lora_kv_seq_read(self.handle, ids, first, n_tokens, layer, kp, ks, vp, vs, n, self._stream(stream)), "lora_kv_seq_read")
 
     def length(self, seq: int) -> int:
         rc, info = B.lora_kv_seq_info(self.handle, seq)

@@ -231,17 +231,20 @@ def test_read_refusals():
         cache.extend([0], [30])
         out = torch.full((2, 30, 2, 64), 5.0, device="cuda", dtype=torch.bfloat16)
         p = out.data_ptr()
-        good = dict(ids=[0], first=[0], n_tokens=[30], layer=0, k=p, k_stride=128, v=p + 30 * 256, v_stride=128)
+        good = dict(ids=[0], first=[0], n_tokens=[30], layer=0, k=p, k_stride=128, v=p + 30 * 256, v_stride=128, n_rows=30)
         for kw, rc in ((dict(ids=[7]), B.LORA_E_NOTFOUND), (dict(n_tokens=[31]), B.LORA_E_INVAL), (dict(first=[1]), B.LORA_E_INVAL), (dict(first=[-1]), B.LORA_E_INVAL),
                        (dict(n_tokens=[-1]), B.LORA_E_INVAL), (dict(ids=[1]), B.LORA_E_INVAL), (dict(layer=2), B.LORA_E_INVAL), (dict(layer=-1), B.LORA_E_INVAL), (dict(k=0), B.LORA_E_INVAL),
-                       (dict(k=p + 2), B.LORA_E_INVAL), (dict(k_stride=120), B.LORA_E_INVAL), (dict(v_stride=132), B.LORA_E_INVAL), (dict(first=[2**31 - 1], n_tokens=[2**31 - 1]), B.LORA_E_INVAL)):
+                       (dict(k=p + 2), B.LORA_E_INVAL), (dict(k_stride=120), B.LORA_E_INVAL), (dict(v_stride=132), B.LORA_E_INVAL), (dict(first=[2**31 - 1], n_tokens=[2**31 - 1]), B.LORA_E_INVAL),
+                       (dict(n_rows=29), B.LORA_E_INVAL), (dict(n_rows=31), B.LORA_E_INVAL), (dict(n_rows=-1), B.LORA_E_INVAL), (dict(n_rows=2**33), B.LORA_E_INVAL), (dict(n_tokens=None, first=[1]), B.LORA_E_INVAL)):
             assert B.lora_kv_seq_read(cache.handle, **{**good, **kw}) == rc, kw
-        for kw in (dict(k=out[0, :29]), dict(k=out[0].float()), dict(v=out[1, :, :1])):
+        for kw in (dict(v=out[1, :29]), dict(k=out[0].float()), dict(v=out[1, :, :1])):
             with pytest.raises(ValueError):
                 cache.read([0], 0, **{**dict(k=out[0], v=out[1]), **kw})
+        with pytest.raises(B.LoraError):
+            cache.read([0], 0, out[0, :29], out[1, :29])
         torch.cuda.synchronize()
         assert bool((out == 5).all())
-        assert B.lora_kv_seq_read(cache.handle, [], [], [], 0, 0, 0, 0, 0) == 0
+        assert B.lora_kv_seq_read(cache.handle, [], [], [], 0, 0, 0, 0, 0, 0) == 0 and B.lora_kv_seq_read(cache.handle, [1], None, None, 0, 0, 0, 0, 0, 0) == 0
         with pytest.raises(ValueError):
             KvCache(1, 2, 2, 64, 8, e4m3=True, pages=torch.empty(8, 1, 2 * 2 * 64 * 65, device="cuda", dtype=torch.int8))
     finally:

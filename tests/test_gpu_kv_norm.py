@@ -53,7 +53,9 @@ def _run(segs, heads, kv, dim, page, dtype, rope_dim=None, neighbours=False, whi
 
         def want(x, w):
             """-> the outputs, and what roundings can do to them.  In fp32 the factor is rounded, its product with the weight, and that with the value: 3 * 2^-24 of each normed
-            value; two products and their sum make 2 more of each term (or 1, fused).  Then the output is rounded, by half a step."""
+            value; two products and their sum make 2 more of each term (or 1, fused).  The squares of bf16 values are summed in fp32: two roundings for each of 8 pairs and one for each
+            of up to 5 exchanges, 21 * 2^-24 of the sum, half of that in its root, and 2 for the quotient, the sum with eps and the root's own ulp (which is 2 * 2^-24): 14 more.  Then the
+            output is rounded, by half a step."""
             x = f(x) if w is None else kv_e4m3_plain.norm(f(x), w.numpy(), EPS)
             y, terms = (kv_plain.turn(x, pos, rope.numpy(), neighbours), None) if rope_dim else (x, None)
             if rope_dim:  # the sum of the terms' sizes: turned with every sign such that nothing cancels
@@ -61,7 +63,7 @@ def _run(segs, heads, kv, dim, page, dtype, rope_dim=None, neighbours=False, whi
                 terms = np.maximum(np.abs(kv_plain.turn(np.abs(x), pos, r, neighbours)), np.abs(kv_plain.turn(np.abs(x), pos, np.concatenate([r[:, : rope_dim // 2], -r[:, rope_dim // 2 :]], 1), neighbours)))
             else:
                 terms = np.abs(x)
-            e = 5 * 2.0**-24 * terms
+            e = (5 if dtype == "f32" or w is None else 19) * 2.0**-24 * terms
             half = 2.0**-8 if dtype == "bf16" else 2.0**-24
             e = e + half * (np.abs(y) + e)
             if w is None:

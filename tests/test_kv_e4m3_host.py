@@ -28,13 +28,13 @@ def test_reads_and_norms_are_checked():
     rc, h = B.lora_kv_create(cfg, 0, 0, 0, 0)
     assert rc == B.LORA_OK
     assert B.lora_kv_seq_add(h, [1]) == 0 and B.lora_kv_seq_extend(h, [1], [70]) == 0
-    assert B.lora_kv_seq_read(h, [1], [0], [70], 0, 256, 256, 256, 256) == B.LORA_E_STATE  # host only
-    assert B.lora_kv_seq_read(None, [1], [0], [70], 0, 256, 256, 256, 256) == B.LORA_E_INVAL
-    assert B.lora_kv_seq_read(h, [1], [0], [70], 2, 256, 256, 256, 256) == B.LORA_E_INVAL
-    assert B._lib.lora_kv_seq_read(h, -1, None, None, None, 0, 256, 256, 256, 256, None) == B.LORA_E_INVAL
-    assert B._lib.lora_kv_seq_read(h, 1, None, None, None, 0, 256, 256, 256, 256, None) == B.LORA_E_INVAL
+    assert B.lora_kv_seq_read(h, [1], [0], [70], 0, 256, 256, 256, 256, 70) == B.LORA_E_STATE  # host only
+    assert B.lora_kv_seq_read(None, [1], [0], [70], 0, 256, 256, 256, 256, 70) == B.LORA_E_INVAL
+    assert B.lora_kv_seq_read(h, [1], [0], [70], 2, 256, 256, 256, 256, 70) == B.LORA_E_INVAL
+    assert B._lib.lora_kv_seq_read(h, -1, None, None, None, 0, 256, 256, 256, 256, 70, None) == B.LORA_E_INVAL
+    assert B._lib.lora_kv_seq_read(h, 1, None, None, None, 0, 256, 256, 256, 256, 70, None) == B.LORA_E_INVAL
     with pytest.raises(ValueError):
-        B.lora_kv_seq_read(h, [1], [0, 0], [70], 0, 256, 256, 256, 256)
+        B.lora_kv_seq_read(h, [1], [0, 0], [70], 0, 256, 256, 256, 256, 70)
     assert B.lora_kv_append_norm(h, None, 0, 256, 256, 256, 256, k_norm=256) == B.LORA_E_INVAL
     B.lora_kv_destroy(h)
 
