@@ -561,12 +561,15 @@ hipError_t launch_append_heads(const AppendHeadsArgs &n, int dtype, bool e4m3, h
     return hipGetLastError();
 }
 
-// What pages hold, as rows: block row y takes a piece of a page.  Keys: a thread takes a chunk of one token; 8 tokens go with a run of 8 threads, so that the page is read in runs of
-// 128 bytes, and 8 threads beside each other in a row's.  Values: a thread takes 16 bytes of a row of all tokens that share their chunks.
+// What pages hold, as rows: block row y takes a piece of a page.  Keys: a thread takes a chunk of a token and of the ones 8, 16 and 24 behind it; 8 tokens go with a run of 8 threads, so
+// that the page is read in runs of 128 bytes, and 8 threads beside each other in a row's.  Values: a thread takes 16 bytes of a row of all tokens that share their chunks.  A launch's
+// first instructions come from memory, so there are few of them: 8 bits become bf16 two at a time, values of two tokens after they changed places by bytes.
+constexpr int READ_KEYS = 4;
 template <typename E, typename P>
 __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
 {
     constexpr int U = CHUNK<P>, W = CHUNK<E>;  // values of 16 bytes of a page, of a row
+    constexpr bool AS_IS = sizeof(P) == sizeof(E);
     // tokens off .. off + n - 1 of a page are rows row ..
     const int at = blockIdx.y, off = a.off[at], n = a.row[at + 1] - a.row[at];
     const int64_t row = a.row[at];
@@ -575,59 +578,82 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
     const P *const values = reinterpret_cast<const P *>(page);
     const uint8_t *const exps = reinterpret_cast<const uint8_t *>(page) + 2 * a.n_kv * head_values;  // (pages of 8 bits)
     uint32_t i = blockIdx.x * 256u + threadIdx.x;
-    const uint32_t n_keys = (uint32_t)(a.dim / U * a.n_kv) << a.page_shift;
+    const uint32_t n_keys = ((uint32_t)(a.dim / U * a.n_kv) << a.page_shift) / READ_KEYS;  // threads that have chunks of keys
     if (i < n_keys) {
-        const int t8 = i & 7;
-        i >>= 3;
-        const int c = i % (a.dim / U);
-        i /= a.dim / U;
-        const int h = i % a.n_kv, t = i / a.n_kv * 8 + t8;
-        if (t < off || t >= off + n) return;
-        const Vals<P> in = *reinterpret_cast<const Vals<P> *>(values + h * head_values + (((size_t)c << a.page_shift) + t) * U);
-        E *const to = static_cast<E *>(a.k) + (row + t - off) * a.k_stride + h * a.dim + c * U;
-        if constexpr (sizeof(P) == sizeof(E)) {
-            *reinterpret_cast<Vals<P> *>(to) = in;
-        } else {
-            const float unit = unit_of(exps[((size_t)h << a.page_shift) + t]);
+        const int chunk_shift = 31 - __builtin_clz(a.dim / U), t8 = i & 7, c = (i >> 3) & (a.dim / U - 1);
+        i >>= 3 + chunk_shift;
+        const int h = i % a.n_kv, t0 = (int)(i / a.n_kv) * 8 * READ_KEYS + t8;
+        const P *const from = values + h * head_values + (((size_t)c << a.page_shift) + t0) * U;
+        E *const to = static_cast<E *>(a.k) + (row + t0 - off) * a.k_stride + h * a.dim + c * U;
+        const auto there = [&](int j) { return (unsigned)(t0 + 8 * j - off) < (unsigned)n; };
+        Vals<P> in[READ_KEYS];
+        uint32_t exp[READ_KEYS];
 #pragma unroll
-            for (int k = 0; k < U / W; ++k) {
-                Vals<E> out;
-#pragma unroll
-                for (int e = 0; e < W; ++e) out.v[e] = (E)(value_of(in.v[k * W + e]) * unit);
-                *reinterpret_cast<Vals<E> *>(to + k * W) = out;
+        for (int j = 0; j < READ_KEYS; ++j)
+            if (there(j)) {
+                in[j] = load_once<true>(from + 8 * j * U);
+                if constexpr (!AS_IS) exp[j] = exps[((size_t)h << a.page_shift) + t0 + 8 * j];
             }
-        }
+#pragma unroll
+        for (int j = 0; j < READ_KEYS; ++j)
+            if (there(j)) {
+                E *const here = to + 8 * j * a.k_stride;
+                if constexpr (AS_IS) {
+                    store_past<true>(here, in[j]);
+                } else {
+                    const uint4 x = __builtin_bit_cast(uint4, in[j]);
+                    store_past<true>(here, __builtin_bit_cast(Vals<E>, eight_bf16(x.x, x.y, unit_of(exp[j]))));
+                    store_past<true>(here + W, __builtin_bit_cast(Vals<E>, eight_bf16(x.z, x.w, unit_of(exp[j]))));
+                }
+            }
         return;
     }
     i -= n_keys;
-    const int c = i % (a.dim / W);
+    const int c = i & (a.dim / W - 1);
     i /= a.dim / W;
     const int h = i % a.n_kv, t0 = i / a.n_kv * U;
     if (t0 + U <= off || t0 >= off + n) return;  // (of blocks beyond the page, too: t0 is no token of it)
     Vals<P> in[W];
 #pragma unroll
-    for (int e = 0; e < W; ++e) in[e] = *reinterpret_cast<const Vals<P> *>(values + (a.n_kv + h) * head_values + ((size_t)(t0 / U) * a.dim + c * W + e) * U);
+    for (int e = 0; e < W; ++e) in[e] = load_once<true>(values + (a.n_kv + h) * head_values + ((size_t)(t0 / U) * a.dim + c * W + e) * U);
+    E *const to = static_cast<E *>(a.v) + (row + t0 - off) * a.v_stride + h * a.dim + c * W;
+    const auto put = [&](int k, const Vals<E> &v) {
+        if ((unsigned)(t0 + k - off) < (unsigned)n) store_past<true>(to + k * a.v_stride, v);
+    };
+    if constexpr (AS_IS) {
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-        const int t = t0 + k;
-        if (t < off || t >= off + n) continue;
-        Vals<E> out;
-        if constexpr (sizeof(P) == sizeof(E)) {
+        for (int k = 0; k < U; ++k) {
+            Vals<E> out;
 #pragma unroll
             for (int e = 0; e < W; ++e) out.v[e] = in[e].v[k];
-        } else {
-            const float unit = unit_of(exps[((size_t)(a.n_kv + h) << a.page_shift) + t]);
-#pragma unroll
-            for (int e = 0; e < W; ++e) out.v[e] = (E)(value_of(in[e].v[k]) * unit);
+            put(k, out);
         }
-        *reinterpret_cast<Vals<E> *>(static_cast<E *>(a.v) + (row + t - off) * a.v_stride + h * a.dim + c * W) = out;
+    } else {
+        const uint4 exp = *reinterpret_cast<const uint4 *>(exps + ((size_t)(a.n_kv + h) << a.page_shift) + t0);
+        const auto word = [](const uint4 &v, int w) { return w == 0 ? v.x : w == 1 ? v.y : w == 2 ? v.z : v.w; };
+#pragma unroll
+        for (int k = 0; k < U; k += 2) {
+            uint32_t two[W / 2];  // values 2 e, 2 e + 1 of token k, and those of token k + 1
+#pragma unroll
+            for (int e = 0; e < W / 2; ++e)
+                two[e] = __builtin_amdgcn_perm(word(__builtin_bit_cast(uint4, in[2 * e + 1]), k / 4), word(__builtin_bit_cast(uint4, in[2 * e]), k / 4), k % 4 ? 0x07030602 : 0x05010400);
+            const float u0 = unit_of(word(exp, k / 4) >> k % 4 * 8 & 255), u1 = unit_of(word(exp, k / 4) >> (k % 4 * 8 + 8) & 255);
+            uint32_t x[W / 2], y[W / 2];
+#pragma unroll
+            for (int e = 0; e < W / 2; ++e) {
+                x[e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(two[e], u0, false));
+                y[e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(two[e], u1, true));
+            }
+            put(k, __builtin_bit_cast(Vals<E>, make_uint4(x[0], x[1], x[2], x[3])));
+            put(k + 1, __builtin_bit_cast(Vals<E>, make_uint4(y[0], y[1], y[2], y[3])));
+        }
     }
 }
 
 hipError_t launch_read(const ReadArgs &a, int dtype, bool e4m3, hipStream_t st)
 {
     const int64_t u = e4m3 ? 16 : dtype == LORA_BF16 ? 8 : 4, w = dtype == LORA_BF16 ? 8 : 4;
-    const int64_t threads = ((int64_t)(a.dim / u) * a.n_kv << a.page_shift) + (int64_t)(a.dim / w) * a.n_kv * ((1 << a.page_shift) / u);
+    const int64_t threads = ((int64_t)(a.dim / u) * a.n_kv << a.page_shift) / READ_KEYS + (int64_t)(a.dim / w) * a.n_kv * ((1 << a.page_shift) / u);
     const int64_t blocks = (threads + 255) / 256;
     if (blocks > INT32_MAX || a.n_reads > KV_MAX_READS) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks, (unsigned)a.n_reads);
