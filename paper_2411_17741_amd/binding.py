@@ -204,7 +204,7 @@ _SIGS = {
     "lora_kv_set_limit": (c_int, [c_void_p, c_int32]),
     "lora_kv_stats": (c_int, [c_void_p, POINTER(lora_kv_stats_t)]),
     "lora_kv_batch_create": (c_int, [c_void_p, c_int32, _i64a, _i32a, c_void_p, POINTER(c_void_p)]),
-    "lora_kv_batch_create_shared": (c_int, [c_void_p, c_int32, _i64a, _i32a, c_void_p, POINTER(c_void_p)]),
+    "lora_kv_batch_create_shared": (c_int, [c_void_p, c_int32, _i64a, _i32a, c_int32, c_void_p, POINTER(c_void_p)]),
     "lora_kv_batch_prefixes": (c_int, [c_void_p, POINTER(lora_kv_prefix_info_t)]),
     "lora_kv_batch_destroy": (c_int, [c_void_p, c_void_p]),
     "lora_kv_batch_info": (c_int, [c_void_p, POINTER(lora_kv_batch_info_t)]),
@@ -696,23 +696,27 @@ def lora_kv_stats(kv):
     return rc, st
 
 
-def _kv_batch(create, kv, seg_seq, seg_offsets, stream: int):
+def _segments(seg_seq, seg_offsets):
     ids, off = _i64(seg_seq), _i32(seg_offsets).reshape(-1)
     if off.size != ids.size + 1:
         raise ValueError(f"{ids.size} segments, {off.size} offsets")
-    b = c_void_p()
-    rc = create(kv, ids.size, _ptr(ids), _ptr(off), c_void_p(stream or None), ctypes.byref(b))
-    return rc, b
+    return ids, off
 
 
 def lora_kv_batch_create(kv, seg_seq, seg_offsets, stream: int = 0):
     """-> (status, batch handle)"""
-    return _kv_batch(_lib.lora_kv_batch_create, kv, seg_seq, seg_offsets, stream)
+    ids, off = _segments(seg_seq, seg_offsets)
+    b = c_void_p()
+    rc = _lib.lora_kv_batch_create(kv, ids.size, _ptr(ids), _ptr(off), c_void_p(stream or None), ctypes.byref(b))
+    return rc, b
 
 
-def lora_kv_batch_create_shared(kv, seg_seq, seg_offsets, stream: int = 0):
+def lora_kv_batch_create_shared(kv, seg_seq, seg_offsets, min_tokens: int = 0, stream: int = 0):
     """-> (status, batch handle)"""
-    return _kv_batch(_lib.lora_kv_batch_create_shared, kv, seg_seq, seg_offsets, stream)
+    ids, off = _segments(seg_seq, seg_offsets)
+    b = c_void_p()
+    rc = _lib.lora_kv_batch_create_shared(kv, ids.size, _ptr(ids), _ptr(off), min_tokens, c_void_p(stream or None), ctypes.byref(b))
+    return rc, b
 
 
 def lora_kv_batch_prefixes(batch):

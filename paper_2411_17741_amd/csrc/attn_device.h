@@ -343,9 +343,17 @@ __device__ __forceinline__ void finish_rows(const AttnArgs &a, const AttnItem &i
             put_row<E, D, false>(a, it, kv_head, i, st);
         }
     };
-    if constexpr (ALONE) {  // (items that one wavefront has to itself are whole)
+    if constexpr (ALONE) {
         if (redo) return again(0, 1);
         if (r >= it.n_rows) return;
+        if (it.part >= 0) {
+            const int64_t at = it.part + (int64_t)kv_head * it.n_rows + r;
+            const float each = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+            for (int j = 0; j < VJ; ++j) *reinterpret_cast<floatx4 *>(a.part_o + at * D + 16 * j + 4 * g) = o[j] * each;
+            if (g == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * at) = make_float2(m, l);
+            return;
+        }
         const float f = 1.f / l;
         E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D;
 #pragma unroll
@@ -1572,35 +1580,62 @@ __global__ __launch_bounds__(256) void attn_join_tiles_kernel(JoinArgs a)
     for (int k = 0; k < N; ++k) put_four(out + (k * 4 + threadIdx.x / 64) * 8 + lane / 32 * 4, l == 0.f ? o[k] / l : o[k]);
 }
 
-// Joins the parts of rows whose segments share prefixes: a wavefront to a row, a lane to a part for their maxima and sums, then D / 4 lanes to a part's values.
+// Joins the parts of rows whose segments share prefixes: a wavefront to a row.  Lanes find the row's sources all at once, then each a part of theirs and its maximum and sum; then D / 4 lanes
+// have a part's values, eight loads on their way at a time.  Trips to memory one after the other, as in the joins above.
 template <typename E, int D>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedJoinArgs a)
 {
-    constexpr int PER = D / 4, AT_ONCE = 64 / PER;  // lanes of a part's values; parts that the lanes have at a time
+    constexpr int PER = D / 4, AT_ONCE = 64 / PER, AHEAD = 8;  // lanes of a part's values; parts that the lanes have at a time; ... loads
     const SharedJoin it = a.items[blockIdx.x / a.n_kv];
     const int kv_head = blockIdx.x % a.n_kv, r = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (r >= it.n_rows) return;
-    const int mine = lane / PER, d = lane % PER * 4;
+    // lane k: source k's first part of the row, of how many
+    int first = 0, stride = 0, n = 0, tile_row = -1;  // tile_row: the row of 32 in a tile's layout, or -1
+    if (lane < it.n_sources) {
+        const SharedSource src = a.sources[it.source0 + lane];
+        const int row = src.row0 + r, at = row / src.rows, rr = row - at * src.rows;
+        const SharedBlock blk = a.blocks[src.block0 + at];
+        first = blk.part + kv_head * (src.tile ? (blk.n_rows + 31) & ~31 : blk.n_rows) + rr;
+        stride = blk.stride, n = blk.n_parts;
+        if (src.tile) tile_row = rr & 31;
+    }
+    int total = 0, begin = 0;  // parts of all sources; of those before the lane's
+    for (int k = 0; k < it.n_sources; ++k) {
+        if (lane == k) begin = total;
+        total += __builtin_amdgcn_readlane(n, k);
+    }
+    const int mine = lane / PER, d = lane % PER * 4, tile_d = (d / 8 * 64 + d / 4 % 2 * 32) * 4;
     float m = -FLT_MAX, l = 0.f;
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < it.n_sources; ++k) {
-        const SharedSource src = a.sources[it.source0 + k];
-        const SharedBlock blk = a.blocks[src.block0 + (src.row0 + r) / src.rows];
-        const int rr = (src.row0 + r) % src.rows;
-        const int64_t first = blk.part + (int64_t)kv_head * (src.tile ? (blk.n_rows + 31) & ~31 : blk.n_rows) + rr;
-        const float *from = a.part_o + (src.tile ? (first - (rr & 31)) * D + tile_part(rr & 31, d) : first * D + d);
-        for (int i0 = 0; i0 < blk.n_parts; i0 += 64) {
-            const int n = min(blk.n_parts - i0, 64);
-            const float2 ml = lane < n ? *reinterpret_cast<const float2 *>(a.part_ml + 2 * (first + (int64_t)(i0 + lane) * blk.stride)) : make_float2(-FLT_MAX, 0.f);
-            const float top = fmaxf(m, wave_max(ml.x)), before = l * __builtin_amdgcn_exp2f(m - top), w = ml.y * __builtin_amdgcn_exp2f(ml.x - top);
-            m = top;
-            l = before + wave_sum(w);
-            const float each = l == 0.f ? 0.f : 1.f / l;
-            o *= before * each;
-            for (int i = 0; i < n; i += AT_ONCE) {
-                const float f = __shfl(w, i + mine, 64) * each;  // (of a part that is not there: 0)
-                if (i + mine < n) o += *reinterpret_cast<const floatx4 *>(from + (int64_t)(i0 + i + mine) * blk.stride * D) * f;
+    for (int p0 = 0; p0 < total; p0 += 64) {
+        // the lane's part: its row of partial results, and where its values begin (less one and negative: in a tile's layout)
+        int row = 0, at = 0;
+        for (int k = 0; k < it.n_sources; ++k) {
+            const int i = p0 + lane - __builtin_amdgcn_readlane(begin, k), t = __builtin_amdgcn_readlane(tile_row, k);
+            if (i < 0) break;
+            row = __builtin_amdgcn_readlane(first, k) + i * __builtin_amdgcn_readlane(stride, k);
+            at = t < 0 ? row * D : ~((row - t) * D + t * 4);
+        }
+        const int n_now = min(total - p0, 64);
+        const float2 ml = lane < n_now ? *reinterpret_cast<const float2 *>(a.part_ml + 2 * (int64_t)row) : make_float2(-FLT_MAX, 0.f);
+        const float top = fmaxf(m, wave_max(ml.x)), before = l * __builtin_amdgcn_exp2f(m - top), w = ml.y * __builtin_amdgcn_exp2f(ml.x - top);
+        m = top;
+        l = before + wave_sum(w);
+        const float each = l == 0.f ? 0.f : 1.f / l;
+        o *= before * each;
+        for (int i0 = 0; i0 < n_now; i0 += AT_ONCE * AHEAD) {
+            floatx4 v[AHEAD];
+            float f[AHEAD];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                const int i = i0 + j * AT_ONCE + mine, where = __shfl(at, i, 64);
+                f[j] = __shfl(w, i, 64) * each;
+                v[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+                if (i < n_now) v[j] = *reinterpret_cast<const floatx4 *>(a.part_o + (where < 0 ? ~where + tile_d : where + d));
             }
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j)
+                if (i0 + j * AT_ONCE + mine < n_now) o += v[j] * f[j];
         }
     }
 #pragma unroll

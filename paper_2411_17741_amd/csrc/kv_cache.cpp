@@ -34,13 +34,20 @@ constexpr int SPARE_BATCHES = 2;
 constexpr int ROW_BLOCKS = 512, ROW_MIN_TOKENS = 512;
 // Tokens times head_dim up to which a wavefront may have an item to itself.
 constexpr int ROW_SHORT_VALUES = 16384;
+// ... in pages of 8 bits.  Heads of 128, 16384 -> this: 512 requests of about 100 tokens with 32 / 8 heads 39.9 -> 37.8 us, 128 of 120 19.0 -> 17.8, 256 of 400 56.2 -> 55.2; but 512 of 600 135 -> 138.
+constexpr int ROW_SHORT_E4M3 = 32768;
 // Tiles are cut into pieces of no fewer tokens than join work is worth -- fp32 products take 8 times as long --, or of half of that where there are few tiles.  Measured for fp32, 512 -> these:
 // prompts of 300, 1 and 77 tokens with 32 / 8 heads of 128, append and attention of two layers, 111 -> 76 us, with 6 / 2 108 -> 56, with 32 / 8 heads of 64 65 -> 56.
 constexpr int tile_min_tokens(const lora_kv_config_t &c) { return c.dtype == LORA_BF16 ? 512 : c.head_dim == 64 ? 256 : 128; }
 constexpr int PIECE_STEP = 64;  // pieces begin at multiples of it: a whole number of every kernel's steps, in one page or at the start of one
 constexpr int MAX_EXTRA = 2048;  // pieces beyond one for each block of rows
-// Prefixes: tokens from which sharing one is worth the join, of how many prefixes of prefixes a segment may have a part, tokens' places in all of them together (times max_batch_tokens)
-constexpr int SHARED_MIN_TOKENS = 256, SHARED_DEPTH = 7, SHARED_TOKENS = 2;
+// Of how many prefixes of prefixes a segment may have a part; tokens' places in all of them together (times max_batch_tokens); tokens of a piece of a prefix with few rows
+constexpr int SHARED_DEPTH = 7, SHARED_TOKENS = 2, SHARED_ROW_MIN_TOKENS = 256;
+// A prefix is worth it if the segments but one are spared more bytes of keys and values than these, and so many for each row of each head of 128, whose parts are written and read again.  (The bytes
+// that are spared would mostly have come out of caches.)  Measured, one by one -> shared, heads of 128, each request 100 tokens of its own behind the prefix: 64 requests with 32 / 8 heads
+// and 512 tokens, 132 MB, 25.0 -> 21.0 us, 256 tokens, 66 MB, 14.2 -> 16.3; 256 requests and 256 tokens, 267 MB, 41.5 -> 39.1, 128 tokens 34.9 -> 39.6; with 64 / 8 heads 512 tokens 57.4 -> 49.6, 256
+// 42.7 -> 48.8.  Of few rows: 2 requests with 40 / 40 heads and 1024 tokens, 21 MB, 14.2 -> 12.5, 512 tokens 12.2 -> 12.5.
+constexpr int64_t SHARED_FEW_BYTES = 16 << 20, SHARED_BYTES = 64 << 20, SHARED_ROW_BYTES = 14 << 10;
 
 struct Seq {
     int64_t id = 0;
@@ -390,9 +397,14 @@ void cut_block(AttnItem base, int32_t kv_len, int32_t piece, int32_t rows, int32
 
 // What segments of few rows have in common.  Larger ones fill tiles of their own: the products take as long, and there is nothing to join.  (Called before the
 // sequences grow: pages that are full by then stay as they are.)
-void find_prefixes(const lora_kv &kv, const Growth &g, Cut &cut)
+void find_prefixes(const lora_kv &kv, const Growth &g, int32_t min_tokens, Cut &cut)
 {
     const int32_t grp = kv.group();
+    const int64_t token_bytes = (int64_t)(kv.layer_bytes / kv.cfg.page_tokens);  // keys and values
+    const auto worth = [&](int64_t shared, int64_t segs, int64_t rows) {
+        if (min_tokens) return shared >= min_tokens;
+        return (segs - 1) * shared * token_bytes >= (rows <= lora::KV_ROW_ITEM ? SHARED_FEW_BYTES : SHARED_BYTES) + rows * kv.cfg.n_kv_heads * SHARED_ROW_BYTES * kv.cfg.head_dim / 128;
+    };
     struct Set {
         int32_t at, base, depth;  // pages that the segments have in common; those of them that are in prefixes already; how many these are
         std::vector<int32_t> segs;
@@ -424,7 +436,7 @@ void find_prefixes(const lora_kv &kv, const Growth &g, Cut &cut)
                 tokens += g.n_tokens[i];
             }
             const int32_t to = part.at & ~(std::max(PIECE_STEP >> kv.page_shift, 1) - 1);  // (what is behind a prefix begins where pieces may)
-            if (((int64_t)(to - part.base) << kv.page_shift) >= SHARED_MIN_TOKENS) {
+            if (to > part.base && worth((int64_t)(to - part.base) << kv.page_shift, (int64_t)part.segs.size(), tokens * grp)) {
                 if (tokens > room) continue;
                 room -= tokens;
                 cut.prefixes.push_back({part.base, to, part.segs, tokens * grp});
@@ -477,6 +489,12 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
         for (const Prefix &p : cut.prefixes)
             if (p.rows > lora::KV_ROW_ITEM) tokens += (p.rows + tile - 1) / tile * tokens_of(p), n_tiles += (p.rows + tile - 1) / tile;
         if (n_tiles * n_kv >= 2 * kv.n_cu && tokens >= 1024 * n_tiles) cut.way = lora::KV_TILES_TURNS;
+        // Prefixes, of which there are few tiles: as many pieces as compute units where each is long enough and the tiles' rows are there.  32 requests behind 100000 tokens with 64 / 8 heads
+        // 150 -> 136 us.
+        int64_t large = 0, small = 0;
+        for (const Prefix &p : cut.prefixes)
+            if (p.rows > lora::KV_ROW_ITEM) large += (p.rows + tile - 1) / tile * tokens_of(p), small += (p.rows + lora::KV_TILE - 1) / lora::KV_TILE * tokens_of(p);
+        if (large * n_kv >= 1024 * kv.n_cu && large * 2 <= small * 5 / 4) cut.way = lora::KV_TILES_TURNS;
     }
     if (cut.way != lora::KV_TILES_TURNS) tile = lora::KV_TILE;
     n_tiles = 0;
@@ -506,6 +524,11 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     // A tile that takes longer than all of a compute unit's share is cut, into pieces of half of that: two at a time are worked on
     const int64_t share = tile_tokens * n_kv / kv.n_cu;
     int32_t tile_piece = at_least(share / 2, tile_min), tile_whole = at_least(share, tile_min);
+    // Prefixes are joined anyway, and cut into as many pieces; but not into shorter ones than the rows beside them keep the machine busy with, three quarters of whose tokens for a compute unit
+    // take a tile about as long (256 requests of about 400 tokens behind 2000 with 32 / 8 heads: 4 pieces 93.6 us, 2 85.5, 1 80.2).
+    int32_t prefix_row_piece = at_least(row_tokens * n_kv / ROW_BLOCKS, SHARED_ROW_MIN_TOKENS);
+    int32_t prefix_tile_piece = at_least(cut.way == lora::KV_TILES_TURNS ? share : share / 2, tile_min);
+    if (cut.way != lora::KV_TILES_TURNS) prefix_tile_piece = std::max(prefix_tile_piece, at_least(row_tokens * n_kv / kv.n_cu * 3 / 4, 0));
     // No more blocks than compute units and no tile of over 1024 tokens: for heads of 64, whose steps are mostly instructions of one wavefront after the other, two groups of
     // wavefronts share a tile's tokens, and tiles stay whole (700 tokens with 32 heads 16.5 -> 12.5 us, with 32 / 8 heads 15.3 -> 12.3).  Longer ones, and heads of 128, do as well
     // or better with pieces.
@@ -544,7 +567,7 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
             for (int64_t r = 0; r < p.rows; r += rows_of) {
                 it.row0 = (int32_t)r;
                 it.n_rows = (int32_t)std::min(p.rows - r, (int64_t)rows_of);
-                cut_shared(it, p.from << kv.page_shift, p.to << kv.page_shift, tiles ? tile_piece : row_piece, tiles ? (it.n_rows + 31) & ~31 : it.n_rows, n_kv, tiles ? cut.tiles : cut.rows,
+                cut_shared(it, p.from << kv.page_shift, p.to << kv.page_shift, tiles ? prefix_tile_piece : prefix_row_piece, tiles ? (it.n_rows + 31) & ~31 : it.n_rows, n_kv, tiles ? cut.tiles : cut.rows,
                            cut.blocks, part);
             }
         }
@@ -580,9 +603,11 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
             continue;
         }
         if (part <= kv.part_rows && cut.joins.size() + cut.tile_joins.size() <= (size_t)MAX_EXTRA && (int64_t)(cut.rows.size() + cut.tiles.size()) <= max_items(kv.cfg)) break;
-        if (!cut.prefixes.empty() && row_piece == LORA_KV_MAX_TOKENS && tile_piece == LORA_KV_MAX_TOKENS) return false;
+        if (!cut.prefixes.empty() && row_piece == LORA_KV_MAX_TOKENS && tile_piece == LORA_KV_MAX_TOKENS && prefix_row_piece == LORA_KV_MAX_TOKENS && prefix_tile_piece == LORA_KV_MAX_TOKENS) return false;
         row_piece = at_least((int64_t)row_piece * 2, 0);
         tile_piece = at_least((int64_t)tile_piece * 2, 0);
+        prefix_row_piece = at_least((int64_t)prefix_row_piece * 2, 0);
+        prefix_tile_piece = at_least((int64_t)prefix_tile_piece * 2, 0);
         tile_whole = std::max(tile_whole, tile_piece);
     }
     // Three blocks on a compute unit, where the tiles fill more than three for each, or more than two and are short (256 tokens in the mean): bf16 heads of 128, two blocks -> three,
@@ -600,7 +625,9 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     // loads and its last stores.  Measured: 512 requests of 20 tokens with 32 heads of 128 96 -> 51 us, 256 of 120 94 -> 78 us; with 200 to 450 tokens, and
     // with half as many for heads of 256, nothing is gained.
     size_t n_short = 0;
-    while (n_short < cut.rows.size() && cut.rows[cut.rows.size() - 1 - n_short].part < 0 && cut.rows[cut.rows.size() - 1 - n_short].kv1 <= ROW_SHORT_VALUES / kv.cfg.head_dim) ++n_short;
+    const int32_t short_tokens = (kv.e4m3() ? ROW_SHORT_E4M3 : ROW_SHORT_VALUES) / kv.cfg.head_dim;
+    const auto is_short = [&](const AttnItem &it) { return (it.part < 0 || !cut.prefixes.empty()) && it.kv1 - it.kv0 <= short_tokens; };
+    while (n_short < cut.rows.size() && is_short(cut.rows[cut.rows.size() - 1 - n_short])) ++n_short;
     cut.n_short = (int64_t)n_short * n_kv > 2 * kv.n_cu ? (int32_t)n_short : 0;
     // Tiles are worked on two at a time on a compute unit, block b beside block b + n_cu: the longest go with the shortest of the first two rounds
     // (2048 tokens with 32 / 8 heads: 70 -> 55 us).
@@ -980,7 +1007,7 @@ int lora_kv_stats(const lora_kv_t *kv, lora_kv_stats_t *out)
 
 // ---- batches --------------------------------------------------------------------------------
 
-static int create_batch(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, const int32_t *seg_offsets, void *stream, bool shared, lora_kv_batch_t **out)
+static int create_batch(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, const int32_t *seg_offsets, void *stream, int32_t shared, lora_kv_batch_t **out)
 {
     if (!out) return LORA_E_INVAL;
     *out = nullptr;
@@ -1025,7 +1052,7 @@ static int create_batch(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, co
             cut.page0[i] = page0;
             if (g.n_tokens[i]) page0 += (int32_t)(((int64_t)g.seqs[i]->n_tokens + g.n_tokens[i] + kv->cfg.page_tokens - 1) >> kv->page_shift);
         }
-        if (shared) find_prefixes(*kv, g, cut);
+        if (shared >= 0) find_prefixes(*kv, g, shared, cut);
         // cut_attention sees the lengths after the growth; they are put back if it runs out of host memory
         for (int32_t i = 0; i < n_seg; ++i) g.seqs[i]->n_tokens += g.n_tokens[i];
         try {
@@ -1113,12 +1140,13 @@ static int create_batch(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, co
 
 int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, const int32_t *seg_offsets, void *stream, lora_kv_batch_t **out)
 {
-    return create_batch(kv, n_seg, seg_seq, seg_offsets, stream, false, out);
+    return create_batch(kv, n_seg, seg_seq, seg_offsets, stream, -1, out);
 }
 
-int lora_kv_batch_create_shared(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, const int32_t *seg_offsets, void *stream, lora_kv_batch_t **out)
+int lora_kv_batch_create_shared(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, const int32_t *seg_offsets, int32_t min_tokens, void *stream, lora_kv_batch_t **out)
 {
-    return create_batch(kv, n_seg, seg_seq, seg_offsets, stream, true, out);
+    if (out) *out = nullptr;
+    return min_tokens < 0 ? LORA_E_INVAL : create_batch(kv, n_seg, seg_seq, seg_offsets, stream, min_tokens, out);
 }
 
 int lora_kv_batch_destroy(lora_kv_t *kv, lora_kv_batch_t *handle)
@@ -1225,6 +1253,7 @@ int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *handle, int32_t layer, const 
     a.page_stride = (int64_t)kv->page_bytes;
     a.page_list = reinterpret_cast<const int32_t *>(batch->dev + batch->off_pages);
     a.row_tokens = reinterpret_cast<const int32_t *>(batch->dev + batch->off_row_tokens);
+    a.prefixes = batch->n_shared_joins != 0;
     a.part_o = kv->part_o, a.part_ml = kv->part_ml;
     a.scale_log2 = scale_log2;
     a.n_kv = c.n_kv_heads, a.group = kv->group(), a.page_shift = kv->page_shift;

@@ -2,7 +2,7 @@
 shapes and strides of the tensors it is given.  No arithmetic of the method happens here."""
 from __future__ import annotations
 
-from typing import Optional
+from typing import Optional, Union
 
 import torch
 
@@ -119,10 +119,14 @@ class KvCache:
         return st
 
     # -- batches --------------------------------------------------------------------------
-    def batch(self, seg_seq, seg_offsets, stream: Optional[torch.cuda.Stream] = None, shared: bool = False):
-        """shared: attention reads pages that sequences of the batch share once for all of them, where that is worth it"""
-        rc, b = (B.lora_kv_batch_create_shared if shared else B.lora_kv_batch_create)(self.handle, seg_seq, seg_offsets, self._stream(stream))
-        B.check(rc, "lora_kv_batch_create_shared" if shared else "lora_kv_batch_create")
+    def batch(self, seg_seq, seg_offsets, stream: Optional[torch.cuda.Stream] = None, shared: Union[bool, int] = False):
+        """shared: attention reads pages that sequences of the batch share once for all of them, where that is worth it (True), or from so many shared tokens on (a number)."""
+        if shared is False:
+            rc, b = B.lora_kv_batch_create(self.handle, seg_seq, seg_offsets, self._stream(stream))
+            B.check(rc, "lora_kv_batch_create")
+        else:
+            rc, b = B.lora_kv_batch_create_shared(self.handle, seg_seq, seg_offsets, 0 if shared is True else int(shared), self._stream(stream))
+            B.check(rc, "lora_kv_batch_create_shared")
         b.n_tokens = int(seg_offsets[-1])
         return b
 

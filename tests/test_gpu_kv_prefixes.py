@@ -21,7 +21,7 @@ def _mods():
 class Tree:
     """Requests given as (parent, tokens of the parent or -1, own cached tokens, new tokens); a request with 0 new tokens is no part of the batch but keeps its pages."""
 
-    def __init__(self, requests, heads, kv, dim, page=64, kind="bf16", seed=0, layers=1, shared=True, beyond=None, order=None, **kw):
+    def __init__(self, requests, heads, kv, dim, page=64, kind="bf16", seed=0, layers=1, shared=256, beyond=None, order=None, **kw):
         B, KvCache = _mods()
         self.B, self.heads, self.kv, self.dim, self.page, self.kind = B, heads, kv, dim, page, kind
         length = []
@@ -294,7 +294,7 @@ def test_batches_in_a_row_and_layers(kind):
             ids = np.asarray([int(i) for i in rng.permutation(list(lengths))])
             off = np.concatenate([[0], np.cumsum([lengths[i] for i in ids])]).astype(np.int32)
             T = int(off[-1])
-            plans = [c.batch(ids, off, shared=k == 0) for k, c in enumerate(caches)]
+            plans = [c.batch(ids, off, shared=256 if k == 0 else False) for k, c in enumerate(caches)]
             assert (B.lora_kv_batch_prefixes(plans[0])[1].n_prefixes > 0) == (it > 0) and B.lora_kv_batch_prefixes(plans[1])[1].n_prefixes == 0
             for layer in range(2):
                 x = torch.randn(T, 12, 64, generator=gen, device="cuda").to(dt)
@@ -364,6 +364,23 @@ def test_what_is_shared():
     assert info([(None, -1, 320, 0), (0, -1, 320, 0)] + [(1, -1, i, 1) for i in range(3)] + [(0, -1, i, 1) for i in range(3)]) == (2, 6, 640)
 
 
+def test_what_is_worth_it():
+    """Without a number of tokens the library shares what saves more bytes than the parts cost: 2 or 64 requests, long prefixes and short ones."""
+    def prefixes(n, tokens, heads, kv, shared, **kw):
+        t = Tree(forks(n, tokens, lambda i: 3), heads, kv, 128, shared=shared, **kw)
+        try:
+            return t.info().n_prefixes
+        finally:
+            t.close()
+
+    for kind, times in (("bf16", 1), ("e4m3", 2)):
+        assert prefixes(64, 512 * times, 32, 8, True, kind=kind) == 1 and prefixes(64, 256 * times - 64, 32, 8, True, kind=kind) == 0
+        assert prefixes(2, 1024 * times, 40, 40, True, kind=kind) == 1 and prefixes(2, 512 * times, 40, 40, True, kind=kind) == 0
+        assert prefixes(2, 64, 40, 40, 64, kind=kind) == 1 and prefixes(2, 64, 40, 40, 65, kind=kind) == 0 and prefixes(2, 64, 40, 40, 1, kind=kind) == 1
+    _check(forks(64, 1024, lambda i: i % 50), 32, 8, 128, 1, 64, kind="bf16", shared=True, seed=18)
+    _check(forks(3, 130, lambda i: i), 4, 2, 64, 1, 3, kind="bf16", shared=1, seed=19)
+
+
 def test_no_room_for_the_parts():
     """More rows than the memory for partial results has room for: the requests are worked on one by one, as if nothing were shared."""
     t = Tree(forks(520, 300, lambda i: 1), 64, 64, 256, page=32, seed=17)
@@ -388,6 +405,7 @@ def test_refusals():
         assert create(cache.handle, [0, 0], [0, 1, 2])[0] == B.LORA_E_INVAL and create(cache.handle, [7], [0, 1])[0] == B.LORA_E_NOTFOUND
         assert create(cache.handle, [0, 1], [0, 2, 1])[0] == B.LORA_E_INVAL and create(cache.handle, [0, 1, 2], [0, 1, 2, 3])[0] == B.LORA_E_NOMEM
         assert create(cache.handle, [0], [0, 41])[0] == B.LORA_E_NOMEM and create(None, [0], [0, 1])[0] == B.LORA_E_INVAL
+        assert create(cache.handle, [0], [0, 1], -1)[0] == B.LORA_E_INVAL
         b = cache.batch([0], [0, 0], shared=True)
         assert B.lora_kv_batch_prefixes(b)[1].n_prefixes == 0
         cache.batch_destroy(b)
