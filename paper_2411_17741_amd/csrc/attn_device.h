@@ -1580,19 +1580,21 @@ __global__ __launch_bounds__(256) void attn_join_tiles_kernel(JoinArgs a)
     for (int k = 0; k < N; ++k) put_four(out + (k * 4 + threadIdx.x / 64) * 8 + lane / 32 * 4, l == 0.f ? o[k] / l : o[k]);
 }
 
-// Joins the parts of rows whose segments share prefixes: a wavefront to a row.  Lanes find the row's sources all at once, then each a part of theirs and its maximum and sum; then D / 4 lanes
-// have a part's values, eight loads on their way at a time.  Trips to memory one after the other, as in the joins above.
+// Joins the parts of rows of batches with shared prefixes: D / 4 lanes to a row, 64 / (D / 4) rows to a wavefront.  A row's lanes find its sources all at once, then each a part of theirs
+// with its maximum and sum; then each has 4 values of part after part, eight loads on their way at a time.  Bound by trips to memory one after the other, as the joins above are.
+template <int D> constexpr int SHARED_JOIN_ROWS = 4 * 256 / D;  // of a block
 template <typename E, int D>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedJoinArgs a)
 {
-    constexpr int PER = D / 4, AT_ONCE = 64 / PER, AHEAD = 8;  // lanes of a part's values; parts that the lanes have at a time; ... loads
+    constexpr int PER = D / 4, AHEAD = 8;
     const SharedJoin it = a.items[blockIdx.x / a.n_kv];
-    const int kv_head = blockIdx.x % a.n_kv, r = blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (r >= it.n_rows) return;
-    // lane k: source k's first part of the row, of how many
+    const int kv_head = blockIdx.x % a.n_kv, lane = threadIdx.x & 63, j = lane % PER, base = lane - j, at_row = blockIdx.y * SHARED_JOIN_ROWS<D> + threadIdx.x / PER;
+    if ((int)(blockIdx.y * SHARED_JOIN_ROWS<D> + (threadIdx.x & ~63u) / PER) >= it.n_rows) return;  // (a wavefront's first row)
+    const int r = it.first + min(at_row, it.n_rows - 1);  // of the rows that the sources are of; rows behind the last are that, and stored by none
+    // lane k of a row: source k's first part of the row, of how many
     int first = 0, stride = 0, n = 0, tile_row = -1;  // tile_row: the row of 32 in a tile's layout, or -1
-    if (lane < it.n_sources) {
-        const SharedSource src = a.sources[it.source0 + lane];
+    if (j < it.n_sources) {
+        const SharedSource src = a.sources[it.source0 + j];
         const int row = src.row0 + r, at = row / src.rows, rr = row - at * src.rows;
         const SharedBlock blk = a.blocks[src.block0 + at];
         first = blk.part + kv_head * (src.tile ? (blk.n_rows + 31) & ~31 : blk.n_rows) + rr;
@@ -1601,48 +1603,50 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedJoinArgs a)
     }
     int total = 0, begin = 0;  // parts of all sources; of those before the lane's
     for (int k = 0; k < it.n_sources; ++k) {
-        if (lane == k) begin = total;
-        total += __builtin_amdgcn_readlane(n, k);
+        if (j == k) begin = total;
+        total += __shfl(n, base + k, 64);
     }
-    const int mine = lane / PER, d = lane % PER * 4, tile_d = (d / 8 * 64 + d / 4 % 2 * 32) * 4;
+    const int d = j * 4, tile_d = (d / 8 * 64 + d / 4 % 2 * 32) * 4;
     float m = -FLT_MAX, l = 0.f;
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int p0 = 0; p0 < total; p0 += 64) {
+    for (int p0 = 0; __any(p0 < total); p0 += PER) {
         // the lane's part: its row of partial results, and where its values begin (less one and negative: in a tile's layout)
         int row = 0, at = 0;
         for (int k = 0; k < it.n_sources; ++k) {
-            const int i = p0 + lane - __builtin_amdgcn_readlane(begin, k), t = __builtin_amdgcn_readlane(tile_row, k);
-            if (i < 0) break;
-            row = __builtin_amdgcn_readlane(first, k) + i * __builtin_amdgcn_readlane(stride, k);
-            at = t < 0 ? row * D : ~((row - t) * D + t * 4);
+            const int i = p0 + j - __shfl(begin, base + k, 64), t = __shfl(tile_row, base + k, 64), from = __shfl(first, base + k, 64) + i * __shfl(stride, base + k, 64);
+            if (i >= 0) row = from, at = t < 0 ? from * D : ~((from - t) * D + t * 4);
         }
-        const int n_now = min(total - p0, 64);
-        const float2 ml = lane < n_now ? *reinterpret_cast<const float2 *>(a.part_ml + 2 * (int64_t)row) : make_float2(-FLT_MAX, 0.f);
-        const float top = fmaxf(m, wave_max(ml.x)), before = l * __builtin_amdgcn_exp2f(m - top), w = ml.y * __builtin_amdgcn_exp2f(ml.x - top);
+        const int n_now = min(total - p0, PER);
+        const float2 ml = j < n_now ? *reinterpret_cast<const float2 *>(a.part_ml + 2 * (int64_t)row) : make_float2(-FLT_MAX, 0.f);
+        float top = fmaxf(m, ml.x);
+#pragma unroll
+        for (int off = PER / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+        const float before = l * __builtin_amdgcn_exp2f(m - top), w = ml.y * __builtin_amdgcn_exp2f(ml.x - top);
         m = top;
-        l = before + wave_sum(w);
+        l = w;
+#pragma unroll
+        for (int off = PER / 2; off > 0; off >>= 1) l += __shfl_xor(l, off, 64);
+        l += before;
         const float each = l == 0.f ? 0.f : 1.f / l;
         o *= before * each;
-        for (int i0 = 0; i0 < n_now; i0 += AT_ONCE * AHEAD) {
+        for (int i0 = 0; __any(i0 < n_now); i0 += AHEAD) {
             floatx4 v[AHEAD];
             float f[AHEAD];
 #pragma unroll
-            for (int j = 0; j < AHEAD; ++j) {
-                const int i = i0 + j * AT_ONCE + mine, where = __shfl(at, i, 64);
-                f[j] = __shfl(w, i, 64) * each;
-                v[j] = floatx4{0.f, 0.f, 0.f, 0.f};
-                if (i < n_now) v[j] = *reinterpret_cast<const floatx4 *>(a.part_o + (where < 0 ? ~where + tile_d : where + d));
+            for (int i = 0; i < AHEAD; ++i) {
+                const int from = base + ((i0 + i) & (PER - 1)), where = __shfl(at, from, 64);
+                f[i] = __shfl(w, from, 64) * each;
+                v[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+                if (i0 + i < n_now) v[i] = *reinterpret_cast<const floatx4 *>(a.part_o + (where < 0 ? ~where + tile_d : where + d));
             }
 #pragma unroll
-            for (int j = 0; j < AHEAD; ++j)
-                if (i0 + j * AT_ONCE + mine < n_now) o += v[j] * f[j];
+            for (int i = 0; i < AHEAD; ++i)
+                if (i0 + i < n_now) o += v[i] * f[i];
         }
     }
-#pragma unroll
-    for (int off = 32; off >= PER; off >>= 1)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], off, 64);
-    if (mine == 0) put_four(static_cast<E *>(a.out) + (int64_t)(it.tok0 + r / a.group) * a.out_stride + (kv_head * a.group + r % a.group) * D + d, l == 0.f ? o / l : o);
+    const int to = it.row0 + r;
+    if (at_row < it.n_rows)
+        put_four(static_cast<E *>(a.out) + (int64_t)(it.tok0 + to / a.group) * a.out_stride + (kv_head * a.group + to % a.group) * D + d, l == 0.f ? o / l : o);
 }
 
 }  // namespace lora

@@ -95,7 +95,7 @@ hipError_t launch_shared_join(const SharedJoinArgs &a, int dtype, int dim, hipSt
     return by_type(dtype, dim, [&](auto e, auto d) {
         typedef decltype(e) E;
         constexpr int D = decltype(d)::value;
-        hipLaunchKernelGGL((shared_join_kernel<E, D>), dim3(a.n_items * a.n_kv, (a.max_rows + 3) / 4), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((shared_join_kernel<E, D>), dim3(a.n_items * a.n_kv, (a.max_rows + SHARED_JOIN_ROWS<D> - 1) / SHARED_JOIN_ROWS<D>), dim3(256), 0, st, a);
     });
 }
 

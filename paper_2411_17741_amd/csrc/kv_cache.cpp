@@ -212,13 +212,20 @@ int64_t max_items(const lora_kv_config_t &c)
     return (int64_t)c.max_batch_tokens * g / lora::KV_TILE + c.max_batch_seqs + MAX_EXTRA;
 }
 
+// Of segments with prefixes, fewer rows than a tile's each, and of blocks that are cut beside them
+int64_t max_shared_joins(const lora_kv_config_t &c)
+{
+    const int64_t g = c.n_heads / c.n_kv_heads;
+    return (int64_t)c.max_batch_tokens * g / lora::KV_JOIN_ROWS + c.max_batch_seqs + MAX_EXTRA;
+}
+
 size_t list_bytes(const lora_kv_config_t &c)
 {
     const size_t T = c.max_batch_tokens;
     return align_up(T * sizeof(KvToken)) + align_up(T * sizeof(KvGroup)) + align_up((size_t)c.max_batch_pages * 4) +
            align_up((size_t)max_items(c) * sizeof(AttnItem)) + align_up((size_t)MAX_EXTRA * sizeof(JoinItem)) + 3 * ALIGN +
-           align_up(T * SHARED_TOKENS * 4) + align_up((size_t)max_items(c) * sizeof(SharedBlock)) + align_up((size_t)c.max_batch_seqs * (SHARED_DEPTH + 1) * sizeof(SharedSource)) +
-           align_up((size_t)c.max_batch_seqs * sizeof(SharedJoin));
+           align_up(T * SHARED_TOKENS * 4) + align_up((size_t)max_items(c) * sizeof(SharedBlock)) + align_up(((size_t)c.max_batch_seqs * (SHARED_DEPTH + 1) + MAX_EXTRA) * sizeof(SharedSource)) +
+           align_up((size_t)max_shared_joins(c) * sizeof(SharedJoin));
 }
 
 // The cache's device is the current one as long as this lives: events, the default stream and kernels are the current device's.
@@ -364,7 +371,8 @@ struct Cut {
     std::vector<SharedSource> sources;
     std::vector<SharedBlock> blocks;
     std::vector<SharedJoin> shared_joins;
-    int32_t prefix_row_items = 0, prefix_tile_items = 0;
+    int32_t prefix_row_items = 0, prefix_tile_items = 0, prefix_segments = 0;
+    int32_t extra_joins = 0;  // blocks that share nothing and are joined with the others
     lora::KvTiles way = lora::KV_TILES_PLAIN;
     int32_t n_short = 0;  // of the rows' items, at the list's end
     std::vector<AttnItem> rows, tiles;
@@ -551,7 +559,13 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
         cut.sources.clear();
         cut.blocks.clear();
         cut.shared_joins.clear();
+        cut.prefix_segments = 0;
         part = 0;
+        cut.extra_joins = 0;
+        const auto put_joins = [&](int32_t tok0, int32_t row0, int32_t rows_of, int32_t n_sources) {
+            for (int32_t r = 0; r < rows_of; r += lora::KV_JOIN_ROWS)
+                cut.shared_joins.push_back({tok0, row0, r, std::min(rows_of - r, (int32_t)lora::KV_JOIN_ROWS), (int32_t)cut.sources.size(), n_sources});
+        };
         // prefixes first, then the segments' own tokens: what of a prefix a segment's rows are, by prefix and segment
         std::vector<std::vector<SharedSource>> of_segment(cut.own.size());
         for (const Prefix &p : cut.prefixes) {
@@ -582,19 +596,28 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
                 of_segment[i].push_back({0, (int32_t)cut.blocks.size(), lora::KV_TILE, tiles});
                 cut_shared(it, (int32_t)from_of(i), (int32_t)(ctx + n), tiles ? tile_piece : row_piece, tiles ? (it.n_rows + 31) & ~31 : it.n_rows, n_kv, tiles ? cut.tiles : cut.rows, cut.blocks,
                            part);
-                cut.shared_joins.push_back({offsets[i], (int32_t)rows, (int32_t)cut.sources.size(), (int32_t)of_segment[i].size()});
+                put_joins(offsets[i], 0, (int32_t)rows, (int32_t)of_segment[i].size());
+                ++cut.prefix_segments;
                 cut.sources.insert(cut.sources.end(), of_segment[i].begin(), of_segment[i].end());
                 continue;
             }
+            // what is cut beside segments with prefixes is joined by their launch
+            const auto cut_one = [&](int32_t end, int32_t piece, int32_t block_rows, std::vector<AttnItem> &items, std::vector<JoinItem> &joins, bool tiles) {
+                if (cut.prefixes.empty() || end <= piece) return cut_block(it, end, piece, block_rows, n_kv, items, joins, part);
+                put_joins(it.tok0, it.row0, it.n_rows, 1);
+                ++cut.extra_joins;
+                cut.sources.push_back({0, (int32_t)cut.blocks.size(), (int32_t)tile, tiles});
+                cut_shared(it, 0, end, piece, block_rows, n_kv, items, cut.blocks, part);
+            };
             if (rows <= lora::KV_ROW_ITEM) {
-                cut_block(it, (int32_t)(ctx + n), row_piece, it.n_rows, n_kv, cut.rows, cut.joins, part);
+                cut_one((int32_t)(ctx + n), row_piece, it.n_rows, cut.rows, cut.joins, false);
                 continue;
             }
             for (int64_t r = 0; r < rows; r += tile) {
                 it.row0 = (int32_t)r;
                 it.n_rows = (int32_t)std::min(rows - r, tile);
                 const int32_t end = tile_end(ctx, rows, r);
-                cut_block(it, end, end > tile_whole ? tile_piece : end, (it.n_rows + 31) & ~31, n_kv, cut.tiles, cut.tile_joins, part);
+                cut_one(end, end > tile_whole ? tile_piece : end, (it.n_rows + 31) & ~31, cut.tiles, cut.tile_joins, true);
             }
         }
         if (cut.way == lora::KV_TILES_PAIRS && (int64_t)(cut.tiles.size() + cut.rows.size()) * n_kv > kv.n_cu) {
@@ -602,7 +625,7 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
             tile_whole = at_least(share, tile_min);
             continue;
         }
-        if (part <= kv.part_rows && cut.joins.size() + cut.tile_joins.size() <= (size_t)MAX_EXTRA && (int64_t)(cut.rows.size() + cut.tiles.size()) <= max_items(kv.cfg)) break;
+        if (part <= kv.part_rows && (int64_t)(cut.joins.size() + cut.tile_joins.size()) + cut.extra_joins <= MAX_EXTRA && (int64_t)cut.shared_joins.size() <= max_shared_joins(kv.cfg) && (int64_t)(cut.rows.size() + cut.tiles.size()) <= max_items(kv.cfg)) break;
         if (!cut.prefixes.empty() && row_piece == LORA_KV_MAX_TOKENS && tile_piece == LORA_KV_MAX_TOKENS && prefix_row_piece == LORA_KV_MAX_TOKENS && prefix_tile_piece == LORA_KV_MAX_TOKENS) return false;
         row_piece = at_least((int64_t)row_piece * 2, 0);
         tile_piece = at_least((int64_t)tile_piece * 2, 0);
@@ -1128,9 +1151,9 @@ static int create_batch(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, co
         b->stale = false;
         ++kv->alive_batches;
         std::lock_guard<std::mutex> lock(g_lock);
-        b->info = {T, n_seg, (int32_t)n_pages, (int32_t)groups.size(), (int32_t)cut.rows.size(), (int32_t)cut.tiles.size(), (int32_t)(cut.joins.size() + cut.tile_joins.size()),
+        b->info = {T, n_seg, (int32_t)n_pages, (int32_t)groups.size(), (int32_t)cut.rows.size(), (int32_t)cut.tiles.size(), (int32_t)(cut.joins.size() + cut.tile_joins.size()) + cut.extra_joins,
                    cut.n_short, (int32_t)cut.way};
-        b->prefixes = {(int32_t)cut.prefixes.size(), b->n_shared_joins, cut.prefix_row_items, cut.prefix_tile_items, 0};
+        b->prefixes = {(int32_t)cut.prefixes.size(), cut.prefix_segments, cut.prefix_row_items, cut.prefix_tile_items, 0};
         for (const Prefix &p : cut.prefixes) b->prefixes.n_tokens += (int64_t)(p.to - p.from) << kv->page_shift;
         b->name = ++g_names << NAME_BITS | (uint64_t)(b - kv->batches.data());
         *out = reinterpret_cast<lora_kv_batch_t *>((uintptr_t)b->name);

@@ -50,8 +50,9 @@ struct AttnItem {
 
 constexpr int KV_SHARED = LORA_KV_MAX_TOKENS;  // (no segment's first token stands there)
 
-// Segments with shared prefixes: every part of what a row attends to -- prefixes, the segment's own tokens -- is a source of partial results, which lie in
-// blocks of rows: row r of the segment is row (row0 + r) % rows of block block0 + (row0 + r) / rows.
+// Batches with shared prefixes: every part of what a row attends to -- prefixes, the segment's own tokens -- is a source of partial results, which lie in
+// blocks of rows: row r of the source is row (row0 + r) % rows of block block0 + (row0 + r) / rows.  A join puts together rows first .. first + n_rows - 1 of its sources (KV_JOIN_ROWS at
+// most), which are rows row0 + first .. of a segment.
 struct SharedSource {
     int32_t row0, block0, rows, tile;  // tile: laid out as a tile's
 };
@@ -59,8 +60,9 @@ struct SharedBlock {
     int32_t part, n_parts, stride, n_rows;
 };
 struct SharedJoin {
-    int32_t tok0, n_rows, source0, n_sources;
+    int32_t tok0, row0, first, n_rows, source0, n_sources;
 };
+constexpr int KV_JOIN_ROWS = 16;
 
 // Rows whose pieces are joined: n_parts pieces, `stride` rows of partial results apart.
 struct JoinItem {

@@ -136,8 +136,11 @@ class KvCache:
     def _rows(self, t: torch.Tensor, name: str, n: int, heads: int):
         """(address, values between tokens) of [n][heads][head_dim] or [n][heads * head_dim], the heads of a token one after the other"""
         d, shape, stride = self.head_dim, t.shape, t.stride()
-        flat = len(shape) == 2 and shape[1] == heads * d and stride[1] == 1
-        if not (flat or (len(shape) == 3 and shape[1] == heads and shape[2] == d and stride[2] == 1 and (stride[1] == d or heads == 1))):
+        if len(shape) == 3:
+            fits = shape[1] == heads and shape[2] == d and stride[2] == 1 and (stride[1] == d or heads == 1)
+        else:
+            fits = len(shape) == 2 and shape[1] == heads * d and stride[1] == 1
+        if not fits:
             raise ValueError(f"{name}: [{n}][{heads}][{d}] with the heads of a token in a row is wanted, got {tuple(shape)}, strides {stride}")
         if shape[0] != n or t.dtype is not self.dtype or t.get_device() != self._index:
             raise ValueError(f"{name}: {n} tokens of {self.dtype} on {self.device} are wanted, got {tuple(shape)} of {t.dtype} on {t.device}")
@@ -148,13 +151,13 @@ class KvCache:
                q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6) -> None:
         """rope: [positions][rope_dim] fp32, the cosines of a position and then its sines.  q_out: q itself if not given.  q_norm, k_norm: the weights, fp32, of norms
         of every head of the queries and keys before they turn: [head_dim], or [heads][head_dim] with weights of each head's own."""
-        rows = self._rows
-        kp, ks = rows(k, "k", batch.n_tokens, self.n_kv_heads)
-        vp, vs = rows(v, "v", batch.n_tokens, self.n_kv_heads)
+        rows, n, heads, kv_heads = self._rows, batch.n_tokens, self.n_heads, self.n_kv_heads
+        kp, ks = rows(k, "k", n, kv_heads)
+        vp, vs = rows(v, "v", n, kv_heads)
         qp = qs = op = os_ = 0
         if q is not None:
-            qp, qs = rows(q, "q", batch.n_tokens, self.n_heads)
-            op, os_ = (qp, qs) if q_out is None else rows(q_out, "q_out", batch.n_tokens, self.n_heads)
+            qp, qs = rows(q, "q", n, heads)
+            op, os_ = (qp, qs) if q_out is None else rows(q_out, "q_out", n, heads)
         elif q_out is not None:
             raise ValueError("q_out without q")
         rp = rn = rd = 0
@@ -162,24 +165,28 @@ class KvCache:
             if rope.dim() != 2 or rope.dtype != torch.float32 or rope.get_device() != self._index or not rope.is_contiguous():
                 raise ValueError(f"rope: a contiguous fp32 tensor [positions][rope_dim] on {self.device} is wanted")
             rp, (rn, rd) = rope.data_ptr(), rope.shape
-        args = (self.handle, batch, layer, kp, vp, ks, vs, qp, op, qs, os_, rp, min(rn, 2**31 - 1), rd, B.LORA_ROPE_NEIGHBOURS if neighbours else B.LORA_ROPE_HALVES)
+            rn = min(rn, 2**31 - 1)
+        pairs = B.LORA_ROPE_NEIGHBOURS if neighbours else B.LORA_ROPE_HALVES
         if q_norm is None and k_norm is None:
-            B.check(B.lora_kv_append(*args, self._stream(stream)), "lora_kv_append")
+            B.check(B.lora_kv_append(self.handle, batch, layer, kp, vp, ks, vs, qp, op, qs, os_, rp, rn, rd, pairs, self._stream(stream)), "lora_kv_append")
             return
         if q_norm is not None and q is None:
             raise ValueError("q_norm without q")
-        qw, qws = self._weights(q_norm, "q_norm", self.n_heads)
-        kw, kws = self._weights(k_norm, "k_norm", self.n_kv_heads)
-        B.check(B.lora_kv_append_norm(*args, qw, kw, qws, kws, eps, self._stream(stream)), "lora_kv_append_norm")
+        qw, qws = self._weights(q_norm, "q_norm", heads)
+        kw, kws = self._weights(k_norm, "k_norm", kv_heads)
+        B.check(B.lora_kv_append_norm(self.handle, batch, layer, kp, vp, ks, vs, qp, op, qs, os_, rp, rn, rd, pairs, qw, kw, qws, kws, eps, self._stream(stream)), "lora_kv_append_norm")
 
     def _weights(self, w: Optional[torch.Tensor], name: str, heads: int):
         """(address, values between heads) of a norm's weights [head_dim] or [heads][head_dim]"""
         if w is None:
             return 0, 0
-        d, shape = self.head_dim, tuple(w.shape)
-        if shape not in ((d,), (heads, d)) or w.dtype != torch.float32 or w.get_device() != self._index or w.stride(-1) != 1:
-            raise ValueError(f"{name}: fp32 weights [{d}] or [{heads}][{d}] on {self.device} are wanted, got {shape} of {w.dtype} on {w.device}")
-        return w.data_ptr(), w.stride(0) if len(shape) == 2 and heads > 1 else 0
+        shape, stride = w.shape, w.stride()
+        if w.dtype is torch.float32 and w.get_device() == self._index and shape[-1:] == (self.head_dim,) and stride[-1] == 1:
+            if len(shape) == 1:
+                return w.data_ptr(), 0
+            if len(shape) == 2 and shape[0] == heads:
+                return w.data_ptr(), stride[0] if heads > 1 else 0
+        raise ValueError(f"{name}: fp32 weights [{self.head_dim}] or [{heads}][{self.head_dim}] on {self.device} are wanted, got {tuple(shape)} of {w.dtype} on {w.device}")
 
     def attend(self, batch, layer: int, q: torch.Tensor, out: torch.Tensor, scale: float, stream: Optional[torch.cuda.Stream] = None) -> None:
         qp, qs = self._rows(q, "q", batch.n_tokens, self.n_heads)
