@@ -753,84 +753,81 @@ template <typename E, int D, int STRIDE> struct Steps {
 };
 
 // The same for pages of 8-bit values, for stages of TK tokens, STRIDE apart, by LOADERS wavefronts.  Their way to LDS leads through registers, where they become bf16 with their tokens' units:
-// what comes to LDS was asked for a step before.  A thread has N chunks of keys, 16 values of a token each, and N chunks of values, 16 tokens of one value; the tokens of the
-// latter are the same for all of a wavefront, their units scalars.  (Heads of 64 have chunks for half the threads: two wavefronts bring keys, two values.)  The work
-// is done in pieces that fall beside the products of the step.
+// what comes to LDS was asked for a step before.  A thread has N chunks of keys, 16 values of a token each, and N chunks of values, 16 tokens of one value (heads of 64: half a chunk of
+// both); the tokens of the latter are the same for all of a wavefront, their units scalars.  The work is done in pieces that fall beside the products of the step.
 template <int D, int TK, int STRIDE, int LOADERS = 4> struct StagesE4m3 {
-    static constexpr int ALL = D * TK / 16, THREADS = 64 * LOADERS, N = ALL < THREADS ? 1 : ALL / THREADS, PIECES = 6 * N;
+    static constexpr int ALL = D * TK / 16, THREADS = 64 * LOADERS, N = ALL < THREADS ? 1 : ALL / THREADS;
     static constexpr bool HALVES = ALL < THREADS;
-    static_assert(HALVES ? ALL * 2 == THREADS && LOADERS == 4 : ALL % THREADS == 0, "the threads' chunks");
+    static constexpr int WORDS = HALVES ? 2 : 4, PIECES = N * (WORDS + WORDS / 2);  // of 4 values, 8 keys
+    static_assert(HALVES ? ALL * 2 == THREADS && TK == 32 : ALL % THREADS == 0, "the threads' chunks");
+    typedef std::conditional_t<HALVES, uint2, uint4> Part;
     PageList pages;
     const char *keys_at, *values_at;  // the head's in page 0, and the thread's first chunk of them
     const char *k_units_at, *v_units_at;
     uint32_t page_stride;
-    int page_shift, loader, w, row, tok, t0, page[2], at;
-    uint4 k[N], v[N], units[N], out;
+    int page_shift, w, row, t0, page[2];
+    Part k[N], v[N], units[N];
+    uint4 out;
     uint32_t k_unit;
-    __device__ __forceinline__ StagesE4m3(const AttnArgs &a, const AttnItem &it, int kv_head, int which_loader, int first)
-        : pages(a.page_list + it.page0, (it.kv1 - 1) >> a.page_shift, it.kv0 >> a.page_shift), page_stride((uint32_t)a.page_stride), page_shift(a.page_shift), loader(which_loader),
-          w(HALVES ? which_loader & 1 : which_loader), t0(first), at(0)
+    __device__ __forceinline__ StagesE4m3(const AttnArgs &a, const AttnItem &it, int kv_head, int loader, int first)
+        : pages(a.page_list + it.page0, (it.kv1 - 1) >> a.page_shift, it.kv0 >> a.page_shift), page_stride((uint32_t)a.page_stride), page_shift(a.page_shift), w(loader), t0(first)
     {
-        const int lane = threadIdx.x & 63;
+        const int lane = threadIdx.x & 63, at = w * 64 + lane;
         row = lane % TK;
-        tok = (row & 32) | key_of_row<__bf16>(row & 31);
+        int tok = (row & 32) | key_of_row<__bf16>(row & 31);
         if (a.page_shift == 5) tok &= 31;
         const size_t head = (size_t)kv_head * D << a.page_shift, half = (size_t)a.n_kv * D << a.page_shift;
-        keys_at = a.pages + head + (size_t)((((w * 64 + lane) / TK) << a.page_shift) + tok) * 16;
-        values_at = a.pages + half + head + (w * 64 + lane) % D * 16;
+        const int chunk = HALVES ? at / TK / 2 : at / TK, rest = HALVES ? at / TK % 2 * 8 : 0;
+        keys_at = a.pages + head + (size_t)((chunk << a.page_shift) + tok) * 16 + rest;
+        values_at = a.pages + half + head + at % D * 16 + (HALVES ? w % 2 * 8 : 0);
         k_units_at = a.pages + 2 * half + ((size_t)kv_head << a.page_shift) + tok;
-        v_units_at = a.pages + 2 * half + ((size_t)(a.n_kv + kv_head) << a.page_shift);
+        v_units_at = a.pages + 2 * half + ((size_t)(a.n_kv + kv_head) << a.page_shift) + (HALVES ? w % 2 * 8 : 0);
         page[0] = page[1] = 0;
         ask_keys();
         ask_values();
     }
-    __device__ __forceinline__ bool has_keys() const { return !HALVES || loader < 2; }
-    __device__ __forceinline__ bool has_values() const { return !HALVES || loader >= 2; }
-    __device__ __forceinline__ int step_of(int i) const { return (i * THREADS + w * 64) / D; }  // of the wavefront's chunks of values: which 16 tokens of the stage
+    __device__ __forceinline__ int step_of(int i) const { return HALVES ? w / 2 : (i * THREADS + w * 64) / D; }  // of the wavefront's chunks of values: which 16 tokens of the stage
     __device__ __forceinline__ void ask_keys()  // of the next stage
     {
         page[0] = pages[t0 >> page_shift];
         if constexpr (TK == 64) page[1] = pages[(t0 + 32) >> page_shift];
         at = t0 & ((1 << page_shift) - 1);
         t0 += STRIDE;
-        if (!has_keys()) return;
         const uint64_t there = (uint64_t)page_stride * (uint32_t)(TK == 32 || row < 32 ? page[0] : page[1]) + at;
 #pragma unroll
-        for (int i = 0; i < N; ++i) k[i] = *reinterpret_cast<const uint4 *>(keys_at + there + at * 15 + ((i * (THREADS / TK)) << page_shift) * 16);
+        for (int i = 0; i < N; ++i) k[i] = *reinterpret_cast<const Part *>(keys_at + there + at * 15 + ((i * (THREADS / TK)) << page_shift) * 16);
         k_unit = *reinterpret_cast<const uint8_t *>(k_units_at + there);
     }
     __device__ __forceinline__ void ask_values()  // of the stage whose keys were asked for last
     {
-        if (!has_values()) return;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int s = step_of(i), in_page = (at + 16 * s) & ((1 << page_shift) - 1);
             const uint64_t there = (uint64_t)page_stride * (uint32_t)(TK == 32 || s < 2 ? page[0] : page[1]);
-            v[i] = *reinterpret_cast<const uint4 *>(values_at + there + in_page * D);
-            units[i] = *reinterpret_cast<const uint4 *>(v_units_at + there + in_page);
+            v[i] = *reinterpret_cast<const Part *>(values_at + there + in_page * D);
+            units[i] = *reinterpret_cast<const Part *>(v_units_at + there + in_page);
         }
     }
+    static __device__ __forceinline__ uint32_t word(const uint2 &x, int n) { return n == 0 ? x.x : x.y; }
+    static __device__ __forceinline__ uint32_t word(const uint4 &x, int n) { return n == 0 ? x.x : n == 1 ? x.y : n == 2 ? x.z : x.w; }
     // piece p of the work that brings to LDS the next stage's keys, and the values of the stage before it
     __device__ __forceinline__ void piece(int p, unsigned char *values_to, unsigned char *keys_to)
     {
-        const int i = p / 6, n = p % 6, lane = threadIdx.x & 63;
-        if (n < 4) {
-            if (!has_values()) return;
-            const uint32_t x = n == 0 ? v[i].x : n == 1 ? v[i].y : n == 2 ? v[i].z : v[i].w;
-            const uint32_t u = __builtin_amdgcn_readfirstlane(n == 0 ? units[i].x : n == 1 ? units[i].y : n == 2 ? units[i].z : units[i].w);
-            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(x, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(x, true);
-            const bf16x2 y = {(__bf16)(lo[0] * unit_of(u & 255)), (__bf16)(lo[1] * unit_of(u >> 8 & 255))};
-            const bf16x2 z = {(__bf16)(hi[0] * unit_of(u >> 16 & 255)), (__bf16)(hi[1] * unit_of(u >> 24))};
+        const int i = p / (WORDS + WORDS / 2), n = p % (WORDS + WORDS / 2), lane = threadIdx.x & 63;
+        if (n < WORDS) {
+            const uint32_t x = word(v[i], n), u = __builtin_amdgcn_readfirstlane(word(units[i], n));
+            const bf16x2 y = {(__bf16)__builtin_amdgcn_cvt_scalef32_f32_fp8(x, unit_of(u & 255), 0), (__bf16)__builtin_amdgcn_cvt_scalef32_f32_fp8(x, unit_of(u >> 8 & 255), 1)};
+            const bf16x2 z = {(__bf16)__builtin_amdgcn_cvt_scalef32_f32_fp8(x, unit_of(u >> 16 & 255), 2), (__bf16)__builtin_amdgcn_cvt_scalef32_f32_fp8(x, unit_of(u >> 24), 3)};
             if (n % 2 == 0) {
                 out.x = __builtin_bit_cast(uint32_t, y), out.y = __builtin_bit_cast(uint32_t, z);
             } else {
                 out.z = __builtin_bit_cast(uint32_t, y), out.w = __builtin_bit_cast(uint32_t, z);
-                *reinterpret_cast<uint4 *>(values_to + ((2 * step_of(i) + n / 2) * D + (w * 64 + lane) % D) * 16) = out;
+                const int eight = HALVES ? w : 2 * step_of(i) + n / 2;  // which 8 tokens of the stage
+                *reinterpret_cast<uint4 *>(values_to + (eight * D + (w * 64 + lane) % D) * 16) = out;
             }
         } else {
-            if (!has_keys()) return;
-            const int c = (i * THREADS + w * 64 + lane) / TK * 2 + n - 4;
-            *reinterpret_cast<uint4 *>(keys_to + (c * TK + row) * 16) = n == 4 ? eight_bf16(k[i].x, k[i].y, unit_of(k_unit)) : eight_bf16(k[i].z, k[i].w, unit_of(k_unit));
+            const int q = n - WORDS, c = HALVES ? (w * 64 + lane) / TK : (i * THREADS + w * 64 + lane) / TK * 2 + q;
+            *reinterpret_cast<uint4 *>(keys_to + (c * TK + row) * 16) = eight_bf16(word(k[i], 2 * q), word(k[i], 2 * q + 1), unit_of(k_unit));
         }
     }
     __device__ __forceinline__ void ask()
@@ -842,16 +839,19 @@ template <int D, int TK, int STRIDE, int LOADERS = 4> struct StagesE4m3 {
     {
 #pragma unroll
         for (int p = 0; p < PIECES; ++p)
-            if (p % 6 >= 4) piece(p, nullptr, to);
+            if (p % (WORDS + WORDS / 2) >= WORDS) piece(p, nullptr, to);
         ask_keys();
     }
     __device__ __forceinline__ void values(unsigned char *to)  // of the stage before the one whose keys were asked for last
     {
 #pragma unroll
         for (int p = 0; p < PIECES; ++p)
-            if (p % 6 < 4) piece(p, to, nullptr);
+            if (p % (WORDS + WORDS / 2) < WORDS) piece(p, to, nullptr);
         ask_values();
     }
+
+private:
+    int at = 0;  // where the stage whose keys were asked for last begins in its page
 };
 
 // 32 rows of a wavefront: lane r + 32 h has row r's queries (chunks 2 c + h), its maximum, half of its weights and outputs.  s: scores of
@@ -1332,16 +1332,16 @@ __global__ __launch_bounds__(256, (TileShape<E, D>::BLOCKS)) void attn_both_kern
 }
 
 // No more blocks than compute units: eight wavefronts to a tile, two on a SIMD, in two groups that take its stages in turn and join their results at the end
-template <typename E, int D>
+template <typename E, int D, typename P = E>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_pairs_kernel(AttnArgs a)
 {
     extern __shared__ __align__(16) unsigned char lds[];
     const uint32_t tiles = (uint32_t)a.n_tiles * a.n_kv;
     if (blockIdx.x < tiles) {
         const AttnItem it = a.tiles[blockIdx.x / a.n_kv];
-        attn_tile<E, D, 2>(a, it, blockIdx.x % a.n_kv, lds);
+        attn_tile<E, D, 2, P>(a, it, blockIdx.x % a.n_kv, lds);
     } else if (threadIdx.x < 64 * ROW_WAVES) {
-        attn_rows_block<E, D>(a, blockIdx.x - tiles, *reinterpret_cast<RowsLds<D> *>(lds));
+        attn_rows_block<E, D, P>(a, blockIdx.x - tiles, *reinterpret_cast<RowsLds<D> *>(lds));
     }
 }
 

@@ -27,6 +27,10 @@ hipError_t prepare_attn_e4m3_kernels()
             constexpr int D = decltype(d)::value, LDS = TileShape<__bf16, D, E4m3>::LDS;
             allow(reinterpret_cast<const void *>(&attn_tiles_kernel<__bf16, D, E4m3>), LDS);
             allow(reinterpret_cast<const void *>(&attn_both_kernel<__bf16, D, E4m3>), LDS);
+            if constexpr (kv_pairs(LORA_BF16, D)) {
+                static_assert(2 * LDS >= 4 * (32 * D * 4 + 512), "one group's results in LDS");
+                allow(reinterpret_cast<const void *>(&attn_pairs_kernel<__bf16, D, E4m3>), 2 * LDS);
+            }
         });
     allow(reinterpret_cast<const void *>(&attn_turns_kernel<128, E4m3>), turn_lds(128));
     return e;
@@ -43,6 +47,11 @@ hipError_t launch_attn_e4m3(const AttnArgs &a, int dim, KvTiles way, int n_cu, h
             hipLaunchKernelGGL((attn_both_kernel<__bf16, D, E4m3>), dim3((unsigned)(n_tiles + n_rows)), dim3(256), LDS, st, a);
             return;
         }
+        if constexpr (kv_pairs(LORA_BF16, D))
+            if (way == KV_TILES_PAIRS) {
+                hipLaunchKernelGGL((attn_pairs_kernel<__bf16, D, E4m3>), dim3((unsigned)(n_tiles + n_rows)), dim3(512), 2 * LDS, st, a);
+                return;
+            }
         bool done = n_tiles == 0;
         if constexpr (kv_turns(LORA_BF16, D))
             if (!done && way == KV_TILES_TURNS) {

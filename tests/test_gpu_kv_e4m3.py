@@ -413,3 +413,15 @@ def test_large_tiles(page):
                     assert (np.abs(got[at, h] - want[0]) <= (2.0**-7 + 2.0**-12) * mass[0]).all(), (i, h, t)
     finally:
         s.close()
+
+
+@pytest.mark.parametrize("segs,heads,kv", [([(0, 700)], 32, 32), ([(0, 700), (333, 1)], 32, 8), ([(300, 333), (0, 5)], 16, 4), ([(0, 1), (0, 129)], 8, 2)])
+@pytest.mark.parametrize("page", [32, 128])
+def test_heads_of_64_with_two_groups_to_a_tile(segs, heads, kv, page):
+    B, _K = _mods()
+    s = Setup(segs, heads, kv, 64, page=page, seed=14)
+    try:
+        assert B.lora_kv_batch_info(s.batch)[1].tiles_way == B.LORA_KV_TILES_PAIRS
+        s.check()
+    finally:
+        s.close()
