@@ -26,7 +26,7 @@
  * 448, no infinities): as above in chunks of u = 16.  Behind the two halves of a page's layer lie its exponents, bytes [2][n_kv_heads][page_tokens]:
  * a value of token p and head h stands for value * 2^(exponent - 127).  lora_kv_append stores the smallest exponent, of 10 to 247, with which
  * no finite value of the token's head is over 448, and of each value the nearest of 8 bits (halves to even); what is infinite or no number
- * is stored as no number.  All that is stored that way is exact in bf16, which is what attention and lora_kv_seq_read work with.  Exponents that the caller puts
+ * is stored as no number.  All that is stored that way is exact in bf16 (but values over 3.29e38 come out infinite), which is what attention and lora_kv_seq_read work with.  Exponents that the caller puts
  * there himself are 1 to 254.
  *
  * Conventions are those of lora_cache.h: every function returns LORA_OK or a negative lora_status, nothing aborts or
@@ -209,11 +209,11 @@ int lora_kv_append(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const l
 typedef struct {
     const float *q, *k;         /* device, weights w: head_dim values, 16-byte aligned; or NULL: queries / keys get no norm */
     int32_t q_stride, k_stride; /* values from one head's weights to the next one's: 0 (all heads have the same), or from head_dim on a multiple of 4 */
-    float eps;                  /* > 0 */
+    float eps;                  /* > 0, and no smaller than the smallest normal fp32 number */
 } lora_kv_norm_t;
 
-/* lora_kv_append with the norms of `norm` (NULL: none), in the same pass: sums of squares and factors are held in 64 bits, the rest in fp32 (keys for pages of 8 bits
- * in 64 bits as a whole), and what is stored is rounded once.  Errors as lora_kv_append; LORA_E_INVAL on a bad norm, on weights for queries without queries. */
+/* lora_kv_append with the norms of `norm` (NULL: none), in the same pass, in fp32 (in 64 bits: sums of squares that leave its range or are of fp32 values, and all that becomes of keys for
+ * pages of 8 bits), and what is stored is rounded once.  Errors as lora_kv_append; LORA_E_INVAL on a bad norm, on weights for queries without queries. */
 int lora_kv_append_norm(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, const lora_kv_append_t *a, const lora_kv_norm_t *norm, void *stream);
 
 /* Attention of the batch's tokens over their sequences' pages in one layer, causal: q and out device [T][n_heads][head_dim], tokens

@@ -4,6 +4,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -36,20 +38,29 @@ def hipcc() -> str:
 
 
 def build(verbose: bool = False) -> str:
-    srcs = [os.path.join(CSRC, s) for s in SOURCES]
-    cmd = [hipcc(), *FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC]
-    for s in srcs:
-        cmd += (["-x", "hip", s] if s.endswith(".hip") else ["-x", "hip", s])
-    cmd += ["-o", LIB]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    out = "\n".join(l for l in res.stdout.splitlines() if "packed-fp32-ops" not in l)
-    if res.returncode != 0:
-        sys.stderr.write(out + "\n")
-        raise RuntimeError("hipcc failed building liblora_cache.so")
-    if verbose and out.strip():
-        print(out)
+    """Every source is compiled each time, several at once, and the objects are linked."""
+    flags = [f for f in FLAGS if f != "-shared"]
+    with tempfile.TemporaryDirectory() as tmp:
+        def compile_one(name: str):
+            obj = os.path.join(tmp, name + ".o")
+            cmd = [hipcc(), *flags, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-x", "hip", "-c", os.path.join(CSRC, name), "-o", obj]
+            return obj, cmd, subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+        with ThreadPoolExecutor(min(len(SOURCES), os.cpu_count() or 1, 8)) as pool:
+            done = list(pool.map(compile_one, SOURCES))
+        link = [hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared", *[obj for obj, _cmd, _res in done], "-o", LIB]
+        steps = [(cmd, res) for _obj, cmd, res in done]
+        if all(res.returncode == 0 for _cmd, res in steps):
+            steps.append((link, subprocess.run(link, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    for cmd, res in steps:
+        out = "\n".join(l for l in res.stdout.splitlines() if "packed-fp32-ops" not in l)
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        if res.returncode != 0:
+            sys.stderr.write(out + "\n")
+            raise RuntimeError("hipcc failed building liblora_cache.so")
+        if verbose and out.strip():
+            print(out)
     return LIB
 
 

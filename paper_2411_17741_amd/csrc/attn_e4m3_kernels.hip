@@ -43,7 +43,7 @@ hipError_t launch_attn_e4m3(const AttnArgs &a, int dim, KvTiles way, int n_cu, h
     const dim3 tiles((unsigned)n_tiles), rows((unsigned)n_rows);
     return by_dim(dim, [&](auto d) {
         constexpr int D = decltype(d)::value, LDS = TileShape<__bf16, D, E4m3>::LDS;
-        if (n_tiles && n_rows && way == KV_TILES_PLAIN && (n_tiles + n_rows <= BOTH_ROUNDS * TileShape<__bf16, D>::BLOCKS * n_cu || (a.prefixes && TileShape<__bf16, D>::BLOCKS > 1))) {
+        if (n_tiles && n_rows && way == KV_TILES_PLAIN && (n_tiles + n_rows <= BOTH_ROUNDS * TileShape<__bf16, D>::BLOCKS * n_cu || (a.prefixes && TileShape<__bf16, D>::BLOCKS > 1 && n_tiles + n_rows <= INT32_MAX))) {
             hipLaunchKernelGGL((attn_both_kernel<__bf16, D, E4m3>), dim3((unsigned)(n_tiles + n_rows)), dim3(256), LDS, st, a);
             return;
         }

@@ -53,7 +53,7 @@ hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, KvTiles way, int n
     return by_type(dtype, dim, [&](auto e, auto d) {
         typedef decltype(e) E;
         constexpr int D = decltype(d)::value;
-        if (n_tiles && n_rows && way == KV_TILES_PLAIN && (n_tiles + n_rows <= BOTH_ROUNDS * TileShape<E, D>::BLOCKS * n_cu || (a.prefixes && TileShape<E, D>::BLOCKS > 1))) {
+        if (n_tiles && n_rows && way == KV_TILES_PLAIN && (n_tiles + n_rows <= BOTH_ROUNDS * TileShape<E, D>::BLOCKS * n_cu || (a.prefixes && TileShape<E, D>::BLOCKS > 1 && n_tiles + n_rows <= INT32_MAX))) {
             hipLaunchKernelGGL((attn_both_kernel<E, D>), dim3((unsigned)(n_tiles + n_rows)), dim3(256), (TileShape<E, D>::LDS), st, a);
             return;
         }

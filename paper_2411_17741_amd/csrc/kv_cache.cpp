@@ -1,6 +1,7 @@
 // Host side of the paged key-value cache: sequences and their pages, batches and how their attention is cut up.
 // include/lora_kv.h has the contract; the kernels are in kv_kernels.hip and attn_kernels.hip.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <mutex>
@@ -1226,7 +1227,7 @@ int lora_kv_append_norm(lora_kv_t *kv, lora_kv_batch_t *handle, int32_t layer, c
         const auto bad_weights = [&](const float *w, int32_t stride) { return w && (!aligned16(w) || stride % 4 || (stride && stride < c.head_dim)); };
         if (norm && (bad_weights(norm->q, norm->q_stride) || bad_weights(norm->k, norm->k_stride) || (norm->q && !a->q))) return LORA_E_INVAL;
     }
-    if (norm && !(norm->eps > 0.f && std::isfinite(norm->eps))) return LORA_E_INVAL;
+    if (norm && !(norm->eps >= FLT_MIN && std::isfinite(norm->eps))) return LORA_E_INVAL;
     if (a->rope && a->rope_pairs != LORA_ROPE_HALVES && a->rope_pairs != LORA_ROPE_NEIGHBOURS) return LORA_E_INVAL;
     if (!batch->info.n_tokens) return LORA_OK;
     hipStream_t st = static_cast<hipStream_t>(stream);

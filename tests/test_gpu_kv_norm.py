@@ -193,7 +193,7 @@ def test_refusals():
         good = dict(layer=0, k=kp, v=kp, k_stride=128, v_stride=128, q=qp, q_out=qp, q_stride=256, q_out_stride=256, q_norm=wp, k_norm=wp, q_norm_stride=68)
         no_q = dict(q=0, q_out=0, q_stride=0, q_out_stride=0)
         for kw in (dict(layer=2), dict(k=0), dict(q_norm=wp + 4), dict(k_norm=wp + 8), dict(q_norm_stride=60), dict(q_norm_stride=66), dict(k_norm_stride=-64), dict(eps=0.0),
-                   dict(eps=-1e-6), dict(eps=float("inf")), dict(eps=float("nan")), no_q):
+                   dict(eps=-1e-6), dict(eps=1e-39), dict(eps=float("inf")), dict(eps=float("nan")), no_q):
             assert B.lora_kv_append_norm(cache.handle, b, **{**good, **kw}) == B.LORA_E_INVAL, kw
         torch.cuda.synchronize()
         assert not cache.pages.any() and bool((q == 1).all())
