@@ -1,11 +1,12 @@
 """Serving a few layers of a model with adapters: what an iteration does with the adapter cache and the key-value cache together.
 
-    python examples/serve_layers.py [--layers 2] [--heads 32] [--kv-heads 8] [--dim 128] [--requests 8] [--iterations 6]
+    python examples/serve_layers.py [--layers 2] [--heads 32] [--kv-heads 8] [--dim 128] [--requests 8] [--iterations 6] [--norms] [--e4m3] [--shared]
 
 Every iteration forms a batch -- the prompts of new requests, one token of each running one -- and runs, per layer, the q, k, v
 projections with the adapters of the requests, lora_kv_append (positions, keys and values into the pages), lora_kv_attend and the o projection with
 its adapters.  Half way one request is forked into continuations that share its pages, some requests end, and the pages in use
-are moved together so that the rest of the memory is free for adapters.  The model is synthetic (random weights, no MLP); the
+are moved together so that the rest of the memory is free for adapters.  --norms norms every head's queries and keys before they turn, --e4m3 holds keys and values in 8 bits,
+--shared reads what requests share once for all of them.  The model is synthetic (random weights, no MLP); the
 base projections are plain matrix products."""
 from __future__ import annotations
 
@@ -31,7 +32,8 @@ def rope_table(positions: int, dim: int) -> torch.Tensor:
 class Layers:
     """Weights of the layers, adapters in their pool, keys and values in their cache."""
 
-    def __init__(self, layers, heads, kv_heads, dim, adapters, ranks=(8, 32), max_tokens=4096, max_seqs=64, n_pages=512, page_tokens=64, seed=0):
+    def __init__(self, layers, heads, kv_heads, dim, adapters, ranks=(8, 32), max_tokens=4096, max_seqs=64, n_pages=512, page_tokens=64, seed=0,
+                 norms=False, e4m3=False, shared=False):
         gen = torch.Generator(device="cuda").manual_seed(seed)
         rnd = lambda *shape: (torch.randn(*shape, generator=gen, device="cuda") * shape[0] ** -0.5).bfloat16()  # noqa: E731
         self.hidden, self.heads, self.kv_heads, self.dim = heads * dim, heads, kv_heads, dim
@@ -50,7 +52,11 @@ class Layers:
                     self.pool.fill(self.slot[a], a, rank, 1.0, layer, p, rng.normal(0, 0.05, (i, rank)).astype(np.float32), rng.normal(0, 0.05, (rank, o)).astype(np.float32))
         torch.cuda.synchronize()
         self.pool.fills_done()
-        self.cache = KvCache(layers, heads, kv_heads, dim, n_pages, page_tokens=page_tokens, max_seqs=max_seqs, max_batch_seqs=max_seqs, max_batch_tokens=max_tokens)
+        self.cache = KvCache(layers, heads, kv_heads, dim, n_pages, page_tokens=page_tokens, max_seqs=max_seqs, max_batch_seqs=max_seqs, max_batch_tokens=max_tokens,
+                             e4m3=e4m3)
+        self.shared = shared
+        weights = lambda: 1 + 0.1 * torch.randn(dim, generator=gen, device="cuda")  # noqa: E731
+        self.norms = [dict(q_norm=weights(), k_norm=weights()) if norms else {} for _ in range(layers)]
         self.rope = rope_table(8192, dim)
 
     def step(self, x, requests, adapters, lengths):
@@ -59,13 +65,13 @@ class Layers:
         slots = np.asarray([self.slot[a] if a >= 0 else -1 for a in adapters], np.int32)
         ranks = np.asarray([self.rank[a] if a >= 0 else 0 for a in adapters], np.int32)
         plan = self.pool.plan(len(x), off, slots, ranks)
-        batch = self.cache.batch(np.asarray(requests, np.int64), off)
+        batch = self.cache.batch(np.asarray(requests, np.int64), off, shared=self.shared)
         scale = 1.0 / math.sqrt(self.dim)
         for layer, w in enumerate(self.w):
             q, k, v = (x @ w[p] for p in range(3))
             for p, y in enumerate((q, k, v)):
                 self.pool.apply_plan(plan, layer, p, x, y, 1.0)
-            self.cache.append(batch, layer, k, v, q=q, rope=self.rope)  # q turns in place
+            self.cache.append(batch, layer, k, v, q=q, rope=self.rope, **self.norms[layer])  # q turns in place
             out = torch.empty_like(q)
             self.cache.attend(batch, layer, q, out, scale)
             y = out @ w[3]
@@ -84,11 +90,14 @@ def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     for name, value in (("layers", 2), ("heads", 32), ("kv-heads", 8), ("dim", 128), ("requests", 8), ("iterations", 6)):
         ap.add_argument("--" + name, type=int, default=value)
+    for name in ("norms", "e4m3", "shared"):
+        ap.add_argument("--" + name, action="store_true")
     a = ap.parse_args(argv)
     rng = np.random.default_rng(1)
     # room for prompts of up to 300 tokens, a token in each iteration after that, and the continuations
     seqs, each = a.requests + 3, 300 + a.iterations
-    model = Layers(a.layers, a.heads, a.kv_heads, a.dim, adapters=4, max_tokens=max(4096, 300 * seqs), max_seqs=max(64, seqs), n_pages=max(512, seqs * (each // 64 + 1) + 64))
+    model = Layers(a.layers, a.heads, a.kv_heads, a.dim, adapters=4, max_tokens=max(4096, 300 * seqs), max_seqs=max(64, seqs), n_pages=max(512, seqs * (each // 64 + 1) + 64),
+                   norms=a.norms, e4m3=a.e4m3, shared=a.shared)
     try:
         gen = torch.Generator(device="cuda").manual_seed(2)
         token = lambda n: torch.randn(n, model.hidden, generator=gen, device="cuda").bfloat16()  # noqa: E731
