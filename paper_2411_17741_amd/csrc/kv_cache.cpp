@@ -534,7 +534,7 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     const int64_t share = tile_tokens * n_kv / kv.n_cu;
     int32_t tile_piece = at_least(share / 2, tile_min), tile_whole = at_least(share, tile_min);
     // Prefixes are joined anyway, and cut into as many pieces; but not into shorter ones than the rows beside them keep the machine busy with, three quarters of whose tokens for a compute unit
-    // take a tile about as long (256 requests of about 400 tokens behind 2000 with 32 / 8 heads: 4 pieces 93.6 us, 2 85.5, 1 80.2).
+    // take a tile about as long (256 requests of about 350 tokens behind 2000 with 32 / 8 heads: 4 pieces 93.6 us, 2 85.5, 1 80.2).
     int32_t prefix_row_piece = at_least(row_tokens * n_kv / ROW_BLOCKS, SHARED_ROW_MIN_TOKENS);
     int32_t prefix_tile_piece = at_least(cut.way == lora::KV_TILES_TURNS ? share : share / 2, tile_min);
     if (cut.way != lora::KV_TILES_TURNS) prefix_tile_piece = std::max(prefix_tile_piece, at_least(row_tokens * n_kv / kv.n_cu * 3 / 4, 0));
