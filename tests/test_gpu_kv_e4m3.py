@@ -425,3 +425,96 @@ def test_heads_of_64_with_two_groups_to_a_tile(segs, heads, kv, page):
         s.check()
     finally:
         s.close()
+
+
+# ---- streams, graphs, large caches --------------------------------------------------------------------
+
+def test_append_attend_and_read_captured_together():
+    """A graph of an append, attention and a read gives an eager run's bits at every replay, with eager work of the same cache between the replays."""
+    segs = [(100, 1), (0, 40), (33, 2)]
+    cache = _cache(segs, 8, 2, 64, 32)
+    try:
+        off = _scatter(cache, segs, 32)
+        cache.pages.random_(0, 120)
+        cache.pages[..., -2 * 2 * 32 :].fill_(120)
+        batch, T = cache.batch(np.arange(3), off), int(off[-1])
+        x, rope = torch.randn(T, 12, 64, device="cuda").bfloat16(), torch.randn(200, 64, device="cuda").clamp(-1, 1)
+        q, out = (torch.empty(T, 8, 64, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+        back = torch.empty(2, sum(c + n for c, n in segs), 2, 64, device="cuda", dtype=torch.bfloat16)
+
+        def run(stream=None):
+            cache.append(batch, 0, x[:, 8:10], x[:, 10:], q=x[:, :8], q_out=q, rope=rope, stream=stream)
+            cache.attend(batch, 0, q, out, 0.125, stream=stream)
+            cache.read([2, 0, 1], 0, back[0], back[1], stream=stream)
+
+        run()
+        torch.cuda.synchronize()
+        graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        with torch.cuda.graph(graph, stream=side):
+            run(side)
+        for i in range(4):
+            x.copy_(torch.randn(x.shape, device="cuda"))
+            run()
+            torch.cuda.synchronize()
+            want = [t.clone() for t in (q, out, back, cache.pages)]
+            for t in (q, out, back):
+                t.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(want, (q, out, back, cache.pages))), i
+    finally:
+        cache.close()
+
+
+def test_reads_follow_appends_on_other_streams():
+    _B, KvCache = _mods()
+    cache = KvCache(1, 2, 2, 128, 70, page_tokens=64, max_seqs=2, max_batch_seqs=2, max_batch_tokens=4096, e4m3=True)
+    try:
+        cache.add([0])
+        b = cache.batch([0], [0, 4000])
+        big = torch.randn(4096, 4096, device="cuda")
+        one, two = torch.cuda.Stream(), torch.cuda.Stream()
+        back = torch.zeros(2, 4000, 2, 128, device="cuda", dtype=torch.bfloat16)
+        for i in range(5):
+            torch.cuda.synchronize()
+            with torch.cuda.stream(one):
+                k = torch.zeros(4000, 2, 128, device="cuda", dtype=torch.bfloat16)
+                for _ in range(3):
+                    big = big @ big * 1e-3
+                k.fill_(float(2**i))
+                cache.append(b, 0, k, k, stream=one)
+            with torch.cuda.stream(two):
+                cache.read([0], 0, back[0], back[1], stream=two)
+            torch.cuda.synchronize()
+            assert bool((back == 2**i).all()), i
+    finally:
+        cache.close()
+
+
+def test_pages_beyond_4_gb():
+    """Pages whose bytes lie beyond what 32 bits name: stored, attended to, read back."""
+    _B, KvCache = _mods()
+    kv, dim, page, n_pages = 32, 128, 64, 9000
+    cache = KvCache(1, kv, kv, dim, n_pages, page_tokens=page, max_seqs=2, max_batch_seqs=2, max_batch_tokens=200, e4m3=True)
+    try:
+        assert cache.pages.numel() > 1 << 32
+        cache.add([0, 1])
+        cache.extend([0], [(n_pages - 4) * page])
+        b = cache.batch([1], [0, 150])
+        assert cache.pages_of(1).min() >= n_pages - 4
+        x = torch.randn(150, 3 * kv, dim, device="cuda").bfloat16()
+        cache.append(b, 0, x[:, kv : 2 * kv], x[:, 2 * kv :])
+        out, back = torch.empty(150, kv, dim, device="cuda", dtype=torch.bfloat16), torch.empty(2, 150, kv, dim, device="cuda", dtype=torch.bfloat16)
+        cache.attend(b, 0, x[:, :kv], out, dim**-0.5)
+        cache.read([1], 0, back[0], back[1])
+        torch.cuda.synchronize()
+        k, v = x[:, kv : 2 * kv].double().cpu().numpy(), x[:, 2 * kv :].double().cpu().numpy()
+        for have, want in ((back[0], k), (back[1], v)):
+            e = plain.exponents(want)
+            assert np.array_equal(have.double().cpu().numpy(), plain.MEANT[plain.to_bytes(want, e)] * 2.0 ** e[..., None])
+        k, v, got, q = back[0].float().cpu().numpy(), back[1].float().cpu().numpy(), out.float().cpu().numpy(), x[:, :kv].float().cpu().numpy()
+        for h in (0, 17, 31):
+            want, mass, _r = kv_plain.attend(q[:, h], k[:, h], v[:, h], 0, dim**-0.5)
+            assert (np.abs(got[:, h] - want) <= (2.0**-7 + 2.0**-12) * mass).all()
+    finally:
+        cache.close()

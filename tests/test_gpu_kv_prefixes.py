@@ -246,6 +246,41 @@ def test_values_that_are_no_numbers():
         t.close()
 
 
+def test_values_that_are_no_numbers_in_prefixes_of_few_rows():
+    """The same where a wavefront has all rows of a prefix."""
+    for kind, bad in (("bf16", float("nan")), ("bf16", float("inf")), ("e4m3", 127)):
+        t = Tree(forks(3, 600, lambda i: 20), 4, 2, 64, kind=kind, seed=14)
+        try:
+            clean = t.check()
+            page = int(t.cache.pages_of(2)[3])
+            if kind == "e4m3":
+                t.cache.pages[page, 0, 2 * 64 * 64 + 7 * 16 + 3] = bad  # head 0's value 7 of token 3
+            else:
+                t.cache.pages[page, 0, 1].view(2, 8, 64, 8)[0, 0, 7, 3] = bad
+            out = t.run()
+            assert not torch.isfinite(out[:, :2, 7]).any() and torch.isfinite(out[:, :2, :7]).all() and torch.isfinite(out[:, :2, 8:]).all() and torch.equal(out[:, 2:], clean[:, 2:]), kind
+        finally:
+            t.close()
+
+
+def test_outputs_in_place_of_queries_and_strides():
+    """Rows of several segments are gathered while others' outputs are written: outputs may take the queries' place, and both may lie in wider rows."""
+    for kind in KINDS:
+        t = Tree(forks(30, 600, lambda i: i) + [(None, -1, 100, 70), (None, -1, 50, 1)], 4, 2, 64, kind=kind, seed=20, order=1)
+        try:
+            want = t.run()
+            q = t.q.cuda()
+            t.run(q=q, out=q)
+            assert torch.equal(q, want)
+            wide = torch.zeros(len(q), 7, 64, device="cuda", dtype=t.dt)
+            wide[:, 1:5] = t.q.cuda()
+            out = torch.full((len(q), 6, 64), 3.0, device="cuda", dtype=t.dt)
+            t.run(q=wide[:, 1:5], out=out[:, 2:])
+            assert torch.equal(out[:, 2:], want) and bool((out[:, :2] == 3).all())
+        finally:
+            t.close()
+
+
 def test_rows_whose_scores_leave_nothing():
     """Scores that are all -inf have no softmax, as without prefixes; where one of a row's tokens has a number, it has all the weight."""
     t = Tree(forks(6, 400, lambda i: 10), 2, 1, 64, seed=15)
