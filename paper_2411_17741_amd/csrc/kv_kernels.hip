@@ -566,15 +566,18 @@ hipError_t launch_append_heads(const AppendHeadsArgs &n, int dtype, bool e4m3, h
     return hipGetLastError();
 }
 
-// What pages hold, as rows: block row y takes a piece of a page.  Keys: a thread takes a chunk of a token and of the ones 8, 16 and 24 behind it; 8 tokens go with a run of 8 threads, so
+// What pages hold, as rows: block row y takes a piece of a page.  Keys: a thread takes chunks of tokens 8 apart, READ_KEYS; 8 tokens go with a run of 8 threads, so
 // that the page is read in runs of 128 bytes, and 8 threads beside each other in a row's.  Values: a thread takes 16 bytes of a row of all tokens that share their chunks.  A launch's
 // first instructions come from memory, so there are few of them: 8 bits become bf16 two at a time, values of two tokens after they changed places by bytes.
-// Past the caches: 4584 tokens of 32 heads of 128 in 8 bits, 113 MB in and out, in 30 us, 3.8 TB/s (value by value and a chunk a thread 50); 297 of 8 heads 4.5 us.
-constexpr int READ_KEYS = 4;
+// Past the caches: 4584 tokens of 32 heads of 128 in 8 bits, 113 MB in and out, in 27 us, 4.1 TB/s (value by value 50, with READ_KEYS 4 30, with 1 25.5); 33600 of 8 heads 45 us
+// (48; 40).  Pages as they are, 4608 tokens of 32 heads of 128 in 2 bytes, 151 MB: 57 us (with READ_KEYS 2 58, 1 58); 16000 of 8 heads of 64 18.4 us (23; 24).  In 4 bytes 63 us (4: 62).
+template <typename P>
+constexpr int READ_KEYS = sizeof(P) == 2 ? 4 : 2;
 template <typename E, typename P>
 __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
 {
     constexpr int U = CHUNK<P>, W = CHUNK<E>;  // values of 16 bytes of a page, of a row
+    constexpr int KEYS = READ_KEYS<P>;
     constexpr bool AS_IS = sizeof(P) == sizeof(E);
     // tokens off .. off + n - 1 of a page are rows row ..
     const int at = blockIdx.y, off = a.off[at], n = a.row[at + 1] - a.row[at];
@@ -584,24 +587,24 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
     const P *const values = reinterpret_cast<const P *>(page);
     const uint8_t *const exps = reinterpret_cast<const uint8_t *>(page) + 2 * a.n_kv * head_values;  // (pages of 8 bits)
     uint32_t i = blockIdx.x * 256u + threadIdx.x;
-    const uint32_t n_keys = ((uint32_t)(a.dim / U * a.n_kv) << a.page_shift) / READ_KEYS;  // threads that have chunks of keys
+    const uint32_t n_keys = ((uint32_t)(a.dim / U * a.n_kv) << a.page_shift) / KEYS;  // threads that have chunks of keys
     if (i < n_keys) {
         const int chunk_shift = 31 - __builtin_clz(a.dim / U), t8 = i & 7, c = (i >> 3) & (a.dim / U - 1);
         i >>= 3 + chunk_shift;
-        const int h = i % a.n_kv, t0 = (int)(i / a.n_kv) * 8 * READ_KEYS + t8;
+        const int h = i % a.n_kv, t0 = (int)(i / a.n_kv) * 8 * KEYS + t8;
         const P *const from = values + h * head_values + (((size_t)c << a.page_shift) + t0) * U;
         E *const to = static_cast<E *>(a.k) + (row + t0 - off) * a.k_stride + h * a.dim + c * U;
         const auto there = [&](int j) { return (unsigned)(t0 + 8 * j - off) < (unsigned)n; };
-        Vals<P> in[READ_KEYS];
-        uint32_t exp[READ_KEYS];
+        Vals<P> in[KEYS];
+        uint32_t exp[KEYS];
 #pragma unroll
-        for (int j = 0; j < READ_KEYS; ++j)
+        for (int j = 0; j < KEYS; ++j)
             if (there(j)) {
                 in[j] = load_once<true>(from + 8 * j * U);
                 if constexpr (!AS_IS) exp[j] = exps[((size_t)h << a.page_shift) + t0 + 8 * j];
             }
 #pragma unroll
-        for (int j = 0; j < READ_KEYS; ++j)
+        for (int j = 0; j < KEYS; ++j)
             if (there(j)) {
                 E *const here = to + 8 * j * a.k_stride;
                 if constexpr (AS_IS) {
@@ -659,7 +662,7 @@ __global__ __launch_bounds__(256) void read_kernel(ReadArgs a)
 hipError_t launch_read(const ReadArgs &a, int dtype, bool e4m3, hipStream_t st)
 {
     const int64_t u = e4m3 ? 16 : dtype == LORA_BF16 ? 8 : 4, w = dtype == LORA_BF16 ? 8 : 4;
-    const int64_t threads = ((int64_t)(a.dim / u) * a.n_kv << a.page_shift) / READ_KEYS + (int64_t)(a.dim / w) * a.n_kv * ((1 << a.page_shift) / u);
+    const int64_t threads = ((int64_t)(a.dim / u) * a.n_kv << a.page_shift) / (e4m3 ? READ_KEYS<E4m3> : dtype == LORA_BF16 ? READ_KEYS<__bf16> : READ_KEYS<float>) + (int64_t)(a.dim / w) * a.n_kv * ((1 << a.page_shift) / u);
     const int64_t blocks = (threads + 255) / 256;
     if (blocks > INT32_MAX || a.n_reads > KV_MAX_READS) return hipErrorInvalidValue;
     const dim3 grid((unsigned)blocks, (unsigned)a.n_reads);
