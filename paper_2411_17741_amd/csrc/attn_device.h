@@ -1050,7 +1050,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it,
         if constexpr (AS_IS) {
             if (i == 1) request();
         } else {
-                        constexpr int FROM = (NV + QC) / 4, OVER = (NV + QC) * 3 / 8, PIECES = Requests::PIECES;
+            constexpr int FROM = (NV + QC) / 4, OVER = (NV + QC) * 3 / 8, PIECES = Requests::PIECES;
             if (i < FROM) return;
 #pragma unroll
             for (int p = (i - FROM) * PIECES / OVER; p < (i + 1 - FROM) * PIECES / OVER && p < PIECES; ++p) stages.piece(p, lds + K_END + put_v, lds + put_k);

@@ -16,7 +16,6 @@ struct E4m3 {
 __device__ __forceinline__ float unit_of(uint32_t exponent) { return __uint_as_float(exponent << 23); }
 __device__ __forceinline__ float value_of(E4m3 v) { return __builtin_amdgcn_cvt_f32_fp8(v.bits, 0); }
 
-
 // 8 values of 8 bits times a unit as bf16
 __device__ __forceinline__ uint4 eight_bf16(uint32_t a, uint32_t b, float unit)
 {

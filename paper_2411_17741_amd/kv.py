@@ -121,12 +121,12 @@ class KvCache:
 
     # -- batches --------------------------------------------------------------------------
     def batch(self, seg_seq, seg_offsets, stream: Optional[torch.cuda.Stream] = None, shared: Union[bool, int] = False):
-        """shared: attention reads pages that sequences of the batch share once for all of them, where that is worth it (True), or from so many shared tokens on (a number)."""
+        """shared: attention reads pages that sequences of the batch share once for all of them, where that is worth it (True, 0), or from so many shared tokens on (a number)."""
         if not shared and isinstance(shared, (bool, np.bool_)):
             rc, b = B.lora_kv_batch_create(self.handle, seg_seq, seg_offsets, self._stream(stream))
             B.check(rc, "lora_kv_batch_create")
         else:
-            rc, b = B.lora_kv_batch_create_shared(self.handle, seg_seq, seg_offsets, 0 if isinstance(shared, (bool, np.bool_)) else int(shared), self._stream(stream))
+            rc, b = B.lora_kv_batch_create_shared(self.handle, seg_seq, seg_offsets, 0 if isinstance(shared, (bool, np.bool_)) else max(-1, min(int(shared), 2**31 - 1)), self._stream(stream))
             B.check(rc, "lora_kv_batch_create_shared")
         b.n_tokens = int(seg_offsets[-1])
         return b

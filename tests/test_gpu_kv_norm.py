@@ -121,6 +121,14 @@ def test_values_whose_squares_leave_fp32(size):
     _run([(0, 33), (70, 1)], 4, 2, 128, 64, "f32", size=size)
 
 
+@pytest.mark.parametrize("size", [1e-19, 4e-19, 1e-16])
+def test_values_whose_squares_are_below_the_normal_numbers(size, monkeypatch):
+    """... with the smallest eps there is, beside which they count."""
+    monkeypatch.setitem(globals(), "EPS", 2.0**-126)
+    for dtype in ("bf16", "f32"):
+        _run([(0, 33), (70, 1)], 4, 2, 128, 64, dtype, size=size)
+
+
 def test_heads_of_zeros_and_of_no_numbers():
     """A head of zeros stays one; a NaN spoils its own head and nothing else."""
     _B, KvCache = _mods()

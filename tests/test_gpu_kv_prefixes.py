@@ -447,3 +447,16 @@ def test_refusals():
         assert B.lora_kv_batch_prefixes(b)[0] == B.LORA_E_INVAL and B.lora_kv_batch_prefixes(None)[0] == B.LORA_E_INVAL
     finally:
         cache.close()
+
+
+def test_numbers_of_tokens_beyond_32_bits():
+    """They are none, or negative: not what is left of them."""
+    B, _K = _mods()
+    t = Tree(forks(2, 640, lambda i: 1), 4, 2, 64, shared=2**32 + 1)
+    try:
+        assert t.info().n_prefixes == 0
+        for n in (-1, -(2**32) + 1):
+            with pytest.raises(B.LoraError):
+                t.cache.batch([1], [0, 1], shared=n)
+    finally:
+        t.close()
