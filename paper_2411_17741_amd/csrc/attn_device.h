@@ -512,7 +512,7 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it,
 
 // Up to 16 rows over pages of 8-bit values.  As above with steps of 64 tokens: a 16-byte chunk is 16 values, and so two operands.  The keys' chunks are turned into
 // bf16 with their tokens' units at once, which is exact; a chunk of values is of 16 tokens, and the weights take their units.  The tokens of a step may lie in two
-// pages (of 32).  Bound by memory where there is much of it: 512 tokens of about 1000 cached ones with 32 / 8 heads of 128, 1.32 GB, in 206 us, 6.4 TB/s (matrix units busy 14 % of the time); one of 131071 with 64 / 8 48 to 50 us, 5.5.
+// pages (of 32).  Bound by memory where there is much of it: 512 tokens of about 1000 cached ones with 32 / 8 heads of 128, 1.32 GB, in 206 us, 6.4 TB/s (matrix units busy 14 % of the time); one of 131071 with 64 / 8 46 to 47 us, 5.8.
 template <int D, bool ALONE>
 __device__ __forceinline__ void attn_rows_e4m3(const AttnArgs &a, const AttnItem &it, int kv_head, RowsLds<D> &lds)
 {

@@ -49,6 +49,12 @@ constexpr int SHARED_DEPTH = 7, SHARED_TOKENS = 2, SHARED_ROW_MIN_TOKENS = 256;
 // and 512 tokens, 132 MB, 25.0 -> 21.0 us, 256 tokens, 66 MB, 14.2 -> 16.3; 256 requests and 256 tokens, 267 MB, 41.5 -> 39.1, 128 tokens 34.9 -> 39.6; with 64 / 8 heads 512 tokens 57.4 -> 49.6, 256
 // 42.7 -> 48.8.  Of few rows: 2 requests with 40 / 40 heads and 1024 tokens, 21 MB, 14.2 -> 12.5, 512 tokens 12.2 -> 12.5.
 constexpr int64_t SHARED_FEW_BYTES = 16 << 20, SHARED_BYTES = 64 << 20, SHARED_ROW_BYTES = 14 << 10;
+// Few blocks are as fast as the compute unit that has most of them: a block takes its tokens and EVEN_BLOCK more, and of rows each over two for a compute unit waits, EVEN_WAIT.  Pieces of an even share of all
+// tokens -> so cut, us.  Rows in 8 bits: 4 tokens of 30000 with 64 / 8 heads of 128 57.3 -> 49.9 (544 blocks, 512), 3 of about 50000 80 -> 70, 20 of 4000 with 32 / 8 38.4 -> 35.0, one of 131071 with 64 / 8
+// 56.2 -> 54.2; 2 of 1500 with 40 / 40 17.2 -> 17.8.  Tiles in 8 bits: 128 tokens behind 20000 with 32 / 8 72 -> 63.6, 500 behind 2000 with 40 / 40 54 -> 45, 256 behind 5000 with 16 / 4 heads of 256 69 -> 48,
+// 1500 44 -> 41.  Prefixes: 4 requests behind 9000 tokens with 32 / 8 heads 20.3 -> 16.0, 8 behind 1500 with 40 / 40 16.9 -> 14.5 (without EVEN_WAIT 16.9), 10 behind 1200 with 32 / 32 14.2 -> 14.4; in tiles, 200 behind
+// 20000 with 40 / 40 242 -> 199, 16 behind 40000 with 48 / 6 53 -> 43, 30 behind 30000 with 32 / 8 heads of 256 102 -> 82.  (Pages that are not of 8 bits, and share nothing, are cut as they always were.)
+constexpr int64_t EVEN_ROUNDS = 4, EVEN_BLOCK = 128, EVEN_WAIT = 3;
 
 struct Seq {
     int64_t id = 0;
@@ -404,6 +410,27 @@ void cut_block(AttnItem base, int32_t kv_len, int32_t piece, int32_t rows, int32
     }
 }
 
+// How many pieces of at most `piece` tokens the cuts here make of `tokens`
+int64_t pieces_of(int64_t tokens, int64_t piece)
+{
+    const int64_t n = std::max((tokens + piece - 1) / piece, (int64_t)1), each = ((tokens + n - 1) / n + PIECE_STEP - 1) / PIECE_STEP * PIECE_STEP;
+    return n == 1 ? 1 : (tokens + each - 1) / each;
+}
+
+// `piece`, or up to twice as much where compute units then have their blocks more evenly.  blocks(piece): blocks of a piece each, and all of them with those beside.
+template <typename F>
+int64_t even_piece(int64_t piece, int64_t n_cu, F blocks)
+{
+    int64_t best = piece, least = INT64_MAX;
+    for (int64_t p = piece; p <= 2 * piece; p += std::max(piece / 16 / PIECE_STEP, (int64_t)1) * PIECE_STEP) {
+        const auto [n, all] = blocks(p);
+        if (p == piece && n > EVEN_ROUNDS * n_cu) break;
+        const int64_t time = (n + n_cu - 1) / n_cu * (p + EVEN_BLOCK) + std::max(all - 2 * n_cu, (int64_t)0) * EVEN_WAIT;
+        if (time < least) least = time, best = p;
+    }
+    return best;
+}
+
 // What segments of few rows have in common.  Larger ones fill tiles of their own: the products take as long, and there is nothing to join.  (Called before the
 // sequences grow: pages that are full by then stay as they are.)
 void find_prefixes(const lora_kv &kv, const Growth &g, int32_t min_tokens, Cut &cut)
@@ -528,6 +555,7 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
         tile_tokens += tiles * tokens_of(p);
         longest = std::max(longest, tokens_of(p));
     }
+    const int32_t short_tokens = (kv.e4m3() ? ROW_SHORT_E4M3 : ROW_SHORT_VALUES) / kv.cfg.head_dim;
     const auto at_least = [](int64_t tokens, int64_t least) { return (int32_t)std::min(std::max(tokens, least), (int64_t)LORA_KV_MAX_TOKENS); };
     int32_t row_piece = at_least(row_tokens * n_kv / ROW_BLOCKS, ROW_MIN_TOKENS);
     // A tile that takes longer than all of a compute unit's share is cut, into pieces of half of that: two at a time are worked on
@@ -538,6 +566,50 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     int32_t prefix_row_piece = at_least(row_tokens * n_kv / ROW_BLOCKS, SHARED_ROW_MIN_TOKENS);
     int32_t prefix_tile_piece = at_least(cut.way == lora::KV_TILES_TURNS ? share : share / 2, tile_min);
     if (cut.way != lora::KV_TILES_TURNS) prefix_tile_piece = std::max(prefix_tile_piece, at_least(row_tokens * n_kv / kv.n_cu * 3 / 4, 0));
+    // The same, evenly for the compute units: prefixes in tiles, tiles, rows of batches that have nothing else
+    const auto evenly = [&](int32_t piece, auto blocks) { return at_least(even_piece(piece, kv.n_cu, blocks), 0); };
+    const auto prefix_blocks = [&](bool tiles, int64_t piece) {
+        int64_t n = 0;
+        for (const Prefix &p : cut.prefixes)
+            if ((p.rows > lora::KV_ROW_ITEM) == tiles) n += (tiles ? (p.rows + tile - 1) / tile : 1) * pieces_of(tokens_of(p), piece) * n_kv;
+        return n;
+    };
+    const auto own_rows = [&](int64_t piece) {  // blocks of rows: that a wavefront may do alone or not
+        int64_t n[2] = {0, 0};
+        for (size_t i = 0; i < g.seqs.size(); ++i)
+            if (g.n_tokens[i]) n[g.seqs[i]->n_tokens - from_of(i) > short_tokens] += pieces_of(g.seqs[i]->n_tokens - from_of(i), piece) * n_kv;
+        return std::pair(n[0], n[1]);
+    };
+    const auto own_tiles = [&](int64_t piece) {
+        int64_t n = 0;
+        for (size_t i = 0; i < g.seqs.size(); ++i) {
+            const int64_t rows = (int64_t)g.n_tokens[i] * grp, ctx = g.seqs[i]->n_tokens - g.n_tokens[i];
+            for (int64_t r = 0; rows > lora::KV_ROW_ITEM && r < rows; r += tile) {
+                const int64_t end = tile_end(ctx, rows, r);
+                n += (end > std::max((int64_t)tile_whole, piece) ? pieces_of(end, piece) : 1) * n_kv;
+            }
+        }
+        return n;
+    };
+    const bool few_rows = !n_tiles && (int64_t)g.seqs.size() * n_kv <= EVEN_ROUNDS * kv.n_cu;
+    if (!cut.prefixes.empty()) {
+        prefix_tile_piece = evenly(prefix_tile_piece, [&](int64_t piece) { return std::pair(prefix_blocks(true, piece), (int64_t)0); });
+        const auto [alone, others] = own_rows(row_piece);
+        const int64_t beside = others + (alone > 2 * kv.n_cu ? alone / 4 : alone);
+        if (few_rows)
+            prefix_row_piece = evenly(prefix_row_piece, [&](int64_t piece) {
+                const int64_t n = prefix_blocks(false, piece);
+                return std::pair(n, n + beside);
+            });
+    } else if (kv.e4m3() && n_tiles) {
+        if (n_tiles * n_kv <= EVEN_ROUNDS * kv.n_cu) tile_piece = evenly(tile_piece, [&](int64_t piece) { return std::pair(own_tiles(piece), (int64_t)0); });
+        tile_whole = std::max(tile_whole, tile_piece);
+    } else if (kv.e4m3() && few_rows) {
+        row_piece = evenly(row_piece, [&](int64_t piece) {
+            const auto [alone, others] = own_rows(piece);
+            return std::pair(alone + others, (int64_t)0);
+        });
+    }
     // No more blocks than compute units and no tile of over 1024 tokens: for heads of 64, whose steps are mostly instructions of one wavefront after the other, two groups of
     // wavefronts share a tile's tokens, and tiles stay whole (700 tokens with 32 heads 16.5 -> 12.5 us, with 32 / 8 heads 15.3 -> 12.3).  Longer ones, and heads of 128, do as well
     // or better with pieces.
@@ -649,7 +721,6 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     // loads and its last stores.  Measured: 512 requests of 20 tokens with 32 heads of 128 96 -> 51 us, 256 of 120 94 -> 78 us; with 200 to 450 tokens, and
     // with half as many for heads of 256, nothing is gained.
     size_t n_short = 0;
-    const int32_t short_tokens = (kv.e4m3() ? ROW_SHORT_E4M3 : ROW_SHORT_VALUES) / kv.cfg.head_dim;
     const auto is_short = [&](const AttnItem &it) { return (it.part < 0 || !cut.prefixes.empty()) && it.kv1 - it.kv0 <= short_tokens; };
     while (n_short < cut.rows.size() && is_short(cut.rows[cut.rows.size() - 1 - n_short])) ++n_short;
     cut.n_short = (int64_t)n_short * n_kv > 2 * kv.n_cu ? (int32_t)n_short : 0;

@@ -345,6 +345,21 @@ def test_long_caches_are_cut_and_joined(segs, heads, kv, dim):
         s.close()
 
 
+def test_few_blocks_are_even():
+    """Pieces are made a little longer where the blocks would be a few more than the compute units take at a time, and outputs are right for all that."""
+    B, _K = _mods()
+    n_cu = torch.cuda.get_device_properties(0).multi_processor_count
+    for segs, heads, kv, dim in (([(16000, 1)] * 4, 16, 8, 64), ([(3000, 40), (2000, 8)], 8, 4, 128), ([(1500, 1)] * 20, 8, 8, 64), ([(4000, 64)], 8, 2, 256)):
+        s = Setup(segs, heads, kv, dim, seed=11)
+        try:
+            rc, info = B.lora_kv_batch_info(s.batch)
+            blocks = (info.n_row_items + info.n_tile_items) * kv
+            assert rc == 0 and (blocks <= 2 * n_cu or n_cu < 256), (segs[0], blocks)
+            s.check()
+        finally:
+            s.close()
+
+
 def test_batches_of_many_requests():
     _check([(20 + i % 90, 1) for i in range(300)], 8, 8, 64, page=32, seed=5)
     _check([(i % 50, 1 + i % 40) for i in range(60)], 8, 2, 128, seed=6, layers=2, layer=1)
