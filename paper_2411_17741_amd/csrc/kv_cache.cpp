@@ -53,7 +53,8 @@ constexpr int64_t SHARED_FEW_BYTES = 16 << 20, SHARED_BYTES = 64 << 20, SHARED_R
 // tokens -> so cut, us.  Rows in 8 bits: 4 tokens of 30000 with 64 / 8 heads of 128 57.3 -> 49.9 (544 blocks, 512), 3 of about 50000 80 -> 70, 20 of 4000 with 32 / 8 38.4 -> 35.0, one of 131071 with 64 / 8
 // 56.2 -> 54.2; 2 of 1500 with 40 / 40 17.2 -> 17.8.  Tiles in 8 bits: 128 tokens behind 20000 with 32 / 8 72 -> 63.6, 500 behind 2000 with 40 / 40 54 -> 45, 256 behind 5000 with 16 / 4 heads of 256 69 -> 48,
 // 1500 44 -> 41.  Prefixes: 4 requests behind 9000 tokens with 32 / 8 heads 20.3 -> 16.0, 8 behind 1500 with 40 / 40 16.9 -> 14.5 (without EVEN_WAIT 16.9), 10 behind 1200 with 32 / 32 14.2 -> 14.4; in tiles, 200 behind
-// 20000 with 40 / 40 242 -> 199, 16 behind 40000 with 48 / 6 53 -> 43, 30 behind 30000 with 32 / 8 heads of 256 102 -> 82.  (Pages that are not of 8 bits, and share nothing, are cut as they always were.)
+// 20000 with 40 / 40 242 -> 199, 16 behind 40000 with 48 / 6 53 -> 43, 30 behind 30000 with 32 / 8 heads of 256 102 -> 82; tiles beside them,
+// 3 x 180 and 20 tokens behind 4000 with 32 / 8 74 -> 66, 2 x 100 behind 6000 53 -> 47; 30 tokens, 40, 7 and 150 behind 2000 30.9 -> 33.0.  (Pages that are not of 8 bits, and share nothing, are cut as they always were.)
 constexpr int64_t EVEN_ROUNDS = 4, EVEN_BLOCK = 128, EVEN_WAIT = 3;
 
 struct Seq {
@@ -585,26 +586,26 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
         for (size_t i = 0; i < g.seqs.size(); ++i) {
             const int64_t rows = (int64_t)g.n_tokens[i] * grp, ctx = g.seqs[i]->n_tokens - g.n_tokens[i];
             for (int64_t r = 0; rows > lora::KV_ROW_ITEM && r < rows; r += tile) {
-                const int64_t end = tile_end(ctx, rows, r);
-                n += (end > std::max((int64_t)tile_whole, piece) ? pieces_of(end, piece) : 1) * n_kv;
+                const int64_t end = tile_end(ctx, rows, r) - from_of(i);
+                n += (from_of(i) || end > std::max((int64_t)tile_whole, piece) ? pieces_of(end, piece) : 1) * n_kv;
             }
         }
         return n;
     };
     const bool few_rows = !n_tiles && (int64_t)g.seqs.size() * n_kv <= EVEN_ROUNDS * kv.n_cu;
-    if (!cut.prefixes.empty()) {
-        prefix_tile_piece = evenly(prefix_tile_piece, [&](int64_t piece) { return std::pair(prefix_blocks(true, piece), (int64_t)0); });
-        const auto [alone, others] = own_rows(row_piece);
-        const int64_t beside = others + (alone > 2 * kv.n_cu ? alone / 4 : alone);
-        if (few_rows)
-            prefix_row_piece = evenly(prefix_row_piece, [&](int64_t piece) {
-                const int64_t n = prefix_blocks(false, piece);
-                return std::pair(n, n + beside);
-            });
-    } else if (kv.e4m3() && n_tiles) {
-        if (n_tiles * n_kv <= EVEN_ROUNDS * kv.n_cu) tile_piece = evenly(tile_piece, [&](int64_t piece) { return std::pair(own_tiles(piece), (int64_t)0); });
+    if (!cut.prefixes.empty()) prefix_tile_piece = evenly(prefix_tile_piece, [&](int64_t piece) { return std::pair(prefix_blocks(true, piece), (int64_t)0); });
+    if (n_tiles && (kv.e4m3() || !cut.prefixes.empty()) && n_tiles * n_kv <= EVEN_ROUNDS * kv.n_cu) {
+        const int64_t beside = prefix_blocks(true, prefix_tile_piece);
+        if (own_tiles(tile_piece)) tile_piece = evenly(tile_piece, [&](int64_t piece) { return std::pair(own_tiles(piece) + beside, (int64_t)0); });
         tile_whole = std::max(tile_whole, tile_piece);
-    } else if (kv.e4m3() && few_rows) {
+    } else if (few_rows && !cut.prefixes.empty()) {
+        const auto [alone, others] = own_rows(row_piece);
+        const int64_t beside = others + (alone > 4 * kv.n_cu ? alone / 4 : alone);
+        prefix_row_piece = evenly(prefix_row_piece, [&](int64_t piece) {
+            const int64_t n = prefix_blocks(false, piece);
+            return std::pair(n, n + beside);
+        });
+    } else if (few_rows && kv.e4m3()) {
         row_piece = evenly(row_piece, [&](int64_t piece) {
             const auto [alone, others] = own_rows(piece);
             return std::pair(alone + others, (int64_t)0);
@@ -719,11 +720,12 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     std::stable_sort(cut.tiles.begin(), cut.tiles.end(), longer);
     // Where there are more items than blocks fit on the machine, a wavefront has a short one to itself: a block on it is mostly waiting for its first
     // loads and its last stores.  Measured: 512 requests of 20 tokens with 32 heads of 128 96 -> 51 us, 256 of 120 94 -> 78 us; with 200 to 450 tokens, and
-    // with half as many for heads of 256, nothing is gained.
+    // with half as many for heads of 256, nothing is gained.  Beside prefixes, whose parts are there to be worked on, from twice as many on: 128 requests with 20 tokens of their own behind 2000 with 32 / 8
+    // heads 26.6 -> 25.5 us, 20 of 50 with 40 / 40 24.9 -> 23.0.
     size_t n_short = 0;
     const auto is_short = [&](const AttnItem &it) { return (it.part < 0 || !cut.prefixes.empty()) && it.kv1 - it.kv0 <= short_tokens; };
     while (n_short < cut.rows.size() && is_short(cut.rows[cut.rows.size() - 1 - n_short])) ++n_short;
-    cut.n_short = (int64_t)n_short * n_kv > 2 * kv.n_cu ? (int32_t)n_short : 0;
+    cut.n_short = (int64_t)n_short * n_kv > (cut.prefixes.empty() ? 2 : 4) * kv.n_cu ? (int32_t)n_short : 0;
     // Tiles are worked on two at a time on a compute unit, block b beside block b + n_cu: the longest go with the shortest of the first two rounds
     // (2048 tokens with 32 / 8 heads: 70 -> 55 us).
     const size_t round = ((size_t)kv.n_cu + n_kv - 1) / n_kv;
