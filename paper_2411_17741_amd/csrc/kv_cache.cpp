@@ -45,10 +45,10 @@ constexpr int MAX_EXTRA = 2048;  // pieces beyond one for each block of rows
 // Of how many prefixes of prefixes a segment may have a part; tokens' places in all of them together (times max_batch_tokens); tokens of a piece of a prefix with few rows
 constexpr int SHARED_DEPTH = 7, SHARED_TOKENS = 2, SHARED_ROW_MIN_TOKENS = 256;
 // A prefix is worth it if the segments but one are spared more bytes of keys and values than these, and so many for each row of each head of 128, whose parts are written and read again.  (The bytes
-// that are spared would mostly have come out of caches.)  Measured, one by one -> shared, heads of 128, each request 100 tokens of its own behind the prefix: 64 requests with 32 / 8 heads
-// and 512 tokens, 132 MB, 25.0 -> 21.0 us, 256 tokens, 66 MB, 14.2 -> 16.3; 256 requests and 256 tokens, 267 MB, 41.5 -> 39.1, 128 tokens 34.9 -> 39.6; with 64 / 8 heads 512 tokens 57.4 -> 49.6, 256
-// 42.7 -> 48.8.  Of few rows: 2 requests with 40 / 40 heads and 1024 tokens, 21 MB, 14.2 -> 12.5, 512 tokens 12.2 -> 12.5.
-constexpr int64_t SHARED_FEW_BYTES = 16 << 20, SHARED_BYTES = 64 << 20, SHARED_ROW_BYTES = 14 << 10;
+// that are spared would mostly have come out of caches.)  Measured, one by one -> shared, us, heads of 128, each request 100 tokens of its own behind the prefix: 64 requests with 32 / 8 heads
+// and 600 tokens, 148 MB, 19.3 -> 18.4, 512 tokens, 132 MB, 17.4 -> 21.1; 256 requests and 256 tokens, 267 MB, 42.3 -> 36.4, 128 tokens 35.8 -> 37.4; 20 of 1800, 140 MB, 21.5 -> 17.8, 1024 tokens 15.5 -> 18.2; with 64 / 8
+// heads 64 of 800 23.7 -> 22.0, 640 20.0 -> 20.4; 60 with 40 / 40 and 200 46 -> 36.  Of few rows: 2 requests with 40 / 40 heads and 1024 tokens, 21 MB, 13.2 -> 12.7, 512 tokens 12.5 -> 12.6.
+constexpr int64_t SHARED_FEW_BYTES = 16 << 20, SHARED_BYTES = 112 << 20, SHARED_ROW_BYTES = 14 << 10;
 // Few blocks are as fast as the compute unit that has most of them: a block takes its tokens and EVEN_BLOCK more, and of rows each over two for a compute unit waits, EVEN_WAIT.  Pieces of an even share of all
 // tokens -> so cut, us.  Rows in 8 bits: 4 tokens of 30000 with 64 / 8 heads of 128 57.3 -> 49.9 (544 blocks, 512), 3 of about 50000 80 -> 70, 20 of 4000 with 32 / 8 38.4 -> 35.0, one of 131071 with 64 / 8
 // 56.2 -> 54.2; 2 of 1500 with 40 / 40 17.2 -> 17.8.  Tiles in 8 bits: 128 tokens behind 20000 with 32 / 8 72 -> 63.6, 500 behind 2000 with 40 / 40 54 -> 45, 256 behind 5000 with 16 / 4 heads of 256 69 -> 48,

@@ -409,7 +409,7 @@ def test_what_is_worth_it():
             t.close()
 
     for kind, times in (("bf16", 1), ("e4m3", 2)):
-        assert prefixes(64, 512 * times, 32, 8, True, kind=kind) == 1 and prefixes(64, 256 * times - 64, 32, 8, True, kind=kind) == 0
+        assert prefixes(64, 704 * times, 32, 8, True, kind=kind) == 1 and prefixes(64, 512 * times, 32, 8, True, kind=kind) == 0
         assert prefixes(2, 1024 * times, 40, 40, True, kind=kind) == 1 and prefixes(2, 512 * times, 40, 40, True, kind=kind) == 0
         assert prefixes(2, 64, 40, 40, 64, kind=kind) == 1 and prefixes(2, 64, 40, 40, 65, kind=kind) == 0 and prefixes(2, 64, 40, 40, 1, kind=kind) == 1
     _check(forks(64, 1024, lambda i: i % 50), 32, 8, 128, 1, 64, kind="bf16", shared=True, seed=18)
