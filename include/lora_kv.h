@@ -159,7 +159,7 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
  * that are full, attention reads those once, for the rows of all of them together, and joins the result with that of each one's own tokens.  Prefixes may branch: what some of
  * the segments share beyond what all do is a prefix of its own.  Which pages are shared is seen from the books (pages with the same keys and values that were appended twice are not).  A
  * prefix is shared from min_tokens tokens on, with 0 where it is long enough, and its segments many enough, to gain by it; all are left to the segments if the pieces' results have no
- * room.  Outputs are those of lora_kv_batch_create up to the rounding of sums.  Errors as there; LORA_E_INVAL if min_tokens is negative. */
+ * room.  Outputs are those of lora_kv_batch_create up to the rounding of sums, and with LORA_BF16 of the weights of segments with more than 16 rows (lora_kv_attend).  Errors as there; LORA_E_INVAL if min_tokens is negative. */
 int lora_kv_batch_create_shared(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, const int32_t *seg_offsets, int32_t min_tokens, void *stream,
                                 lora_kv_batch_t **out);
 int lora_kv_batch_destroy(lora_kv_t *kv, lora_kv_batch_t *batch);
@@ -219,7 +219,7 @@ int lora_kv_append_norm(lora_kv_t *kv, lora_kv_batch_t *batch, int32_t layer, co
 /* Attention of the batch's tokens over their sequences' pages in one layer, causal: q and out device [T][n_heads][head_dim], tokens
  * q_stride / out_stride values apart, 16-byte aligned; out may be q itself with the same stride; scale > 0.  Scores, sums and outputs are held in fp32 and outputs
  * rounded once; with LORA_BF16 the weights exp(score - max) are rounded to bf16 for the product with the values (of segments with up to 16
- * rows -- tokens times n_heads / n_kv_heads -- to 16 significant bits, which costs nothing there).  A key or value
+ * rows -- tokens times n_heads / n_kv_heads -- to 16 significant bits, whether they share a prefix or not).  A key or value
  * beyond a token's position has no influence on its output, whatever it is.  Sums are kept in range: an output is finite where the scores and
  * values that its token sees are, and infinite where one of the values is (if its weight is not 0).  The batch's parts are summed in an order
  * that depends on the batch alone: the same call gives the same bits. */

@@ -47,7 +47,7 @@ __device__ __forceinline__ const uint8_t *exponents(const AttnArgs &a, int page,
 }
 
 // The token in the packed batch of an item's rows t * group, t * group + 1, ...
-__device__ __forceinline__ int token_of(const AttnArgs &a, const AttnItem &it, int t) { return it.ctx == KV_SHARED ? a.row_tokens[it.tok0 + t] : it.tok0 + t; }
+__device__ __forceinline__ int token_of(const AttnArgs &a, const AttnItem &it, int t) { return it.ctx >= KV_SHARED ? a.row_tokens[it.tok0 + t] : it.tok0 + t; }
 
 // One row by one wavefront, a token a lane for the scores and D / 64 values of the output a lane.  Lane i holds values i, i + 64, ...  The weights, and their sum l, are
 // 2^28 times smaller than elsewhere: a sequence has no more tokens than that, so their sums with values of any size stay in range.
@@ -208,7 +208,8 @@ __device__ __forceinline__ float sum16(float v)
 
 // A chunk of weights, in the values' type: 4 fp32 weights as they are, 8 weights rounded to nearest bf16, the type of the product's operands.  Rows make up for what is lost with a second product;
 // tiles, which are bound by their products and instructions, do not: it would be half as many products again.  Their outputs are off by 2.0e-3 of their norm where rounding the outputs
-// alone makes 1.6e-3 (bf16, 8192 tokens).
+// alone makes 1.6e-3 (bf16, 8192 tokens).  But tiles of a prefix do whose rows are of segments that have few (KV_EXACT): sharing must not cost those any bits.  It costs time where the prefix
+// is most of the work: 32 requests behind 100000 tokens with 64 / 8 heads of 128 129 -> 162 us, 256 of about 350 behind 2000 with 32 / 8 76.9 -> 78.4.
 __device__ __forceinline__ uint4 weights(const float (&p)[8])
 {
     bf16x8 v;
@@ -219,6 +220,18 @@ __device__ __forceinline__ uint4 weights(const float (&p)[8])
 __device__ __forceinline__ uint4 weights(const float (&p)[4])
 {
     return make_uint4(__float_as_uint(p[0]), __float_as_uint(p[1]), __float_as_uint(p[2]), __float_as_uint(p[3]));
+}
+
+// ... and what they lost when they were rounded
+__device__ __forceinline__ uint4 weights(const float (&p)[8], uint4 &rest)
+{
+    const uint4 w = weights(p);
+    const Vals<__bf16> rounded = __builtin_bit_cast(Vals<__bf16>, w);
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = p[e] - (float)rounded.v[e];
+    rest = weights(x);
+    return w;
 }
 
 // the first n values of a chunk, zeros for the others
@@ -856,10 +869,11 @@ private:
 };
 
 // 32 rows of a wavefront: lane r + 32 h has row r's queries (chunks 2 c + h), its maximum, half of its weights and outputs.  s: scores of
-// the stage; w: its weights; o[j][4 k + i]: value 32 j + 8 k + 4 h + i
-template <typename E, int D, int TK> struct TileRows {
+// the stage; w: its weights; o[j][4 k + i]: value 32 j + 8 k + 4 h + i.  EXACT: what the weights lost when they were rounded is kept too, for a second product
+template <typename E, int D, int TK, bool EXACT = false> struct TileRows {
     static constexpr int U = CHUNK<E>, SUB = TK / 32, QC = D / (2 * U), DJ = D / 32, PK = 32 / (2 * U);
-    uint4 q[QC], w[SUB * PK];
+    static_assert(!EXACT || sizeof(E) == 2, "only bf16 weights lose anything");
+    uint4 q[QC], w[SUB * PK], rest[EXACT ? SUB * PK : 1];
     floatx16 o[DJ], s[SUB];
     float m, l;
     int end, least;  // tokens that the lane's row sees, and the wavefront's first
@@ -883,6 +897,18 @@ template <typename E, int D, int TK> struct TileRows {
     {
 #pragma unroll
         for (int c = 0; c < QC; ++c) asm volatile("" : "+v"(q[c].x), "+v"(q[c].y), "+v"(q[c].z), "+v"(q[c].w));
+    }
+    __device__ __forceinline__ void take(int k, const float (&p)[U])  // chunk k of the stage's weights
+    {
+        if constexpr (EXACT) w[k] = weights(p, rest[k]);
+        else w[k] = weights(p);
+        asm volatile("" : "+v"(w[k].x), "+v"(w[k].y), "+v"(w[k].z), "+v"(w[k].w), "+v"(l));  // now, not where they are used
+        if constexpr (EXACT) asm volatile("" : "+v"(rest[k].x), "+v"(rest[k].y), "+v"(rest[k].z), "+v"(rest[k].w));
+    }
+    __device__ __forceinline__ void add(int j, const uint4 &values, int k)  // o[j] += values . chunk k of the weights
+    {
+        mma32<E>(o[j], values, w[k]);
+        if constexpr (EXACT) mma32<E>(o[j], values, rest[k]);
     }
     // the stage at t0: its scores become weights
     __device__ __forceinline__ void weigh(int t0, float scale_log2)
@@ -919,15 +945,14 @@ template <typename E, int D, int TK> struct TileRows {
                 p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k / PK][k % PK * U + e], scale_log2, -m));
                 l += p[e];
             }
-            w[k] = weights(p);
-            asm volatile("" : "+v"(w[k].x), "+v"(w[k].y), "+v"(w[k].z), "+v"(w[k].w), "+v"(l));  // now, not where they are used
+            take(k, p);
         }
     }
 };
 
 // The end of a wavefront's 32 rows
-template <typename E, int D, int TK, typename P = E>
-__device__ __forceinline__ void finish_tile(const AttnArgs &a, const AttnItem &it, int kv_head, int part, const TileRows<E, D, TK> &t)
+template <typename E, int D, typename P = E, int TK, bool EXACT>
+__device__ __forceinline__ void finish_tile(const AttnArgs &a, const AttnItem &it, int kv_head, int part, const TileRows<E, D, TK, EXACT> &t)
 {
     constexpr int DJ = D / 32;
     const int lane = threadIdx.x & 63, r = lane & 31, h = lane >> 5, my = part * 32 + r, row = it.row0 + min(my, it.n_rows - 1);
@@ -995,14 +1020,14 @@ template <typename E, int D, typename P = E> struct TileShape {
     static constexpr int LDS = (2 * DEEP + 3) * PLACE;
 };
 
-template <typename E, int D, int GROUPS, typename P = E>
+template <typename E, int D, int GROUPS, typename P, bool EXACT>
 __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it, int kv_head, unsigned char *all_lds)
 {
     typedef TileShape<E, D, P> Shape;
     constexpr bool AS_IS = std::is_same_v<P, E>;  // pages hold what the products take
     constexpr int TK = Shape::TK, PLACE = Shape::PLACE, DEEP = Shape::DEEP, K_END = (DEEP + 1) * PLACE, V_END = (DEEP + 2) * PLACE;
     constexpr int U = CHUNK<E>;
-    typedef TileRows<E, D, TK> Rows;
+    typedef TileRows<E, D, TK, EXACT> Rows;
     constexpr int QC = Rows::QC, DJ = Rows::DJ, PK = Rows::PK, NV = PK * DJ, AHEAD = NV < 8 ? NV : 8, STRIDE = GROUPS * TK;
     typedef std::conditional_t<AS_IS, Steps<E, D, STRIDE>, StagesE4m3<D, 32, STRIDE>> Requests;
     // up to `steps` steps' requests are still on their way
@@ -1090,8 +1115,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it,
             p[i % U] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale_log2, -t.m));
             t.l += p[i % U];
             if (i % U == U - 1) {
-                t.w[i / U] = weights(p);
-                asm volatile("" : "+v"(t.w[i / U].x), "+v"(t.w[i / U].y), "+v"(t.w[i / U].z), "+v"(t.w[i / U].w), "+v"(t.l));  // now, not where they are used
+                t.take(i / U, p);
             }
         }
     };
@@ -1112,7 +1136,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it,
 #pragma unroll
             for (int e = 0; e < NV; ++e) {
                 __builtin_amdgcn_sched_barrier(0);
-                mma32<E>(t.o[e % DJ], fv[e % AHEAD], t.w[e / DJ]);
+                t.add(e % DJ, fv[e % AHEAD], e / DJ);
                 if (e + AHEAD < NV) fv[e % AHEAD] = value(e + AHEAD, v_last);
                 if (e < NV / 2) {
 #pragma unroll
@@ -1174,7 +1198,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it,
         request();
         if (last) {
 #pragma unroll
-            for (int e = 0; e < NV; ++e) mma32<E>(t.o[e % DJ], e < AHEAD ? fv[e] : value(e, v_last), t.w[e / DJ]);
+            for (int e = 0; e < NV; ++e) t.add(e % DJ, e < AHEAD ? fv[e] : value(e, v_last), e / DJ);
         }
         hide(s0);
         float top = -INFINITY;
@@ -1183,7 +1207,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it,
         follow(top);
         weigh(s0, 0, 16);
 #pragma unroll
-        for (int e = 0; e < NV; ++e) mma32<E>(t.o[e % DJ], first_values<E>(value(e, v), it.kv1 - t0 - (2 * (e / DJ) + h) * U), t.w[e / DJ]);
+        for (int e = 0; e < NV; ++e) t.add(e % DJ, first_values<E>(value(e, v), it.kv1 - t0 - (2 * (e / DJ) + h) * U), e / DJ);
     }
     for (int i = mine; i < n; ++i) {
         next();
@@ -1216,7 +1240,7 @@ __device__ __forceinline__ void attn_tile(const AttnArgs &a, const AttnItem &it,
                 for (int e = 0; e < 4; ++e) t.o[j][4 * i + e] = t.o[j][4 * i + e] * f0 + x[e] * f1;
             }
     }
-    if (wave * 32 < it.n_rows) finish_tile<E, D, TK, P>(a, it, kv_head, wave, t);
+    if (wave * 32 < it.n_rows) finish_tile<E, D, P>(a, it, kv_head, wave, t);
 }
 
 // Without the steps' overlap, whose registers would leave room for two blocks on a compute unit, for three: their wavefronts' products and exponentials fall beside each other's, and
@@ -1273,7 +1297,7 @@ __device__ __forceinline__ void attn_tile_plain(const AttnArgs &a, const AttnIte
 #pragma unroll
         for (int e = 0; e < NV; ++e) {
             __builtin_amdgcn_sched_barrier(0);
-            mma32<E>(t.o[e % DJ], f[e % AHEAD], t.w[e / DJ]);
+            t.add(e % DJ, f[e % AHEAD], e / DJ);
             if (e + AHEAD < NV) f[e % AHEAD] = value(e + AHEAD);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -1290,17 +1314,27 @@ __device__ __forceinline__ void attn_tile_plain(const AttnArgs &a, const AttnIte
         t.weigh(t0, a.scale_log2);
         // behind the last token: whatever is there, it is no value
 #pragma unroll
-        for (int i = 0; i < NV; ++i) mma32<E>(t.o[i % DJ], first_values<E>(value(i), it.kv1 - t0 - (2 * (i / DJ) + h) * U), t.w[i / DJ]);
+        for (int i = 0; i < NV; ++i) t.add(i % DJ, first_values<E>(value(i), it.kv1 - t0 - (2 * (i / DJ) + h) * U), i / DJ);
     }
-    if (wave * 32 < it.n_rows) finish_tile<E, D, TK>(a, it, kv_head, wave, t);
+    if (wave * 32 < it.n_rows) finish_tile<E, D>(a, it, kv_head, wave, t);
 }
 
-template <typename E, int D, typename P = E>
+// A tile as its item wants it.  EXACT: some of the batch's tiles are KV_EXACT; the kernels of batches without any are of their own
+template <bool EXACT, typename F>
+__device__ __forceinline__ void tile_of(const AttnItem &it, F work)
+{
+    if constexpr (EXACT) {
+        if (it.ctx == KV_EXACT) return work(std::true_type{});
+    }
+    work(std::false_type{});
+}
+
+template <typename E, int D, typename P, bool EXACT>
 __global__ __launch_bounds__(256, (TileShape<E, D>::BLOCKS)) void attn_tiles_kernel(AttnArgs a)
 {
     extern __shared__ __align__(16) unsigned char lds[];
     const AttnItem it = a.tiles[blockIdx.x / a.n_kv];
-    attn_tile<E, D, 1, P>(a, it, blockIdx.x % a.n_kv, lds);
+    tile_of<EXACT>(it, [&](auto exact) { attn_tile<E, D, 1, P, decltype(exact)::value>(a, it, blockIdx.x % a.n_kv, lds); });
 }
 
 template <typename E, int D> constexpr int MANY_LDS = 4 * 32 * D * (int)sizeof(E);
@@ -1318,7 +1352,7 @@ __global__ __launch_bounds__(256, 3) void attn_many_kernel(AttnArgs a)
 // time: 20 of 3000 beside 900 + 700 72.0 -> 74.2, 20 of 8000 135.1 -> 145.7; 30 of 2000 beside 700 with 40 heads 203 -> 219.  Of larger batches nothing is gained, or lost where rows have
 // fewer blocks on a compute unit this way (heads of 256, 100 tokens of 500 beside 600: 109 -> 122).
 constexpr int BOTH_ROUNDS = 4;
-template <typename E, int D, typename P = E>
+template <typename E, int D, typename P, bool EXACT>
 __global__ __launch_bounds__(256, (TileShape<E, D>::BLOCKS)) void attn_both_kernel(AttnArgs a)
 {
     extern __shared__ __align__(16) unsigned char lds[];
@@ -1326,7 +1360,7 @@ __global__ __launch_bounds__(256, (TileShape<E, D>::BLOCKS)) void attn_both_kern
     const uint32_t tiles = (uint32_t)a.n_tiles * a.n_kv;
     if (blockIdx.x < tiles) {
         const AttnItem it = a.tiles[blockIdx.x / a.n_kv];
-        attn_tile<E, D, 1, P>(a, it, blockIdx.x % a.n_kv, lds);
+        tile_of<EXACT>(it, [&](auto exact) { attn_tile<E, D, 1, P, decltype(exact)::value>(a, it, blockIdx.x % a.n_kv, lds); });
     } else {
         attn_rows_block<E, D, P>(a, blockIdx.x - tiles, *reinterpret_cast<RowsLds<D> *>(lds));
     }
@@ -1340,7 +1374,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const uint32_t tiles = (uint32_t)a.n_tiles * a.n_kv;
     if (blockIdx.x < tiles) {
         const AttnItem it = a.tiles[blockIdx.x / a.n_kv];
-        attn_tile<E, D, 2, P>(a, it, blockIdx.x % a.n_kv, lds);
+        attn_tile<E, D, 2, P, false>(a, it, blockIdx.x % a.n_kv, lds);
     } else if (threadIdx.x < 64 * ROW_WAVES) {
         attn_rows_block<E, D, P>(a, blockIdx.x - tiles, *reinterpret_cast<RowsLds<D> *>(lds));
     }
@@ -1359,17 +1393,14 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 // 3985 us).
 constexpr int turn_lds(int dim) { return 6 * 64 * dim * 2; }
 
-template <int D, typename P = __bf16>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_turns_kernel(AttnArgs a)
+template <int D, typename P, bool EXACT>
+__device__ __forceinline__ void attn_tile_turns(const AttnArgs &a, const AttnItem &it, int kv_head, unsigned char *lds)  // lds: keys of three stages, values of three
 {
     typedef __bf16 E;
     constexpr bool AS_IS = std::is_same_v<P, E>;  // pages hold what the products take
     typedef std::conditional_t<AS_IS, Stages<E, D>, StagesE4m3<D, 64, 64, 8>> Requests;
     constexpr int U = 8, TK = Stages<E, D>::TK, HALF = Stages<E, D>::HALF, PER = Stages<E, D>::PER, DJ = D / 32;
     constexpr int AHEAD = 8, NV = 4 * DJ, NK = D / 8;  // products of values, of keys
-    extern __shared__ __align__(16) unsigned char lds[];  // keys of three stages, values of three
-    const AttnItem it = a.tiles[blockIdx.x / a.n_kv];
-    const int kv_head = blockIdx.x % a.n_kv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 31, h = lane >> 5;
     const bool second = wave >= 4;
     const int n = (it.kv1 - it.kv0 + TK - 1) / TK;
@@ -1397,7 +1428,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         request_values();
         request_keys();
     }
-    TileRows<E, D, TK> t(a, it, kv_head, wave);
+    TileRows<E, D, TK, EXACT> t(a, it, kv_head, wave);
     t.wait_for_queries();
 
     // The products of a slot, NV of the values in place `v` of LDS and then NK of the keys in place `k`: operands come out of LDS AHEAD
@@ -1417,7 +1448,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int i = FROM; i < TO; ++i) {
             const int n_f = (i - FROM) % AHEAD;
             __builtin_amdgcn_sched_barrier(0);
-            if (i < NV) mma32<E>(t.o[i % DJ], f[n_f], t.w[i / DJ]);
+            if (i < NV) t.add(i % DJ, f[n_f], i / DJ);
             else if (i - NV < 2) mma32_first<E>(t.s[(i - NV) % 2], f[n_f], t.q[(i - NV) / 2]);
             else mma32<E>(t.s[(i - NV) % 2], f[n_f], t.q[(i - NV) / 2]);
             if (i + AHEAD < TO) f[n_f] = operand(i + AHEAD, v, k);
@@ -1475,9 +1506,17 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     if (!second) turn_over();
     // behind the last token: whatever is there, it is no value
 #pragma unroll
-    for (int i = 0; i < NV; ++i) mma32<E>(t.o[i % DJ], first_values<E>(operand(i, v, 0), it.kv1 - t0 - (2 * (i / DJ) + h) * U), t.w[i / DJ]);
+    for (int i = 0; i < NV; ++i) t.add(i % DJ, first_values<E>(operand(i, v, 0), it.kv1 - t0 - (2 * (i / DJ) + h) * U), i / DJ);
     wait_requests<0>();  // none is on its way to LDS when the block ends
-    if (wave * 32 < it.n_rows) finish_tile<E, D, TK, P>(a, it, kv_head, wave, t);
+    if (wave * 32 < it.n_rows) finish_tile<E, D, P>(a, it, kv_head, wave, t);
+}
+
+template <int D, typename P, bool EXACT>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_turns_kernel(AttnArgs a)
+{
+    extern __shared__ __align__(16) unsigned char lds[];
+    const AttnItem it = a.tiles[blockIdx.x / a.n_kv];
+    tile_of<EXACT>(it, [&](auto exact) { attn_tile_turns<D, P, decltype(exact)::value>(a, it, blockIdx.x % a.n_kv, lds); });
 }
 
 // A block joins the parts of one row: each wavefront finds the joined maximum and weight from all parts', then groups of D / 4 threads add

@@ -33,15 +33,20 @@ hipError_t prepare_attn_kernels()
             (void)by_type(dtype, dim, [&](auto t, auto d) {
                 typedef decltype(t) E;
                 constexpr int D = decltype(d)::value;
-                allow(reinterpret_cast<const void *>(&attn_tiles_kernel<E, D>), TileShape<E, D>::LDS);
-                allow(reinterpret_cast<const void *>(&attn_both_kernel<E, D>), TileShape<E, D>::LDS);
+                const auto allow_tiles = [&](auto exact) {
+                    allow(reinterpret_cast<const void *>(&attn_tiles_kernel<E, D, E, decltype(exact)::value>), TileShape<E, D>::LDS);
+                    allow(reinterpret_cast<const void *>(&attn_both_kernel<E, D, E, decltype(exact)::value>), TileShape<E, D>::LDS);
+                };
+                allow_tiles(std::false_type{});
+                if constexpr (sizeof(E) == 2) allow_tiles(std::true_type{});
                 if constexpr (kv_many(sizeof(E) == 2 ? LORA_BF16 : LORA_F32, D)) allow(reinterpret_cast<const void *>(&attn_many_kernel<E, D>), MANY_LDS<E, D>);
                 if constexpr (kv_pairs(sizeof(E) == 2 ? LORA_BF16 : LORA_F32, D)) {
                     static_assert(2 * TileShape<E, D>::LDS >= 4 * (32 * D * 4 + 512), "one group's results in LDS");
                     allow(reinterpret_cast<const void *>(&attn_pairs_kernel<E, D>), 2 * TileShape<E, D>::LDS);
                 }
             });
-    allow(reinterpret_cast<const void *>(&attn_turns_kernel<128>), turn_lds(128));
+    allow(reinterpret_cast<const void *>(&attn_turns_kernel<128, __bf16, false>), turn_lds(128));
+    allow(reinterpret_cast<const void *>(&attn_turns_kernel<128, __bf16, true>), turn_lds(128));
     return e;
 }
 
@@ -53,28 +58,34 @@ hipError_t launch_attn(const AttnArgs &a, int dtype, int dim, KvTiles way, int n
     return by_type(dtype, dim, [&](auto e, auto d) {
         typedef decltype(e) E;
         constexpr int D = decltype(d)::value;
-        if (n_tiles && n_rows && way == KV_TILES_PLAIN && (n_tiles + n_rows <= BOTH_ROUNDS * TileShape<E, D>::BLOCKS * n_cu || (a.prefixes && TileShape<E, D>::BLOCKS > 1 && n_tiles + n_rows <= INT32_MAX))) {
-            hipLaunchKernelGGL((attn_both_kernel<E, D>), dim3((unsigned)(n_tiles + n_rows)), dim3(256), (TileShape<E, D>::LDS), st, a);
-            return;
-        }
-        if constexpr (kv_pairs(sizeof(E) == 2 ? LORA_BF16 : LORA_F32, D))
-            if (way == KV_TILES_PAIRS) {
-                hipLaunchKernelGGL((attn_pairs_kernel<E, D>), dim3((unsigned)(n_tiles + n_rows)), dim3(512), (2 * TileShape<E, D>::LDS), st, a);
+        const auto launch = [&](auto exact) {
+            constexpr bool EXACT = decltype(exact)::value;
+            if (n_tiles && n_rows && way == KV_TILES_PLAIN && (n_tiles + n_rows <= BOTH_ROUNDS * TileShape<E, D>::BLOCKS * n_cu || (a.prefixes && TileShape<E, D>::BLOCKS > 1 && n_tiles + n_rows <= INT32_MAX))) {
+                hipLaunchKernelGGL((attn_both_kernel<E, D, E, EXACT>), dim3((unsigned)(n_tiles + n_rows)), dim3(256), (TileShape<E, D>::LDS), st, a);
                 return;
             }
-        bool done = n_tiles == 0;
-        if constexpr (kv_turns(sizeof(E) == 2 ? LORA_BF16 : LORA_F32, D))
-            if (!done && way == KV_TILES_TURNS) {
-                hipLaunchKernelGGL((attn_turns_kernel<D>), tiles, dim3(512), turn_lds(D), st, a);
-                done = true;
-            }
-        if constexpr (kv_many(sizeof(E) == 2 ? LORA_BF16 : LORA_F32, D))
-            if (!done && way == KV_TILES_MANY) {
-                hipLaunchKernelGGL((attn_many_kernel<E, D>), tiles, dim3(256), (MANY_LDS<E, D>), st, a);
-                done = true;
-            }
-        if (!done) hipLaunchKernelGGL((attn_tiles_kernel<E, D>), tiles, dim3(256), (TileShape<E, D>::LDS), st, a);
-        if (n_rows) hipLaunchKernelGGL((attn_rows_kernel<E, D>), rows, dim3(64 * ROW_WAVES), 0, st, a);
+            if constexpr (kv_pairs(sizeof(E) == 2 ? LORA_BF16 : LORA_F32, D))
+                if (way == KV_TILES_PAIRS) {  // (no batch with prefixes)
+                    hipLaunchKernelGGL((attn_pairs_kernel<E, D>), dim3((unsigned)(n_tiles + n_rows)), dim3(512), (2 * TileShape<E, D>::LDS), st, a);
+                    return;
+                }
+            bool done = n_tiles == 0;
+            if constexpr (kv_turns(sizeof(E) == 2 ? LORA_BF16 : LORA_F32, D))
+                if (!done && way == KV_TILES_TURNS) {
+                    hipLaunchKernelGGL((attn_turns_kernel<D, E, EXACT>), tiles, dim3(512), turn_lds(D), st, a);
+                    done = true;
+                }
+            if constexpr (kv_many(sizeof(E) == 2 ? LORA_BF16 : LORA_F32, D))
+                if (!done && way == KV_TILES_MANY) {  // (no batch with KV_EXACT tiles)
+                    hipLaunchKernelGGL((attn_many_kernel<E, D>), tiles, dim3(256), (MANY_LDS<E, D>), st, a);
+                    done = true;
+                }
+            if (!done) hipLaunchKernelGGL((attn_tiles_kernel<E, D, E, EXACT>), tiles, dim3(256), (TileShape<E, D>::LDS), st, a);
+            if (n_rows) hipLaunchKernelGGL((attn_rows_kernel<E, D>), rows, dim3(64 * ROW_WAVES), 0, st, a);
+        };
+        if constexpr (sizeof(E) == 2)
+            if (a.exact) return launch(std::true_type{});
+        launch(std::false_type{});
     });
 }
 

@@ -74,6 +74,7 @@ struct Batch {
     hipEvent_t uploaded = nullptr;
     lora_kv_batch_info_t info{};
     int32_t max_pos = -1;  // of the batch's tokens
+    bool exact = false;    // some of its tiles are KV_EXACT
     int32_t n_joins = 0, n_tile_joins = 0, join_rows = 0;  // join_rows: the most rows of a join of row items
     int32_t n_shared_joins = 0, shared_rows = 0;  // segments with prefixes; the most rows of one
     lora_kv_prefix_info_t prefixes{};
@@ -369,6 +370,7 @@ struct Prefix {
     int32_t from, to;
     std::vector<int32_t> segs;
     int64_t rows;
+    bool exact;  // tiles of it keep weights to 16 bits
 };
 
 // How the attention of a batch is cut up.
@@ -379,6 +381,7 @@ struct Cut {
     std::vector<SharedSource> sources;
     std::vector<SharedBlock> blocks;
     std::vector<SharedJoin> shared_joins;
+    bool exact = false;  // some of the prefixes' tiles are KV_EXACT
     int32_t prefix_row_items = 0, prefix_tile_items = 0, prefix_segments = 0;
     int32_t extra_joins = 0;  // blocks that share nothing and are joined with the others
     lora::KvTiles way = lora::KV_TILES_PLAIN;
@@ -476,7 +479,11 @@ void find_prefixes(const lora_kv &kv, const Growth &g, int32_t min_tokens, Cut &
             if (to > part.base && worth((int64_t)(to - part.base) << kv.page_shift, (int64_t)part.segs.size(), tokens * grp)) {
                 if (tokens > room) continue;
                 room -= tokens;
-                cut.prefixes.push_back({part.base, to, part.segs, tokens * grp});
+                // in bf16 the weights of few rows have 16 bits: they must not lose them by sharing
+                const bool exact = tokens * grp > lora::KV_ROW_ITEM && kv.cfg.dtype == LORA_BF16 &&
+                                   std::any_of(part.segs.begin(), part.segs.end(), [&](int32_t i) { return (int64_t)g.n_tokens[i] * grp <= lora::KV_ROW_ITEM; });
+                cut.exact = cut.exact || exact;
+                cut.prefixes.push_back({part.base, to, part.segs, tokens * grp, exact});
                 for (const int32_t i : part.segs) cut.own[i] = to;
                 part.base = to;
                 ++part.depth;
@@ -527,7 +534,7 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
             if (p.rows > lora::KV_ROW_ITEM) tokens += (p.rows + tile - 1) / tile * tokens_of(p), n_tiles += (p.rows + tile - 1) / tile;
         if (n_tiles * n_kv >= 2 * kv.n_cu && tokens >= 1024 * n_tiles) cut.way = lora::KV_TILES_TURNS;
         // Prefixes, of which there are few tiles: as many pieces as compute units where each is long enough and the tiles' rows are there.  32 requests behind 100000 tokens with 64 / 8 heads
-        // 150 -> 136 us.
+        // 180 -> 162 us.
         int64_t large = 0, small = 0;
         for (const Prefix &p : cut.prefixes)
             if (p.rows > lora::KV_ROW_ITEM) large += (p.rows + tile - 1) / tile * tokens_of(p), small += (p.rows + lora::KV_TILE - 1) / lora::KV_TILE * tokens_of(p);
@@ -651,7 +658,7 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
                 for (int32_t t = 0; t < g.n_tokens[i]; ++t) cut.row_tokens.push_back(offsets[i] + t);
                 row += (int64_t)g.n_tokens[i] * grp;
             }
-            AttnItem it{list0, lora::KV_SHARED, cut.page0[p.segs[0]], 0, 0, 0, 0, -1};
+            AttnItem it{list0, p.exact ? lora::KV_EXACT : lora::KV_SHARED, cut.page0[p.segs[0]], 0, 0, 0, 0, -1};
             for (int64_t r = 0; r < p.rows; r += rows_of) {
                 it.row0 = (int32_t)r;
                 it.n_rows = (int32_t)std::min(p.rows - r, (int64_t)rows_of);
@@ -709,7 +716,7 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     }
     // Three blocks on a compute unit, where the tiles fill more than three for each, or more than two and are short (256 tokens in the mean): bf16 heads of 128, two blocks -> three,
     // 8 x 500 tokens with 32 heads 42.6 -> 39.2 us, 6 x 300 24.4 -> 17.3; but 2048 with 40 heads 68.2 -> 74.5.
-    if (cut.way == lora::KV_TILES_PLAIN && !kv.e4m3() && lora::kv_many(kv.cfg.dtype, kv.cfg.head_dim)) {
+    if (cut.way == lora::KV_TILES_PLAIN && !kv.e4m3() && !cut.exact && lora::kv_many(kv.cfg.dtype, kv.cfg.head_dim)) {
         int64_t blocks = (int64_t)cut.tiles.size() * n_kv, tokens = 0;
         for (const AttnItem &t : cut.tiles) tokens += t.kv1 - t.kv0;
         if (blocks > 3 * kv.n_cu || (blocks > 2 * kv.n_cu && tokens < 256 * (int64_t)cut.tiles.size())) cut.way = lora::KV_TILES_MANY;
@@ -1156,6 +1163,7 @@ static int create_batch(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, co
             if (!cut_attention(*kv, g, seg_offsets, cut)) {
                 cut.prefixes.clear();
                 cut.own.clear();
+                cut.exact = false;
                 cut.way = lora::KV_TILES_PLAIN;
                 (void)cut_attention(*kv, g, seg_offsets, cut);
             }
@@ -1185,7 +1193,7 @@ static int create_batch(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, co
         b->off_shared_joins = place(cut.shared_joins.size() * sizeof(SharedJoin));
         KvToken *tokens = reinterpret_cast<KvToken *>(b->pinned + b->off_tokens);
         int32_t *pages = reinterpret_cast<int32_t *>(b->pinned + b->off_pages);
-        b->max_pos = -1;
+        b->max_pos = -1, b->exact = cut.exact;
         const int u = kv->chunk();
         for (int32_t i = 0; i < n_seg; ++i) {
             const Seq &s = *g.seqs[i];
@@ -1350,7 +1358,7 @@ int lora_kv_attend(lora_kv_t *kv, lora_kv_batch_t *handle, int32_t layer, const 
     a.page_stride = (int64_t)kv->page_bytes;
     a.page_list = reinterpret_cast<const int32_t *>(batch->dev + batch->off_pages);
     a.row_tokens = reinterpret_cast<const int32_t *>(batch->dev + batch->off_row_tokens);
-    a.prefixes = batch->n_shared_joins != 0;
+    a.prefixes = batch->n_shared_joins != 0, a.exact = batch->exact;
     a.part_o = kv->part_o, a.part_ml = kv->part_ml;
     a.scale_log2 = scale_log2;
     a.n_kv = c.n_kv_heads, a.group = kv->group(), a.page_shift = kv->page_shift;

@@ -40,7 +40,7 @@ struct KvGroup {
 // sequence.  Row r is query head kv_head * g + r % g of the segment's token r / g.
 struct AttnItem {
     int32_t tok0;   // the segment's first token in the packed batch; of rows that share a prefix: where their tokens are listed
-    int32_t ctx;    // its position; KV_SHARED: the rows of several segments, which see all the tokens
+    int32_t ctx;    // its position; KV_SHARED, KV_EXACT: the rows of several segments, which see all the tokens
     int32_t page0;  // the sequence's first entry of the page list
     int32_t row0, n_rows;
     int32_t kv0, kv1;
@@ -49,6 +49,7 @@ struct AttnItem {
 };
 
 constexpr int KV_SHARED = LORA_KV_MAX_TOKENS;  // (no segment's first token stands there)
+constexpr int KV_EXACT = KV_SHARED + 1;        // ... and a tile of them keeps its weights to 16 bits as row items do: some of the segments have no more rows than those
 
 // Batches with shared prefixes: every part of what a row attends to -- prefixes, the segment's own tokens -- is a source of partial results, which lie in
 // blocks of rows: row r of the source is row (row0 + r) % rows of block block0 + (row0 + r) / rows.  A join puts together rows first .. first + n_rows - 1 of its sources (KV_JOIN_ROWS at
@@ -123,7 +124,7 @@ struct AttnArgs {
     float *part_o, *part_ml;
     float scale_log2;  // scale * log2(e)
     int32_t n_tiles, n_rows, n_short, n_kv, group, page_shift;  // n_short: items behind the n_rows that a wavefront takes alone
-    bool prefixes;  // some of the items are rows of several segments
+    bool prefixes, exact;  // some of the items are rows of several segments; some of the tiles are KV_EXACT
 };
 
 struct JoinArgs {
