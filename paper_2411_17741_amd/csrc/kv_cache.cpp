@@ -476,8 +476,8 @@ void find_prefixes(const lora_kv &kv, const Growth &g, int32_t min_tokens, Cut &
                 tokens += g.n_tokens[i];
             }
             const int32_t to = part.at & ~(std::max(PIECE_STEP >> kv.page_shift, 1) - 1);  // (what is behind a prefix begins where pieces may)
-            if (to > part.base && worth((int64_t)(to - part.base) << kv.page_shift, (int64_t)part.segs.size(), tokens * grp)) {
-                if (tokens > room) continue;
+            // (one that has no room is left out; fewer segments that share more may have)
+            if (to > part.base && tokens <= room && worth((int64_t)(to - part.base) << kv.page_shift, (int64_t)part.segs.size(), tokens * grp)) {
                 room -= tokens;
                 // in bf16 the weights of few rows have 16 bits: they must not lose them by sharing
                 const bool exact = tokens * grp > lora::KV_ROW_ITEM && kv.cfg.dtype == LORA_BF16 &&
