@@ -27,7 +27,7 @@
  * a value of token p and head h stands for value * 2^(exponent - 127).  lora_kv_append stores the smallest exponent, of 10 to 247, with which
  * no finite value of the token's head is over 448, and of each value the nearest of 8 bits (halves to even); what is infinite or no number
  * is stored as no number.  All that is stored that way is exact in bf16 (but values over 3.29e38 come out infinite), which is what attention and lora_kv_seq_read work with.  Exponents that the caller puts
- * there himself are 1 to 254.
+ * there himself are 1 to 254; with those below 10 values under 2^-126 may come out as 0.
  *
  * Conventions are those of lora_cache.h: every function returns LORA_OK or a negative lora_status, nothing aborts or
  * throws; device memory is the caller's; streams are hipStream_t as void* (NULL = the default stream); calls only

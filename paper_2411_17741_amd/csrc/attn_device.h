@@ -50,16 +50,18 @@ __device__ __forceinline__ const uint8_t *exponents(const AttnArgs &a, int page,
 __device__ __forceinline__ int token_of(const AttnArgs &a, const AttnItem &it, int t) { return it.ctx >= KV_SHARED ? a.row_tokens[it.tok0 + t] : it.tok0 + t; }
 
 // One row by one wavefront, a token a lane for the scores and D / 64 values of the output a lane.  Lane i holds values i, i + 64, ...  The weights, and their sum l, are
-// 2^28 times smaller than elsewhere: a sequence has no more tokens than that, so their sums with values of any size stay in range.
+// 2^28 times smaller than elsewhere: a sequence has no more tokens than that, so their sums with values of any size stay in range.  Sums over pages of 8 bits, whose values are small
+// or large by whole tokens, are held in 64 bits: so small weights would leave the smallest values' products few bits.
 constexpr float ROW_ROOM = 1 << 28;
 static_assert(LORA_KV_MAX_TOKENS <= 1 << 28, "the room of one_row's sums");
-template <typename E, int D> struct RowState {
-    float m, l, o[D / 64];
+// P: the pages' values
+template <typename E, int D, typename P> struct RowState {
+    float m, l;
+    std::conditional_t<std::is_same_v<P, E>, float, double> o[D / 64];
 };
 
-// P: the pages' values
 template <typename E, int D, typename P = E>
-__device__ void one_row(const AttnArgs &a, const AttnItem &it, int kv_head, int row, int kv0, int kv1, RowState<E, D> &st)
+__device__ void one_row(const AttnArgs &a, const AttnItem &it, int kv_head, int row, int kv0, int kv1, RowState<E, D, P> &st)
 {
     constexpr int U = CHUNK<P>;
     const int lane = threadIdx.x & 63;
@@ -70,7 +72,7 @@ __device__ void one_row(const AttnArgs &a, const AttnItem &it, int kv_head, int 
     st.m = -FLT_MAX;
     st.l = 0.f;
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) st.o[j] = 0.f;
+    for (int j = 0; j < D / 64; ++j) st.o[j] = 0;
     for (int s0 = kv0; s0 < end; s0 += 64) {
         const int tok = min(s0 + lane, end - 1), page = a.page_list[it.page0 + (tok >> a.page_shift)];
         const P *k = half_page<P, D>(a, page, kv_head, 0) + (tok & in_page) * U;
@@ -109,7 +111,7 @@ __device__ void one_row(const AttnArgs &a, const AttnItem &it, int kv_head, int 
                     const float w = __shfl(p, c * U + e, 64);
                     if (at + e < end) {
                         if constexpr (std::is_same_v<P, E>) st.o[j] += w * (float)vc.v[e];
-                        else st.o[j] += w * (value_of(vc.v[e]) * unit_of(exponents<D>(a, page, kv_head, 1)[(at & in_page) + e]));
+                        else st.o[j] += (double)w * (value_of(vc.v[e]) * unit_of(exponents<D>(a, page, kv_head, 1)[(at & in_page) + e]));
                     }
                 }
             }
@@ -288,8 +290,8 @@ constexpr float SLACK = 8.f;
 __device__ __forceinline__ int tile_part(int r, int d) { return ((d / 8) * 64 + (d / 4 % 2) * 32 + r) * 4 + d % 4; }
 
 // A row that one_row() has done: to its place in the output, or with the partial results (`at`: the row's; tiles keep theirs in another order)
-template <typename E, int D, bool TILE>
-__device__ __forceinline__ void put_row(const AttnArgs &a, const AttnItem &it, int kv_head, int r, const RowState<E, D> &st)
+template <typename E, int D, bool TILE, typename P>
+__device__ __forceinline__ void put_row(const AttnArgs &a, const AttnItem &it, int kv_head, int r, const RowState<E, D, P> &st)
 {
     const int lane = threadIdx.x & 63;
     const float f = it.part >= 0 && st.l == 0.f ? 0.f : 1.f / st.l;
@@ -298,15 +300,15 @@ __device__ __forceinline__ void put_row(const AttnArgs &a, const AttnItem &it, i
 #pragma unroll
         for (int j = 0; j < D / 64; ++j) {
             const int d = lane + 64 * j;
-            if (TILE) a.part_o[(at - (r & 31)) * D + tile_part(r & 31, d)] = st.o[j] * f;  // (32 rows' results begin wherever the pieces before them end)
-            else a.part_o[at * D + d] = st.o[j] * f;
+            if (TILE) a.part_o[(at - (r & 31)) * D + tile_part(r & 31, d)] = (float)(st.o[j] * f);  // (32 rows' results begin wherever the pieces before them end)
+            else a.part_o[at * D + d] = (float)(st.o[j] * f);
         }
         if (lane == 0) a.part_ml[2 * at] = st.m, a.part_ml[2 * at + 1] = st.l * ROW_ROOM;
     } else {
         const int row = it.row0 + r;
         E *out = static_cast<E *>(a.out) + (int64_t)(it.tok0 + row / a.group) * a.out_stride + (kv_head * a.group + row % a.group) * D;
 #pragma unroll
-        for (int j = 0; j < D / 64; ++j) out[lane + 64 * j] = (E)(st.o[j] * f);
+        for (int j = 0; j < D / 64; ++j) out[lane + 64 * j] = (E)(float)(st.o[j] * f);
     }
 }
 
@@ -351,7 +353,7 @@ __device__ __forceinline__ void finish_rows(const AttnArgs &a, const AttnItem &i
     const bool redo = __any(none != 0.f);
     const auto again = [&](int from, int step) {
         for (int i = from; i < it.n_rows; i += step) {
-            RowState<E, D> st;
+            RowState<E, D, P> st;
             one_row<E, D, P>(a, it, kv_head, it.row0 + i, it.kv0, it.kv1, st);
             put_row<E, D, false>(a, it, kv_head, i, st);
         }
@@ -524,8 +526,10 @@ __device__ __forceinline__ void attn_rows(const AttnArgs &a, const AttnItem &it,
 }
 
 // Up to 16 rows over pages of 8-bit values.  As above with steps of 64 tokens: a 16-byte chunk is 16 values, and so two operands.  The keys' chunks are turned into
-// bf16 with their tokens' units at once, which is exact; a chunk of values is of 16 tokens, and the weights take their units.  The tokens of a step may lie in two
+// bf16 with their tokens' units at once, which is exact; a chunk of values is of 16 tokens, and the weights take their units.  Those may be 2^-126, and a weight that leaves the normal numbers loses
+// bits: the maximum that weights are measured by lies ROWS_LEAD below the scores' (weights that leave them at the other end have their rows done again).  The tokens of a step may lie in two
 // pages (of 32).  Bound by memory where there is much of it: 512 tokens of about 1000 cached ones with 32 / 8 heads of 128, 1.32 GB, in 206 us, 6.4 TB/s (matrix units busy 14 % of the time); one of 131071 with 64 / 8 46 to 47 us, 5.8.
+constexpr float ROWS_LEAD = 24.f;
 template <int D, bool ALONE>
 __device__ __forceinline__ void attn_rows_e4m3(const AttnArgs &a, const AttnItem &it, int kv_head, RowsLds<D> &lds)
 {
@@ -591,6 +595,7 @@ __device__ __forceinline__ void attn_rows_e4m3(const AttnArgs &a, const AttnItem
 #pragma unroll
         for (int e = 1; e < U; ++e) top = fmaxf(top, p[e]);
         top = max16(max32(top));
+        top -= ROWS_LEAD;
         if (__any(top > m + SLACK)) {
             const float now = fmaxf(m, top), fade = __builtin_amdgcn_exp2f(m - now);
             m = now;
@@ -965,7 +970,7 @@ __device__ __forceinline__ void finish_tile(const AttnArgs &a, const AttnItem &i
         for (int i = 0; i < 16; ++i) none += t.o[j][i] * 0.f;
     if (__any(none != 0.f)) {
         for (int i = part * 32; i < min(it.n_rows, part * 32 + 32); ++i) {
-            RowState<E, D> st;
+            RowState<E, D, P> st;
             one_row<E, D, P>(a, it, kv_head, it.row0 + i, it.kv0, it.kv1, st);
             put_row<E, D, true>(a, it, kv_head, i, st);
         }
