@@ -520,7 +520,7 @@ __global__ __launch_bounds__(256) void append_heads_kernel(AppendHeadsArgs n, ui
             if (w) {
                 const float by = (float)factor;
 #pragma unroll
-                for (int e = 0; e < U; ++e) u[e] *= by * wx[e], v[e] *= by * wy[e];
+                for (int e = 0; e < U; ++e) u[e] = u[e] * by * wx[e], v[e] = v[e] * by * wy[e];  // (what is normed is of an ordinary size, a factor times a weight may be of none)
             }
             if (turn) turn_pairs(u, v, c, s, halves);
 #pragma unroll
