@@ -471,7 +471,7 @@ __global__ __launch_bounds__(256) void append_heads_kernel(AppendHeadsArgs n, ui
                     const auto add = [&](uint32_t two) { sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, two), sum, false); };
                     add(xw.x), add(xw.y), add(xw.z), add(xw.w), add(yw.x), add(yw.y), add(yw.z), add(yw.w);
                     sum = over_pairs(sum, tokens);
-                    const bool far = !(sum < 1e37f);
+                    const bool far = !(sum < 1e37f) || n.eps > 1e37;
                     factor = (double)__builtin_amdgcn_rsqf(sum / (float)a.dim + (float)n.eps);
                     if (__any(far)) {
                         const double f = exactly();

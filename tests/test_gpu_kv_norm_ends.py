@@ -13,7 +13,7 @@ torch = pytest.importorskip("torch")
 @pytest.mark.parametrize("dim", [64, 128, 256])
 @pytest.mark.parametrize("size,weight,eps", [
     (1e36, 1e-8, 1e-5), (1e30, 1e-14, 1e-5), (1e-15, 1e28, 1e-30),  # the factor of a head times a weight leaves them
-    ])
+    (1e17, 1.0, float(np.finfo(np.float32).max)), (1e10, 1e6, 1e38)])  # the mean of the squares and eps do
 def test_results_in_range_of_what_is_not(size, weight, eps, dim, kind):
     from paper_2411_17741_amd import binding as B
     from paper_2411_17741_amd.kv import KvCache
