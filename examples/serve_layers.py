@@ -1,12 +1,12 @@
 """Serving a few layers of a model with adapters: what an iteration does with the adapter cache and the key-value cache together.
 
-    python examples/serve_layers.py [--layers 2] [--heads 32] [--kv-heads 8] [--dim 128] [--requests 8] [--iterations 6] [--norms] [--e4m3] [--shared]
+    python examples/serve_layers.py [--layers 2] [--heads 32] [--kv-heads 8] [--dim 128] [--requests 8] [--iterations 6] [--norms] [--e4m3] [--shared [64]]
 
 Every iteration forms a batch -- the prompts of new requests, one token of each running one -- and runs, per layer, the q, k, v
 projections with the adapters of the requests, lora_kv_append (positions, keys and values into the pages), lora_kv_attend and the o projection with
 its adapters.  Half way one request is forked into continuations that share its pages, some requests end, and the pages in use
 are moved together so that the rest of the memory is free for adapters.  --norms norms every head's queries and keys before they turn, --e4m3 holds keys and values in 8 bits,
---shared reads what requests share once for all of them.  The model is synthetic (random weights, no MLP); the
+--shared reads what requests share once for all of them, from so many tokens on (0: where it is worth it, which takes more requests or longer prompts than these).  The model is synthetic (random weights, no MLP); the
 base projections are plain matrix products."""
 from __future__ import annotations
 
@@ -66,6 +66,7 @@ class Layers:
         ranks = np.asarray([self.rank[a] if a >= 0 else 0 for a in adapters], np.int32)
         plan = self.pool.plan(len(x), off, slots, ranks)
         batch = self.cache.batch(np.asarray(requests, np.int64), off, shared=self.shared)
+        self.prefixes = B.lora_kv_batch_prefixes(batch)[1]
         scale = 1.0 / math.sqrt(self.dim)
         for layer, w in enumerate(self.w):
             q, k, v = (x @ w[p] for p in range(3))
@@ -90,8 +91,9 @@ def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     for name, value in (("layers", 2), ("heads", 32), ("kv-heads", 8), ("dim", 128), ("requests", 8), ("iterations", 6)):
         ap.add_argument("--" + name, type=int, default=value)
-    for name in ("norms", "e4m3", "shared"):
+    for name in ("norms", "e4m3"):
         ap.add_argument("--" + name, action="store_true")
+    ap.add_argument("--shared", type=int, nargs="?", const=64, default=False)
     a = ap.parse_args(argv)
     rng = np.random.default_rng(1)
     # room for prompts of up to 300 tokens, a token in each iteration after that, and the continuations
@@ -123,7 +125,8 @@ def main(argv=None):
             t = time.perf_counter()
             y = model.step(x, ids, [adapter[i] for i in ids], lens)
             torch.cuda.synchronize()
-            print(f"iteration {it}: {len(ids)} requests, {sum(lens)} tokens, {1e3 * (time.perf_counter() - t):.2f} ms, output rms {float(y.float().square().mean().sqrt()):.3f}")
+            print(f"iteration {it}: {len(ids)} requests, {sum(lens)} tokens, {1e3 * (time.perf_counter() - t):.2f} ms, output rms {float(y.float().square().mean().sqrt()):.3f}"
+                  + (f", {model.prefixes.n_segments} behind {model.prefixes.n_tokens} shared tokens" if model.prefixes.n_prefixes else ""))
             lengths = {i: 1 for i in ids}
         return model.cache.stats()
     finally:
