@@ -45,16 +45,19 @@ constexpr int MAX_EXTRA = 2048;  // pieces beyond one for each block of rows
 // Of how many prefixes of prefixes a segment may have a part; tokens' places in all of them together (times max_batch_tokens); tokens of a piece of a prefix with few rows
 constexpr int SHARED_DEPTH = 7, SHARED_TOKENS = 2, SHARED_ROW_MIN_TOKENS = 256;
 // A prefix is worth it if the segments but one are spared more bytes of keys and values than these, and so many for each row of each head of 128, whose parts are written and read again.  (The bytes
-// that are spared would mostly have come out of caches.)  Measured, one by one -> shared, us, heads of 128, each request 100 tokens of its own behind the prefix: 64 requests with 32 / 8 heads
-// and 600 tokens, 148 MB, 19.3 -> 18.4, 512 tokens, 132 MB, 17.4 -> 21.1; 256 requests and 256 tokens, 267 MB, 42.3 -> 36.4, 128 tokens 35.8 -> 37.4; 20 of 1800, 140 MB, 21.5 -> 17.8, 1024 tokens 15.5 -> 18.2; with 64 / 8
-// heads 64 of 800 23.7 -> 22.0, 640 20.0 -> 20.4; 60 with 40 / 40 and 200 46 -> 36.  Of few rows: 2 requests with 40 / 40 heads and 1024 tokens, 21 MB, 13.2 -> 12.7, 512 tokens 12.5 -> 12.6.
+// that are spared would mostly have come out of caches.)  Measured, one by one -> shared, us, heads of 128, each request 100 tokens of its own behind the prefix, with a deviation of the logarithm of 0.4 (in
+// brackets: 100 for all): 64 requests with 32 / 8 heads and 600 tokens, 148 MB, 27.9 -> 20.0 (19.3 -> 20.1), 1024 tokens 35.4 -> 24.9 (26.1 -> 24.9), 512 tokens, 132 MB, 25.1 -> 23.2 (17.3 -> 23.4); with 64 / 8 heads 800
+// tokens 33.2 -> 23.6 (23.4 -> 23.4), 640 29.2 -> 21.5 (19.8 -> 21.6).  256 requests with 32 / 8 heads and 256 tokens, 267 MB, 41.8 -> 35.4, 128 tokens 35.5 -> 36.7; 20 of 1800, 140 MB, 22.1 -> 20.0, 1500 20.1 -> 21.0; 5 of
+// 8000 28.1 -> 23.1, 5000 21.0 -> 21.7; 60 with 40 / 40 and 200 46.4 -> 35.9.  In 8 bits 64 with 32 / 8 and 2000 31.6 -> 26.2, 1500 25.9 -> 26.1, 1024 20.9 -> 25.6.  Of few rows: 2 requests with 40 / 40 heads and 1024
+// tokens, 21 MB, 14.2 -> 13.0, 512 tokens 12.5 -> 12.5.  The rule counts bytes alone, and not the pieces that either way cuts: it loses with 64 requests and 512 or 640 tokens of lengths that differ, with 128 of 320
+// (25.5 -> 22.3) and with 20 of 300 with 40 / 40 heads (25.0 -> 20.9).
 constexpr int64_t SHARED_FEW_BYTES = 16 << 20, SHARED_BYTES = 112 << 20, SHARED_ROW_BYTES = 14 << 10;
 // Few blocks are as fast as the compute unit that has most of them: a block takes its tokens and EVEN_BLOCK more, and of rows each over two for a compute unit waits, EVEN_WAIT.  Pieces of an even share of all
 // tokens -> so cut, us.  Rows in 8 bits: 4 tokens of 30000 with 64 / 8 heads of 128 57.3 -> 49.9 (544 blocks, 512), 3 of about 50000 80 -> 70, 20 of 4000 with 32 / 8 38.4 -> 35.0, one of 131071 with 64 / 8
 // 56.2 -> 54.2; 2 of 1500 with 40 / 40 17.2 -> 17.8.  Tiles in 8 bits: 128 tokens behind 20000 with 32 / 8 72 -> 63.6, 500 behind 2000 with 40 / 40 54 -> 45, 256 behind 5000 with 16 / 4 heads of 256 69 -> 48,
-// 1500 44 -> 41.  Prefixes: 4 requests behind 9000 tokens with 32 / 8 heads 20.3 -> 16.0, 8 behind 1500 with 40 / 40 16.9 -> 14.5 (without EVEN_WAIT 16.9), 10 behind 1200 with 32 / 32 14.2 -> 14.4; in tiles, 200 behind
-// 20000 with 40 / 40 242 -> 199, 16 behind 40000 with 48 / 6 53 -> 43, 30 behind 30000 with 32 / 8 heads of 256 102 -> 82; tiles beside them,
-// 3 x 180 and 20 tokens behind 4000 with 32 / 8 74 -> 66, 2 x 100 behind 6000 53 -> 47; 30 tokens, 40, 7 and 150 behind 2000 30.9 -> 33.0.  (Pages that are not of 8 bits, and share nothing, are cut as they always were.)
+// 1500 44 -> 41.  Prefixes: 4 requests behind 9000 tokens with 32 / 8 heads 20.3 -> 15.9, 8 behind 1500 with 40 / 40 16.5 -> 14.1 (without EVEN_WAIT 16.9), 10 behind 1200 with 32 / 32 15.4 -> 15.3; in tiles, 200 behind
+// 20000 with 40 / 40 332 -> 271, 16 behind 40000 with 48 / 6 56 -> 52, 30 behind 30000 with 32 / 8 heads of 256 110 -> 89; tiles beside them,
+// 3 x 180 and 20 tokens behind 4000 with 32 / 8 74 -> 64, 2 x 100 and 8 behind 6000 55 -> 44; 30 tokens, 40, 7 and 150 behind 2000 30.1 -> 29.3.  (Pages that are not of 8 bits, and share nothing, are cut as they always were.)
 constexpr int64_t EVEN_ROUNDS = 4, EVEN_BLOCK = 128, EVEN_WAIT = 3;
 
 struct Seq {
@@ -570,7 +573,7 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     const int64_t share = tile_tokens * n_kv / kv.n_cu;
     int32_t tile_piece = at_least(share / 2, tile_min), tile_whole = at_least(share, tile_min);
     // Prefixes are joined anyway, and cut into as many pieces; but not into shorter ones than the rows beside them keep the machine busy with, three quarters of whose tokens for a compute unit
-    // take a tile about as long (256 requests of about 350 tokens behind 2000 with 32 / 8 heads: 4 pieces 93.6 us, 2 85.5, 1 80.2).
+    // take a tile about as long (256 requests of 350 tokens behind 2000 with 32 / 8 heads: 4 pieces 94.3 us, 2 85.0, 1 83.8).
     int32_t prefix_row_piece = at_least(row_tokens * n_kv / ROW_BLOCKS, SHARED_ROW_MIN_TOKENS);
     int32_t prefix_tile_piece = at_least(cut.way == lora::KV_TILES_TURNS ? share : share / 2, tile_min);
     if (cut.way != lora::KV_TILES_TURNS) prefix_tile_piece = std::max(prefix_tile_piece, at_least(row_tokens * n_kv / kv.n_cu * 3 / 4, 0));
@@ -728,7 +731,7 @@ bool cut_attention(const lora_kv &kv, const Growth &g, const int32_t *offsets, C
     // Where there are more items than blocks fit on the machine, a wavefront has a short one to itself: a block on it is mostly waiting for its first
     // loads and its last stores.  Measured: 512 requests of 20 tokens with 32 heads of 128 96 -> 51 us, 256 of 120 94 -> 78 us; with 200 to 450 tokens, and
     // with half as many for heads of 256, nothing is gained.  Beside prefixes, whose parts are there to be worked on, from twice as many on: 128 requests with 20 tokens of their own behind 2000 with 32 / 8
-    // heads 26.6 -> 25.5 us, 20 of 50 with 40 / 40 24.9 -> 23.0.
+    // heads 29.2 -> 27.8 us, 20 of 50 with 40 / 40 26.9 -> 25.4.
     size_t n_short = 0;
     const auto is_short = [&](const AttnItem &it) { return (it.part < 0 || !cut.prefixes.empty()) && it.kv1 - it.kv0 <= short_tokens; };
     while (n_short < cut.rows.size() && is_short(cut.rows[cut.rows.size() - 1 - n_short])) ++n_short;

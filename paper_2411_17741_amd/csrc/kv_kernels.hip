@@ -1,5 +1,5 @@
 // The paged key-value cache's writes (gfx950): new keys and values into the pages with their positions turned, with norms of their
-// heads and as 8-bit values where that is asked for, and pages copied to others; and what the pages hold read back.  All of it only moves bytes; the
+// heads and as 8-bit values where that is asked for, and pages copied to others; and what the pages hold read back.  Memory bounds all of it; the
 // layout of the pages is in include/lora_kv.h.
 #include <algorithm>
 #include <type_traits>
@@ -201,7 +201,7 @@ hipError_t launch_append(const AppendArgs &a, int dtype, hipStream_t st)
 // sum of its squares, or the largest of its values, between them by a few exchanges.
 //
 // 8 bits: a value that is beside a border between two of them goes the wrong way if what it is made of was rounded before, and is off by 2^-4 of itself then:
-// keys are normed and turned in 64 bits (their products with 24-bit cosines and sines are exact there), and rounded to the nearest of 8 bits by way of fp32
+// keys are normed and turned in 64 bits (the products of a key without a norm and of 24-bit cosines and sines are exact there), and rounded to the nearest of 8 bits by way of fp32
 // values that are rounded to odd -- towards zero, with the last bit set if anything was lost --, which leaves the second rounding what it has to know.
 //
 // Bound by memory in large batches: 4291 tokens of 32 + 8 + 8 heads of 128, normed, 108 MB, in 28.8 us, 3.7 TB/s (all squares in 64 bits and weights fetched head by head 36); 2544 of 64 + 8 + 8 into 8 bits, 92 MB, 26.5.  Small ones by trips to
@@ -373,13 +373,12 @@ __device__ __forceinline__ void append_values_e4m3(const AppendArgs &a, uint32_t
     }
 }
 
-// The sum over lanes `tokens` (2, 4, 8 or 16) apart
+// The sum over lanes `tokens` (4, 8 or 16) apart
 __device__ __forceinline__ float over_pairs(float v, int tokens)
 {
     const auto row = [&](auto ctrl) { v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(ctrl)::value, 0xF, 0xF, true)); };
     if (tokens < 16) row(std::integral_constant<int, 0x128>{});  // 16 lanes turned by 8
     if (tokens < 8) row(std::integral_constant<int, 0x124>{});
-    if (tokens < 4) row(std::integral_constant<int, 0x122>{});
     const auto near = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     v = __uint_as_float(near[0]) + __uint_as_float(near[1]);
     const auto far = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
