@@ -53,6 +53,7 @@ def _want(tokens):
         (8, 1, 64, 1920, 150, 128),
         (32, 8, 128, 1280, 130, 64),
         (32, 8, 128, 40000, 64, 64),  # tiles of 256 rows
+        (16, 16, 256, 640, 300, 32),  # tiles and rows in launches of their own
         (16, 1, 64, 64, 1, 64),       # as many rows as a row item has
     ],
 )
