@@ -159,7 +159,7 @@ int lora_kv_batch_create(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, c
  * that are full, attention reads those once, for the rows of all of them together, and joins the result with that of each one's own tokens.  Prefixes may branch: what some of
  * the segments share beyond what all do is a prefix of its own.  Which pages are shared is seen from the books (pages with the same keys and values that were appended twice are not).  A
  * prefix is shared from min_tokens tokens on, with 0 where it is long enough, and its segments many enough, to gain by it, as long as there is room: a segment has up to 7 of them, one behind
- * the other, and all prefixes' segments up to 2 * max_batch_tokens tokens together (what does not fit is left out); all are left to the segments if the pieces' results have no room.  Outputs are those of lora_kv_batch_create up to the rounding of sums, and with LORA_BF16 of the weights of segments with more than 16 rows (lora_kv_attend).  Errors as there; LORA_E_INVAL if min_tokens is negative. */
+ * the other, and all prefixes' segments up to 2 * max_batch_tokens tokens together (what does not fit is left out, and so is all behind more than 16 in a row that do not); all are left to the segments if the pieces' results have no room.  Outputs are those of lora_kv_batch_create up to the rounding of sums, and with LORA_BF16 of the weights of segments with more than 16 rows (lora_kv_attend).  Errors as there; LORA_E_INVAL if min_tokens is negative. */
 int lora_kv_batch_create_shared(lora_kv_t *kv, int32_t n_seg, const int64_t *seg_seq, const int32_t *seg_offsets, int32_t min_tokens, void *stream,
                                 lora_kv_batch_t **out);
 int lora_kv_batch_destroy(lora_kv_t *kv, lora_kv_batch_t *batch);

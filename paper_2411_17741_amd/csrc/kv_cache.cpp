@@ -44,6 +44,8 @@ constexpr int PIECE_STEP = 64;  // pieces begin at multiples of it: a whole numb
 constexpr int MAX_EXTRA = 2048;  // pieces beyond one for each block of rows
 // Of how many prefixes of prefixes a segment may have a part; tokens' places in all of them together (times max_batch_tokens); tokens of a piece of a prefix with few rows
 constexpr int SHARED_DEPTH = 7, SHARED_TOKENS = 2, SHARED_ROW_MIN_TOKENS = 256;
+// Behind how many prefixes without room, one behind the other, fewer segments are still looked for that share more: 2000 requests, each a fork of the one before it, would otherwise take 23 ms.
+constexpr int SHARED_MISSES = 16;
 // A prefix is worth it if the segments but one are spared more bytes of keys and values than these, and so many for each row of each head of 128, whose parts are written and read again.  (The bytes
 // that are spared would mostly have come out of caches.)  Measured, one by one -> shared, us, heads of 128, each request 100 tokens of its own behind the prefix, with a deviation of the logarithm of 0.4 (in
 // brackets: 100 for all): 64 requests with 32 / 8 heads and 600 tokens, 148 MB, 27.9 -> 20.0 (19.3 -> 20.1), 1024 tokens 35.4 -> 24.9 (26.1 -> 24.9), 512 tokens, 132 MB, 25.1 -> 23.2 (17.3 -> 23.4); with 64 / 8 heads 800
@@ -449,7 +451,7 @@ void find_prefixes(const lora_kv &kv, const Growth &g, int32_t min_tokens, Cut &
         return (segs - 1) * shared * token_bytes >= (rows <= lora::KV_ROW_ITEM ? SHARED_FEW_BYTES : SHARED_BYTES) + rows * kv.cfg.n_kv_heads * SHARED_ROW_BYTES * kv.cfg.head_dim / 128;
     };
     struct Set {
-        int32_t at, base, depth;  // pages that the segments have in common; those of them that are in prefixes already; how many these are
+        int32_t at, base, depth, misses;  // pages that the segments have in common; those of them that are in prefixes already; how many these are; and how many had no room since the last
         std::vector<int32_t> segs;
     };
     const auto full = [&](int32_t i) { return g.seqs[i]->n_tokens >> kv.page_shift; };
@@ -457,10 +459,10 @@ void find_prefixes(const lora_kv &kv, const Growth &g, int32_t min_tokens, Cut &
     std::vector<Set> sets(1);
     for (size_t i = 0; i < g.seqs.size(); ++i)
         if (g.n_tokens[i] && (int64_t)g.n_tokens[i] * grp < lora::KV_TILE) sets[0].segs.push_back((int32_t)i);
-    sets[0].at = sets[0].base = sets[0].depth = 0;
+    sets[0].at = sets[0].base = sets[0].depth = sets[0].misses = 0;
     cut.own.assign(g.seqs.size(), 0);
     int64_t room = (int64_t)kv.cfg.max_batch_tokens * SHARED_TOKENS;
-    while (!sets.empty()) {
+    while (!sets.empty() && room >= 2) {  // (a prefix has two segments at least)
         Set set = std::move(sets.back());
         sets.pop_back();
         if (set.depth == SHARED_DEPTH) continue;
@@ -470,7 +472,7 @@ void find_prefixes(const lora_kv &kv, const Growth &g, int32_t min_tokens, Cut &
         for (size_t first = 0, last; first < segs.size(); first = last) {
             for (last = first + 1; last < segs.size() && page(segs[last], set.at) == page(segs[first], set.at);) ++last;
             if (last - first < 2) continue;
-            Set part{full(segs[first]), set.base, set.depth, {segs.begin() + first, segs.begin() + last}};
+            Set part{full(segs[first]), set.base, set.depth, set.misses, {segs.begin() + first, segs.begin() + last}};
             const int32_t *const p = g.seqs[segs[first]]->pages.data();
             int64_t tokens = 0;
             for (const int32_t i : part.segs) {
@@ -479,8 +481,13 @@ void find_prefixes(const lora_kv &kv, const Growth &g, int32_t min_tokens, Cut &
                 tokens += g.n_tokens[i];
             }
             const int32_t to = part.at & ~(std::max(PIECE_STEP >> kv.page_shift, 1) - 1);  // (what is behind a prefix begins where pieces may)
-            // (one that has no room is left out; fewer segments that share more may have)
-            if (to > part.base && tokens <= room && worth((int64_t)(to - part.base) << kv.page_shift, (int64_t)part.segs.size(), tokens * grp)) {
+            if (to > part.base && worth((int64_t)(to - part.base) << kv.page_shift, (int64_t)part.segs.size(), tokens * grp)) {
+                if (tokens > room) {  // left out; fewer segments that share more may have room
+                    if (++part.misses > SHARED_MISSES) continue;
+                    sets.push_back(std::move(part));
+                    continue;
+                }
+                part.misses = 0;
                 room -= tokens;
                 // in bf16 the weights of few rows have 16 bits: they must not lose them by sharing
                 const bool exact = tokens * grp > lora::KV_ROW_ITEM && kv.cfg.dtype == LORA_BF16 &&

@@ -76,6 +76,13 @@ def test_prefixes_without_room_are_left_out_and_those_behind_them_are_not(kind):
     _levels(CHAIN, 8, 2, 128, 11, (3, 10, 2048), kind=kind, seed=34, page=32)
 
 
+@pytest.mark.parametrize("n,want", [(21, (3, 21, 19 * 64)), (22, (2, 22, 2 * 64))])
+def test_what_is_behind_many_prefixes_without_room(n, want):
+    """n requests, each a fork of the one before it with 64 tokens more, room for 2 n + 2: n share the first 64 tokens, n - 1 the next, 3 places are left.  Three requests are n - 5 prefixes on: found
+    behind 16, not behind 17."""
+    _levels([(None, -1, 64, 1)] + [(i, -1, 64, 1) for i in range(n - 1)], 4, 4, 64, n + 1, want, shared=64, seed=39)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 def test_three_levels_that_branch(kind):
     """A system prompt, two prompts behind it, conversations behind those; one that forks early, one that shares nothing."""
